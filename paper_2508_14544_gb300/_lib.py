@@ -34,6 +34,17 @@ class sim_result(ctypes.Structure):
                 ("status", ctypes.c_int32), ("_pad", ctypes.c_int32)]
 
 
+class sim_kv(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pool", "table", "length", "ref", "status", "scratch")] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "n_layers", "n_kv_heads", "page_size", "head_dim",
+                                              "max_seqs", "max_pages")]
+
+
+class sim_kv_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n", "n_q", "q_heads", "n_groups")] + \
+               [(n, ctypes.c_void_p) for n in ("seqs", "cu_q", "cu_group", "plan", "workspace")]
+
+
 RESULT_DTYPE = np.dtype([
     ("total_latency", "<i8"), ("makespan", "<i8"), ("peak_memory", "<i8"), ("evictions", "<i8"),
     ("steps", "<i8"), ("request_steps", "<i8"), ("status", "<i4"), ("_pad", "<i4"),
@@ -43,7 +54,9 @@ assert RESULT_DTYPE.itemsize == ctypes.sizeof(sim_result) == 56
 EXPORTS = ("sim_create", "sim_load", "sim_load_csr", "sim_load_ranked_csr", "sim_run", "sim_get_completions", "sim_competitive_ratio",
            "sim_set_option", "sim_set_tie_seeds", "sim_get_work_counts", "sim_batch_time",
            "sim_get_batch_time_sums", "sim_last_error", "sim_destroy", "sim_kernel_launches", "sim_run_noalloc",
-           "sim_cr_amin_lemma", "sim_cr_amin_rho", "sim_measure_peaks")
+           "sim_cr_amin_lemma", "sim_cr_amin_rho", "sim_measure_peaks",
+           "sim_kv_scratch_bytes", "sim_kv_extend", "sim_kv_write", "sim_kv_fork", "sim_kv_copy", "sim_kv_free",
+           "sim_kv_compact", "sim_kv_plan_bytes", "sim_kv_workspace_bytes", "sim_kv_plan", "sim_kv_attend")
 
 _lib = None
 
@@ -108,6 +121,19 @@ def lib() -> ctypes.CDLL:
     L.sim_cr_amin_rho.restype = ctypes.c_int
     L.sim_measure_peaks.argtypes = [vp]
     L.sim_measure_peaks.restype = ctypes.c_int
+    kv, batch, i32, i64 = ctypes.POINTER(sim_kv), ctypes.POINTER(sim_kv_batch), ctypes.c_int32, ctypes.c_int64
+    for name, res, args in (("sim_kv_scratch_bytes", i64, [kv]),
+                            ("sim_kv_extend", ctypes.c_int, [kv, i32, vp, vp, i32, vp, vp]),
+                            ("sim_kv_write", ctypes.c_int, [kv, i32, i32, vp, vp, i64, i64, vp, i64, i64, vp]),
+                            ("sim_kv_fork", ctypes.c_int, [kv, i32, vp, vp, vp, vp]),
+                            ("sim_kv_copy", ctypes.c_int, [kv, i32, vp, vp, vp]),
+                            ("sim_kv_free", ctypes.c_int, [kv, i32, vp, vp, vp]),
+                            ("sim_kv_compact", ctypes.c_int, [kv, vp, vp]),
+                            ("sim_kv_plan_bytes", i64, [kv, batch]),
+                            ("sim_kv_workspace_bytes", i64, [kv, batch]),
+                            ("sim_kv_plan", ctypes.c_int, [kv, batch, vp]),
+                            ("sim_kv_attend", ctypes.c_int, [kv, batch, i32, vp, i64, i64, ctypes.c_float, vp, i64, i64, vp, vp])):
+        getattr(L, name).restype, getattr(L, name).argtypes = res, args
     _lib = L
     return L
 

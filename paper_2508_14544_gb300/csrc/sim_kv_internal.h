@@ -1,0 +1,165 @@
+// Declarations shared by the C ABI of the paged cache (sim_kv_api.cpp) and its kernels (sim_kv.cu, sim_kv_attend.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sim_kv.h"
+
+namespace simgb {
+
+constexpr int kKvMaxSeqs = 1 << 17;
+
+// kv->scratch, in ints: a header, then per entry of a call its first new page and their number, then lists of
+// pages (as many as the pool has): copies' sources and destinations, free pages.
+constexpr int kKvHdr = 64;  // [0]: copies to make
+__host__ __device__ inline int64_t kv_scratch_ints(const sim_kv &kv) { return kKvHdr + 2 * int64_t(kv.max_seqs) + 3 * int64_t(kv.n_pages); }
+struct KvScratch {
+    int32_t *hdr, *base, *need, *src, *dst, *free;
+};
+__host__ __device__ inline KvScratch kv_scratch(const sim_kv &kv) {
+    KvScratch s;
+    s.hdr = static_cast<int32_t *>(kv.scratch);
+    s.base = s.hdr + kKvHdr;
+    s.need = s.base + kv.max_seqs;
+    s.src = s.need + kv.max_seqs;
+    s.dst = s.src + kv.n_pages;
+    s.free = s.dst + kv.n_pages;
+    return s;
+}
+
+__host__ __device__ inline int64_t kv_layer_elems(const sim_kv &kv) { return 2 * int64_t(kv.n_kv_heads) * kv.page_size * kv.head_dim; }
+__host__ __device__ inline int64_t kv_page_bytes(const sim_kv &kv) { return 2 * kv.n_layers * kv_layer_elems(kv); }
+
+// n / d for 0 <= n < 2^31 and 1 <= d < 2^31 by a multiplication: with 2^(k-1) < d <= 2^k, m = ceil(2^(31+k) / d)
+// < 2^32 gives floor(n m / 2^(31+k)), since n (m d - 2^(31+k)) < n 2^k <= 2^(31+k).
+struct FastDiv {
+    uint32_t d, m, s;
+    __host__ __device__ FastDiv() : d(1), m(0), s(0) {}
+    __host__ explicit FastDiv(uint32_t dd) : d(dd), m(0), s(0) {
+        if (dd > 1) {
+            uint32_t k = 1;
+            while ((uint64_t(1) << k) < dd) ++k;
+            m = uint32_t(((uint64_t(1) << (31 + k)) + dd - 1) / dd);
+            s = k - 1;
+        }
+    }
+#ifdef __CUDACC__
+    __device__ uint32_t div(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> s; }
+#endif
+};
+
+cudaError_t launch_kv_extend(const sim_kv &kv, int32_t n, const int32_t *seqs, const int32_t *cu_new, int32_t n_new,
+                             int64_t *slots, cudaStream_t st);
+cudaError_t launch_kv_copy(const sim_kv &kv, int32_t n, const int32_t *src, const int32_t *dst, cudaStream_t st);
+cudaError_t launch_kv_fork(const sim_kv &kv, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *tokens,
+                           cudaStream_t st);
+cudaError_t launch_kv_free(const sim_kv &kv, int32_t n, const int32_t *seqs, const int32_t *keep, cudaStream_t st);
+cudaError_t launch_kv_compact(const sim_kv &kv, int32_t *to, cudaStream_t st);
+struct KvWrite {
+    const void *k, *v;
+    int64_t kt, kh, vt, vh;  // strides in elements
+    const int64_t *slots;
+    int32_t layer, n_new;
+};
+cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st);
+
+constexpr int kAttTile = 128;  // keys of a tile
+constexpr int kAttRows = 256;  // query rows of an item, at most
+
+// A run of query rows (token x head of the group, for every kv head alike) against a range of one table's keys.
+struct alignas(16) KvItem {
+    int32_t q0;       // query token of row 0 of its source
+    int32_t row0;     // first row within the source
+    int32_t rows;     // 1 .. kAttRows
+    int32_t seq;      // row of the table
+    int32_t kv0, kv1; // keys
+    int32_t pos0;     // position of token q0: token q0 + t sees the keys up to pos0 + t
+    int32_t tiles;
+    int64_t unit;     // tiles of the items before, all kv heads
+    int64_t row_off;  // rows of the items before, all kv heads
+    int32_t partial;  // its rows have another item too: always through the workspace
+    int32_t pad[3];
+};
+static_assert(sizeof(KvItem) == 64, "KvItem");
+
+// Items of more than 128 rows are heavy, the others light: two lists, each divided among blocks of its own.
+// b->plan: header, per group the pages shared and its entries' tile rows, the first heavy and the first light item
+// of every source (groups, then entries, and the end), each entry's group and the pages that it shares with its
+// group's first entry, the items.
+struct KvPlan {
+    int32_t *hdr;       // [0], [1] items, [2..3], [4..5] tiles in all (int64): heavy, light; [6..7] rows of the heavy items
+    int32_t *used;      // [n_groups]
+    int32_t *alone;     // [n_groups]
+    int32_t *first[2];  // [n_groups + n + 1]
+    int32_t *group;     // [n]
+    int32_t *same;      // [n]
+    KvItem *items[2];
+    int64_t bytes;
+    int32_t max_heavy;
+};
+__host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &b) {
+    KvPlan p;
+    const int64_t G = b.q_heads / kv.n_kv_heads, src = int64_t(b.n_groups) + b.n;
+    p.max_heavy = int32_t(2 * (int64_t(b.n_q) * G / (kAttRows / 2 + 1)) + 1);
+    p.hdr = static_cast<int32_t *>(b.plan);
+    p.used = p.hdr + 16;
+    p.alone = p.used + b.n_groups;
+    p.first[0] = p.alone + b.n_groups;
+    p.first[1] = p.first[0] + src + 1;
+    p.group = p.first[1] + src + 1;
+    p.same = p.group + b.n;
+    const int64_t ints = (16 + 2 * int64_t(b.n_groups) + 2 * (src + 1) + 2 * int64_t(b.n) + 3) / 4 * 4;
+    p.items[0] = reinterpret_cast<KvItem *>(static_cast<char *>(b.plan) + ints * 4);
+    p.items[1] = p.items[0] + p.max_heavy;
+    p.bytes = ints * 4 + (p.max_heavy + src) * int64_t(sizeof(KvItem));
+    return p;
+}
+// Blocks of the two lists for a number of SMs.
+__host__ __device__ inline int kv_blocks(int sms, int light) { return light ? 2 * sms : sms; }
+// Partial results: rows of head_dim floats, then a float per row (log2 of the sum of exponentials).  A piece of an
+// item begins at the rows before it plus room for the pieces that blocks have cut off before.
+__host__ __device__ inline int64_t kv_partial_rows(const sim_kv_batch &b, int sms) {
+    return 2 * int64_t(b.n_q) * b.q_heads + int64_t(kAttRows) * kv_blocks(sms, 0) + int64_t(kAttRows / 2) * kv_blocks(sms, 1);
+}
+
+struct KvAttend {
+    const void *q;
+    void *out;
+    float *lse;
+    float *part, *part_lse;
+    int64_t qt, qh, ot, oh;  // strides in elements
+    float scale, scale_log2;
+    int32_t layer;
+    int32_t q_vec;           // q may be read 16 bytes at a time
+    int32_t sms;
+};
+cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t st);
+cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st);
+
+// Launch that may begin before the kernel ahead of it in the stream has ended: each kernel waits for that one
+// (kv_wait_previous) before it touches memory, so only the launch itself overlaps.
+template <typename... Params, typename... Args>
+cudaError_t launch_chained(void (*fn)(Params...), int blocks, int threads, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(blocks));
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, args...);
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void kv_wait_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+#endif
+
+int kv_sm_count();  // of the current device
+
+}  // namespace simgb
