@@ -461,7 +461,7 @@ int kv_sm_count() {
         cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev);
         dev_of = dev;
     }
-    return std::max(count, 1);
+    return std::min(std::max(count, 1), kKvMaxSms);
 }
 
 cudaError_t launch_kv_extend(const sim_kv &kv, int32_t n, const int32_t *seqs, const int32_t *cu_new, int32_t n_new,

@@ -154,6 +154,7 @@ int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const 
     a.out = out;
     a.lse = lse;
     a.sms = simgb::kv_sm_count();
+    a.group = simgb::FastDiv(uint32_t(b->q_heads / kv->n_kv_heads));
     a.part = static_cast<float *>(b->workspace);
     a.part_lse = a.part + simgb::kv_partial_rows(*b, a.sms) * kv->head_dim;
     a.qt = q_token_stride;

@@ -39,11 +39,15 @@ constexpr int kSegs = 4;               // segments that the loading warp may be 
 constexpr int kShareCost = 4;          // tiles of 128 rows that a second partial result of as many rows costs
 constexpr float kGrow = 8.f;           // log2 of what P may reach before O is rescaled
 
+// Tiles [line_at(c), line_at(c + 1)) of a list's line are block c's.
+__device__ __forceinline__ int64_t line_at(int64_t units, int c, int blocks) { return units * c / blocks; }
+__device__ __forceinline__ int block_at(int64_t units, int64_t u, int blocks) { return int(((u + 1) * blocks - 1) / units); }
+
 // ---- plan ---------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// Entry i's query tokens [a, a + t), none if the offsets are not in order; the table's row, or -1.
+// Entry i's query tokens [a, a + t), none if the offsets are not in order; the table's row, or -1 (and no keys).
 struct Entry {
     int a, t, seq, len;
 };
@@ -51,10 +55,10 @@ __device__ __forceinline__ Entry entry_at(const sim_kv &kv, const sim_kv_batch &
     Entry e;
     e.a = b.cu_q[i];
     const int z = b.cu_q[i + 1], s = b.seqs[i];
-    const bool ok = 0 <= e.a && e.a <= z && z <= b.n_q && unsigned(s) < unsigned(kv.max_seqs);
+    const bool ok = 0 <= e.a && e.a <= z && z <= b.n_q;
     e.t = ok ? z - e.a : 0;
-    e.seq = ok ? s : -1;
-    e.len = ok ? min(kv.length[s], kv.max_pages * kv.page_size) : 0;
+    e.seq = unsigned(s) < unsigned(kv.max_seqs) ? s : -1;
+    e.len = e.seq >= 0 ? min(kv.length[s], kv.max_pages * kv.page_size) : 0;
     return e;
 }
 
@@ -146,7 +150,7 @@ __device__ __forceinline__ int light_items(int r) { return r % kAttRows > 0 && r
 
 // One block: which prefixes are shared, the items of every source (a group's prefix, an entry's own keys), and
 // where each begins on its list's line of work.
-__global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim_kv_batch b) {
+__global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim_kv_batch b, int sms) {
     __shared__ int64_t sums[32];
     kv_wait_previous();
     const KvPlan p = kv_plan(kv, b);
@@ -215,6 +219,7 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
     if (tid == 0) {
         p.first[0][n_src] = p.hdr[0] = n_heavy;
         p.first[1][n_src] = p.hdr[1] = n_light;
+        p.hdr[8] = order;
     }
     __syncthreads();
     int64_t rows = 0;
@@ -243,6 +248,7 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
                     it.kv1 = p.used[lo] * P;
                     it.pos0 = 1 << 30;
                     it.partial = 1;
+                    it.entry = -1;
                 } else {
                     const Entry e = entry_at(kv, b, lo - ng);
                     const int g = p.group[lo - ng], shared = g < 0 ? 0 : p.used[g];
@@ -253,6 +259,7 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
                     it.pos0 = e.len - e.t;
                     it.kv1 = min(e.len, it.pos0 + (it.row0 + min(it.rows, kAttRows) - 1) / G + 1);
                     it.partial = shared > 0;
+                    it.entry = lo - ng;
                 }
                 it.rows = min(it.rows, light ? kAttRows / 2 : kAttRows);
                 it.tiles = ceil_div(max(it.kv1 - it.kv0, 0), kAttTile);
@@ -267,14 +274,21 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
         if (tid == 0) *reinterpret_cast<int64_t *>(p.hdr + 2 + 2 * light) = units;
         rows += list_rows;
         if (tid == 0 && !light) *reinterpret_cast<int64_t *>(p.hdr + 6) = rows;
+        __syncthreads();
+        for (int c = tid; c < kv_blocks(sms, light); c += kPlan) {
+            const int64_t u = line_at(units, c, kv_blocks(sms, light));
+            int lo = 0, hi = n_items;  // the last item that begins at or before the block's stretch
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (p.items[light][mid].unit <= u) lo = mid;
+                else hi = mid;
+            }
+            p.start[light][c] = lo;
+        }
     }
 }
 
 // ---- the line of work ---------------------------------------------------------------------------------------
-
-// Units [first, last) of block c of `blocks`.
-__device__ __forceinline__ int64_t line_at(int64_t units, int c, int blocks) { return units * c / blocks; }
-__device__ __forceinline__ int block_at(int64_t units, int64_t u, int blocks) { return int(((u + 1) * blocks - 1) / units); }
 
 // First row of the partial results of block c's piece of a list whose rows follow `base` others.
 __device__ __forceinline__ int64_t piece_row(const KvItem &it, int h, int c, int64_t base, int light) {
@@ -307,13 +321,7 @@ struct Line {
         u = line_at(units, c, kv_blocks(sms, light));
         u1 = line_at(units, c + 1, kv_blocks(sms, light));
         base = list_base(p, light, sms);
-        int lo = 0, hi = n_items;  // the last item that begins at or before u
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (items[mid].unit <= u) lo = mid;
-            else hi = mid;
-        }
-        k = lo;
+        k = p.start[light][c];
         h = -1;
     }
     // The next item and head with work for this block; s.n = 0 at the end.
@@ -380,6 +388,17 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         }
     }
     return true;
+}
+
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(p));
+    return p;
 }
 
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z, int w) {
@@ -453,6 +472,32 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\t"
+        "mov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, w;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 w, x, y;\n\t"
+        "mov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 template <bool BF>
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     uint32_t r;
@@ -480,7 +525,7 @@ struct Shape {
     static constexpr int kSlots = (HEAVY ? 131072 : 65536) / kTile;           // tiles of keys or values in flight
     static constexpr int kTmem = HEAVY ? 512 : 256;
     static constexpr int kOffO = kGroups * 128;                               // TMEM column of the first group's O
-    static constexpr int kSoftRegs = HEAVY ? 208 : 184, kOtherRegs = HEAVY ? 80 : 72;
+    static constexpr int kSoftRegs = HEAVY ? 208 : 184, kOtherRegs = HEAVY ? 88 : 72;
     // the launch gives 168 (128) registers a thread: no more are handed out
     static_assert(kGroups * kSoftRegs + kOtherRegs <= (kGroups + 1) * (HEAVY ? 168 : 128), "registers");
     static constexpr int kOffRing = kGroups * kTile;
@@ -545,7 +590,7 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_at;
+    const uint32_t tmem = __shfl_sync(FULL, *tmem_at, 0);
     kv_wait_previous();
 
     const int G = b.q_heads / kv.n_kv_heads, D = kv.head_dim;
@@ -611,81 +656,95 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
                 if (lane == 0) atomicMin(kv.status, SIM_E_STATE);
             }
         } else if (role == 1) {
-            // ---- tensor products, issued by one thread
+            // ---- tensor products: the whole warp keeps the same (uniform) state, one lane issues
             const uint32_t type = BF ? 1u << 7 | 1u << 10 : 0u;
             const uint32_t idesc_s = 1u << 4 | type | (128 / 8) << 17 | (128 / 16) << 24;
             const uint32_t idesc_o = 1u << 4 | type | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
+            const uint64_t op_q = operand(sbase, 16, 1024), op_k = operand(sbase + Sh::kOffRing, 16, 1024), op_v = operand(sbase + Sh::kOffRing, Sh::kHalf, 1024);
             uint32_t at = 0, np = 0;
             bool ok = true;
+            const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, bar_wait(bar, parity, gave_up)) != 0; };
+            const auto wait_full = [&](uint32_t y) { return wait(full(y), (y / NS) & 1); };
             Segment sg;
-            for (uint32_t x = 0; (ok = take(x, sg)) && sg.n > 0; ++x) {
-                if (lane == 0) {
-                    const auto keys = [&](int j, int g) {  // S of group g and tile j
-                        const uint32_t q = sbase + g * Sh::kTile, k = sbase + Sh::kOffRing + ((at + 2 * j) % NS) * Sh::kTile;
+            for (uint32_t x = 0; (ok = take(x, sg)); ++x) {
+                const int n = __shfl_sync(FULL, sg.n, 0);
+                if (n == 0) break;
+                const auto keys = [&](int j, int g) {  // S of group g and tile j
+                    if (elect_one()) {
+                        const uint32_t slot = (at + 2 * j) % NS;
 #pragma unroll
                         for (int kk = 0; kk < DP / 16; ++kk) {
                             const uint32_t off = (kk / 4) * Sh::kHalf + (kk % 4) * 32;
-                            mma_ss(tmem + g * 128, operand(q + off, 16, 1024), operand(k + off, 16, 1024), idesc_s, kk > 0);
+                            mma_ss(tmem + g * 128, op_q + ((g * Sh::kTile + off) >> 4), op_k + ((slot * Sh::kTile + off) >> 4), idesc_s, kk > 0);
                         }
                         tc_commit(s_full(g));
                         if (g == NG - 1) {
                             tc_commit(empty(at + 2 * j));
-                            if (j == sg.n - 1) tc_commit(q_empty);
-                        }
-                    };
-                    const auto wait_full = [&](uint32_t y) { return bar_wait(full(y), (y / NS) & 1, gave_up); };
-                    ok = bar_wait(q_full, x & 1, gave_up) && wait_full(at);
-                    tc_fence_after();
-                    for (int g = 0; g < NG && ok; ++g) keys(0, g);
-                    for (int j = 0; j < sg.n && ok; ++j, ++np) {
-                        const uint32_t v = sbase + Sh::kOffRing + ((at + 2 * j + 1) % NS) * Sh::kTile;
-                        ok = wait_full(at + 2 * j + 1);
-                        for (int g = 0; g < NG && ok; ++g) {
-                            ok = bar_wait(p_ready(g), np & 1, gave_up);
-                            if (!ok) break;
-                            tc_fence_after();
-#pragma unroll
-                            for (int kk = 0; kk < kAttTile / 16; ++kk)
-                                mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + kk * 8, operand(v + kk * 2048, Sh::kHalf, 1024), idesc_o, j > 0 || kk > 0);
-                            if (g == NG - 1) tc_commit(empty(at + 2 * j + 1));
-                            if (j + 1 == sg.n) {
-                                tc_commit(o_full(g));
-                            } else {
-                                if (g == 0) ok = wait_full(at + 2 * j + 2);
-                                if (ok) keys(j + 1, g);
-                            }
+                            if (j == n - 1) tc_commit(q_empty);
                         }
                     }
-                    at += 2 * sg.n;
-                }
-                ok = __shfl_sync(FULL, ok, 0);
+                    __syncwarp();
+                };
+                ok = wait(q_full, x & 1) && wait_full(at);
                 if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int g = 0; g < NG; ++g) keys(0, g);
+                for (int j = 0; j < n && ok; ++j, ++np) {
+                    ok = wait_full(at + 2 * j + 1);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        ok = ok && wait(p_ready(g), np & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t slot = (at + 2 * j + 1) % NS;
+#pragma unroll
+                            for (int kk = 0; kk < kAttTile / 16; ++kk)
+                                mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + kk * 8, op_v + ((slot * Sh::kTile + kk * 2048) >> 4), idesc_o, j > 0 || kk > 0);
+                            if (g == NG - 1) tc_commit(empty(at + 2 * j + 1));
+                            if (j + 1 == n) tc_commit(o_full(g));
+                        }
+                        __syncwarp();
+                        if (j + 1 < n) {
+                            if (g == 0) ok = wait_full(at + 2 * j + 2);
+                            if (!ok) break;
+                            keys(j + 1, g);
+                        }
+                    }
+                }
+                if (!ok) break;
+                at += 2 * n;
             }
-            if (!ok && lane == 0) {
-                tc_commit(drained);
+            if (!ok) {
+                if (elect_one()) {
+                    tc_commit(drained);
+                    atomicMin(kv.status, SIM_E_STATE);
+                }
+                __syncwarp();
                 for (int n = 0; n < 1000000 && !bar_try(drained, 0); ++n) {
                 }
-                atomicMin(kv.status, SIM_E_STATE);
             }
             __syncwarp();
         } else {
-            // ---- query rows: two warps, 16 bytes a lane, the lanes of a row side by side
+            // ---- query rows: two warps, 16 bytes a lane, the lanes of a row side by side.  Rows past the item's are
+            // left as they are: what they hold meets no other row and is masked.
+            constexpr int kVec = DP / 8, kStep = 64 / kVec;
+            const int j = (tid & 63) % kVec;
+            const bool has = j * 8 < D;
             Segment sg;
             for (uint32_t x = 0; take(x, sg) && sg.n > 0; ++x) {
                 // 64 (32) rows or fewer lie in the tile twice (four times)
                 const int span = HEAVY ? 256 : sg.rows > 64 ? 128 : sg.rows > 32 ? 64 : 32;
+                const uint16_t *const from0 = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0) * a.qt + int64_t(sg.h * G) * a.qh + (has ? j * 8 : 0);
                 if (!__all_sync(FULL, bar_wait(q_empty, (x + 1) & 1, gave_up))) break;
-                constexpr int kVec = DP / 8;
-                const int first = tid & 63;
 #pragma unroll 4
-                for (int e = first; e < span * kVec; e += 64) {
-                    const int r = e / kVec, j = e % kVec;
-                    const bool has = r < sg.rows && j * 8 < D;
-                    const int y = sg.row0 + (has ? r : 0), t = y / G;
-                    const uint16_t *from = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0 + t) * a.qt + int64_t(sg.h * G + (y - t * G)) * a.qh + (has ? j * 8 : 0);
+                for (int r = (tid & 63) / kVec; r < sg.rows; r += kStep) {
+                    const int y = sg.row0 + r, t = a.group.div(y);
+                    const uint16_t *from = from0 + int64_t(t) * a.qt + int64_t(y - t * G) * a.qh;
                     const uint32_t to = sbase + (r >> 7) * Sh::kTile + (j / 8) * Sh::kHalf + (r & 127) * 128 + (((j % 8) ^ (r & 7)) << 4);
                     if (a.q_vec) {
-                        const int bytes = has ? 16 : 0;  // the rest is zeros
+                        const int bytes = has ? 16 : 0;  // columns past the head's are zeros
                         for (int c = 0; c < 128; c += span)
                             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + c * 128), "l"(from), "r"(bytes) : "memory");
                     } else {
@@ -722,7 +781,7 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
         for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
             const int rows = sg.rows;
             const int r = HEAVY ? g * 128 + lr : rows > 64 ? lr : rows > 32 ? lr & 63 : lr & 31;  // the row in this thread's lane
-            const int last = r < rows ? min(sg.kv1 - 1, sg.pos0 + (sg.row0 + r) / G) : -1;  // key position that it sees last
+            const int last = r < rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : -1;  // key position that it sees last
             float m = -INFINITY, l = 0.f;
 
             const auto tiles = [&](auto copies) {
@@ -746,7 +805,7 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
                     }
                     float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int y = 0; y < NC; ++y) top[y & 3] = fmaxf(top[y & 3], __uint_as_float(s[y]));
+                    for (int y = 0; y < NC; y += 2) top[y / 2 & 3] = max3(top[y / 2 & 3], __uint_as_float(s[y]), __uint_as_float(s[y + 1]));
                     const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                     if (j == 0) {
                         m = mx;
@@ -765,15 +824,17 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
                         }
                     }
                     const float off = m == -INFINITY ? 0.f : m * c;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    float2 sum[4] = {};
                     uint32_t pk[NC / 2];
 #pragma unroll
                     for (int y = 0; y < NC; y += 2) {
-                        const float p0 = ex2(fmaf(__uint_as_float(s[y]), c, -off)), p1 = ex2(fmaf(__uint_as_float(s[y + 1]), c, -off));
-                        sum[y / 2 & 3] += p0 + p1;
-                        pk[y / 2] = pack<BF>(p0, p1);
+                        float2 e = fma2(make_float2(__uint_as_float(s[y]), __uint_as_float(s[y + 1])), make_float2(c, c), make_float2(-off, -off));
+                        e = make_float2(ex2(e.x), ex2(e.y));
+                        sum[y / 2 & 3] = add2(sum[y / 2 & 3], e);
+                        pk[y / 2] = pack<BF>(e.x, e.y);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+                    l += sum[0].x + sum[0].y;
                     if constexpr (R == 1) {
                         tm_st32(t_s, pk);
                         tm_st32(t_s + 32, pk + 32);
@@ -819,7 +880,7 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
             at += 2 * sg.n;
 
             const auto out_row = [&](int y) {  // of row y of the item
-                const int t = (sg.row0 + y) / G;
+                const int t = a.group.div(sg.row0 + y);
                 return static_cast<uint16_t *>(a.out) + int64_t(sg.q0 + t) * a.ot + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.oh;
             };
             const auto put_lse = [&](int y, float top, float total) {
@@ -827,7 +888,7 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
                 if (!sg.direct) {
                     a.part_lse[sg.row + y] = e;
                 } else if (a.lse) {
-                    const int t = (sg.row0 + y) / G;
+                    const int t = a.group.div(sg.row0 + y);
                     a.lse[int64_t(sg.q0 + t) * b.q_heads + sg.h * G + (sg.row0 + y - t * G)] = e * 0.69314718055994531f;
                 }
             };
@@ -927,66 +988,115 @@ __global__ void __launch_bounds__(Shape<DP, HEAVY>::kThreads, HEAVY ? 1 : 2)
 
 // ---- k_combine ----------------------------------------------------------------------------------------------
 
-// A warp for each row whose keys were divided among items or blocks, or that sees none.
+// The pieces of one item and head: those of blocks c0 .. c1 that have any of its tiles.
+struct Pieces {
+    int64_t row, units;
+    int c0, n, blocks, rows;
+    __device__ Pieces() : row(0), units(0), c0(0), n(0), blocks(1), rows(0) {}
+    __device__ Pieces(const KvPlan &p, const KvItem &it, int h, int light, int sms) : units(0), c0(0), n(0), blocks(kv_blocks(sms, light)) {
+        rows = light ? kAttRows / 2 : kAttRows;
+        if (it.tiles > 0) {
+            units = *reinterpret_cast<const int64_t *>(p.hdr + (light ? 4 : 2));
+            const int64_t from = it.unit + int64_t(h) * it.tiles;
+            c0 = block_at(units, from, blocks);
+            n = block_at(units, from + it.tiles - 1, blocks) - c0 + 1;
+        }
+        row = piece_row(it, h, c0, list_base(p, light, sms), light);
+    }
+    // Row `in` of the item in piece i, -1 if the block has none of its tiles (where there are fewer tiles than blocks).
+    __device__ int64_t at(int i, int in) const {
+        const bool some = units >= blocks || line_at(units, c0 + i, blocks) < line_at(units, c0 + i + 1, blocks);
+        return i >= 0 && i < n && some ? row + int64_t(rows) * i + in : -1;
+    }
+};
+
+// Rows whose keys were divided among items or blocks, or that see none: a block for 32 rows of an entry's item
+// and one head, eight lanes for each row.  The lanes first read the sums of eight pieces, then, without waiting
+// in between, those pieces' columns.
 template <bool BF>
 __global__ void __launch_bounds__(256) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
-    const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, lane = threadIdx.x & 31;
-    const int64_t rows = int64_t(b.n_q) * b.q_heads;
-    for (int64_t x = (int64_t(blockIdx.x) * 256 + threadIdx.x) >> 5; x < rows; x += int64_t(gridDim.x) * 8) {
-        const int t = int(x / b.q_heads), qh = int(x % b.q_heads), h = qh / G;
-        int lo = -1, hi = b.n;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (b.cu_q[mid] <= t) lo = mid;
-            else hi = mid;
+    const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, sub = (threadIdx.x & 31) >> 3, sl = threadIdx.x & 7, warp = threadIdx.x >> 5;
+    const auto put = [&](int t, int qh, const float4 *v, float f, float lse) {
+        uint16_t *o = static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int d = 4 * (sl + 8 * q);
+            if (d < D) *reinterpret_cast<uint2 *>(o + d) = make_uint2(pack<BF>(v[q].x * f, v[q].y * f), pack<BF>(v[q].z * f, v[q].w * f));
         }
-        bool direct = false;
-        float top = -INFINITY, total = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-        const bool has = lane * 4 < D;
-        if (lo >= 0 && t < b.cu_q[lo + 1]) {
-            const int g = plan.group[lo];
-            for (int e = 0; e < 2 && !direct; ++e) {
-                const int src = e == 0 ? g : b.n_groups + lo;
-                if (src < 0 || (e == 0 && plan.used[g] == 0)) continue;
-                const int row = (t - b.cu_q[e == 0 ? b.cu_group[g] : lo]) * G + qh % G;
-                const int nth = row / kAttRows, h0 = plan.first[0][src], h1 = plan.first[0][src + 1], light = nth >= h1 - h0;
-                const int k = light ? plan.first[1][src] : h0 + nth, in = row % kAttRows;
-                if (light && k >= plan.first[1][src + 1]) continue;
-                const KvItem it = plan.items[light][k];
-                if (it.tiles == 0) continue;
-                const int blocks = kv_blocks(a.sms, light);
-                const int64_t units = *reinterpret_cast<const int64_t *>(plan.hdr + 2 + 2 * light), base = list_base(plan, light, a.sms);
-                const int64_t from = it.unit + int64_t(h) * it.tiles;
-                const int c0 = block_at(units, from, blocks), c1 = block_at(units, from + it.tiles - 1, blocks);
-                if (c0 == c1 && !it.partial) {
-                    direct = true;  // k_attend wrote the row
-                    break;
+        if (sl == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = lse;
+    };
+    const int heavy0 = plan.first[0][b.n_groups], light0 = plan.first[1][b.n_groups];
+    const int64_t heavy = int64_t(plan.hdr[0] - heavy0) * H * 8, all = heavy + int64_t(plan.hdr[1] - light0) * H * 4;
+    for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+        const bool light = x >= heavy;
+        const uint32_t y = uint32_t(light ? x - heavy : x), ih = light ? y >> 2 : y >> 3;
+        const int r0 = 32 * int(light ? y & 3 : y & 7), k = int(ih / H), h = int(ih % H);
+        const KvItem *const at_item = light ? plan.items[1] + light0 + k : plan.items[0] + heavy0 + k;
+        if (r0 >= at_item->rows) continue;
+        const KvItem it = *at_item;
+        const Pieces own(plan, it, h, light, a.sms);
+        if (own.n == 1 && !it.partial) continue;  // k_attend wrote these rows
+        const int r = r0 + warp * 4 + sub;
+        const bool row = r < it.rows;
+        const int z = it.row0 + min(r, it.rows - 1), t = it.q0 + int(a.group.div(z)), qh = h * G + z - (t - it.q0) * G;
+        Pieces prefix;
+        int in = 0;
+        if (it.partial) {
+            const int g = plan.group[it.entry], nth_row = (t - b.cu_q[b.cu_group[g]]) * G + qh - h * G, nth = nth_row / kAttRows, h0 = plan.first[0][g];
+            const bool l = nth >= plan.first[0][g + 1] - h0;
+            prefix = Pieces(plan, l ? plan.items[1][plan.first[1][g]] : plan.items[0][h0 + nth], h, l, a.sms);
+            in = nth_row % kAttRows;
+        }
+        const int n = prefix.n + own.n, most = int(__reduce_max_sync(FULL, unsigned(n)));
+        float top = -INFINITY, total = 0.f;
+        float4 acc[4] = {};
+        for (int p0 = 0; p0 < most; p0 += 8) {
+            const int p = p0 + sl;
+            const int64_t at = p < prefix.n ? prefix.at(p, in) : own.at(p - prefix.n, min(r, it.rows - 1));
+            const float s = at >= 0 ? a.part_lse[at] : -INFINITY;
+            float up = s;
+#pragma unroll
+            for (int d = 4; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(FULL, up, d));
+            up = fmaxf(up, top);
+            const float w = s == -INFINITY ? 0.f : ex2(s - up), f = top == -INFINITY ? 0.f : ex2(top - up);
+            top = up;
+            total *= f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[q] = make_float4(acc[q].x * f, acc[q].y * f, acc[q].z * f, acc[q].w * f);
+#pragma unroll
+            for (int i0 = 0; i0 < 8; i0 += 4) {
+                if (p0 + i0 >= most) break;
+                float4 v[4][4];  // a piece that is not there: row 0, with weight 0
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 *from = reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(FULL, at, i0 + i, 8), int64_t(0)) * D);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[i][q] = __ldcs(from + (4 * (sl + 8 * q) < D ? sl + 8 * q : 0));
                 }
-                for (int c = c0; c <= c1; ++c) {
-                    if (line_at(units, c, blocks) == line_at(units, c + 1, blocks)) continue;  // fewer tiles than blocks
-                    const int64_t r = piece_row(it, h, c, base, light) + in;
-                    const float s = a.part_lse[r];
-                    if (s == -INFINITY) continue;
-                    const float4 v = has ? *reinterpret_cast<const float4 *>(a.part + r * D + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    const float up = fmaxf(top, s), f = top == -INFINITY ? 0.f : ex2(top - up), y = ex2(s - up);
-                    total = total * f + y;
-                    acc[0] = acc[0] * f + v.x * y;
-                    acc[1] = acc[1] * f + v.y * y;
-                    acc[2] = acc[2] * f + v.z * y;
-                    acc[3] = acc[3] * f + v.w * y;
-                    top = up;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float wi = __shfl_sync(FULL, w, i0 + i, 8);
+                    total += wi;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float4 x = v[i][q];
+                        acc[q] = wi == 0.f ? acc[q] : make_float4(fmaf(x.x, wi, acc[q].x), fmaf(x.y, wi, acc[q].y), fmaf(x.z, wi, acc[q].z), fmaf(x.w, wi, acc[q].w));
+                    }
                 }
             }
         }
-        if (direct) continue;
-        const float f = total == 0.f ? 0.f : 1.f / total;
-        if (has) {
-            uint16_t *o = static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh + 4 * lane;
-            *reinterpret_cast<uint2 *>(o) = make_uint2(pack<BF>(acc[0] * f, acc[1] * f), pack<BF>(acc[2] * f, acc[3] * f));
-        }
-        if (lane == 0 && a.lse) a.lse[x] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+        if (row) put(t, qh, acc, total == 0.f ? 0.f : 1.f / total, total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f);
+    }
+    // query tokens of no entry
+    const bool order = b.n > 0 && plan.hdr[8];
+    const int first = order ? b.cu_q[0] : b.n_q, last = order ? b.cu_q[b.n] : b.n_q;
+    const int64_t rest = int64_t(first + b.n_q - last) * b.q_heads;
+    const float4 zero[4] = {};
+    for (int64_t x = int64_t(blockIdx.x) * 32 + warp * 4 + sub; x < rest; x += int64_t(gridDim.x) * 32) {
+        const int i = int(x / b.q_heads);
+        put(i < first ? i : i - first + last, int(x % b.q_heads), zero, 0.f, -INFINITY);
     }
 }
 
@@ -1018,8 +1128,14 @@ cudaError_t attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
             return cudaErrorInvalidValue;
     }
     const auto heavy = k_attend<DP, BF, true>, light = k_attend<DP, BF, false>;
-    cudaError_t e = cudaFuncSetAttribute((const void *)heavy, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP, true>::kAlloc);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute((const void *)light, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP, false>::kAlloc);
+    static thread_local int ready = -1;  // the device whose kernels have their shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev != ready) {
+        e = cudaFuncSetAttribute((const void *)heavy, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP, true>::kAlloc);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute((const void *)light, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP, false>::kAlloc);
+        if (e == cudaSuccess) ready = dev;
+    }
     if (e != cudaSuccess) return e;
     const int64_t rows = int64_t(b.n_q) * b.q_heads;
     if (rows / kv.n_kv_heads > kAttRows / 2)  // fewer rows make no heavy item
@@ -1027,7 +1143,7 @@ cudaError_t attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
     if (e == cudaSuccess)
         e = launch_chained(light, kv_blocks(a.sms, 1), Shape<DP, false>::kThreads, Shape<DP, false>::kAlloc, st, kv, b, a, maps[0], maps[1]);
     if (e != cudaSuccess) return e;
-    return launch_chained(k_combine<BF>, int(std::min<int64_t>((rows + 7) / 8, int64_t(a.sms) * 32)), 256, 0, st, kv, b, a);
+    return launch_chained(k_combine<BF>, int(std::min<int64_t>(rows, int64_t(a.sms) * 8)), 256, 0, st, kv, b, a);
 }
 
 }  // namespace
@@ -1037,7 +1153,7 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
         cudaError_t e = launch_chained(k_plan_shared, std::max((b.n + 7) / 8, 1), 256, 0, st, kv, b);
         if (e != cudaSuccess) return e;
     }
-    return launch_chained(k_plan_items, 1, kPlan, 0, st, kv, b);
+    return launch_chained(k_plan_items, 1, kPlan, 0, st, kv, b, kv_sm_count());
 }
 
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {

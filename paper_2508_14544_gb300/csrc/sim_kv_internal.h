@@ -79,16 +79,20 @@ struct alignas(16) KvItem {
     int64_t unit;     // tiles of the items before, all kv heads
     int64_t row_off;  // rows of the items before, all kv heads
     int32_t partial;  // its rows have another item too: always through the workspace
-    int32_t pad[3];
+    int32_t entry;    // entry of the batch, -1 for a group's prefix
+    int32_t pad[2];
 };
 static_assert(sizeof(KvItem) == 64, "KvItem");
 
 // Items of more than 128 rows are heavy, the others light: two lists, each divided among blocks of its own.
-// b->plan: header, per group the pages shared and its entries' tile rows, the first heavy and the first light item
-// of every source (groups, then entries, and the end), each entry's group and the pages that it shares with its
-// group's first entry, the items.
+// b->plan: header, where each block's stretch begins, per group the pages shared and its entries' tile rows, the
+// first heavy and the first light item of every source (groups, then entries, and the end), each entry's group and
+// the pages that it shares with its group's first entry, the items.
+constexpr int kKvMaxSms = 256;
 struct KvPlan {
-    int32_t *hdr;       // [0], [1] items, [2..3], [4..5] tiles in all (int64): heavy, light; [6..7] rows of the heavy items
+    int32_t *hdr;       // [0], [1] items, [2..3], [4..5] tiles in all (int64): heavy, light; [6..7] rows of the heavy items;
+                        // [8] offsets in order
+    int32_t *start[2];  // [kv_blocks] item in which each block's stretch begins
     int32_t *used;      // [n_groups]
     int32_t *alone;     // [n_groups]
     int32_t *first[2];  // [n_groups + n + 1]
@@ -103,13 +107,15 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     const int64_t G = b.q_heads / kv.n_kv_heads, src = int64_t(b.n_groups) + b.n;
     p.max_heavy = int32_t(2 * (int64_t(b.n_q) * G / (kAttRows / 2 + 1)) + 1);
     p.hdr = static_cast<int32_t *>(b.plan);
-    p.used = p.hdr + 16;
+    p.start[0] = p.hdr + 16;
+    p.start[1] = p.start[0] + kKvMaxSms;
+    p.used = p.start[1] + 2 * kKvMaxSms;
     p.alone = p.used + b.n_groups;
     p.first[0] = p.alone + b.n_groups;
     p.first[1] = p.first[0] + src + 1;
     p.group = p.first[1] + src + 1;
     p.same = p.group + b.n;
-    const int64_t ints = (16 + 2 * int64_t(b.n_groups) + 2 * (src + 1) + 2 * int64_t(b.n) + 3) / 4 * 4;
+    const int64_t ints = (16 + 3 * kKvMaxSms + 2 * int64_t(b.n_groups) + 2 * (src + 1) + 2 * int64_t(b.n) + 3) / 4 * 4;
     p.items[0] = reinterpret_cast<KvItem *>(static_cast<char *>(b.plan) + ints * 4);
     p.items[1] = p.items[0] + p.max_heavy;
     p.bytes = ints * 4 + (p.max_heavy + src) * int64_t(sizeof(KvItem));
@@ -133,6 +139,7 @@ struct KvAttend {
     int32_t layer;
     int32_t q_vec;           // q may be read 16 bytes at a time
     int32_t sms;
+    FastDiv group;           // query heads of a kv head
 };
 cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t st);
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st);

@@ -68,6 +68,8 @@ class KVCache:
             raise ValueError("sizes outside the cache's limits (see include/sim_kv.h)")
         self._scratch = torch.empty(size, dtype=torch.uint8, device=pool.device)
         self._kv.scratch = self._scratch.data_ptr()
+        self._index, self._dim = pool.device.index, dim
+        self._sizes = {}  # bytes of a plan and its workspace by the batch's sizes
         torch.cuda.current_stream(self.device).synchronize()  # the first call may be on any stream
 
     def _empty(self, stream, *shape, dtype):
@@ -80,9 +82,9 @@ class KVCache:
 
     def _stream(self, stream):
         import torch
-        if torch.cuda.current_device() != self.device.index:
+        if torch.cuda.current_device() != self._index:
             raise ValueError(f"the cache is on {self.device}, which is not the current device")
-        return torch._C._cuda_getCurrentRawStream(self.device.index) if stream is None else int(stream)
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else int(stream)
 
     def _done(self, rc):
         if rc != L.SIM_OK:
@@ -95,9 +97,10 @@ class KVCache:
         return x.data_ptr()
 
     def _rows(self, name, x, n, heads):
-        if x.dtype != self.dtype or x.device != self.device or x.shape != (n, heads, self._kv.head_dim) or x.stride(2) != 1:
-            raise ValueError(f"{name} must be {self.dtype} [{n}, {heads}, {self._kv.head_dim}] on {self.device}, the last dimension contiguous")
-        return x.data_ptr(), x.stride(0), x.stride(1)
+        token, head, last = x.stride() if x.dim() == 3 else (0, 0, 0)
+        if last != 1 or x.dtype != self.dtype or x.device != self.device or x.shape != (n, heads, self._dim):
+            raise ValueError(f"{name} must be {self.dtype} [{n}, {heads}, {self._dim}] on {self.device}, the last dimension contiguous")
+        return x.data_ptr(), token, head
 
     def check(self) -> None:
         """Raise if a call has been refused, in part or as a whole, since the last check (waits for the device)."""
@@ -166,14 +169,19 @@ class KVCache:
         all of them begin with are read once.  Valid until lengths or tables change."""
         import torch
         n, st = seqs.shape[0], self._stream(stream)
-        ng = 0 if cu_group is None else cu_group.shape[0] - 1
-        b = L.sim_kv_batch(n, n_q, heads, max(ng, 0), self._ints("seqs", seqs, n), self._ints("cu_q", cu_q, n + 1),
+        ng = 0 if cu_group is None else max(cu_group.shape[0] - 1, 0)
+        b = L.sim_kv_batch(n, n_q, heads, ng, self._ints("seqs", seqs, n), self._ints("cu_q", cu_q, n + 1),
                            None if cu_group is None else self._ints("cu_group", cu_group, ng + 1), None, None)
-        size = self._lib.sim_kv_plan_bytes(self._ref, ctypes.byref(b))
-        work = self._lib.sim_kv_workspace_bytes(self._ref, ctypes.byref(b))
-        size = (size + 255) // 256 * 256
-        buffer = self._empty(stream, size + work + 16, dtype=torch.uint8)
-        b.plan, b.workspace = buffer.data_ptr(), buffer.data_ptr() + size
+        sizes = self._sizes.get((n, n_q, heads, ng))
+        if sizes is None:
+            size = self._lib.sim_kv_plan_bytes(self._ref, ctypes.byref(b))
+            sizes = (size + 255) // 256 * 256, self._lib.sim_kv_workspace_bytes(self._ref, ctypes.byref(b))
+            if len(self._sizes) > 1000:
+                self._sizes.clear()
+            self._sizes[n, n_q, heads, ng] = sizes
+        buffer = self._empty(stream, sizes[0] + sizes[1] + 16, dtype=torch.uint8)
+        b.plan = buffer.data_ptr()
+        b.workspace = b.plan + sizes[0]
         plan = AttentionPlan(b, seqs, cu_q, cu_group, buffer)
         self._done(self._lib.sim_kv_plan(self._ref, plan._ref, st))
         return plan
@@ -182,14 +190,17 @@ class KVCache:
         """softmax(scale q k^T) v of queries [n_q, heads, head_dim] over the keys that each sees, and the log of the
         sum of exponentials [n_q, heads] (float32); scale is head_dim ** -0.5 by default."""
         import torch
-        st = self._stream(stream)
+        st, dim = self._stream(stream), self._dim
         rows = self._rows("q", q, plan.n_q, plan.heads)
         if out is None:
-            out = self._empty(stream, plan.n_q, plan.heads, self._kv.head_dim, dtype=self.dtype)
+            out = self._empty(stream, plan.n_q, plan.heads, dim, dtype=self.dtype)
+            to = out.data_ptr(), plan.heads * dim, dim
+        else:
+            to = self._rows("out", out, plan.n_q, plan.heads)
         if lse is None:
             lse = self._empty(stream, plan.n_q, plan.heads, dtype=torch.float32)
         elif lse.dtype != torch.float32 or lse.device != self.device or lse.shape != (plan.n_q, plan.heads) or not lse.is_contiguous():
             raise ValueError(f"lse must be a contiguous float32 tensor [{plan.n_q}, {plan.heads}] on {self.device}")
-        self._done(self._lib.sim_kv_attend(self._ref, plan._ref, layer, *rows, 1.0 / math.sqrt(self._kv.head_dim) if scale is None else scale,
-                                           *self._rows("out", out, plan.n_q, plan.heads), lse.data_ptr(), st))
+        self._done(self._lib.sim_kv_attend(self._ref, plan._ref, layer, *rows, 1.0 / math.sqrt(dim) if scale is None else scale,
+                                           *to, lse.data_ptr(), st))
         return out, lse
