@@ -15,7 +15,7 @@ INCLUDE = ROOT / "include"
 BUILD = PKG / "_build"
 LIB = BUILD / "libsim.so"
 SOURCES = ["sim_kernels.cu", "sim_stage.cu", "sim_api.cpp", "sim_noalloc.cu", "sim_analytic.cu", "sim_peaks.cu", "sim_kv.cu",
-           "sim_kv_attend.cu", "sim_kv_api.cpp"]
+           "sim_kv_attend.cu", "sim_kv_heavy.cu", "sim_kv_light.cu", "sim_kv_api.cpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -30,7 +30,7 @@ def _stale() -> bool:
     if not LIB.exists():
         return True
     t = LIB.stat().st_mtime
-    deps = [CSRC / s for s in SOURCES] + sorted(CSRC.glob("*.h")) + [Path(__file__)] + sorted(INCLUDE.glob("*.h"))
+    deps = [CSRC / s for s in SOURCES] + sorted(CSRC.glob("*.h")) + sorted(CSRC.glob("*.cuh")) + [Path(__file__)] + sorted(INCLUDE.glob("*.h"))
     return any(d.stat().st_mtime > t for d in deps)
 
 

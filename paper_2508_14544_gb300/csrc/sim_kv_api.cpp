@@ -62,6 +62,7 @@ const char *bad_batch_sizes(const sim_kv *kv, const sim_kv_batch *b) {
     if (!b) return "NULL batch";
     if (b->n < 0 || b->n > simgb::kKvMaxSeqs || b->n_groups < 0 || b->n_groups > b->n) return "n outside [0, 2^17] or n_groups outside [0, n]";
     if (b->q_heads < 1 || b->q_heads % kv->n_kv_heads) return "q_heads must be a positive multiple of n_kv_heads";
+    if (int64_t(b->n) * kv->n_kv_heads > 1 << 26) return "n * n_kv_heads > 2^26";
     if (b->n_q < 0 || int64_t(b->n_q) * b->q_heads > 1 << 30) return "n_q < 0 or n_q * q_heads > 2^30";
     return nullptr;
 }

@@ -1,0 +1,395 @@
+// Device code shared by the attention kernels over the paged cache (sim_kv_attend.cu, sim_kv_heavy.cu, sim_kv_light.cu).
+#pragma once
+
+#include <cuda.h>
+
+#include <climits>
+#include <cmath>
+
+#include "sim.h"
+#include "sim_kv_internal.h"
+
+namespace simgb {
+
+namespace {
+
+constexpr unsigned FULL = 0xffffffffu;
+constexpr int kStage = 128 * 17;       // floats through which the results of 128 rows pass
+constexpr int kSegs = 4;               // segments that the loading warp may be ahead
+constexpr float kGrow = 8.f;           // log2 of what P may reach before O is rescaled
+
+// A list's tiles divided among its blocks: [at(c), at(c + 1)) are block c's.  (With no division but one of small
+// numbers: code that runs once is paid for by its size.)
+struct Share {
+    int64_t units, each;  // units = each * blocks + rest
+    int rest, blocks;
+    __device__ Share() : units(0), each(0), rest(0), blocks(1) {}
+    __device__ Share(const KvPlan &p, int light, int sms) : blocks(kv_blocks(sms, light)) {
+        const int32_t *h = p.hdr + 16 * light;
+        units = *reinterpret_cast<const int64_t *>(h + 2);
+        each = *reinterpret_cast<const int64_t *>(h + 4);
+        rest = h[6];
+    }
+    __device__ int64_t at(int c) const { return each * c + uint32_t(rest * c) / uint32_t(blocks); }
+    __device__ int of(int64_t u) const {  // the block that has tile u
+        int c = min(int(float(u) * (float(blocks) / float(units))), blocks - 1);  // off by one at most
+        while (at(c + 1) <= u) ++c;
+        while (at(c) > u) --c;
+        return c;
+    }
+};
+
+// First row of the partial results of block c's piece of a list whose rows follow `base` others.
+__device__ __forceinline__ int64_t piece_row(const KvItem &it, int h, int c, int64_t base, int light) {
+    return base + it.row_off + int64_t(h) * it.rows + int64_t(light ? kAttRows / 2 : kAttRows) * c;
+}
+__device__ __forceinline__ int64_t list_base(const KvPlan &p, int light, int sms) {
+    return light ? *reinterpret_cast<const int64_t *>(p.hdr + 24) + int64_t(kAttRows) * kv_blocks(sms, 0) : 0;
+}
+
+// A stretch of one item and kv head, as the warps of a block pass it on.
+struct alignas(16) Segment {
+    int32_t n;               // tiles, 0: the end
+    int32_t h;
+    int32_t q0, row0, rows, pos0;
+    int32_t k0, kv1;         // first key, end of the keys
+    int32_t direct;          // results go to the output, not to the workspace
+    int32_t pad;
+    int64_t row;             // row of the partial results
+};
+
+// Walks the stretch of a list's line that is block c's.
+struct Line {
+    const KvItem *items;
+    KvItem it;
+    int64_t u, u1, base;
+    int n_items, heads, k, h, c, light;
+    __device__ Line(const KvPlan &p, int heads_, int light_, int c_, int sms) : items(p.items[light_]), heads(heads_), c(c_), light(light_) {
+        n_items = p.hdr[16 * light];
+        const Share share(p, light, sms);
+        u = share.at(c);
+        u1 = share.at(c + 1);
+        base = list_base(p, light, sms);
+        k = p.start[light][c];
+        h = -1;
+    }
+    // The next item and head with work for this block; s.n = 0 at the end.
+    __device__ void next(Segment &s) {
+        s.n = 0;
+        while (u < u1 && k < n_items) {
+            if (h < 0) it = items[k];
+            if (it.tiles == 0 || h + 1 == heads) {
+                ++k;
+                h = -1;
+                continue;
+            }
+            h = h < 0 ? int(uint32_t(u - it.unit) / uint32_t(it.tiles)) : h + 1;
+            const int64_t a = it.unit + int64_t(h) * it.tiles;
+            const int t0 = int(u - a), t1 = int(min(u1 - a, int64_t(it.tiles)));
+            s.n = t1 - t0;
+            s.h = h;
+            s.q0 = it.q0;
+            s.row0 = it.row0;
+            s.rows = it.rows;
+            s.pos0 = it.pos0;
+            s.k0 = it.kv0 + t0 * kv_tile(light);
+            s.kv1 = it.kv1;
+            s.direct = s.n == it.tiles && !it.partial;
+            s.row = piece_row(it, h, c, base, light);
+            u = a + t1;
+            return;
+        }
+    }
+};
+
+// ---- PTX ----------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+// Waits for the phase of that parity to end; gives up after about a second, or when another warp has.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+    if (bar_try(bar, parity)) return true;
+    const long long start = clock64();
+    while (!bar_try(bar, parity)) {
+        if (*gave_up) return false;
+        if (clock64() - start > 2000000000LL) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(p));
+    return p;
+}
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z, int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void smem_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// D (TMEM) = A (shared memory) B (shared memory), 16 of the inner dimension.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        : "memory");
+}
+// A from TMEM.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        : "memory");
+}
+
+#define REG4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define VAL4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
+__device__ __forceinline__ void tm_ld32(uint32_t addr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : REG4(r, 0), REG4(r, 4), REG4(r, 8), REG4(r, 12), REG4(r, 16), REG4(r, 20), REG4(r, 24), REG4(r, 28)
+        : "r"(addr));
+}
+__device__ __forceinline__ void tm_ld16(uint32_t addr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : REG4(r, 0), REG4(r, 4), REG4(r, 8), REG4(r, 12)
+        : "r"(addr));
+}
+__device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        VAL4(r, 0), VAL4(r, 4), VAL4(r, 8), VAL4(r, 12), VAL4(r, 16), VAL4(r, 20), VAL4(r, 24), VAL4(r, 28)
+        : "memory");
+}
+__device__ __forceinline__ void tm_st8(uint32_t addr, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), VAL4(r, 0), VAL4(r, 4) : "memory");
+}
+#undef REG4
+#undef VAL4
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\t"
+        "mov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, w;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 w, x, y;\n\t"
+        "mov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    if (BF) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Shared-memory operand: 128-byte rows, 8 rows of 1024 bytes swizzled as one; `sbo` bytes between groups of 8
+// rows, `lbo` between 64-column blocks where the long dimension is the contiguous one.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+    return uint64_t((addr >> 4) & 0x3fff) | uint64_t(lbo >> 4) << 16 | uint64_t(sbo >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+
+// ---- softmax ------------------------------------------------------------------------------------------------
+
+// A tile of NK keys: S (columns t_s on) becomes P in 16 bits, in the same columns.  Every row lies in R lanes, one
+// in each of R warps (1 or 4); warp w takes NK / R keys of its rows and leaves zeros for the others.  lim: the last
+// of this thread's keys that its row sees.  m, l: the maximum that P refers to and the sum so far of this
+// thread's keys; DP columns of O from t_o on.
+template <int NK, int R, int DP, bool BF>
+__device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, int lim, bool first, float c, float &m, float &l) {
+    constexpr int NC = NK / R;
+    static_assert(R == 1 || (R == 4 && NC == 16), "copies");
+    const int c0 = R == 4 ? w * NC : 0;
+    uint32_t s[NC];
+    if constexpr (NC == 16) {
+        tm_ld16(t_s + c0, s);
+    } else {
+#pragma unroll
+        for (int q = 0; q < NC / 32; ++q) tm_ld32(t_s + c0 + 32 * q, s + 32 * q);
+    }
+    tc_wait_ld();
+    if (__any_sync(FULL, lim < NC - 1)) {
+#pragma unroll
+        for (int y = 0; y < NC; ++y)
+            if (y > lim) s[y] = 0xff800000u;
+    }
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int y = 0; y < NC; y += 2) top[y / 2 & 3] = max3(top[y / 2 & 3], __uint_as_float(s[y]), __uint_as_float(s[y + 1]));
+    const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    if (first) {
+        m = mx;
+    } else if (__any_sync(FULL, (mx - m) * c > kGrow)) {
+        const float up = fmaxf(m, mx), f = up == m ? 1.f : ex2((m - up) * c);
+        m = up;
+        l *= f;
+#pragma unroll 1
+        for (int q = 0; q < DP / 32; ++q) {
+            uint32_t o[32];
+            tm_ld32(t_o + 32 * q, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+            tm_st32(t_o + 32 * q, o);
+        }
+    }
+    const float off = m == -INFINITY ? 0.f : m * c;
+    float2 sum[4] = {};
+    uint32_t pk[NC / 2];
+#pragma unroll
+    for (int y = 0; y < NC; y += 2) {
+        float2 e = fma2(make_float2(__uint_as_float(s[y]), __uint_as_float(s[y + 1])), make_float2(c, c), make_float2(-off, -off));
+        e = make_float2(ex2(e.x), ex2(e.y));
+        sum[y / 2 & 3] = add2(sum[y / 2 & 3], e);
+        pk[y / 2] = pack<BF>(e.x, e.y);
+    }
+    sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+    l += sum[0].x + sum[0].y;
+    if constexpr (R == 1) {
+#pragma unroll
+        for (int q = 0; q < NC / 64; ++q) tm_st32(t_s + 32 * q, pk + 32 * q);
+    } else {
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            uint32_t z[NC / 2];
+#pragma unroll
+            for (int y = 0; y < NC / 2; ++y) z[y] = q == w ? pk[y] : 0;
+            tm_st8(t_s + 8 * q, z);
+        }
+    }
+    tc_wait_st();
+}
+
+// Where the results of a segment go.
+template <bool BF>
+struct Sink {
+    const KvAttend &a;
+    const Segment &sg;
+    int G, D, q_heads;
+    __device__ uint16_t *out_row(int y) const {  // of row y of the item
+        const int t = a.group.div(sg.row0 + y);
+        return static_cast<uint16_t *>(a.out) + int64_t(sg.q0 + t) * a.ot + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.oh;
+    }
+    __device__ void lse(int y, float top, float total) const {
+        const float e = total == 0.f ? -INFINITY : top * a.scale_log2 + log2f(total);
+        if (!sg.direct) {
+            a.part_lse[sg.row + y] = e;
+        } else if (a.lse) {
+            const int t = a.group.div(sg.row0 + y);
+            a.lse[int64_t(sg.q0 + t) * q_heads + sg.h * G + (sg.row0 + y - t * G)] = e * 0.69314718055994531f;
+        }
+    }
+    // A warp's 32 rows from row0 on, 16 columns at a time through `mine` (32 x 17 floats), so that stores fill sectors;
+    // f is what the lane's row is multiplied by, empty: it has seen no key.
+    template <int DP>
+    __device__ void warp_rows(uint32_t t_o, float *mine, int row0, int rows, float f, bool empty) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll 1
+        for (int d0 = 0; d0 < DP && d0 < D; d0 += 16) {
+            uint32_t o[16];
+            tm_ld16(t_o + d0, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 16; ++y) mine[lane * 17 + y] = empty ? 0.f : __uint_as_float(o[y]) * f;
+            __syncwarp();
+            if (sg.direct) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int y = q * 16 + lane / 2, d = lane % 2 * 8;
+                    const float *v = mine + y * 17 + d;
+                    if (row0 + y < rows && d0 + d < D)
+                        *reinterpret_cast<uint4 *>(out_row(row0 + y) + d0 + d) = make_uint4(pack<BF>(v[0], v[1]), pack<BF>(v[2], v[3]), pack<BF>(v[4], v[5]), pack<BF>(v[6], v[7]));
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int y = q * 8 + lane / 4, d = lane % 4 * 4;
+                    const float *v = mine + y * 17 + d;
+                    if (row0 + y < rows && d0 + d < D)
+                        *reinterpret_cast<float4 *>(a.part + (sg.row + row0 + y) * D + d0 + d) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            }
+            __syncwarp();
+        }
+    }
+};
+
+}  // namespace
+
+// Tensor maps of one layer's keys and values, [page][head][token][dim], with boxes of up to kAttTile (light: 64)
+// tokens of one page and head and 64 columns.
+struct KvMaps {
+    CUtensorMap keys, values;
+};
+cudaError_t launch_kv_heavy(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
+cudaError_t launch_kv_light(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
+
+}  // namespace simgb

@@ -1,0 +1,330 @@
+// Attention of heavy items (129 .. 256 query rows; see sim_kv_attend.cu), bound by the tensor products.
+//
+// One block per SM, two groups of four softmax warps with 128 rows each.  Both groups use every tile of 128 keys,
+// so a byte that enters shared memory serves 256 rows; the tensor unit works for one group while the other is in its
+// softmax.  Per tile and group: S = Q K^T (128 x 128 x D, operands in shared memory), P = exp2(c (S - m)) written over
+// S in TMEM as 16 bits, O += P V (128 x D x 128, P from TMEM, V as it lies, the N dimension contiguous).  TMEM is full:
+// 128 columns each for S / P and O of the two groups.
+#include "sim_kv_attend.cuh"
+
+namespace simgb {
+
+namespace {
+
+// ---- k_attend -----------------------------------------------------------------------------------------------
+
+template <int DP>
+struct Shape {
+    static constexpr int kGroups = 2;
+    static constexpr int kThreads = kGroups * 128 + 128;
+    static constexpr int kTile = DP * 256;                                    // bytes of 128 query rows, or of a tile of keys or values
+    static constexpr int kHalf = 16384;                                       // 128 rows of 64 columns
+    static constexpr int kSlots = 131072 / kTile;                             // tiles of keys or values in flight
+    static constexpr int kTmem = 512;
+    static constexpr int kOffO = kGroups * 128;                               // TMEM column of the first group's O
+    static constexpr int kSoftRegs = 208, kOtherRegs = 88;
+    static_assert(kGroups * kSoftRegs + kOtherRegs <= (kGroups + 1) * 168, "the launch gives 168 registers a thread: no more are handed out");
+    static constexpr int kOffRing = kGroups * kTile;
+    static constexpr int kOffStage = kOffRing + kSlots * kTile;
+    static constexpr int kOffSeg = kOffStage + kGroups * kStage * 4;
+    static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
+    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 3 * kGroups + 1;
+    static constexpr int kBytes = kOffBar + kBars * 8 + 16;
+    static constexpr int kAlloc = kBytes + 1024;                              // the base is rounded up to 1024
+    static_assert(kAlloc <= 232448, "shared memory");
+};
+
+template <int DP, bool BF>
+__global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
+    k_heavy(const sim_kv kv, const sim_kv_batch b, const KvAttend a, const __grid_constant__ KvMaps maps) {
+    using Sh = Shape<DP>;
+    constexpr int NS = Sh::kSlots, NG = Sh::kGroups;
+    extern __shared__ unsigned char raw[];
+    unsigned char *const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+    const uint32_t sbase = smem_addr(base), bars = sbase + Sh::kOffBar;
+    volatile int *const gave_up = reinterpret_cast<int *>(base + Sh::kOffBar + Sh::kBars * 8);
+    uint32_t *const tmem_at = reinterpret_cast<uint32_t *>(base + Sh::kOffBar + Sh::kBars * 8 + 4);
+    Segment *const segs = reinterpret_cast<Segment *>(base + Sh::kOffSeg);
+    const auto full = [&](uint32_t x) { return bars + 8 * (x % NS); };
+    const auto empty = [&](uint32_t x) { return bars + 8 * (NS + x % NS); };
+    const auto seg_full = [&](uint32_t x) { return bars + 8 * (2 * NS + x % kSegs); };
+    const auto seg_empty = [&](uint32_t x) { return bars + 8 * (2 * NS + kSegs + x % kSegs); };
+    constexpr int kRest = 2 * NS + 2 * kSegs;
+    const uint32_t q_full = bars + 8 * kRest, q_empty = bars + 8 * (kRest + 1);
+    const auto s_full = [&](int g) { return bars + 8 * (kRest + 2 + g); };
+    const auto p_ready = [&](int g) { return bars + 8 * (kRest + 2 + NG + g); };
+    const auto o_full = [&](int g) { return bars + 8 * (kRest + 2 + 2 * NG + g); };
+    const uint32_t drained = bars + 8 * (kRest + 2 + 3 * NG);
+    const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31, role = warp - 4 * NG;
+
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) {
+            bar_init(full(s), 1);
+            bar_init(empty(s), 1);
+        }
+        for (int s = 0; s < kSegs; ++s) {
+            bar_init(seg_full(s), 1);
+            bar_init(seg_empty(s), 4 * NG + 3);
+        }
+        bar_init(q_full, 2);
+        bar_init(q_empty, 1);
+        for (int g = 0; g < NG; ++g) {
+            bar_init(s_full(g), 1);
+            bar_init(p_ready(g), 4);
+            bar_init(o_full(g), 1);
+        }
+        bar_init(drained, 1);
+        *gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (role == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "n"(Sh::kTmem) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(FULL, *tmem_at, 0);
+    kv_wait_previous();
+
+    const int G = b.q_heads / kv.n_kv_heads, D = kv.head_dim;
+    // Segment number x, for the warps that are told of it; empty if the wait gave up.
+    const auto take = [&](uint32_t x, Segment &s) {
+        const bool ok = __all_sync(FULL, bar_wait(seg_full(x), (x / kSegs) & 1, gave_up));
+        if (ok) s = segs[x % kSegs];
+        else s.n = 0;
+        __syncwarp();
+        if (lane == 0) bar_arrive(seg_empty(x));
+        return ok;
+    };
+
+    if (role >= 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOtherRegs));
+        if (role == 0) {
+            // ---- the line of work, and loads: lane l brings page l of each tile
+            const KvPlan plan = kv_plan(kv, b);
+            Line line(plan, kv.n_kv_heads, 0, blockIdx.x, a.sms);
+            const int P = kv.page_size, per = kv_tile(0) / P;
+            uint32_t at = 0;  // tiles loaded
+            bool ok = true;
+            for (uint32_t x = 0; ok; ++x) {
+                Segment sg;
+                line.next(sg);
+                ok = __all_sync(FULL, bar_wait(seg_empty(x), (x / kSegs + 1) & 1, gave_up));
+                if (!ok) break;
+                if (lane == 0) {
+                    segs[x % kSegs] = sg;
+                    bar_arrive(seg_full(x));
+                }
+                if (sg.n == 0) break;
+                const int32_t *row = kv.table + int64_t(line.it.seq) * kv.max_pages;
+                const int first = sg.k0 / P + lane;
+                const auto page_of = [&](int j) {  // of this lane in tile j; past the keys: none, zeros
+                    const int idx = first + j * per;
+                    return lane < per && j < sg.n && idx * P < sg.kv1 ? row[idx] : -1;
+                };
+                int page = page_of(0);
+                for (int j = 0; j < sg.n && ok; ++j) {
+                    const int next_page = page_of(j + 1);
+                    const int w = unsigned(page) < unsigned(kv.n_pages) ? page : kv.n_pages;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v, ++at) {  // keys, values
+                        ok = __all_sync(FULL, bar_wait(empty(at), (at / NS + 1) & 1, gave_up));
+                        if (!ok) break;
+                        if (lane == 0) bar_expect(full(at), Sh::kTile);
+                        __syncwarp();
+                        if (lane < per) {
+                            const uint32_t dst = sbase + Sh::kOffRing + (at % NS) * Sh::kTile + lane * P * 128;
+#pragma unroll
+                            for (int half = 0; half < DP / 64; ++half)
+                                tma_load(dst + half * Sh::kHalf, v ? &maps.values : &maps.keys, full(at), half * 64, 0, sg.h, w);
+                        }
+                    }
+                    page = next_page;
+                }
+            }
+            if (!ok) {  // let what is on its way arrive
+                for (uint32_t k = at > NS ? at - NS : 0; k < at; ++k)
+                    for (int n = 0; n < 1000000 && !bar_try(full(k), (k / NS) & 1); ++n) {
+                    }
+                if (lane == 0) atomicMin(kv.status, SIM_E_STATE);
+            }
+        } else if (role == 1) {
+            // ---- tensor products: the whole warp keeps the same (uniform) state, one lane issues
+            const uint32_t type = BF ? 1u << 7 | 1u << 10 : 0u;
+            const uint32_t idesc_s = 1u << 4 | type | (128 / 8) << 17 | (128 / 16) << 24;
+            const uint32_t idesc_o = 1u << 4 | type | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
+            const uint64_t op_q = operand(sbase, 16, 1024), op_k = operand(sbase + Sh::kOffRing, 16, 1024), op_v = operand(sbase + Sh::kOffRing, Sh::kHalf, 1024);
+            uint32_t at = 0, np = 0;
+            bool ok = true;
+            const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, bar_wait(bar, parity, gave_up)) != 0; };
+            const auto wait_full = [&](uint32_t y) { return wait(full(y), (y / NS) & 1); };
+            Segment sg;
+            for (uint32_t x = 0; (ok = take(x, sg)); ++x) {
+                const int n = __shfl_sync(FULL, sg.n, 0);
+                if (n == 0) break;
+                const auto keys = [&](int j, int g) {  // S of group g and tile j
+                    if (elect_one()) {
+                        const uint32_t slot = (at + 2 * j) % NS;
+#pragma unroll
+                        for (int kk = 0; kk < DP / 16; ++kk) {
+                            const uint32_t off = (kk / 4) * Sh::kHalf + (kk % 4) * 32;
+                            mma_ss(tmem + g * 128, op_q + ((g * Sh::kTile + off) >> 4), op_k + ((slot * Sh::kTile + off) >> 4), idesc_s, kk > 0);
+                        }
+                        tc_commit(s_full(g));
+                        if (g == NG - 1) {
+                            tc_commit(empty(at + 2 * j));
+                            if (j == n - 1) tc_commit(q_empty);
+                        }
+                    }
+                    __syncwarp();
+                };
+                ok = wait(q_full, x & 1) && wait_full(at);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int g = 0; g < NG; ++g) keys(0, g);
+                for (int j = 0; j < n && ok; ++j, ++np) {
+                    ok = wait_full(at + 2 * j + 1);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        ok = ok && wait(p_ready(g), np & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t slot = (at + 2 * j + 1) % NS;
+#pragma unroll
+                            for (int kk = 0; kk < kv_tile(0) / 16; ++kk)
+                                mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + kk * 8, op_v + ((slot * Sh::kTile + kk * 2048) >> 4), idesc_o, j > 0 || kk > 0);
+                            if (g == NG - 1) tc_commit(empty(at + 2 * j + 1));
+                            if (j + 1 == n) tc_commit(o_full(g));
+                        }
+                        __syncwarp();
+                        if (j + 1 < n) {
+                            if (g == 0) ok = wait_full(at + 2 * j + 2);
+                            if (!ok) break;
+                            keys(j + 1, g);
+                        }
+                    }
+                }
+                if (!ok) break;
+                at += 2 * n;
+            }
+            if (!ok) {
+                if (elect_one()) {
+                    tc_commit(drained);
+                    atomicMin(kv.status, SIM_E_STATE);
+                }
+                __syncwarp();
+                for (int n = 0; n < 1000000 && !bar_try(drained, 0); ++n) {
+                }
+            }
+            __syncwarp();
+        } else {
+            // ---- query rows: two warps, 16 bytes a lane, the lanes of a row side by side.  Rows past the item's are
+            // left as they are: what they hold meets no other row and is masked.
+            constexpr int kVec = DP / 8, kStep = 64 / kVec;
+            const int j = (tid & 63) % kVec;
+            const bool has = j * 8 < D;
+            Segment sg;
+            for (uint32_t x = 0; take(x, sg) && sg.n > 0; ++x) {
+                const uint16_t *const from0 = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0) * a.qt + int64_t(sg.h * G) * a.qh + (has ? j * 8 : 0);
+                if (!__all_sync(FULL, bar_wait(q_empty, (x + 1) & 1, gave_up))) break;
+#pragma unroll 4
+                for (int r = (tid & 63) / kVec; r < sg.rows; r += kStep) {
+                    const int y = sg.row0 + r, t = a.group.div(y);
+                    const uint16_t *from = from0 + int64_t(t) * a.qt + int64_t(y - t * G) * a.qh;
+                    const uint32_t to = sbase + (r >> 7) * Sh::kTile + (j / 8) * Sh::kHalf + (r & 127) * 128 + (((j % 8) ^ (r & 7)) << 4);
+                    if (a.q_vec) {
+                        const int bytes = has ? 16 : 0;  // columns past the head's are zeros
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+                    } else {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (has)
+                            v = make_uint4(from[0] | uint32_t(from[1]) << 16, from[2] | uint32_t(from[3]) << 16, from[4] | uint32_t(from[5]) << 16,
+                                           from[6] | uint32_t(from[7]) << 16);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+                    }
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                smem_to_async();
+                __syncwarp();
+                if (lane == 0) bar_arrive(q_full);
+            }
+        }
+    } else {
+        // ---- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kSoftRegs));
+        const int g = warp >> 2, w = warp & 3, lr = tid & 127;
+        const uint32_t t_lane = tmem + (uint32_t(w * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + Sh::kOffO + g * 128;
+        float *const stage = reinterpret_cast<float *>(base + Sh::kOffStage) + g * kStage;
+        const float c = a.scale_log2;
+        uint32_t ns = 0, at = 0;
+        bool ok = true;
+        Segment sg;
+        for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
+            const int r = g * 128 + lr;  // the row in this thread's lane
+            const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : -1;  // key position that it sees last
+            float m = -INFINITY, l = 0.f;
+            for (int j = 0; j < sg.n; ++j) {
+                const int k0 = sg.k0 + j * kv_tile(0);  // first key of the tile
+                ok = __all_sync(FULL, bar_wait(s_full(g), ns & 1, gave_up));
+                if (!ok) break;
+                ++ns;
+                tc_fence_after();
+                softmax_tile<128, 1, DP, BF>(t_s, t_o, w, last - k0, j == 0, c, m, l);
+                // values past the end of the keys, whatever they are, must not meet their zero probabilities
+                const int valid = sg.kv1 - k0;
+                if (valid < kv_tile(0) && g == 0) {
+                    const uint32_t y = at + 2 * j + 1;
+                    ok = __all_sync(FULL, bar_wait(full(y), (y / NS) & 1, gave_up));
+                    if (lr >= valid) {
+                        unsigned char *v = base + Sh::kOffRing + (y % NS) * Sh::kTile + lr * 128;
+#pragma unroll
+                        for (int z = 0; z < DP / 8; ++z) *reinterpret_cast<uint4 *>(v + (z / 8) * Sh::kHalf + (z % 8) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    smem_to_async();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_ready(g));
+            }
+            if (!ok) break;
+            at += 2 * sg.n;
+            const Sink<BF> sink = {a, sg, G, D, b.q_heads};
+            if (r < sg.rows) sink.lse(r, m, l);
+            ok = __all_sync(FULL, bar_wait(o_full(g), x & 1, gave_up));
+            if (!ok) break;
+            tc_fence_after();
+            sink.template warp_rows<DP>(t_o, stage + w * 32 * 17, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+            tc_fence_before();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (role == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Sh::kTmem));
+    }
+}
+
+template <int DP, bool BF>
+cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st) {
+    static thread_local int ready = -1;  // the device on which the kernel has its shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev != ready) {
+        e = cudaFuncSetAttribute((const void *)k_heavy<DP, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kAlloc);
+        if (e == cudaSuccess) ready = dev;
+    }
+    return e == cudaSuccess ? launch_chained(k_heavy<DP, BF>, kv_blocks(a.sms, 0), Shape<DP>::kThreads, Shape<DP>::kAlloc, st, kv, b, a, maps) : e;
+}
+
+}  // namespace
+
+cudaError_t launch_kv_heavy(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st) {
+    if (kv.dtype == SIM_KV_BF16) return kv.head_dim > 64 ? launch<128, true>(kv, b, a, maps, st) : launch<64, true>(kv, b, a, maps, st);
+    return kv.head_dim > 64 ? launch<128, false>(kv, b, a, maps, st) : launch<64, false>(kv, b, a, maps, st);
+}
+
+}  // namespace simgb

@@ -64,8 +64,9 @@ struct KvWrite {
 };
 cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st);
 
-constexpr int kAttTile = 128;  // keys of a tile
 constexpr int kAttRows = 256;  // query rows of an item, at most
+// Items of more than 128 rows are heavy, the others light: two lists, each divided among blocks of its own.
+__host__ __device__ constexpr int kv_tile(int light) { return light ? 64 : 128; }  // keys of a tile
 
 // A run of query rows (token x head of the group, for every kv head alike) against a range of one table's keys.
 struct alignas(16) KvItem {
@@ -84,15 +85,15 @@ struct alignas(16) KvItem {
 };
 static_assert(sizeof(KvItem) == 64, "KvItem");
 
-// Items of more than 128 rows are heavy, the others light: two lists, each divided among blocks of its own.
 // b->plan: header, where each block's stretch begins, per group the pages shared and its entries' tile rows, the
 // first heavy and the first light item of every source (groups, then entries, and the end), each entry's group and
 // the pages that it shares with its group's first entry, the items.
 constexpr int kKvMaxSms = 256;
 struct KvPlan {
-    int32_t *hdr;       // [0], [1] items, [2..3], [4..5] tiles in all (int64): heavy, light; [6..7] rows of the heavy items;
-                        // [8] offsets in order
+    int32_t *hdr;       // heavy, and 16 further light: [0] items, [2..3] tiles in all, [4..5] of each block, [6] left over;
+                        // [1] offsets in order, [24..25] rows of the heavy items
     int32_t *start[2];  // [kv_blocks] item in which each block's stretch begins
+    int32_t *cut[2];    // [kv_blocks] item (without a prefix) and kv head whose first cut is where the stretch begins, or -1
     int32_t *used;      // [n_groups]
     int32_t *alone;     // [n_groups]
     int32_t *first[2];  // [n_groups + n + 1]
@@ -107,15 +108,17 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     const int64_t G = b.q_heads / kv.n_kv_heads, src = int64_t(b.n_groups) + b.n;
     p.max_heavy = int32_t(2 * (int64_t(b.n_q) * G / (kAttRows / 2 + 1)) + 1);
     p.hdr = static_cast<int32_t *>(b.plan);
-    p.start[0] = p.hdr + 16;
+    p.start[0] = p.hdr + 32;
     p.start[1] = p.start[0] + kKvMaxSms;
-    p.used = p.start[1] + 2 * kKvMaxSms;
+    p.cut[0] = p.start[1] + 2 * kKvMaxSms;  // two numbers each
+    p.cut[1] = p.cut[0] + 2 * kKvMaxSms;
+    p.used = p.cut[1] + 4 * kKvMaxSms;
     p.alone = p.used + b.n_groups;
     p.first[0] = p.alone + b.n_groups;
     p.first[1] = p.first[0] + src + 1;
     p.group = p.first[1] + src + 1;
     p.same = p.group + b.n;
-    const int64_t ints = (16 + 3 * kKvMaxSms + 2 * int64_t(b.n_groups) + 2 * (src + 1) + 2 * int64_t(b.n) + 3) / 4 * 4;
+    const int64_t ints = (32 + 9 * kKvMaxSms + 2 * int64_t(b.n_groups) + 2 * (src + 1) + 2 * int64_t(b.n) + 3) / 4 * 4;
     p.items[0] = reinterpret_cast<KvItem *>(static_cast<char *>(b.plan) + ints * 4);
     p.items[1] = p.items[0] + p.max_heavy;
     p.bytes = ints * 4 + (p.max_heavy + src) * int64_t(sizeof(KvItem));
