@@ -130,7 +130,7 @@ int sim_kv_compact(const sim_kv *kv, int32_t *to, void *cuda_stream) {
     return done(simgb::launch_kv_compact(*kv, to, static_cast<cudaStream_t>(cuda_stream)), "sim_kv_compact");
 }
 
-int64_t sim_kv_plan_bytes(const sim_kv *kv, const sim_kv_batch *b) { return bad_batch_sizes(kv, b) ? 0 : simgb::kv_plan(*kv, *b).bytes; }
+int64_t sim_kv_plan_bytes(const sim_kv *kv, const sim_kv_batch *b) { return bad_batch_sizes(kv, b) ? 0 : (simgb::kv_plan(*kv, *b).bytes + 15) / 16 * 16; }
 
 int64_t sim_kv_workspace_bytes(const sim_kv *kv, const sim_kv_batch *b) {
     return bad_batch_sizes(kv, b) ? 0 : simgb::kv_partial_rows(*b, simgb::kv_sm_count()) * (kv->head_dim + 1) * 4;

@@ -95,30 +95,29 @@ __global__ void __launch_bounds__(256) k_plan_shared(const sim_kv kv, const sim_
     if (lane == 0) p.same[i] = same;
 }
 
-__device__ __noinline__ int64_t plan_scan(int64_t v, int64_t *sums, int64_t &total) {
+// Exclusive prefix sums of two values per thread, and the totals.
+struct Two {
+    int64_t a, b;
+};
+__device__ __forceinline__ Two plan_scan(Two v, Two *sums, Two &total) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    int64_t x = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int64_t y = __shfl_up_sync(FULL, x, d);
-        if (lane >= d) x += y;
-    }
+    const auto scan = [&](Two x) {
+#pragma unroll 1
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t y = __shfl_up_sync(FULL, x.a, d), z = __shfl_up_sync(FULL, x.b, d);
+            if (lane >= d) x = {x.a + y, x.b + z};
+        }
+        return x;
+    };
+    const Two x = scan(v);
     if (lane == 31) sums[w] = x;
     __syncthreads();
-    if (w == 0) {
-        int64_t s = sums[lane];
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t y = __shfl_up_sync(FULL, s, d);
-            if (lane >= d) s += y;
-        }
-        sums[lane] = s;
-    }
+    if (w == 0) sums[lane] = scan(sums[lane]);
     __syncthreads();
     total = sums[31];
-    const int64_t before = (w ? sums[w - 1] : 0) + x - v;
+    const Two before = w ? sums[w - 1] : Two{0, 0};
     __syncthreads();
-    return before;
+    return {before.a + x.a - v.a, before.b + x.b - v.b};
 }
 
 // Tile rows of 128 that r query rows take: two where they are more than 128 in their block of 256.
@@ -129,30 +128,52 @@ __device__ __forceinline__ int tile_rows(int r) {
 __device__ __forceinline__ int heavy_items(int r) { return r / kAttRows + (r % kAttRows > kAttRows / 2); }
 __device__ __forceinline__ int light_items(int r) { return r % kAttRows > 0 && r % kAttRows <= kAttRows / 2; }
 
-// One block: which prefixes are shared, the items of every source (a group's prefix, an entry's own keys), and
-// where each begins on its list's line of work.
+constexpr int kFewSources = 480, kFewItems = 1024;
+
+// The last of n + 1 ascending numbers x[0] .. x[n] that is at most v, below n.
+template <typename T>
+__device__ __forceinline__ int last_at_most(const T *x, int n, T v) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (x[mid] <= v) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// One block: which prefixes are shared, the sources and items, and where each begins on its list's line of work.
+// FEW: what the searches read is in shared memory (the steps are a chain of dependent loads).
+template <bool FEW>
 __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim_kv_batch b, int sms) {
-    __shared__ int64_t sums[32];
+    __shared__ Two sums[32];
+    __shared__ KvSource few_sources[FEW ? kFewSources : 1];
+    __shared__ int32_t few_first[FEW ? 2 : 1][FEW ? kFewSources + 1 : 1], few_used[FEW ? kFewSources : 1], few_alone[FEW ? kFewSources : 1];
+    __shared__ int64_t few_units[FEW ? kFewItems : 1];
     kv_wait_previous();
     const KvPlan p = kv_plan(kv, b);
+    KvSource *const source = FEW ? few_sources : p.source;
+    int32_t *const used = FEW ? few_used : p.used, *const alone = FEW ? few_alone : p.alone;
+    int32_t *const first0 = FEW ? few_first[0] : p.first[0], *const first1 = FEW ? few_first[FEW ? 1 : 0] : p.first[1];
     const int tid = threadIdx.x, ng = b.n_groups, n_src = ng + b.n, G = b.q_heads / kv.n_kv_heads, P = kv.page_size;
     // Offsets that are not in order: no queries at all, or no groups.
     bool order = true, groups = true, known = true;
+#pragma unroll 1
     for (int i = tid; i < b.n; i += kPlan) {
         order = order && 0 <= b.cu_q[i] && b.cu_q[i] <= b.cu_q[i + 1] && b.cu_q[i + 1] <= b.n_q;
         known = known && unsigned(b.seqs[i]) < unsigned(kv.max_seqs);
     }
-    for (int g = tid; g < ng; g += kPlan) groups = groups && 0 <= b.cu_group[g] && b.cu_group[g] <= b.cu_group[g + 1] && b.cu_group[g + 1] <= b.n;
+#pragma unroll 1
+    for (int g = tid; g < ng; g += kPlan) {
+        groups = groups && 0 <= b.cu_group[g] && b.cu_group[g] <= b.cu_group[g + 1] && b.cu_group[g + 1] <= b.n;
+        used[g] = INT_MAX;
+        alone[g] = 0;
+    }
     if (!order || !groups || !known) atomicMin(kv.status, SIM_E_INVAL);
     order = __syncthreads_and(order);
     groups = __syncthreads_and(groups);
-    const auto group_tokens = [&](int g) { return b.cu_q[b.cu_group[g + 1]] - b.cu_q[b.cu_group[g]]; };
     if (ng > 0) {
-        for (int g = tid; g < ng; g += kPlan) {
-            p.used[g] = INT_MAX;
-            p.alone[g] = 0;
-        }
-        __syncthreads();
+#pragma unroll 1
         for (int i0 = 0; i0 < b.n; i0 += kPlan) {  // the least number of pages of each group, the sum of its tile rows
             const int i = i0 + tid, g = i < b.n ? group_of(b, i) : -1, v = g < 0 ? INT_MAX : p.same[i];
             const int t = g < 0 ? 0 : tile_rows(entry_at(kv, b, i).t * G);
@@ -161,264 +182,324 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
             if (same_group) {
                 const int least = __reduce_min_sync(FULL, v), all = __reduce_add_sync(FULL, t);
                 if (g >= 0 && (tid & 31) == 0) {
-                    atomicMin(&p.used[g], least);
-                    atomicAdd(&p.alone[g], all);
+                    atomicMin(&used[g], least);
+                    atomicAdd(&alone[g], all);
                 }
             } else if (g >= 0) {
-                atomicMin(&p.used[g], v);
-                atomicAdd(&p.alone[g], t);
+                atomicMin(&used[g], v);
+                atomicAdd(&alone[g], t);
             }
-        }
-        __syncthreads();
-        for (int g = tid; g < ng; g += kPlan) {
-            // Sharing saves tiles, and costs every row a second partial result.
-            const int rows = order && groups ? group_tokens(g) * G : 0, found = rows > 0 && p.used[g] != INT_MAX ? p.used[g] : 0;
-            const int64_t saved = int64_t(found * P / kv_tile(0)) * (p.alone[g] - tile_rows(rows));
-            p.used[g] = saved > kShareCost * int64_t(ceil_div(rows, kAttRows / 2)) ? found : 0;
         }
         __syncthreads();
     }
     int64_t sum = 0;  // heavy items, light ones above
+#pragma unroll 1
     for (int s0 = 0; s0 < n_src; s0 += kPlan) {
-        const int s = s0 + tid;
-        int rows = 0;
-        if (s < ng) {
-            if (p.used[s] > 0) rows = group_tokens(s) * G;
-        } else if (s < n_src) {
-            rows = order ? entry_at(kv, b, s - ng).t * G : 0;
-            p.group[s - ng] = group_of(b, s - ng);
+        if (s0 < ng) {  // groups: sharing saves tiles, and costs every row a second partial result
+            const int g = s0 + tid;
+            if (g < ng) {
+                const int a = order && groups ? b.cu_group[g] : 0, z = order && groups ? b.cu_group[g + 1] : 0;
+                KvSource x = {};
+                if (a < z) {
+                    x.q0 = b.cu_q[a];
+                    const int rows = (b.cu_q[z] - x.q0) * G, found = used[g] != INT_MAX ? used[g] : 0;
+                    const int64_t saved = int64_t(found * P / kv_tile(0)) * (alone[g] - tile_rows(rows));
+                    if (saved > kShareCost * int64_t(ceil_div(rows, kAttRows / 2))) {
+                        x.rows = rows;
+                        x.seq = b.seqs[a];
+                        x.kv1 = found * P;
+                        x.pos0 = 1 << 30;
+                    }
+                }
+                x.prefix = -1;
+                source[g] = x;
+            }
+            __syncthreads();
         }
-        int64_t total;
-        const int64_t before = sum + plan_scan(int64_t(light_items(rows)) << 32 | heavy_items(rows), sums, total);
-        sum += total;
+        const int s = s0 + tid;
+        KvSource x = {};
+        if (s < ng) {
+            x = source[s];
+        } else if (s < n_src) {
+            const Entry e = entry_at(kv, b, s - ng);
+            const int g = group_of(b, s - ng), shared = g < 0 ? 0 : source[g].kv1;
+            x.q0 = e.a;
+            x.rows = order ? e.t * G : 0;
+            x.seq = e.seq;
+            x.kv0 = shared;
+            x.kv1 = e.len;
+            x.pos0 = e.len - e.t;
+            x.prefix = shared > 0 ? g : -1;
+            x.blind = e.len < e.t;
+        }
+        Two total;
+        const int64_t before = sum + plan_scan({int64_t(light_items(x.rows)) << 32 | heavy_items(x.rows), 0}, sums, total).a;
+        sum += total.a;
         if (s < n_src) {
-            p.first[0][s] = int(before & 0xffffffff);
-            p.first[1][s] = int(before >> 32);
+            x.heavy0 = first0[s] = int(before & 0xffffffff);
+            x.light0 = first1[s] = int(before >> 32);
+            x.n_heavy = heavy_items(x.rows);
+            source[s] = x;
+            if (FEW) p.source[s] = x;
         }
     }
     const int n_heavy = int(sum & 0xffffffff), n_light = int(sum >> 32);
     if (tid == 0) {
-        p.first[0][n_src] = p.hdr[0] = n_heavy;
-        p.first[1][n_src] = p.hdr[16] = n_light;
+        first0[n_src] = p.hdr[0] = n_heavy;
+        first1[n_src] = p.hdr[16] = n_light;
         p.hdr[1] = order;
     }
     __syncthreads();
 #pragma unroll 1
     for (int light = 0; light < 2; ++light) {
-        const int n_items = light ? n_light : n_heavy;
-        const int32_t *first = p.first[light];
-        int64_t units = 0, list_rows = 0;
+        const int n_items = light ? n_light : n_heavy, blocks = kv_blocks(sms, light);
+        const int32_t *first = light ? first1 : first0;
+        KvItem *const items = light ? p.items[1] : p.items[0];
+        Two done = {0, 0};  // tiles, rows
+#pragma unroll 1
         for (int k0 = 0; k0 < n_items; k0 += kPlan) {
             const int k = k0 + tid;
             KvItem it = {};
             if (k < n_items) {
-                int lo = 0, hi = n_src;  // the last source that begins at or before item k
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (first[mid] <= k) lo = mid;
-                    else hi = mid;
-                }
-                // a source's light item comes after its heavy ones
-                const int in = light ? p.first[0][lo + 1] - p.first[0][lo] : k - first[lo];
-                it.row0 = in * kAttRows;
-                if (lo < ng) {
-                    const int a = b.cu_group[lo];
-                    it.q0 = b.cu_q[a];
-                    it.rows = group_tokens(lo) * G - it.row0;
-                    it.seq = b.seqs[a];
-                    it.kv1 = p.used[lo] * P;
-                    it.pos0 = 1 << 30;
-                    it.partial = 1;
-                    it.entry = -1;
-                } else {
-                    const Entry e = entry_at(kv, b, lo - ng);
-                    const int g = p.group[lo - ng], shared = g < 0 ? 0 : p.used[g];
-                    it.q0 = e.a;
-                    it.rows = e.t * G - it.row0;
-                    it.seq = e.seq;
-                    it.kv0 = shared * P;
-                    it.pos0 = e.len - e.t;
-                    it.kv1 = min(e.len, it.pos0 + (it.row0 + min(it.rows, kAttRows) - 1) / G + 1);
-                    it.partial = shared > 0;
-                    it.entry = lo - ng;
-                }
-                it.rows = min(it.rows, light ? kAttRows / 2 : kAttRows);
+                const int s = last_at_most(first, n_src, k);
+                const KvSource x = source[s];
+                it.row0 = (light ? x.n_heavy : k - x.heavy0) * kAttRows;
+                it.rows = min(x.rows - it.row0, light ? kAttRows / 2 : kAttRows);
+                it.q0 = x.q0;
+                it.seq = x.seq;
+                it.kv0 = x.kv0;
+                it.pos0 = x.pos0;
+                it.kv1 = min(x.kv1, x.pos0 + (it.row0 + it.rows - 1) / G + 1);
+                it.partial = s < ng || x.prefix >= 0;
                 it.tiles = ceil_div(max(it.kv1 - it.kv0, 0), kv_tile(light));
             }
-            int64_t total;
-            it.unit = units + plan_scan(int64_t(it.tiles) * kv.n_kv_heads, sums, total);
-            units += total;
-            it.row_off = list_rows + plan_scan(int64_t(it.rows) * kv.n_kv_heads, sums, total);
-            list_rows += total;
-            if (k < n_items) p.items[light][k] = it;
+            Two total;
+            const Two before = plan_scan({int64_t(it.tiles) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
+            it.unit = done.a + before.a;
+            it.row_off = done.b + before.b;
+            done = {done.a + total.a, done.b + total.b};
+            if (k < n_items) {
+                items[k] = it;
+                if (FEW) few_units[k] = it.unit;
+                if (light) {
+                    KvSource *const to = p.source + last_at_most(first, n_src, k);
+                    to->tiles = it.tiles;
+                    to->unit = it.unit;
+                    to->row_off = it.row_off;
+                }
+            }
         }
-        const int blocks = kv_blocks(sms, light);
+        const Share share(done.a, blocks);
         if (tid == 0) {
             int32_t *h = p.hdr + 16 * light;
-            *reinterpret_cast<int64_t *>(h + 2) = units;
-            *reinterpret_cast<int64_t *>(h + 4) = units / blocks;
-            h[6] = int(units - units / blocks * blocks);
-            if (!light) *reinterpret_cast<int64_t *>(p.hdr + 24) = list_rows;
+            *reinterpret_cast<int64_t *>(h + 2) = done.a;
+            *reinterpret_cast<int64_t *>(h + 4) = share.each;
+            h[6] = share.rest;
+            if (!light) *reinterpret_cast<int64_t *>(p.hdr + 24) = done.b;
         }
         __syncthreads();
-        const Share share(p, light, sms);
+        if (n_items == 0) continue;
+        const int64_t base = list_base(p, light, sms);
+#pragma unroll 1
         for (int c = tid; c < blocks; c += kPlan) {
             const int64_t u = share.at(c);
-            int lo = 0, hi = n_items;  // the last item that begins at or before the block's stretch
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (p.items[light][mid].unit <= u) lo = mid;
-                else hi = mid;
+            int k;
+            if (FEW) {
+                k = last_at_most(few_units, n_items, u);
+            } else {
+                int lo = 0, hi = n_items;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (items[mid].unit <= u) lo = mid;
+                    else hi = mid;
+                }
+                k = lo;
             }
-            p.start[light][c] = lo;
-            // an entry's item that has no prefix and is cut here for the first time: k_combine joins its pieces
-            int cut_k = -1, cut_h = 0;
-            if (u < units && c > 0) {
-                const KvItem *it = p.items[light] + lo;
-                cut_h = int(uint32_t(u - it->unit) / uint32_t(it->tiles));
-                const int64_t from = it->unit + int64_t(cut_h) * it->tiles, before = share.at(c - 1);
-                if (u > from && before <= from && before < u && !it->partial) cut_k = lo;
+            (light ? p.start[1] : p.start[0])[c] = k;
+            KvCut cut = {};
+            if (u < done.a && c > 0) {
+                const KvItem it = items[k];
+                cut.h = int(uint32_t(u - it.unit) / uint32_t(it.tiles));
+                const int64_t from = it.unit + int64_t(cut.h) * it.tiles, before = share.at(c - 1);
+                if (u > from && before <= from && before < u && !it.partial) {
+                    cut.c0 = share.of(from);
+                    cut.n = share.of(from + it.tiles - 1) - cut.c0 + 1;
+                    cut.row = piece_row(it, cut.h, cut.c0, base, light);
+                    cut.q0 = it.q0;
+                    cut.row0 = it.row0;
+                    cut.rows = it.rows;
+                }
             }
-            p.cut[light][2 * c] = cut_k;
-            p.cut[light][2 * c + 1] = cut_h;
+            (light ? p.cut[1] : p.cut[0])[c] = cut;
         }
+        __syncthreads();
     }
 }
 
 // ---- k_combine ----------------------------------------------------------------------------------------------
 
-// The pieces of one item and head: those of blocks c0 .. c0 + n - 1 that have any of its tiles.
+// The partial results of one item and head: row `row` in the first of n pieces of blocks c0, c0 + 1, ..
 struct Pieces {
-    Share share;
     int64_t row;
-    int c0, n, rows;
-    __device__ Pieces() : row(0), c0(0), n(0), rows(0) {}
-    __device__ Pieces(const KvPlan &p, const KvItem &it, int h, int light, int sms) : share(p, light, sms), c0(0), n(0) {
-        rows = light ? kAttRows / 2 : kAttRows;
-        if (it.tiles > 0) {
-            const int64_t from = it.unit + int64_t(h) * it.tiles;
+    int c0, n, light;
+    __device__ Pieces() : row(0), c0(0), n(0), light(0) {}
+    // unit, tiles, row_off, rows: of the item
+    __device__ Pieces(const Share &share, int64_t base, int64_t unit, int tiles, int64_t row_off, int rows, int h, int light_) : row(0), c0(0), n(0), light(light_) {
+        if (tiles > 0) {
+            const int64_t from = unit + int64_t(h) * tiles;
             c0 = share.of(from);
-            n = share.of(from + it.tiles - 1) - c0 + 1;
+            n = share.of(from + tiles - 1) - c0 + 1;
+            row = base + row_off + int64_t(h) * rows + int64_t(light ? kAttRows / 2 : kAttRows) * c0;
         }
-        row = piece_row(it, h, c0, list_base(p, light, sms), light);
     }
     // Row `in` of the item in piece i, -1 if the block has none of its tiles (where there are fewer tiles than blocks).
-    __device__ int64_t at(int i, int in) const {
-        const bool some = share.each > 0 || share.at(c0 + i) < share.at(c0 + i + 1);
-        return i >= 0 && i < n && some ? row + int64_t(rows) * i + in : -1;
+    __device__ int64_t at(const Share &share, int i, int in) const {
+        if (i < 0 || i >= n) return -1;
+        if (share.each == 0 && share.at(c0 + i) == share.at(c0 + i + 1)) return -1;
+        return row + int64_t(light ? kAttRows / 2 : kAttRows) * i + in;
     }
 };
 
-constexpr int kJoin = 256;     // threads
-constexpr int kJoinHeavy = 4;  // blocks for each place where heavy items may be cut, light items
+constexpr int kJoin = 256;      // threads
+constexpr int kJoinRows = 16;   // rows of a block at a time, 16 lanes each
+constexpr int kJoinHeavy = 8;   // blocks for each place where heavy items may be cut, light items
 constexpr int kJoinLight = 2;
 
-// Rows whose keys were divided among items or blocks, or that see none: a warp for each row, whose lanes first
-// read the sums of 32 pieces and then, eight at a time without waiting in between, the pieces.  The first blocks go by
-// the places where blocks' stretches meet, of which each cuts at most one item; the others by entry and kv head (`parts`
-// blocks for each), for entries with a shared prefix and rows without keys.
+// Rows whose keys were divided among items or blocks, or that see none.  A chain of dependent loads bounds it, so it is
+// kept short (what a row needs of its source lies in one record) and every row is a half warp's own: its lanes
+// read the sums of 16 pieces at once and then, four at a time without waiting in between, the pieces.  The first
+// blocks go by the places where blocks' stretches meet, of which each cuts at most one item; the others by entry and kv
+// head (`parts` blocks for each), for entries with a shared prefix and rows without keys.
 template <bool BF>
 __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
-    const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int cols = 4 * lane < D ? lane : 0;  // this lane's four columns
-    const auto put = [&](int t, int qh, float4 v, float lse) {
-        if (4 * lane < D)
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh + 4 * lane) = make_uint2(pack<BF>(v.x, v.y), pack<BF>(v.z, v.w));
-        if (lane == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = lse;
-    };
-    const auto join = [&](const Pieces &first, int in, const Pieces &own, int r, int t, int qh) {
-        const int n = first.n + own.n;
-        float top = -INFINITY, total = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-        for (int p0 = 0; p0 < n; p0 += 32) {
-            const int p = p0 + lane;
-            const int64_t at = p < first.n ? first.at(p, in) : own.at(p - first.n, r);
-            const float s = at >= 0 ? a.part_lse[at] : -INFINITY;
-            float up = s;
+    const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, sl = threadIdx.x & 15, sub = threadIdx.x >> 4;
+    const unsigned mine = 0xffffu << (threadIdx.x & 16);
+    const auto put = [&](int t, int qh, const float4 *v, float lse) {
+        uint16_t *o = static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh;
 #pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(FULL, up, d));
-            up = fmaxf(up, top);
-            const float w = s == -INFINITY ? 0.f : ex2(s - up), f = top == -INFINITY ? 0.f : ex2(top - up);
-            top = up;
-            total *= f;
-            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-#pragma unroll 1
-            for (int i0 = 0; i0 < min(32, n - p0); i0 += 8) {
-                float4 v[8];  // a piece that is not there: row 0, with weight 0
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = __ldcs(reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(FULL, at, i0 + i), int64_t(0)) * D) + cols);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float wi = __shfl_sync(FULL, w, i0 + i);
-                    total += wi;
-                    acc = wi == 0.f ? acc : make_float4(fmaf(v[i].x, wi, acc.x), fmaf(v[i].y, wi, acc.y), fmaf(v[i].z, wi, acc.z), fmaf(v[i].w, wi, acc.w));
-                }
-            }
-        }
-        const float f = total == 0.f ? 0.f : 1.f / total;
-        put(t, qh, make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f), total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f);
+        for (int q = 0; q < 2; ++q)
+            if (4 * (sl + 16 * q) < D) *reinterpret_cast<uint2 *>(o + 4 * (sl + 16 * q)) = make_uint2(pack<BF>(v[q].x, v[q].y), pack<BF>(v[q].z, v[q].w));
+        if (sl == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = lse;
     };
     const int heavy = kv_blocks(a.sms, 0) * kJoinHeavy, cuts = heavy + kv_blocks(a.sms, 1) * kJoinLight;
     const bool by_cut = int(blockIdx.x) < cuts;
-    const int64_t all = by_cut ? cuts : int64_t(b.n) * H * parts + cuts;
+    const Share share0(plan, 0, a.sms), share1(plan, 1, a.sms);
+    const int64_t base1 = list_base(plan, 1, a.sms);
+    const uint32_t all = uint32_t(b.n) * uint32_t(H) * uint32_t(parts);  // at most 2^30
 #pragma unroll 1
-    for (int64_t x = blockIdx.x; x < all; x += by_cut ? cuts : gridDim.x - cuts) {
-        // rows z0, z0 + step, .. below z1 of the entry and head; a cut item's own rows
-        int i, h, z0, z1, step;
-        bool shared = false;
+    for (uint32_t y = by_cut ? blockIdx.x : blockIdx.x - cuts; y < (by_cut ? cuts : all); y += by_cut ? cuts : gridDim.x - cuts) {
+        // rows z, z + step, .. below z1 of query tokens from q0 on, and kv head h
+        Pieces first, own;
+        KvSource x;
+        int q0, h, z, z1, step;
         if (by_cut) {
-            const bool light = int(x) >= heavy;
-            const int y = light ? int(x) - heavy : int(x), per = light ? kJoinLight : kJoinHeavy, c = y / per;
-            const int k = plan.cut[light][2 * c];
-            if (k < 0) break;
-            h = plan.cut[light][2 * c + 1];
-            const KvItem *it = plan.items[light] + k;
-            i = it->entry;
-            z0 = it->row0 + (y - c * per) * 8 + warp;
-            z1 = it->row0 + it->rows;
-            step = 8 * per;
+            const bool light = int(y) >= heavy;
+            const int nth = light ? int(y) - heavy : int(y), per = light ? kJoinLight : kJoinHeavy, c = nth / per;
+            if ((light ? share1 : share0).units == 0) break;
+            const KvCut cut = (light ? plan.cut[1] : plan.cut[0])[c];
+            if (cut.n == 0) break;
+            own.row = cut.row - cut.row0;
+            own.c0 = cut.c0;
+            own.n = cut.n;
+            own.light = light;
+            q0 = cut.q0;
+            h = cut.h;
+            z = cut.row0 + (nth - c * per) * kJoinRows + sub;
+            z1 = cut.row0 + cut.rows;
+            step = kJoinRows * per;
         } else {
-            const uint32_t y = uint32_t(x - cuts), ih = y / uint32_t(parts);
-            i = int(ih / uint32_t(H));
-            h = int(ih) - i * H;
-            const Entry e = entry_at(kv, b, i);
-            const int g = plan.group[i];
-            shared = g >= 0 && plan.used[g] > 0;
-            z0 = int(y - ih * parts) * 8 + warp;
-            z1 = !plan.hdr[1] || (!shared && e.len >= e.t) ? 0 : e.t * G;  // none: k_attend has written these, or the cuts
-            step = 8 * parts;
+            const uint32_t ih = y / uint32_t(parts), i = ih / uint32_t(H);
+            h = int(ih - i * H);
+            x = plan.source[b.n_groups + i];
+            if (x.prefix < 0 && !x.blind) continue;  // written by the other kernels, or by the cuts
+            q0 = x.q0;
+            z = int(y - ih * parts) * kJoinRows + sub;
+            z1 = x.rows;
+            step = kJoinRows * parts;
         }
-        if (z0 >= z1) continue;
-        const int q0 = b.cu_q[i], src = b.n_groups + i, heavy0 = plan.first[0][src], n_heavy = plan.first[0][src + 1] - heavy0, light0 = plan.first[1][src];
-        const int g = shared ? plan.group[i] : 0, group_q0 = shared ? b.cu_q[b.cu_group[g]] : 0;
 #pragma unroll 1
-        for (int z = z0; z < z1; z += step) {
-            const int dt = a.group.div(z), t = q0 + dt, qh = h * G + z - dt * G, nth = z / kAttRows;
-            const bool light = nth >= n_heavy;
-            const KvItem it = plan.items[light][light ? light0 : heavy0 + nth];
-            if (!by_cut && !shared && it.tiles > 0) continue;  // only rows without keys
-            Pieces first;
-            int in = 0;
-            if (shared) {
-                const int row = (t - group_q0) * G + qh - h * G, pth = row / kAttRows, p0 = plan.first[0][g];
-                const bool pl = pth >= plan.first[0][g + 1] - p0;
-                first = Pieces(plan, plan.items[pl][pl ? plan.first[1][g] : p0 + pth], h, pl, a.sms);
-                in = row % kAttRows;
+        for (; z < z1; z += step) {
+            const int dt = a.group.div(z), t = q0 + dt, qh = h * G + z - dt * G;
+            int in = z, pin = 0;
+            if (!by_cut) {
+                const int nth = z / kAttRows;
+                in = z % kAttRows;
+                if (nth >= x.n_heavy) {
+                    own = Pieces(share1, base1, x.unit, x.tiles, x.row_off, min(x.rows - nth * kAttRows, kAttRows), h, 1);
+                    if (x.prefix < 0 && x.tiles > 0) continue;  // only rows without keys
+                } else {
+                    const KvItem it = plan.items[0][x.heavy0 + nth];
+                    own = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
+                    if (x.prefix < 0 && it.tiles > 0) continue;
+                }
+                if (x.prefix >= 0) {
+                    const KvSource px = plan.source[x.prefix];
+                    const int row = (q0 - px.q0) * G + z, pth = row / kAttRows;
+                    pin = row % kAttRows;
+                    if (pth >= px.n_heavy) {
+                        first = Pieces(share1, base1, px.unit, px.tiles, px.row_off, min(px.rows - pth * kAttRows, kAttRows), h, 1);
+                    } else {
+                        const KvItem it = plan.items[0][px.heavy0 + pth];
+                        first = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
+                    }
+                }
             }
-            join(first, in, Pieces(plan, it, h, light, a.sms), z % kAttRows, t, qh);
+            const int n = first.n + own.n;
+            float top = -INFINITY, total = 0.f;
+            float4 acc[2] = {};
+#pragma unroll 1
+            for (int p0 = 0; p0 < n; p0 += 16) {
+                const int p = p0 + sl;
+                const int64_t at = p < first.n ? first.at(first.light ? share1 : share0, p, pin) : own.at(own.light ? share1 : share0, p - first.n, in);
+                const float s = at >= 0 ? a.part_lse[at] : -INFINITY;
+                float up = s;
+#pragma unroll
+                for (int d = 8; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(mine, up, d));
+                up = fmaxf(up, top);
+                const float w = s == -INFINITY ? 0.f : ex2(s - up), f = top == -INFINITY ? 0.f : ex2(top - up);
+                top = up;
+                total *= f;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) acc[q] = make_float4(acc[q].x * f, acc[q].y * f, acc[q].z * f, acc[q].w * f);
+#pragma unroll 1
+                for (int i0 = 0; i0 < min(16, n - p0); i0 += 4) {
+                    float4 v[4][2];  // a piece that is not there: row 0, with weight 0
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 *from = reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(mine, at, i0 + e, 16), int64_t(0)) * D);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) v[e][q] = from[4 * (sl + 16 * q) < D ? sl + 16 * q : 0];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float we = __shfl_sync(mine, w, i0 + e, 16);
+                        total += we;
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const float4 u = v[e][q];
+                            acc[q] = we == 0.f ? acc[q] : make_float4(fmaf(u.x, we, acc[q].x), fmaf(u.y, we, acc[q].y), fmaf(u.z, we, acc[q].z), fmaf(u.w, we, acc[q].w));
+                        }
+                    }
+                }
+            }
+            const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) acc[q] = make_float4(acc[q].x * f, acc[q].y * f, acc[q].z * f, acc[q].w * f);
+            put(t, qh, acc, total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f);
         }
     }
+    if (by_cut) return;
     // query tokens of no entry
     const bool order = b.n > 0 && plan.hdr[1];
-    const int first = order ? b.cu_q[0] : b.n_q, last = order ? b.cu_q[b.n] : b.n_q;
-    const uint32_t rest = uint32_t(first + b.n_q - last) * uint32_t(b.q_heads);  // at most 2^30
+    const int before = order ? b.cu_q[0] : b.n_q, after = order ? b.cu_q[b.n] : b.n_q;
+    const uint32_t rest = uint32_t(before + b.n_q - after) * uint32_t(b.q_heads);  // at most 2^30
+    const float4 zero[2] = {};
 #pragma unroll 1
-    for (uint32_t x = blockIdx.x * 8 + warp; x < rest; x += gridDim.x * 8) {
-        const int i = int(x / uint32_t(b.q_heads));
-        put(i < first ? i : i - first + last, int(x) - i * b.q_heads, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY);
+    for (uint32_t x = (blockIdx.x - cuts) * kJoinRows + sub; x < rest; x += (gridDim.x - cuts) * kJoinRows) {
+        const int e = int(x / uint32_t(b.q_heads));
+        put(e < before ? e : e - before + after, int(x) - e * b.q_heads, zero, -INFINITY);
     }
 }
 
@@ -440,7 +521,9 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
         cudaError_t e = launch_chained(k_plan_shared, std::max((b.n + 7) / 8, 1), 256, 0, st, kv, b);
         if (e != cudaSuccess) return e;
     }
-    return launch_chained(k_plan_items, 1, kPlan, 0, st, kv, b, kv_sm_count());
+    const KvPlan p = kv_plan(kv, b);
+    const bool few = b.n_groups + b.n <= kFewSources && int64_t(p.max_heavy) <= kFewItems;  // at most one light item a source
+    return launch_chained(few ? k_plan_items<true> : k_plan_items<false>, 1, kPlan, 0, st, kv, b, kv_sm_count());
 }
 
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
@@ -468,8 +551,8 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     if (rows / kv.n_kv_heads > kAttRows / 2) e = launch_kv_heavy(kv, b, a, heavy, st);  // fewer rows make no heavy item
     if (e == cudaSuccess) e = launch_kv_light(kv, b, a, light, st);
     if (e != cudaSuccess) return e;
-    // as many blocks for an entry and head as its rows can use on average
-    const int64_t parts = std::min<int64_t>(std::max<int64_t>(rows / kv.n_kv_heads / std::max(b.n, 1) / 8, 1), 16);
+    // blocks for an entry and head: for twice the rows that they have on average
+    const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
     const int cuts = kv_blocks(a.sms, 0) * kJoinHeavy + kv_blocks(a.sms, 1) * kJoinLight;
     const int blocks = cuts + int(std::min<int64_t>(std::max<int64_t>(b.n * int64_t(kv.n_kv_heads) * parts, 1), int64_t(a.sms) * 16));
     return launch_chained(kv.dtype == SIM_KV_BF16 ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));

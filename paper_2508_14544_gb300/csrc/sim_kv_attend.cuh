@@ -24,6 +24,7 @@ struct Share {
     int64_t units, each;  // units = each * blocks + rest
     int rest, blocks;
     __device__ Share() : units(0), each(0), rest(0), blocks(1) {}
+    __device__ Share(int64_t units_, int blocks_) : units(units_), each(units_ / blocks_), blocks(blocks_) { rest = int(units - each * blocks); }
     __device__ Share(const KvPlan &p, int light, int sms) : blocks(kv_blocks(sms, light)) {
         const int32_t *h = p.hdr + 16 * light;
         units = *reinterpret_cast<const int64_t *>(h + 2);

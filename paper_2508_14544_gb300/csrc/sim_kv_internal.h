@@ -80,26 +80,47 @@ struct alignas(16) KvItem {
     int64_t unit;     // tiles of the items before, all kv heads
     int64_t row_off;  // rows of the items before, all kv heads
     int32_t partial;  // its rows have another item too: always through the workspace
-    int32_t entry;    // entry of the batch, -1 for a group's prefix
-    int32_t pad[2];
+    int32_t pad[3];
 };
 static_assert(sizeof(KvItem) == 64, "KvItem");
 
-// b->plan: header, where each block's stretch begins, per group the pages shared and its entries' tile rows, the
-// first heavy and the first light item of every source (groups, then entries, and the end), each entry's group and
-// the pages that it shares with its group's first entry, the items.
+// Where the rows of items come from: a group's prefix, or an entry's own keys.  Groups come first, then entries.
+struct alignas(16) KvSource {
+    int32_t q0, rows;         // first query token, rows of a kv head
+    int32_t seq, kv0, kv1;    // row of the table, keys
+    int32_t pos0;             // as KvItem's
+    int32_t heavy0, n_heavy;  // its heavy items
+    int32_t light0;           // its light item, after them
+    int32_t prefix;           // source of the prefix that it shares, or -1
+    int32_t blind;            // some of its rows see no key
+    int32_t tiles;            // of its light item, whose .unit and .row_off follow
+    int64_t unit, row_off;
+};
+static_assert(sizeof(KvSource) == 64, "KvSource");
+
+// A place where the stretches of two blocks meet within an item that has no prefix, the item's first: k_combine joins
+// its pieces there.
+struct alignas(16) KvCut {
+    int64_t row;        // partial results of the first piece
+    int32_t c0, n;      // pieces; 0: no cut
+    int32_t q0, row0, rows, h;
+};
+static_assert(sizeof(KvCut) == 32, "KvCut");
+
+// b->plan: header, where each block's stretch begins and what it cuts, the sources and the pages that entries share
+// with their group's first, the items; numbers for searches: each source's first items, pages used by groups.
 constexpr int kKvMaxSms = 256;
 struct KvPlan {
     int32_t *hdr;       // heavy, and 16 further light: [0] items, [2..3] tiles in all, [4..5] of each block, [6] left over;
                         // [1] offsets in order, [24..25] rows of the heavy items
+    KvCut *cut[2];      // [kv_blocks]
+    KvSource *source;   // [n_groups + n]
+    KvItem *items[2];
     int32_t *start[2];  // [kv_blocks] item in which each block's stretch begins
-    int32_t *cut[2];    // [kv_blocks] item (without a prefix) and kv head whose first cut is where the stretch begins, or -1
+    int32_t *first[2];  // [n_groups + n + 1]
     int32_t *used;      // [n_groups]
     int32_t *alone;     // [n_groups]
-    int32_t *first[2];  // [n_groups + n + 1]
-    int32_t *group;     // [n]
     int32_t *same;      // [n]
-    KvItem *items[2];
     int64_t bytes;
     int32_t max_heavy;
 };
@@ -108,20 +129,19 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     const int64_t G = b.q_heads / kv.n_kv_heads, src = int64_t(b.n_groups) + b.n;
     p.max_heavy = int32_t(2 * (int64_t(b.n_q) * G / (kAttRows / 2 + 1)) + 1);
     p.hdr = static_cast<int32_t *>(b.plan);
-    p.start[0] = p.hdr + 32;
-    p.start[1] = p.start[0] + kKvMaxSms;
-    p.cut[0] = p.start[1] + 2 * kKvMaxSms;  // two numbers each
-    p.cut[1] = p.cut[0] + 2 * kKvMaxSms;
-    p.used = p.cut[1] + 4 * kKvMaxSms;
-    p.alone = p.used + b.n_groups;
-    p.first[0] = p.alone + b.n_groups;
-    p.first[1] = p.first[0] + src + 1;
-    p.group = p.first[1] + src + 1;
-    p.same = p.group + b.n;
-    const int64_t ints = (32 + 9 * kKvMaxSms + 2 * int64_t(b.n_groups) + 2 * (src + 1) + 2 * int64_t(b.n) + 3) / 4 * 4;
-    p.items[0] = reinterpret_cast<KvItem *>(static_cast<char *>(b.plan) + ints * 4);
+    p.cut[0] = reinterpret_cast<KvCut *>(p.hdr + 32);
+    p.cut[1] = p.cut[0] + kKvMaxSms;
+    p.source = reinterpret_cast<KvSource *>(p.cut[1] + 2 * kKvMaxSms);
+    p.items[0] = reinterpret_cast<KvItem *>(p.source + src);
     p.items[1] = p.items[0] + p.max_heavy;
-    p.bytes = ints * 4 + (p.max_heavy + src) * int64_t(sizeof(KvItem));
+    p.start[0] = reinterpret_cast<int32_t *>(p.items[1] + src);
+    p.start[1] = p.start[0] + kKvMaxSms;
+    p.first[0] = p.start[1] + 2 * kKvMaxSms;
+    p.first[1] = p.first[0] + src + 1;
+    p.used = p.first[1] + src + 1;
+    p.alone = p.used + b.n_groups;
+    p.same = p.alone + b.n_groups;
+    p.bytes = reinterpret_cast<char *>(p.same + b.n) - static_cast<char *>(b.plan);
     return p;
 }
 // Blocks of the two lists for a number of SMs.
