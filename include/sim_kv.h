@@ -50,7 +50,7 @@ typedef struct {
     int32_t page_size;  /* tokens: 16, 32, 64 or 128 */
     int32_t head_dim;   /* a multiple of 8, 8 .. 128 */
     int32_t max_seqs;   /* 1 .. 2^17 */
-    int32_t max_pages;  /* pages per sequence, >= 1, max_pages * page_size < 2^30 */
+    int32_t max_pages;  /* pages per sequence, >= 1, max_pages * page_size < 2^30 (2^37 / n_kv_heads) */
 } sim_kv;
 
 /* sim_kv_scratch_bytes: size of kv->scratch (the pointers of *kv are not read); 0 for bad sizes. */

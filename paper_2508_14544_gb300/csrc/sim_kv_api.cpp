@@ -46,6 +46,7 @@ const char *bad_sizes(const sim_kv *kv) {
     if (kv->head_dim < 8 || kv->head_dim > 128 || kv->head_dim % 8) return "head_dim must be a multiple of 8 in [8, 128]";
     if (kv->max_seqs < 1 || kv->max_seqs > simgb::kKvMaxSeqs) return "max_seqs outside [1, 2^17]";
     if (kv->max_pages < 1 || int64_t(kv->max_pages) * kv->page_size >= 1 << 30) return "max_pages < 1 or max_pages * page_size >= 2^30";
+    if (int64_t(kv->max_pages) * kv->page_size * kv->n_kv_heads >= int64_t(1) << 37) return "max_pages * page_size * n_kv_heads >= 2^37";
     if (simgb::kv_page_bytes(*kv) >= int64_t(1) << 40) return "a page of 2^40 bytes or more";
     return nullptr;
 }

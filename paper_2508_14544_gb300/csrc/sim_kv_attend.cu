@@ -23,7 +23,6 @@ namespace {
 
 // ---- plan ---------------------------------------------------------------------------------------------------
 
-constexpr int kPlan = 1024;
 constexpr int kShareCost = 4;          // tiles of 128 rows that a second partial result of as many rows costs
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -95,27 +94,28 @@ __global__ void __launch_bounds__(256) k_plan_shared(const sim_kv kv, const sim_
     if (lane == 0) p.same[i] = same;
 }
 
-// Exclusive prefix sums of two values per thread, and the totals.
+// Exclusive prefix sums of two values per thread over W warps, and the totals.
 struct Two {
     int64_t a, b;
 };
+template <int W>
 __device__ __forceinline__ Two plan_scan(Two v, Two *sums, Two &total) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const auto scan = [&](Two x) {
+    Two x = v;
 #pragma unroll 1
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t y = __shfl_up_sync(FULL, x.a, d), z = __shfl_up_sync(FULL, x.b, d);
-            if (lane >= d) x = {x.a + y, x.b + z};
-        }
-        return x;
-    };
-    const Two x = scan(v);
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t y = __shfl_up_sync(FULL, x.a, d), z = __shfl_up_sync(FULL, x.b, d);
+        if (lane >= d) x = {x.a + y, x.b + z};
+    }
     if (lane == 31) sums[w] = x;
     __syncthreads();
-    if (w == 0) sums[lane] = scan(sums[lane]);
-    __syncthreads();
-    total = sums[31];
-    const Two before = w ? sums[w - 1] : Two{0, 0};
+    Two before = {0, 0};
+    total = {0, 0};
+#pragma unroll 8
+    for (int k = 0; k < W; ++k) {  // faster than a second scan by shuffles
+        if (k == w) before = total;
+        total = {total.a + sums[k].a, total.b + sums[k].b};
+    }
     __syncthreads();
     return {before.a + x.a - v.a, before.b + x.b - v.b};
 }
@@ -128,7 +128,7 @@ __device__ __forceinline__ int tile_rows(int r) {
 __device__ __forceinline__ int heavy_items(int r) { return r / kAttRows + (r % kAttRows > kAttRows / 2); }
 __device__ __forceinline__ int light_items(int r) { return r % kAttRows > 0 && r % kAttRows <= kAttRows / 2; }
 
-constexpr int kFewSources = 480, kFewItems = 1024;
+constexpr int kFewSources = 448, kFewItems = 1024;
 
 // The last of n + 1 ascending numbers x[0] .. x[n] that is at most v, below n.
 template <typename T>
@@ -145,17 +145,21 @@ __device__ __forceinline__ int last_at_most(const T *x, int n, T v) {
 // One block: which prefixes are shared, the sources and items, and where each begins on its list's line of work.
 // FEW: what the searches read is in shared memory (the steps are a chain of dependent loads).
 template <bool FEW>
-__global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim_kv_batch b, int sms) {
+__global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv, const sim_kv_batch b, int sms) {
+    constexpr int kPlan = FEW ? 512 : 1024;
     __shared__ Two sums[32];
+    __shared__ int32_t counts[3];  // cuts of heavy, of light items, entries to join
     __shared__ KvSource few_sources[FEW ? kFewSources : 1];
     __shared__ int32_t few_first[FEW ? 2 : 1][FEW ? kFewSources + 1 : 1], few_used[FEW ? kFewSources : 1], few_alone[FEW ? kFewSources : 1];
     __shared__ int64_t few_units[FEW ? kFewItems : 1];
+    __shared__ int32_t few_tiles[FEW ? kFewItems : 1];  // -1: its results are not joined here
     kv_wait_previous();
     const KvPlan p = kv_plan(kv, b);
     KvSource *const source = FEW ? few_sources : p.source;
     int32_t *const used = FEW ? few_used : p.used, *const alone = FEW ? few_alone : p.alone;
     int32_t *const first0 = FEW ? few_first[0] : p.first[0], *const first1 = FEW ? few_first[FEW ? 1 : 0] : p.first[1];
     const int tid = threadIdx.x, ng = b.n_groups, n_src = ng + b.n, G = b.q_heads / kv.n_kv_heads, P = kv.page_size;
+    if (tid < 3) counts[tid] = 0;
     // Offsets that are not in order: no queries at all, or no groups.
     bool order = true, groups = true, known = true;
 #pragma unroll 1
@@ -233,7 +237,7 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
             x.blind = e.len < e.t;
         }
         Two total;
-        const int64_t before = sum + plan_scan({int64_t(light_items(x.rows)) << 32 | heavy_items(x.rows), 0}, sums, total).a;
+        const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows)) << 32 | heavy_items(x.rows), 0}, sums, total).a;
         sum += total.a;
         if (s < n_src) {
             x.heavy0 = first0[s] = int(before & 0xffffffff);
@@ -241,6 +245,7 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
             x.n_heavy = heavy_items(x.rows);
             source[s] = x;
             if (FEW) p.source[s] = x;
+            if (x.rows > 0 && (x.prefix >= 0 || x.blind)) p.join[atomicAdd(&counts[2], 1)] = s - ng;
         }
     }
     const int n_heavy = int(sum & 0xffffffff), n_light = int(sum >> 32);
@@ -255,7 +260,7 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
         const int n_items = light ? n_light : n_heavy, blocks = kv_blocks(sms, light);
         const int32_t *first = light ? first1 : first0;
         KvItem *const items = light ? p.items[1] : p.items[0];
-        Two done = {0, 0};  // tiles, rows
+        Two done = {0, 0};  // spans, rows
 #pragma unroll 1
         for (int k0 = 0; k0 < n_items; k0 += kPlan) {
             const int k = k0 + tid;
@@ -274,13 +279,16 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
                 it.tiles = ceil_div(max(it.kv1 - it.kv0, 0), kv_tile(light));
             }
             Two total;
-            const Two before = plan_scan({int64_t(it.tiles) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
+            const Two before = plan_scan<kPlan / 32>({int64_t(kv_span(it.tiles, light)) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
             it.unit = done.a + before.a;
             it.row_off = done.b + before.b;
             done = {done.a + total.a, done.b + total.b};
             if (k < n_items) {
                 items[k] = it;
-                if (FEW) few_units[k] = it.unit;
+                if (FEW) {
+                    few_units[k] = it.unit;
+                    few_tiles[k] = it.partial ? -1 : it.tiles;
+                }
                 if (light) {
                     KvSource *const to = p.source + last_at_most(first, n_src, k);
                     to->tiles = it.tiles;
@@ -316,23 +324,29 @@ __global__ void __launch_bounds__(kPlan) k_plan_items(const sim_kv kv, const sim
                 k = lo;
             }
             (light ? p.start[1] : p.start[0])[c] = k;
-            KvCut cut = {};
-            if (u < done.a && c > 0) {
+            if (u < done.a && c > 0 && (!FEW || (few_tiles[k] > 0 && few_units[k] != u))) {
                 const KvItem it = items[k];
-                cut.h = int(uint32_t(u - it.unit) / uint32_t(it.tiles));
-                const int64_t from = it.unit + int64_t(cut.h) * it.tiles, before = share.at(c - 1);
-                if (u > from && before <= from && before < u && !it.partial) {
+                const int span = kv_span(it.tiles, light), h = span > 0 ? int(uint32_t(u - it.unit) / uint32_t(span)) : 0;
+                const int64_t from = it.unit + int64_t(h) * span + kv_lead(light), before = share.at(c - 1);  // tile 0
+                if (u > from && u < from + it.tiles && before <= from && !it.partial) {
+                    KvCut cut;
+                    cut.h = h;
                     cut.c0 = share.of(from);
                     cut.n = share.of(from + it.tiles - 1) - cut.c0 + 1;
                     cut.row = piece_row(it, cut.h, cut.c0, base, light);
                     cut.q0 = it.q0;
                     cut.row0 = it.row0;
                     cut.rows = it.rows;
+                    (light ? p.cut[1] : p.cut[0])[atomicAdd(&counts[light], 1)] = cut;
                 }
             }
-            (light ? p.cut[1] : p.cut[0])[c] = cut;
         }
         __syncthreads();
+    }
+    if (tid == 0) {
+        p.hdr[7] = counts[0];
+        p.hdr[23] = counts[1];
+        p.hdr[17] = counts[2];
     }
 }
 
@@ -346,7 +360,7 @@ struct Pieces {
     // unit, tiles, row_off, rows: of the item
     __device__ Pieces(const Share &share, int64_t base, int64_t unit, int tiles, int64_t row_off, int rows, int h, int light_) : row(0), c0(0), n(0), light(light_) {
         if (tiles > 0) {
-            const int64_t from = unit + int64_t(h) * tiles;
+            const int64_t from = unit + int64_t(h) * kv_span(tiles, light) + kv_lead(light);
             c0 = share.of(from);
             n = share.of(from + tiles - 1) - c0 + 1;
             row = base + row_off + int64_t(h) * rows + int64_t(light ? kAttRows / 2 : kAttRows) * c0;
@@ -362,14 +376,14 @@ struct Pieces {
 
 constexpr int kJoin = 256;      // threads
 constexpr int kJoinRows = 16;   // rows of a block at a time, 16 lanes each
-constexpr int kJoinHeavy = 8;   // blocks for each place where heavy items may be cut, light items
+constexpr int kJoinHeavy = 8;   // blocks for each cut of a heavy item, of a light one
 constexpr int kJoinLight = 2;
 
 // Rows whose keys were divided among items or blocks, or that see none.  A chain of dependent loads bounds it, so it is
 // kept short (what a row needs of its source lies in one record) and every row is a half warp's own: its lanes
-// read the sums of 16 pieces at once and then, four at a time without waiting in between, the pieces.  The first
-// blocks go by the places where blocks' stretches meet, of which each cuts at most one item; the others by entry and kv
-// head (`parts` blocks for each), for entries with a shared prefix and rows without keys.
+// read the sums of 16 pieces at once and then, four at a time without waiting in between, the pieces.  One wave of blocks
+// goes over what there is to join: items without a prefix that blocks' stretches cut, then entries with a shared prefix
+// and rows without keys, by kv head (`parts` blocks for each).
 template <bool BF>
 __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
@@ -383,39 +397,36 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
             if (4 * (sl + 16 * q) < D) *reinterpret_cast<uint2 *>(o + 4 * (sl + 16 * q)) = make_uint2(pack<BF>(v[q].x, v[q].y), pack<BF>(v[q].z, v[q].w));
         if (sl == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = lse;
     };
-    const int heavy = kv_blocks(a.sms, 0) * kJoinHeavy, cuts = heavy + kv_blocks(a.sms, 1) * kJoinLight;
-    const bool by_cut = int(blockIdx.x) < cuts;
+    const uint32_t heavy = uint32_t(plan.hdr[7]) * kJoinHeavy, cuts = heavy + uint32_t(plan.hdr[23]) * kJoinLight;
+    const uint32_t all = cuts + uint32_t(plan.hdr[17]) * uint32_t(H) * uint32_t(parts);  // at most 2^30 and the cuts
     const Share share0(plan, 0, a.sms), share1(plan, 1, a.sms);
     const int64_t base1 = list_base(plan, 1, a.sms);
-    const uint32_t all = uint32_t(b.n) * uint32_t(H) * uint32_t(parts);  // at most 2^30
 #pragma unroll 1
-    for (uint32_t y = by_cut ? blockIdx.x : blockIdx.x - cuts; y < (by_cut ? cuts : all); y += by_cut ? cuts : gridDim.x - cuts) {
+    for (uint32_t y = blockIdx.x; y < all; y += gridDim.x) {
         // rows z, z + step, .. below z1 of query tokens from q0 on, and kv head h
         Pieces first, own;
         KvSource x;
         int q0, h, z, z1, step;
+        const bool by_cut = y < cuts;
         if (by_cut) {
-            const bool light = int(y) >= heavy;
-            const int nth = light ? int(y) - heavy : int(y), per = light ? kJoinLight : kJoinHeavy, c = nth / per;
-            if ((light ? share1 : share0).units == 0) break;
+            const bool light = y >= heavy;
+            const uint32_t nth = light ? y - heavy : y, per = light ? kJoinLight : kJoinHeavy, c = nth / per;
             const KvCut cut = (light ? plan.cut[1] : plan.cut[0])[c];
-            if (cut.n == 0) break;
             own.row = cut.row - cut.row0;
             own.c0 = cut.c0;
             own.n = cut.n;
             own.light = light;
             q0 = cut.q0;
             h = cut.h;
-            z = cut.row0 + (nth - c * per) * kJoinRows + sub;
+            z = cut.row0 + int(nth - c * per) * kJoinRows + sub;
             z1 = cut.row0 + cut.rows;
-            step = kJoinRows * per;
+            step = kJoinRows * int(per);
         } else {
-            const uint32_t ih = y / uint32_t(parts), i = ih / uint32_t(H);
+            const uint32_t part = (y - cuts) % uint32_t(parts), ih = (y - cuts) / uint32_t(parts), i = ih / uint32_t(H);
             h = int(ih - i * H);
-            x = plan.source[b.n_groups + i];
-            if (x.prefix < 0 && !x.blind) continue;  // written by the other kernels, or by the cuts
+            x = plan.source[b.n_groups + plan.join[i]];
             q0 = x.q0;
-            z = int(y - ih * parts) * kJoinRows + sub;
+            z = int(part) * kJoinRows + sub;
             z1 = x.rows;
             step = kJoinRows * parts;
         }
@@ -490,14 +501,13 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
             put(t, qh, acc, total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f);
         }
     }
-    if (by_cut) return;
     // query tokens of no entry
     const bool order = b.n > 0 && plan.hdr[1];
     const int before = order ? b.cu_q[0] : b.n_q, after = order ? b.cu_q[b.n] : b.n_q;
     const uint32_t rest = uint32_t(before + b.n_q - after) * uint32_t(b.q_heads);  // at most 2^30
     const float4 zero[2] = {};
 #pragma unroll 1
-    for (uint32_t x = (blockIdx.x - cuts) * kJoinRows + sub; x < rest; x += (gridDim.x - cuts) * kJoinRows) {
+    for (uint32_t x = blockIdx.x * kJoinRows + sub; x < rest; x += gridDim.x * kJoinRows) {
         const int e = int(x / uint32_t(b.q_heads));
         put(e < before ? e : e - before + after, int(x) - e * b.q_heads, zero, -INFINITY);
     }
@@ -523,7 +533,7 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
     }
     const KvPlan p = kv_plan(kv, b);
     const bool few = b.n_groups + b.n <= kFewSources && int64_t(p.max_heavy) <= kFewItems;  // at most one light item a source
-    return launch_chained(few ? k_plan_items<true> : k_plan_items<false>, 1, kPlan, 0, st, kv, b, kv_sm_count());
+    return launch_chained(few ? k_plan_items<true> : k_plan_items<false>, 1, few ? 512 : 1024, 0, st, kv, b, kv_sm_count());
 }
 
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
@@ -553,8 +563,7 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
-    const int cuts = kv_blocks(a.sms, 0) * kJoinHeavy + kv_blocks(a.sms, 1) * kJoinLight;
-    const int blocks = cuts + int(std::min<int64_t>(std::max<int64_t>(b.n * int64_t(kv.n_kv_heads) * parts, 1), int64_t(a.sms) * 16));
+    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 4));
     return launch_chained(kv.dtype == SIM_KV_BF16 ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 

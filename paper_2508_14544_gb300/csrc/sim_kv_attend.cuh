@@ -18,13 +18,16 @@ constexpr int kStage = 128 * 17;       // floats through which the results of 12
 constexpr int kSegs = 4;               // segments that the loading warp may be ahead
 constexpr float kGrow = 8.f;           // log2 of what P may reach before O is rescaled
 
-// A list's tiles divided among its blocks: [at(c), at(c + 1)) are block c's.  (With no division but one of small
+// A list's line (the spans of its items, one after the other) divided among its blocks: [at(c), at(c + 1)) is block c's.  (With no division but one of small
 // numbers: code that runs once is paid for by its size.)
 struct Share {
     int64_t units, each;  // units = each * blocks + rest
     int rest, blocks;
     __device__ Share() : units(0), each(0), rest(0), blocks(1) {}
-    __device__ Share(int64_t units_, int blocks_) : units(units_), each(units_ / blocks_), blocks(blocks_) { rest = int(units - each * blocks); }
+    __device__ Share(int64_t units_, int blocks_) : units(units_), blocks(blocks_) {
+        each = units_ < INT_MAX ? int64_t(uint32_t(units_) / uint32_t(blocks_)) : units_ / blocks_;
+        rest = int(units - each * blocks);
+    }
     __device__ Share(const KvPlan &p, int light, int sms) : blocks(kv_blocks(sms, light)) {
         const int32_t *h = p.hdr + 16 * light;
         units = *reinterpret_cast<const int64_t *>(h + 2);
@@ -32,8 +35,8 @@ struct Share {
         rest = h[6];
     }
     __device__ int64_t at(int c) const { return each * c + uint32_t(rest * c) / uint32_t(blocks); }
-    __device__ int of(int64_t u) const {  // the block that has tile u
-        int c = min(int(float(u) * (float(blocks) / float(units))), blocks - 1);  // off by one at most
+    __device__ int of(int64_t u) const {  // the block that has place u
+        int c = min(int(float(u) * __fdividef(float(blocks), float(units))), blocks - 1);  // off by one at most
         while (at(c + 1) <= u) ++c;
         while (at(c) > u) --c;
         return c;
@@ -79,14 +82,17 @@ struct Line {
         s.n = 0;
         while (u < u1 && k < n_items) {
             if (h < 0) it = items[k];
-            if (it.tiles == 0 || h + 1 == heads) {
+            const int span = kv_span(it.tiles, light);
+            if (span == 0 || h + 1 == heads) {
                 ++k;
                 h = -1;
                 continue;
             }
-            h = h < 0 ? int(uint32_t(u - it.unit) / uint32_t(it.tiles)) : h + 1;
-            const int64_t a = it.unit + int64_t(h) * it.tiles;
-            const int t0 = int(u - a), t1 = int(min(u1 - a, int64_t(it.tiles)));
+            h = h < 0 ? int(uint32_t(u - it.unit) / uint32_t(span)) : h + 1;
+            const int64_t a = it.unit + int64_t(h) * span, tile0 = a + kv_lead(light);
+            const int t0 = int(max(u - tile0, int64_t(0))), t1 = int(min(u1 - tile0, int64_t(it.tiles)));
+            u = a + span;
+            if (t0 >= t1) continue;
             s.n = t1 - t0;
             s.h = h;
             s.q0 = it.q0;
@@ -97,7 +103,6 @@ struct Line {
             s.kv1 = it.kv1;
             s.direct = s.n == it.tiles && !it.partial;
             s.row = piece_row(it, h, c, base, light);
-            u = a + t1;
             return;
         }
     }

@@ -67,6 +67,10 @@ cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st)
 constexpr int kAttRows = 256;  // query rows of an item, at most
 // Items of more than 128 rows are heavy, the others light: two lists, each divided among blocks of its own.
 __host__ __device__ constexpr int kv_tile(int light) { return light ? 64 : 128; }  // keys of a tile
+// What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
+// tiles.
+__host__ __device__ constexpr int kv_lead(int light) { return light ? 3 : 4; }
+__host__ __device__ inline int kv_span(int tiles, int light) { return tiles > 0 ? tiles + kv_lead(light) : 0; }
 
 // A run of query rows (token x head of the group, for every kv head alike) against a range of one table's keys.
 struct alignas(16) KvItem {
@@ -77,7 +81,7 @@ struct alignas(16) KvItem {
     int32_t kv0, kv1; // keys
     int32_t pos0;     // position of token q0: token q0 + t sees the keys up to pos0 + t
     int32_t tiles;
-    int64_t unit;     // tiles of the items before, all kv heads
+    int64_t unit;     // spans of the items before, all kv heads
     int64_t row_off;  // rows of the items before, all kv heads
     int32_t partial;  // its rows have another item too: always through the workspace
     int32_t pad[3];
@@ -102,7 +106,7 @@ static_assert(sizeof(KvSource) == 64, "KvSource");
 // its pieces there.
 struct alignas(16) KvCut {
     int64_t row;        // partial results of the first piece
-    int32_t c0, n;      // pieces; 0: no cut
+    int32_t c0, n;      // pieces
     int32_t q0, row0, rows, h;
 };
 static_assert(sizeof(KvCut) == 32, "KvCut");
@@ -111,9 +115,9 @@ static_assert(sizeof(KvCut) == 32, "KvCut");
 // with their group's first, the items; numbers for searches: each source's first items, pages used by groups.
 constexpr int kKvMaxSms = 256;
 struct KvPlan {
-    int32_t *hdr;       // heavy, and 16 further light: [0] items, [2..3] tiles in all, [4..5] of each block, [6] left over;
-                        // [1] offsets in order, [24..25] rows of the heavy items
-    KvCut *cut[2];      // [kv_blocks]
+    int32_t *hdr;       // heavy, and 16 further light: [0] items, [2..3] spans in all, [4..5] of each block, [6] left over,
+                        // [7] cuts; [1] offsets in order, [17] entries to join, [24..25] rows of the heavy items
+    KvCut *cut[2];      // as many as there are, in any order
     KvSource *source;   // [n_groups + n]
     KvItem *items[2];
     int32_t *start[2];  // [kv_blocks] item in which each block's stretch begins
@@ -121,6 +125,7 @@ struct KvPlan {
     int32_t *used;      // [n_groups]
     int32_t *alone;     // [n_groups]
     int32_t *same;      // [n]
+    int32_t *join;      // [n] entries with a shared prefix or rows without keys, in any order
     int64_t bytes;
     int32_t max_heavy;
 };
@@ -141,7 +146,8 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     p.used = p.first[1] + src + 1;
     p.alone = p.used + b.n_groups;
     p.same = p.alone + b.n_groups;
-    p.bytes = reinterpret_cast<char *>(p.same + b.n) - static_cast<char *>(b.plan);
+    p.join = p.same + b.n;
+    p.bytes = reinterpret_cast<char *>(p.join + b.n) - static_cast<char *>(b.plan);
     return p;
 }
 // Blocks of the two lists for a number of SMs.

@@ -21,8 +21,10 @@ struct Shape {
     static constexpr int kSlots = 98304 / kTile;
     static constexpr int kTmem = 256, kColQ = 64, kColO = 128;  // S / P below
     static constexpr int kOffStage = kSlots * kTile;
-    static constexpr int kOffStat = kOffStage + kStage * 4;
-    static constexpr int kOffSeg = kOffStat + 128 * 8;
+    static constexpr int kJoinStage = 2560;          // floats: 4 copies of 32 rows x (16 + 4), or of fewer and longer ones
+    static_assert(kJoinStage >= kStage, "stage");
+    static constexpr int kOffStat = kOffStage + kJoinStage * 4;
+    static constexpr int kOffSeg = kOffStat + 2 * 128 * 8;
     static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
     static constexpr int kBars = 2 * kSlots + 2 * kSegs + 6;
     static constexpr int kBytes = kOffBar + kBars * 8 + 16;
@@ -271,12 +273,15 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                 int k0 = sg.k0;  // first key of the tile
                 const int kv1 = sg.kv1;
                 for (int j = 0; j < n; ++j, k0 += NK) {
-                    if (j + 1 == n) {  // the next item's queries come to L2 meanwhile
+                    if (j == max(n - 2, 0)) {  // the next item's queries come to L1 meanwhile: two lines a row
                         ok = take(x + 1);
                         if (!ok) return;
-                        if (next.n > 0 && lr < next.rows)
-#pragma unroll 1
-                            for (int d = 0; d < D; d += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q_row(next) + d));
+                        if (next.n > 0 && lr < next.rows) {
+                            const uint16_t *from = q_row(next);
+                            uint16_t v;
+                            asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from));
+                            asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from + D - 1));
+                        }
                     }
                     ok = __all_sync(FULL, bar_wait(s_full, ns & 1, gave_up));
                     if (!ok) return;
@@ -309,64 +314,70 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (!real) continue;
 
             const Sink<BF> sink = {a, sg, G, D, b.q_heads};
-            float f;  // what this thread's part of O is multiplied by
             if (span == 128) {
-                f = l == 0.f ? 0.f : 1.f / l;
                 if (row < rows) sink.lse(row, m, l);
-            } else {
-                stat[lr] = make_float2(m, l);
+                ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up));
+                if (!ok) break;
+                tc_fence_after();
+                sink.template warp_rows<DP>(t_o, stage + w * 32 * 17, row - lane, rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+            } else {  // join the four copies of each row: first what each is multiplied by
+                float2 *const st = stat + (x & 1) * 128;
+                st[lr] = make_float2(m, l);
                 join();
                 float top = -INFINITY, total = 0.f;
 #pragma unroll
-                for (int p = lane; p < 128; p += 32)
-                    if (stat[p].y != 0.f) top = fmaxf(top, stat[p].x);
+                for (int p = 0; p < 4; ++p)
+                    if (st[32 * p + lane].y != 0.f) top = fmaxf(top, st[32 * p + lane].x);
 #pragma unroll
-                for (int p = lane; p < 128; p += 32)
-                    if (stat[p].y != 0.f) total += stat[p].y * ex2((stat[p].x - top) * c);
-                f = l == 0.f ? 0.f : ex2((m - top) * c) / total;
+                for (int p = 0; p < 4; ++p)
+                    if (st[32 * p + lane].y != 0.f) total += st[32 * p + lane].y * ex2((st[32 * p + lane].x - top) * c);
+                const float f = l == 0.f ? 0.f : ex2((m - top) * c) / total;
                 if (lr < rows) sink.lse(lr, top, total);
-            }
-            ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
-            if (!ok) break;
-            tc_fence_after();
-            if (span == 128) {
-                sink.template warp_rows<DP>(t_o, stage + w * 32 * 17, row - lane, rows, f, l == 0.f);
-            } else {  // join the copies of each row, as many columns at a time as the stage holds of all of them
-                int cols = 16, shift = 3;
-                while (cols < DP && 4 * rows * (2 * cols + 1) <= kStage) {
-                    cols *= 2;
-                    ++shift;
+                // As many columns at a time as the stage holds of all copies.  No wait is needed after the last ones: the stage is
+                // used again only after the other warps have gone on to another item.
+                int cols = DP, shift = DP == 128 ? 5 : 4;  // log2 of the columns / 4
+                while (4 * rows * (cols + 4) > Sh::kJoinStage) {
+                    cols /= 2;
+                    --shift;
                 }
-                float *const to = stage + (w * rows + lane) * (cols + 1);
+                float *const to = stage + (w * rows + lane) * (cols + 4);
+                ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
+                if (!ok) break;
+                tc_fence_after();
 #pragma unroll 1
-                for (int d0 = 0; d0 < D && ok; d0 += cols) {
+                for (int d0 = 0; d0 < D; d0 += cols) {
+                    if (d0 > 0) join();
 #pragma unroll 1
-                    for (int d = 0; d < cols; d += 16) {
-                        uint32_t o[16];
-                        tm_ld16(t_o + d0 + d, o);
+                    for (int d = 0; d < cols; d += 32) {
+                        uint32_t o[32];
+                        if (cols == 16) tm_ld16(t_o + d0, o);
+                        else tm_ld32(t_o + d0 + d, o);
                         tc_wait_ld();
                         if (lane < rows) {
 #pragma unroll
-                            for (int y = 0; y < 16; ++y) to[d + y] = l == 0.f ? 0.f : __uint_as_float(o[y]) * f;
+                            for (int y = 0; y < 32; y += 4)
+                                if (y < 16 || cols > 16)
+                                    *reinterpret_cast<float4 *>(to + d + y) =
+                                        l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                 : make_float4(__uint_as_float(o[y]) * f, __uint_as_float(o[y + 1]) * f, __uint_as_float(o[y + 2]) * f, __uint_as_float(o[y + 3]) * f);
                         }
                     }
                     join();
+                    if (!ok) break;
 #pragma unroll 1
                     for (int e = lr; e < rows << shift; e += 128) {
-                        const int y = e >> shift, d = 2 * (e & ((1 << shift) - 1));
+                        const int y = e >> shift, d = 4 * (e & ((1 << shift) - 1));
                         if (d0 + d >= D) continue;
-                        float v0 = 0.f, v1 = 0.f;
+                        float4 v[4];
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            const float *v = stage + (p * rows + y) * (cols + 1) + d;
-                            v0 += v[0];
-                            v1 += v[1];
-                        }
-                        if (sg.direct) *reinterpret_cast<uint32_t *>(sink.out_row(y) + d0 + d) = pack<BF>(v0, v1);
-                        else *reinterpret_cast<float2 *>(a.part + (sg.row + y) * D + d0 + d) = make_float2(v0, v1);
+                        for (int p = 0; p < 4; ++p) v[p] = *reinterpret_cast<const float4 *>(stage + (p * rows + y) * (cols + 4) + d);
+                        const float4 t = make_float4((v[0].x + v[1].x) + (v[2].x + v[3].x), (v[0].y + v[1].y) + (v[2].y + v[3].y),
+                                                     (v[0].z + v[1].z) + (v[2].z + v[3].z), (v[0].w + v[1].w) + (v[2].w + v[3].w));
+                        if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d0 + d) = make_uint2(pack<BF>(t.x, t.y), pack<BF>(t.z, t.w));
+                        else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d0 + d) = t;
                     }
-                    join();
                 }
+                if (!ok) break;
             }
             tc_fence_before();
             give_back(x);
