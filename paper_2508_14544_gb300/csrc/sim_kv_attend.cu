@@ -526,6 +526,17 @@ EncodeFn encode_fn() {
 
 }  // namespace
 
+bool kv_encode_map(const sim_kv &kv, CUtensorMap *map, int rank, const void *at, const uint64_t *dim, const uint64_t *stride, const uint32_t *box) {
+    const EncodeFn encode = encode_fn();
+    const cuuint32_t step[5] = {1, 1, 1, 1, 1};
+    cuuint64_t dims[5], strides[5];
+    for (int i = 0; i < rank; ++i) dims[i] = dim[i];
+    for (int i = 0; i + 1 < rank; ++i) strides[i] = stride[i];
+    return encode && encode(map, kv.dtype == SIM_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void *>(at), dims, strides,
+                            box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t st) {
     if (b.n_groups > 0) {
         cudaError_t e = launch_chained(k_plan_shared, std::max((b.n + 7) / 8, 1), 256, 0, st, kv, b);
@@ -537,22 +548,18 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
 }
 
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
-    const EncodeFn encode = encode_fn();
-    if (!encode) return cudaErrorNotSupported;
+    if (!encode_fn()) return cudaErrorNotSupported;
     const auto encode_maps = [&](KvMaps &maps, int light) {
         for (int v = 0; v < 2; ++v) {
             uint16_t *at = static_cast<uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + v * (kv_layer_elems(kv) / 2);
-            const cuuint64_t dim[4] = {cuuint64_t(kv.head_dim), cuuint64_t(kv.page_size), cuuint64_t(kv.n_kv_heads), cuuint64_t(kv.n_pages)};
-            const cuuint64_t stride[3] = {cuuint64_t(kv.head_dim) * 2, cuuint64_t(kv.head_dim) * 2 * kv.page_size, cuuint64_t(kv_page_bytes(kv))};
-            const cuuint32_t box[4] = {64, cuuint32_t(std::min(kv.page_size, kv_tile(light))), 1, 1}, step[4] = {1, 1, 1, 1};
-            if (encode(v ? &maps.values : &maps.keys, kv.dtype == SIM_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, at, dim, stride,
-                       box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-                return false;
+            const uint64_t dim[4] = {uint64_t(kv.head_dim), uint64_t(kv.page_size), uint64_t(kv.n_kv_heads), uint64_t(kv.n_pages)};
+            const uint64_t stride[3] = {uint64_t(kv.head_dim) * 2, uint64_t(kv.head_dim) * 2 * kv.page_size, uint64_t(kv_page_bytes(kv))};
+            const uint32_t box[4] = {64, uint32_t(std::min(kv.page_size, kv_tile(light))), 1, 1};
+            if (!kv_encode_map(kv, v ? &maps.values : &maps.keys, 4, at, dim, stride, box)) return false;
         }
         return true;
     };
-    KvMaps heavy, light;
+    KvMaps heavy = {}, light = {};
     if (!encode_maps(light, 1)) return cudaErrorInvalidValue;
     heavy = light;
     if (kv.page_size > kv_tile(1) && !encode_maps(heavy, 0)) return cudaErrorInvalidValue;

@@ -14,7 +14,8 @@ namespace simgb {
 namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr int kStage = 128 * 17;       // floats through which the results of 128 rows pass
+constexpr int kPitch = 20;             // words between rows on the stage, 16 of them used: no bank conflicts
+constexpr int kStage = 128 * kPitch;   // words through which the results of 128 rows pass
 constexpr int kSegs = 4;               // segments that the loading warp may be ahead
 constexpr float kGrow = 8.f;           // log2 of what P may reach before O is rescaled
 
@@ -160,6 +161,13 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, u
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
         "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map),
+        "r"(bar), "r"(x), "r"(y), "r"(z)
         : "memory");
 }
 
@@ -353,35 +361,43 @@ struct Sink {
             a.lse[int64_t(sg.q0 + t) * q_heads + sg.h * G + (sg.row0 + y - t * G)] = e * 0.69314718055994531f;
         }
     }
-    // A warp's 32 rows from row0 on, 16 columns at a time through `mine` (32 x 17 floats), so that stores fill sectors;
-    // f is what the lane's row is multiplied by, empty: it has seen no key.
+    // A warp's 32 rows from row0 on, 16 words of each at a time through `mine` (32 x kPitch words), so that stores
+    // fill sectors; f is what the lane's row is multiplied by, empty: it has seen no key.
     template <int DP>
-    __device__ void warp_rows(uint32_t t_o, float *mine, int row0, int rows, float f, bool empty) const {
+    __device__ void warp_rows(uint32_t t_o, uint32_t *mine, int row0, int rows, float f, bool empty) const {
         const int lane = threadIdx.x & 31;
+        char *to[4];  // this lane's 16 bytes of four rows
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int y = min(row0 + q * 8 + lane / 4, rows - 1);
+            to[q] = (sg.direct ? reinterpret_cast<char *>(out_row(y)) : reinterpret_cast<char *>(a.part + (sg.row + y) * D)) + lane % 4 * 16;
+        }
+        const int cols = sg.direct ? 32 : 16;
 #pragma unroll 1
-        for (int d0 = 0; d0 < DP && d0 < D; d0 += 16) {
-            uint32_t o[16];
-            tm_ld16(t_o + d0, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int y = 0; y < 16; ++y) mine[lane * 17 + y] = empty ? 0.f : __uint_as_float(o[y]) * f;
-            __syncwarp();
+        for (int d0 = 0; d0 < D; d0 += cols) {
+            uint32_t x[16];
             if (sg.direct) {
+                uint32_t o[32];
+                tm_ld32(t_o + d0, o);
+                tc_wait_ld();
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int y = q * 16 + lane / 2, d = lane % 2 * 8;
-                    const float *v = mine + y * 17 + d;
-                    if (row0 + y < rows && d0 + d < D)
-                        *reinterpret_cast<uint4 *>(out_row(row0 + y) + d0 + d) = make_uint4(pack<BF>(v[0], v[1]), pack<BF>(v[2], v[3]), pack<BF>(v[4], v[5]), pack<BF>(v[6], v[7]));
-                }
+                for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
             } else {
+                tm_ld16(t_o + d0, x);
+                tc_wait_ld();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int y = q * 8 + lane / 4, d = lane % 4 * 4;
-                    const float *v = mine + y * 17 + d;
-                    if (row0 + y < rows && d0 + d < D)
-                        *reinterpret_cast<float4 *>(a.part + (sg.row + row0 + y) * D + d0 + d) = make_float4(v[0], v[1], v[2], v[3]);
-                }
+                for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
+            }
+#pragma unroll
+            for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4 *>(mine + lane * kPitch + y) = make_uint4(x[y], x[y + 1], x[y + 2], x[y + 3]);
+            __syncwarp();
+            const bool in = d0 + lane % 4 * (cols / 4) < D;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int y = q * 8 + lane / 4;
+                const uint4 v = *reinterpret_cast<const uint4 *>(mine + y * kPitch + lane % 4 * 4);
+                if (in && row0 + y < rows) *reinterpret_cast<uint4 *>(to[q]) = v;
+                to[q] += 64;
             }
             __syncwarp();
         }
@@ -390,11 +406,14 @@ struct Sink {
 
 }  // namespace
 
-// Tensor maps of one layer's keys and values, [page][head][token][dim], with boxes of up to kAttTile (light: 64)
-// tokens of one page and head and 64 columns.
+// Tensor maps of one layer's keys and values, [page][head][token][dim], with boxes of up to a tile's tokens of one
+// page and head and 64 columns; of the queries [token][head][dim], with boxes of 128 rows (if q_boxes).
 struct KvMaps {
-    CUtensorMap keys, values;
+    CUtensorMap keys, values, queries;
+    int q_boxes;
 };
+// 16-bit floats of kv.dtype; strides in bytes from the second dimension on.  False if the driver refuses.
+bool kv_encode_map(const sim_kv &kv, CUtensorMap *map, int rank, const void *at, const uint64_t *dim, const uint64_t *stride, const uint32_t *box);
 cudaError_t launch_kv_heavy(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
 cudaError_t launch_kv_light(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
 

@@ -77,6 +77,11 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid == 128 * NG) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.keys) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.values) : "memory");
+        if (maps.q_boxes) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.queries) : "memory");
+    }
     if (role == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "n"(Sh::kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -221,15 +226,31 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             }
             __syncwarp();
         } else {
-            // ---- query rows: two warps, 16 bytes a lane, the lanes of a row side by side.  Rows past the item's are
-            // left as they are: what they hold meets no other row and is masked.
+            // ---- query rows, by TMA where heads and tokens make boxes of 128 rows (rows of other entries, past the item's,
+            // come with them); else two warps, 16 bytes a lane, the lanes of a row side by side.  What rows past the item's
+            // hold meets no other row and is masked.
             constexpr int kVec = DP / 8, kStep = 64 / kVec;
             const int j = (tid & 63) % kVec;
             const bool has = j * 8 < D;
             Segment sg;
-            for (uint32_t x = 0; take(x, sg) && sg.n > 0; ++x) {
-                const uint16_t *const from0 = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0) * a.qt + int64_t(sg.h * G) * a.qh + (has ? j * 8 : 0);
+            uint32_t x = 0;
+            for (; take(x, sg) && sg.n > 0; ++x) {
                 if (!__all_sync(FULL, bar_wait(q_empty, (x + 1) & 1, gave_up))) break;
+                if (maps.q_boxes) {
+                    if (lane == 0) {
+                        if (role == 2) {
+                            bar_expect(q_full, NG * Sh::kTile);
+                            for (int g = 0; g < NG; ++g)
+                                for (int half = 0; half < DP / 64; ++half)
+                                    tma_load3(sbase + g * Sh::kTile + half * Sh::kHalf, &maps.queries, q_full, half * 64, sg.h * G, sg.q0 + a.group.div(sg.row0 + g * 128));
+                        } else {
+                            bar_arrive(q_full);
+                        }
+                    }
+                    __syncwarp();
+                    continue;
+                }
+                const uint16_t *const from0 = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0) * a.qt + int64_t(sg.h * G) * a.qh + (has ? j * 8 : 0);
 #pragma unroll 4
                 for (int r = (tid & 63) / kVec; r < sg.rows; r += kStep) {
                     const int y = sg.row0 + r, t = a.group.div(y);
@@ -251,13 +272,17 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 __syncwarp();
                 if (lane == 0) bar_arrive(q_full);
             }
+            // after a wait that gave up: the last boxes may be on their way
+            if (maps.q_boxes && x > 0)
+                for (int n = 0; n < 1000000 && *gave_up && !bar_try(q_full, (x - 1) & 1); ++n) {
+                }
         }
     } else {
         // ---- softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kSoftRegs));
         const int g = warp >> 2, w = warp & 3, lr = tid & 127;
         const uint32_t t_lane = tmem + (uint32_t(w * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + Sh::kOffO + g * 128;
-        float *const stage = reinterpret_cast<float *>(base + Sh::kOffStage) + g * kStage;
+        uint32_t *const stage = reinterpret_cast<uint32_t *>(base + Sh::kOffStage) + g * kStage;
         const float c = a.scale_log2;
         uint32_t ns = 0, at = 0;
         bool ok = true;
@@ -296,7 +321,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             ok = __all_sync(FULL, bar_wait(o_full(g), x & 1, gave_up));
             if (!ok) break;
             tc_fence_after();
-            sink.template warp_rows<DP>(t_o, stage + w * 32 * 17, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+            sink.template warp_rows<DP>(t_o, stage + w * 32 * kPitch, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
             tc_fence_before();
         }
     }
@@ -317,7 +342,15 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
         e = cudaFuncSetAttribute((const void *)k_heavy<DP, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kAlloc);
         if (e == cudaSuccess) ready = dev;
     }
-    return e == cudaSuccess ? launch_chained(k_heavy<DP, BF>, kv_blocks(a.sms, 0), Shape<DP>::kThreads, Shape<DP>::kAlloc, st, kv, b, a, maps) : e;
+    // queries by TMA: 128 rows are 128 / G tokens of G heads
+    KvMaps m = maps;
+    const uint32_t G = uint32_t(b.q_heads / kv.n_kv_heads);
+    if (a.q_vec && 128 % G == 0 && a.qt > 0 && a.qh > 0) {
+        const uint64_t dim[3] = {uint64_t(kv.head_dim), uint64_t(b.q_heads), uint64_t(b.n_q)}, stride[2] = {uint64_t(a.qh) * 2, uint64_t(a.qt) * 2};
+        const uint32_t box[3] = {64, G, 128 / G};
+        m.q_boxes = kv_encode_map(kv, &m.queries, 3, a.q, dim, stride, box);
+    }
+    return e == cudaSuccess ? launch_chained(k_heavy<DP, BF>, kv_blocks(a.sms, 0), Shape<DP>::kThreads, Shape<DP>::kAlloc, st, kv, b, a, m) : e;
 }
 
 }  // namespace

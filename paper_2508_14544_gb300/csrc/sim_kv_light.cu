@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                 ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up));
                 if (!ok) break;
                 tc_fence_after();
-                sink.template warp_rows<DP>(t_o, stage + w * 32 * 17, row - lane, rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+                sink.template warp_rows<DP>(t_o, reinterpret_cast<uint32_t *>(stage) + w * 32 * kPitch, row - lane, rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
             } else {  // join the four copies of each row: first what each is multiplied by
                 float2 *const st = stat + (x & 1) * 128;
                 st[lr] = make_float2(m, l);
