@@ -6,8 +6,9 @@
 //                page is shared and has room; an exclusive scan over the entries places each entry's pages in the list of
 //                the sum(n_i) lowest free ones, which 32 warps find by counting zeros of `ref` in a run of pages each,
 //                a scan over the warps and a second walk.  Nothing is changed before the sum is known to fit.
-//   k_move     - the copies that k_extend or k_compact listed, whole pages of all layers, and the slots of the new
-//                tokens.  Bound by HBM: every byte read once and written once, 16 bytes a load, eight in flight a thread.
+//   k_move     - puts the pages into the tables, and makes the slots of the new tokens and the copies that k_extend
+//                listed, whole pages of all layers.  Bound by HBM: every byte read once and written once, 16 bytes a
+//                load, eight in flight a thread.
 //   k_free, k_fork - a warp for each entry; `ref` changes by atomics whose order does not matter.
 //   k_compact  - one block: with N pages in use, the i-th used page at or above N goes to the i-th free one below N.
 //   k_write    - a thread for each 16 bytes of a token's keys and of its values.
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kMeta) k_extend(const sim_kv kv, int n, const 
             const int64_t nth = before & ((uint64_t(1) << kCowShift) - 1), copy = before >> kCowShift;
             sc.base[i] = int(min(nth, int64_t(kv.n_pages)));
             sc.need[i] = need < 0 ? -1 : need << 1 | cow;
+            if (!COPY && need >= 0) sc.len[i] = kv.length[seqs[i]];
             if (!COPY && cow && copy < kv.n_pages) {  // the copy's source; its destination is known once the pages are
                 const int s = seqs[i];
                 sc.src[copy] = kv.table[int64_t(s) * kv.max_pages + pages_of(kv.length[s], P) - 1];
@@ -210,28 +212,25 @@ __global__ void __launch_bounds__(kMeta) k_extend(const sim_kv kv, int n, const 
         __syncthreads();
     }
     if (tid == 0) sc.hdr[0] = COPY ? n_need : n_cow;
-    if (!COPY)
-        for (int c = tid; c < n_cow; c += kMeta) {
-            atomicSub(&kv.ref[sc.src[c]], 1);
-            sc.dst[c] = sc.free[sc.dst[c]];
-        }
-    for (int i = w; i < n; i += kMeta / 32) {
-        const int need = sc.need[i] >> 1, base = sc.base[i];
-        if (need < 0) continue;
-        const int s = seqs[i], L = kv.length[s], first = pages_of(L, P) - (sc.need[i] & 1);
-        int32_t *row = kv.table + int64_t(s) * kv.max_pages + first;
-        const int32_t *from = COPY ? kv.table + int64_t(src[i]) * kv.max_pages : nullptr;
-        for (int j = lane; j < need; j += 32) {
-            const int page = sc.free[base + j];
-            row[j] = page;
-            kv.ref[page] = 1;
-            if (COPY) {
+    if constexpr (!COPY) {  // k_move does the rest
+        for (int c = tid; c < n_cow; c += kMeta) sc.dst[c] = sc.free[sc.dst[c]];
+    } else {
+        for (int i = w; i < n; i += kMeta / 32) {
+            const int need = sc.need[i] >> 1, base = sc.base[i];
+            if (need < 0) continue;
+            const int s = seqs[i];
+            int32_t *row = kv.table + int64_t(s) * kv.max_pages;
+            const int32_t *from = kv.table + int64_t(src[i]) * kv.max_pages;
+            for (int j = lane; j < need; j += 32) {
+                const int page = sc.free[base + j];
+                row[j] = page;
+                kv.ref[page] = 1;
                 sc.src[base + j] = from[j];
                 sc.dst[base + j] = page;
             }
+            __syncwarp();
+            if (lane == 0) kv.length[s] = kv.length[src[i]];
         }
-        __syncwarp();
-        if (lane == 0) kv.length[s] = COPY ? kv.length[src[i]] : L + (cu[i + 1] - cu[i]);
     }
 }
 
@@ -270,14 +269,33 @@ __global__ void __launch_bounds__(kMove) k_move(const sim_kv kv, int n, const in
                                                 const int32_t *__restrict__ cu, int n_new, int64_t *__restrict__ slots) {
     kv_wait_previous();
     const KvScratch sc = kv_scratch(kv);
-    for (int64_t t = int64_t(blockIdx.x) * kMove + threadIdx.x; t < n_new; t += int64_t(gridDim.x) * kMove) {
-        const int i = entry_of(cu, n, int(t));
-        int64_t slot = -1;
-        if (i >= 0 && t < cu[i + 1] && sc.need[i] >= 0) {
-            const int s = seqs[i], pos = kv.length[s] - (cu[i + 1] - int(t));
-            slot = int64_t(kv.table[int64_t(s) * kv.max_pages + pos / kv.page_size]) * kv.page_size + pos % kv.page_size;
+    const int P = kv.page_size, lane = threadIdx.x & 31, first = blockIdx.x * kMove + threadIdx.x, all = gridDim.x * kMove;
+    if (cu) {
+        // a warp for each entry: its new pages, from the one that replaces a shared last page on
+        for (int i = first >> 5; i < n; i += all >> 5) {
+            const int need = sc.need[i] >> 1, cow = sc.need[i] & 1, base = sc.base[i];
+            if (need < 0) continue;
+            const int s = seqs[i], L = sc.len[i];
+            int32_t *row = kv.table + int64_t(s) * kv.max_pages + pages_of(L, P) - cow;
+            for (int j = lane; j < need; j += 32) {
+                const int page = sc.free[base + j];
+                row[j] = page;
+                kv.ref[page] = 1;
+            }
+            if (lane == 0) kv.length[s] = L + (cu[i + 1] - cu[i]);
         }
-        slots[t] = slot;
+        for (int c = first; c < sc.hdr[0]; c += all) atomicSub(&kv.ref[sc.src[c]], 1);
+        for (int64_t t = first; t < n_new; t += all) {
+            const int i = entry_of(cu, n, int(t));
+            int64_t slot = -1;
+            if (i >= 0 && t < cu[i + 1] && sc.need[i] >= 0) {
+                // of pages that were there only the table knows, of new ones the list
+                const int L = sc.len[i], pos = L + int(t) - cu[i], nth = pos / P - (pages_of(L, P) - (sc.need[i] & 1));
+                const int page = nth >= 0 ? sc.free[sc.base[i] + nth] : kv.table[int64_t(seqs[i]) * kv.max_pages + pos / P];
+                slot = int64_t(page) * P + pos % P;
+            }
+            slots[t] = slot;
+        }
     }
     move_pages(kv, sc.hdr[0], sc.src, sc.dst);
 }

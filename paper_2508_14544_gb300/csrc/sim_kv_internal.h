@@ -10,19 +10,20 @@ namespace simgb {
 
 constexpr int kKvMaxSeqs = 1 << 17;
 
-// kv->scratch, in ints: a header, then per entry of a call its first new page and their number, then lists of
-// pages (as many as the pool has): copies' sources and destinations, free pages.
+// kv->scratch, in ints: a header, then per entry of a call its first new page, their number and its length before,
+// then lists of pages (as many as the pool has): copies' sources and destinations, free pages.
 constexpr int kKvHdr = 64;  // [0]: copies to make
-__host__ __device__ inline int64_t kv_scratch_ints(const sim_kv &kv) { return kKvHdr + 2 * int64_t(kv.max_seqs) + 3 * int64_t(kv.n_pages); }
+__host__ __device__ inline int64_t kv_scratch_ints(const sim_kv &kv) { return kKvHdr + 3 * int64_t(kv.max_seqs) + 3 * int64_t(kv.n_pages); }
 struct KvScratch {
-    int32_t *hdr, *base, *need, *src, *dst, *free;
+    int32_t *hdr, *base, *need, *len, *src, *dst, *free;
 };
 __host__ __device__ inline KvScratch kv_scratch(const sim_kv &kv) {
     KvScratch s;
     s.hdr = static_cast<int32_t *>(kv.scratch);
     s.base = s.hdr + kKvHdr;
     s.need = s.base + kv.max_seqs;
-    s.src = s.need + kv.max_seqs;
+    s.len = s.need + kv.max_seqs;
+    s.src = s.len + kv.max_seqs;
     s.dst = s.src + kv.n_pages;
     s.free = s.dst + kv.n_pages;
     return s;

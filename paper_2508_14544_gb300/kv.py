@@ -21,8 +21,8 @@ def _dtypes():
 class AttentionPlan:
     """How the attention of one batch is divided (``KVCache.plan``); holds what the calls with it read."""
 
-    def __init__(self, batch, seqs, cu_q, cu_group, buffer):
-        self.batch, self.seqs, self.cu_q, self.cu_group, self._buffer = batch, seqs, cu_q, cu_group, buffer
+    def __init__(self, cache, batch, seqs, cu_q, cu_group, buffer):
+        self.cache, self.batch, self.seqs, self.cu_q, self.cu_group, self._buffer = cache, batch, seqs, cu_q, cu_group, buffer
         self._ref = ctypes.byref(batch)
         self.n_q, self.heads = batch.n_q, batch.q_heads
 
@@ -68,37 +68,36 @@ class KVCache:
             raise ValueError("sizes outside the cache's limits (see include/sim_kv.h)")
         self._scratch = torch.empty(size, dtype=torch.uint8, device=pool.device)
         self._kv.scratch = self._scratch.data_ptr()
-        self._index, self._dim = pool.device.index, dim
+        self._index, self._dim, self._heads, self._n_pages = pool.device.index, dim, heads, n_pages
+        self._torch, self._i32 = torch, torch.int32
         self._sizes = {}  # bytes of a plan and its workspace by the batch's sizes
         torch.cuda.current_stream(self.device).synchronize()  # the first call may be on any stream
 
-    def _empty(self, stream, *shape, dtype):
+    def _empty(self, stream, shape, dtype):
         """A tensor whose memory belongs to the stream that the call runs on."""
-        import torch
+        torch = self._torch
         if stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=self.device)):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _stream(self, stream):
-        import torch
-        if torch.cuda.current_device() != self._index:
+        torch = self._torch
+        if torch._C._cuda_getDevice() != self._index:
             raise ValueError(f"the cache is on {self.device}, which is not the current device")
         return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else int(stream)
 
-    def _done(self, rc):
-        if rc != L.SIM_OK:
-            raise L.SimError(rc, L.sim_last_error(None))
+    def _fail(self, rc):
+        raise L.SimError(rc, L.sim_last_error(None))
 
     def _ints(self, name, x, n):
-        import torch
-        if x.dtype != torch.int32 or x.device != self.device or x.dim() != 1 or x.shape[0] != n or not x.is_contiguous():
+        if x.dtype is not self._i32 or x.shape != (n,) or x.get_device() != self._index or not x.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values on {self.device}")
         return x.data_ptr()
 
     def _rows(self, name, x, n, heads):
         token, head, last = x.stride() if x.dim() == 3 else (0, 0, 0)
-        if last != 1 or x.dtype != self.dtype or x.device != self.device or x.shape != (n, heads, self._dim):
+        if last != 1 or x.dtype is not self.dtype or x.shape != (n, heads, self._dim) or x.get_device() != self._index:
             raise ValueError(f"{name} must be {self.dtype} [{n}, {heads}, {self._dim}] on {self.device}, the last dimension contiguous")
         return x.data_ptr(), token, head
 
@@ -118,47 +117,55 @@ class KVCache:
     def extend(self, seqs, cu_new, n_new: int, stream: int | None = None):
         """Room for cu_new[i + 1] - cu_new[i] tokens at the end of seqs[i] (``n_new`` in all); returns their slots
         (int64, -1 where refused).  A shared last page is copied first."""
-        import torch
-        n = seqs.shape[0]
-        st = self._stream(stream)
-        slots = self._empty(stream, n_new, dtype=torch.int64)
-        self._done(self._lib.sim_kv_extend(self._ref, n, self._ints("seqs", seqs, n), self._ints("cu_new", cu_new, n + 1), n_new,
-                                           slots.data_ptr(), st))
+        n, st = seqs.shape[0], self._stream(stream)
+        slots = self._empty(stream, (n_new,), self._torch.int64)
+        rc = self._lib.sim_kv_extend(self._ref, n, self._ints("seqs", seqs, n), self._ints("cu_new", cu_new, n + 1), n_new,
+                                     slots.data_ptr(), st)
+        if rc:
+            self._fail(rc)
         return slots
 
     def write(self, slots, k, v, layer: int = 0, stream: int | None = None) -> None:
         """Keys and values [n_new, n_kv_heads, head_dim] of one layer into their slots."""
-        import torch
         n = slots.shape[0]
-        if slots.dtype != torch.int64 or slots.device != self.device or slots.dim() != 1 or not slots.is_contiguous():
+        if slots.dtype is not self._torch.int64 or slots.get_device() != self._index or slots.dim() != 1 or not slots.is_contiguous():
             raise ValueError(f"slots must be a contiguous int64 tensor on {self.device}")
         st = self._stream(stream)
-        self._done(self._lib.sim_kv_write(self._ref, layer, n, slots.data_ptr(), *self._rows("k", k, n, self._kv.n_kv_heads),
-                                          *self._rows("v", v, n, self._kv.n_kv_heads), st))
+        rc = self._lib.sim_kv_write(self._ref, layer, n, slots.data_ptr(), *self._rows("k", k, n, self._heads),
+                                    *self._rows("v", v, n, self._heads), st)
+        if rc:
+            self._fail(rc)
 
     def fork(self, src, dst, tokens=None, stream: int | None = None) -> None:
         """dst[i] (empty) becomes the first tokens[i] tokens of src[i], on the same pages."""
         n, st = src.shape[0], self._stream(stream)
-        self._done(self._lib.sim_kv_fork(self._ref, n, self._ints("src", src, n), self._ints("dst", dst, n),
-                                         None if tokens is None else self._ints("tokens", tokens, n), st))
+        rc = self._lib.sim_kv_fork(self._ref, n, self._ints("src", src, n), self._ints("dst", dst, n),
+                                   None if tokens is None else self._ints("tokens", tokens, n), st)
+        if rc:
+            self._fail(rc)
 
     def copy(self, src, dst, stream: int | None = None) -> None:
         """dst[i] (empty) becomes src[i], on pages of its own."""
         n, st = src.shape[0], self._stream(stream)
-        self._done(self._lib.sim_kv_copy(self._ref, n, self._ints("src", src, n), self._ints("dst", dst, n), st))
+        rc = self._lib.sim_kv_copy(self._ref, n, self._ints("src", src, n), self._ints("dst", dst, n), st)
+        if rc:
+            self._fail(rc)
 
     def free(self, seqs, keep=None, stream: int | None = None) -> None:
         """seqs[i] keeps its first keep[i] tokens (none by default) and gives the other pages back."""
         n, st = seqs.shape[0], self._stream(stream)
-        self._done(self._lib.sim_kv_free(self._ref, n, self._ints("seqs", seqs, n),
-                                         None if keep is None else self._ints("keep", keep, n), st))
+        rc = self._lib.sim_kv_free(self._ref, n, self._ints("seqs", seqs, n),
+                                   None if keep is None else self._ints("keep", keep, n), st)
+        if rc:
+            self._fail(rc)
 
     def compact(self, stream: int | None = None):
         """Move the pages in use to the lowest numbers; returns each page's new number (int32, -1: was free)."""
-        import torch
         st = self._stream(stream)
-        to = self._empty(stream, self._kv.n_pages, dtype=torch.int32)
-        self._done(self._lib.sim_kv_compact(self._ref, to.data_ptr(), st))
+        to = self._empty(stream, (self._n_pages,), self._i32)
+        rc = self._lib.sim_kv_compact(self._ref, to.data_ptr(), st)
+        if rc:
+            self._fail(rc)
         return to
 
     # ---- attention ----------------------------------------------------------------------------------------------
@@ -167,7 +174,6 @@ class KVCache:
         """Divide a batch's attention: entry i has the query tokens cu_q[i] .. cu_q[i + 1] - 1 (``n_q`` in all), the
         last ones of sequence seqs[i].  Entries cu_group[g] .. cu_group[g + 1] - 1 may share a prefix: pages that
         all of them begin with are read once.  Valid until lengths or tables change."""
-        import torch
         n, st = seqs.shape[0], self._stream(stream)
         ng = 0 if cu_group is None else max(cu_group.shape[0] - 1, 0)
         b = L.sim_kv_batch(n, n_q, heads, ng, self._ints("seqs", seqs, n), self._ints("cu_q", cu_q, n + 1),
@@ -179,28 +185,33 @@ class KVCache:
             if len(self._sizes) > 1000:
                 self._sizes.clear()
             self._sizes[n, n_q, heads, ng] = sizes
-        buffer = self._empty(stream, sizes[0] + sizes[1] + 16, dtype=torch.uint8)
+        buffer = self._empty(stream, (sizes[0] + sizes[1] + 16,), self._torch.uint8)
         b.plan = buffer.data_ptr()
         b.workspace = b.plan + sizes[0]
-        plan = AttentionPlan(b, seqs, cu_q, cu_group, buffer)
-        self._done(self._lib.sim_kv_plan(self._ref, plan._ref, st))
+        plan = AttentionPlan(self, b, seqs, cu_q, cu_group, buffer)
+        rc = self._lib.sim_kv_plan(self._ref, plan._ref, st)
+        if rc:
+            self._fail(rc)
         return plan
 
     def attend(self, q, plan: AttentionPlan, layer: int = 0, scale: float | None = None, out=None, lse=None, stream: int | None = None):
         """softmax(scale q k^T) v of queries [n_q, heads, head_dim] over the keys that each sees, and the log of the
         sum of exponentials [n_q, heads] (float32); scale is head_dim ** -0.5 by default."""
-        import torch
-        st, dim = self._stream(stream), self._dim
+        torch, st, dim = self._torch, self._stream(stream), self._dim
+        if plan.cache is not self:
+            raise ValueError("the plan is another cache's")
         rows = self._rows("q", q, plan.n_q, plan.heads)
         if out is None:
-            out = self._empty(stream, plan.n_q, plan.heads, dim, dtype=self.dtype)
+            out = self._empty(stream, (plan.n_q, plan.heads, dim), self.dtype)
             to = out.data_ptr(), plan.heads * dim, dim
         else:
             to = self._rows("out", out, plan.n_q, plan.heads)
         if lse is None:
-            lse = self._empty(stream, plan.n_q, plan.heads, dtype=torch.float32)
-        elif lse.dtype != torch.float32 or lse.device != self.device or lse.shape != (plan.n_q, plan.heads) or not lse.is_contiguous():
+            lse = self._empty(stream, (plan.n_q, plan.heads), torch.float32)
+        elif lse.dtype is not torch.float32 or lse.get_device() != self._index or lse.shape != (plan.n_q, plan.heads) or not lse.is_contiguous():
             raise ValueError(f"lse must be a contiguous float32 tensor [{plan.n_q}, {plan.heads}] on {self.device}")
-        self._done(self._lib.sim_kv_attend(self._ref, plan._ref, layer, *rows, 1.0 / math.sqrt(dim) if scale is None else scale,
-                                           *to, lse.data_ptr(), st))
+        rc = self._lib.sim_kv_attend(self._ref, plan._ref, layer, *rows, 1.0 / math.sqrt(dim) if scale is None else scale,
+                                     *to, lse.data_ptr(), st)
+        if rc:
+            self._fail(rc)
         return out, lse
