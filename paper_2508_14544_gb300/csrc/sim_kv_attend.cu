@@ -331,9 +331,9 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                 if (u > from && u < from + it.tiles && before <= from && !it.partial) {
                     KvCut cut;
                     cut.h = h;
-                    cut.c0 = share.of(from);
-                    cut.n = share.of(from + it.tiles - 1) - cut.c0 + 1;
-                    cut.row = piece_row(it, cut.h, cut.c0, base, light);
+                    const int c0 = share.of(from);
+                    cut.n = share.of(from + it.tiles - 1) - c0 + 1;
+                    cut.row = piece_row(it, cut.h, c0, base, light);
                     cut.q0 = it.q0;
                     cut.row0 = it.row0;
                     cut.rows = it.rows;
@@ -355,29 +355,26 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
 // The partial results of one item and head: row `row` in the first of n pieces of blocks c0, c0 + 1, ..
 struct Pieces {
     int64_t row;
-    int c0, n, light;
-    __device__ Pieces() : row(0), c0(0), n(0), light(0) {}
+    int n, light;
+    __device__ Pieces() : row(0), n(0), light(0) {}
     // unit, tiles, row_off, rows: of the item
-    __device__ Pieces(const Share &share, int64_t base, int64_t unit, int tiles, int64_t row_off, int rows, int h, int light_) : row(0), c0(0), n(0), light(light_) {
+    __device__ Pieces(const Share &share, int64_t base, int64_t unit, int tiles, int64_t row_off, int rows, int h, int light_) : row(0), n(0), light(light_) {
         if (tiles > 0) {
             const int64_t from = unit + int64_t(h) * kv_span(tiles, light) + kv_lead(light);
-            c0 = share.of(from);
+            const int c0 = share.of(from);
             n = share.of(from + tiles - 1) - c0 + 1;
             row = base + row_off + int64_t(h) * rows + int64_t(light ? kAttRows / 2 : kAttRows) * c0;
         }
     }
-    // Row `in` of the item in piece i, -1 if the block has none of its tiles (where there are fewer tiles than blocks).
-    __device__ int64_t at(const Share &share, int i, int in) const {
-        if (i < 0 || i >= n) return -1;
-        if (share.each == 0 && share.at(c0 + i) == share.at(c0 + i + 1)) return -1;
-        return row + int64_t(light ? kAttRows / 2 : kAttRows) * i + in;
-    }
+    // Row `in` of the item in piece i, -1 if there is none.
+    __device__ int64_t at(int i, int in) const { return i >= 0 && i < n ? row + int64_t(light ? kAttRows / 2 : kAttRows) * i + in : -1; }
 };
 
-constexpr int kJoin = 256;      // threads
-constexpr int kJoinRows = 16;   // rows of a block at a time, 16 lanes each
-constexpr int kJoinHeavy = 8;   // blocks for each cut of a heavy item, of a light one
-constexpr int kJoinLight = 2;
+constexpr int kJoin = 128;      // threads
+constexpr int kJoinRows = 8;    // rows of a block at a time, 16 lanes each: as many as a token has heads in a group, often
+constexpr int kJoinHeavy = 16;  // blocks for each cut of a heavy item, of a light one
+constexpr int kJoinLight = 4;
+constexpr int kJoinMany = 12;   // more pieces than this are read by the whole block
 
 // Rows whose keys were divided among items or blocks, or that see none.  A chain of dependent loads bounds it, so it is
 // kept short (what a row needs of its source lies in one record) and every row is a half warp's own: its lanes
@@ -385,7 +382,7 @@ constexpr int kJoinLight = 2;
 // goes over what there is to join: items without a prefix that blocks' stretches cut, then entries with a shared prefix
 // and rows without keys, by kv head (`parts` blocks for each).
 template <bool BF>
-__global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
+__global__ void __launch_bounds__(kJoin, 8) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
     const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, sl = threadIdx.x & 15, sub = threadIdx.x >> 4;
@@ -397,9 +394,67 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
             if (4 * (sl + 16 * q) < D) *reinterpret_cast<uint2 *>(o + 4 * (sl + 16 * q)) = make_uint2(pack<BF>(v[q].x, v[q].y), pack<BF>(v[q].z, v[q].w));
         if (sl == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = lse;
     };
+    // A row in many pieces: every warp takes each fourth of them, up to 32 sums and then eight pieces at once; a lane has
+    // four columns.
+    __shared__ float4 many_acc[kJoin / 32][32];
+    __shared__ float2 many_sum[kJoin / 32];
+    const auto join_many = [&](const Pieces &own, int in, int t, int qh) {
+        constexpr int W = kJoin / 32;
+        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, col = 4 * lane < D ? lane : 0;
+        float top = -INFINITY, total = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int p0 = w; p0 < own.n; p0 += 32 * W) {
+            const int64_t at = own.at(p0 + W * lane, in);
+            const float s = at >= 0 ? __ldcg(a.part_lse + at) : -INFINITY;
+            float up = s;
+#pragma unroll
+            for (int d = 16; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(FULL, up, d));
+            up = fmaxf(up, top);
+            const float wl = s == -INFINITY ? 0.f : ex2(s - up), f = top == -INFINITY ? 0.f : ex2(top - up);
+            top = up;
+            total *= f;
+            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+#pragma unroll 1
+            for (int i0 = 0; i0 < 32 && p0 + W * i0 < own.n; i0 += 8) {
+                float4 v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __ldcg(reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(FULL, at, i0 + e), int64_t(0)) * D) + col);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float we = __shfl_sync(FULL, wl, i0 + e);
+                    total += we;
+                    acc = we == 0.f ? acc : make_float4(fmaf(v[e].x, we, acc.x), fmaf(v[e].y, we, acc.y), fmaf(v[e].z, we, acc.z), fmaf(v[e].w, we, acc.w));
+                }
+            }
+        }
+        many_acc[w][lane] = acc;
+        if (lane == 0) many_sum[w] = make_float2(top, total);
+        __syncthreads();
+        if (w == 0) {
+            float up = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < W; ++k) up = fmaxf(up, many_sum[k].y == 0.f ? -INFINITY : many_sum[k].x);
+            top = up;
+            total = 0.f;
+            acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                const float wk = many_sum[k].y == 0.f ? 0.f : ex2(many_sum[k].x - up);
+                const float4 u = many_acc[k][lane];
+                total += wk * many_sum[k].y;
+                acc = make_float4(fmaf(u.x, wk, acc.x), fmaf(u.y, wk, acc.y), fmaf(u.z, wk, acc.z), fmaf(u.w, wk, acc.w));
+            }
+            const float f = total == 0.f ? 0.f : 1.f / total;
+            if (4 * lane < D)
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh + 4 * lane) = make_uint2(pack<BF>(acc.x * f, acc.y * f), pack<BF>(acc.z * f, acc.w * f));
+            if (lane == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+        }
+        __syncthreads();
+    };
     const uint32_t heavy = uint32_t(plan.hdr[7]) * kJoinHeavy, cuts = heavy + uint32_t(plan.hdr[23]) * kJoinLight;
     const uint32_t all = cuts + uint32_t(plan.hdr[17]) * uint32_t(H) * uint32_t(parts);  // at most 2^30 and the cuts
-    const Share share0(plan, 0, a.sms), share1(plan, 1, a.sms);
+    const Share share0(plan, 0), share1(plan, 1);
     const int64_t base1 = list_base(plan, 1, a.sms);
 #pragma unroll 1
     for (uint32_t y = blockIdx.x; y < all; y += gridDim.x) {
@@ -413,7 +468,6 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
             const uint32_t nth = light ? y - heavy : y, per = light ? kJoinLight : kJoinHeavy, c = nth / per;
             const KvCut cut = (light ? plan.cut[1] : plan.cut[0])[c];
             own.row = cut.row - cut.row0;
-            own.c0 = cut.c0;
             own.n = cut.n;
             own.light = light;
             q0 = cut.q0;
@@ -421,8 +475,12 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
             z = cut.row0 + int(nth - c * per) * kJoinRows + sub;
             z1 = cut.row0 + cut.rows;
             step = kJoinRows * int(per);
+            if (own.n > kJoinMany) {  // the whole block for each row
+                for (int r = cut.row0 + int(nth - c * per); r < z1; r += int(per)) join_many(own, r, q0 + int(a.group.div(r)), h * G + r - int(a.group.div(r)) * G);
+                continue;
+            }
         } else {
-            const uint32_t part = (y - cuts) % uint32_t(parts), ih = (y - cuts) / uint32_t(parts), i = ih / uint32_t(H);
+            const uint32_t pairs = uint32_t(plan.hdr[17]) * uint32_t(H), part = (y - cuts) / pairs, ih = (y - cuts) - part * pairs, i = ih / uint32_t(H);
             h = int(ih - i * H);
             x = plan.source[b.n_groups + plan.join[i]];
             q0 = x.q0;
@@ -463,8 +521,8 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
 #pragma unroll 1
             for (int p0 = 0; p0 < n; p0 += 16) {
                 const int p = p0 + sl;
-                const int64_t at = p < first.n ? first.at(first.light ? share1 : share0, p, pin) : own.at(own.light ? share1 : share0, p - first.n, in);
-                const float s = at >= 0 ? a.part_lse[at] : -INFINITY;
+                const int64_t at = p < first.n ? first.at(p, pin) : own.at(p - first.n, in);
+                const float s = at >= 0 ? __ldcg(a.part_lse + at) : -INFINITY;
                 float up = s;
 #pragma unroll
                 for (int d = 8; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(mine, up, d));
@@ -481,7 +539,7 @@ __global__ void __launch_bounds__(kJoin, 4) k_combine(const sim_kv kv, const sim
                     for (int e = 0; e < 4; ++e) {
                         const float4 *from = reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(mine, at, i0 + e, 16), int64_t(0)) * D);
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) v[e][q] = from[4 * (sl + 16 * q) < D ? sl + 16 * q : 0];
+                        for (int q = 0; q < 2; ++q) v[e][q] = __ldcg(from + (4 * (sl + 16 * q) < D ? sl + 16 * q : 0));
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -570,7 +628,7 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
-    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 4));
+    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 8));
     return launch_chained(kv.dtype == SIM_KV_BF16 ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 

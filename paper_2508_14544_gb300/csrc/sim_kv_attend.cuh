@@ -19,28 +19,28 @@ constexpr int kStage = 128 * kPitch;   // words through which the results of 128
 constexpr int kSegs = 4;               // segments that the loading warp may be ahead
 constexpr float kGrow = 8.f;           // log2 of what P may reach before O is rescaled
 
-// A list's line (the spans of its items, one after the other) divided among its blocks: [at(c), at(c + 1)) is block c's.  (With no division but one of small
-// numbers: code that runs once is paid for by its size.)
+// A list's line (the spans of its items, one after the other) divided among its blocks: [at(c), at(c + 1)) is block c's,
+// each + 1 places for the first `rest` blocks and `each` for the others.
 struct Share {
-    int64_t units, each;  // units = each * blocks + rest
-    int rest, blocks;
-    __device__ Share() : units(0), each(0), rest(0), blocks(1) {}
-    __device__ Share(int64_t units_, int blocks_) : units(units_), blocks(blocks_) {
-        each = units_ < INT_MAX ? int64_t(uint32_t(units_) / uint32_t(blocks_)) : units_ / blocks_;
+    int64_t units, each;
+    int rest;
+    __device__ Share(int64_t units_, int blocks) : units(units_) {
+        each = units_ <= INT_MAX ? int64_t(uint32_t(units_) / uint32_t(blocks)) : units_ / blocks;
         rest = int(units - each * blocks);
     }
-    __device__ Share(const KvPlan &p, int light, int sms) : blocks(kv_blocks(sms, light)) {
+    __device__ Share(const KvPlan &p, int light) {
         const int32_t *h = p.hdr + 16 * light;
         units = *reinterpret_cast<const int64_t *>(h + 2);
         each = *reinterpret_cast<const int64_t *>(h + 4);
         rest = h[6];
     }
-    __device__ int64_t at(int c) const { return each * c + uint32_t(rest * c) / uint32_t(blocks); }
-    __device__ int of(int64_t u) const {  // the block that has place u
-        int c = min(int(float(u) * __fdividef(float(blocks), float(units))), blocks - 1);  // off by one at most
-        while (at(c + 1) <= u) ++c;
-        while (at(c) > u) --c;
-        return c;
+    __device__ int64_t at(int c) const { return each * c + min(c, rest); }
+    __device__ int of(int64_t u) const {  // the block that has place u < units
+        const int64_t more = (each + 1) * rest;
+        const bool front = u < more;
+        const int64_t n = front ? u : u - more, d = front ? each + 1 : each;
+        const int c = n <= INT_MAX && d <= INT_MAX ? int(uint32_t(n) / uint32_t(d)) : int(n / d);
+        return front ? c : rest + c;
     }
 };
 
@@ -71,7 +71,7 @@ struct Line {
     int n_items, heads, k, h, c, light;
     __device__ Line(const KvPlan &p, int heads_, int light_, int c_, int sms) : items(p.items[light_]), heads(heads_), c(c_), light(light_) {
         n_items = p.hdr[16 * light];
-        const Share share(p, light, sms);
+        const Share share(p, light);
         u = share.at(c);
         u1 = share.at(c + 1);
         base = list_base(p, light, sms);

@@ -107,7 +107,7 @@ static_assert(sizeof(KvSource) == 64, "KvSource");
 // its pieces there.
 struct alignas(16) KvCut {
     int64_t row;        // partial results of the first piece
-    int32_t c0, n;      // pieces
+    int32_t n, pad;     // pieces
     int32_t q0, row0, rows, h;
 };
 static_assert(sizeof(KvCut) == 32, "KvCut");
