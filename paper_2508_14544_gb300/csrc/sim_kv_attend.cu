@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             x.pos0 = e.len - e.t;
             x.prefix = shared > 0 ? g : -1;
             x.blind = e.len < e.t;
+
         }
         Two total;
         const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows)) << 32 | heavy_items(x.rows), 0}, sums, total).a;
@@ -382,7 +383,7 @@ constexpr int kJoinMany = 12;   // more pieces than this are read by the whole b
 // goes over what there is to join: items without a prefix that blocks' stretches cut, then entries with a shared prefix
 // and rows without keys, by kv head (`parts` blocks for each).
 template <bool BF>
-__global__ void __launch_bounds__(kJoin, 8) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
+__global__ void __launch_bounds__(kJoin, 6) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
     const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, sl = threadIdx.x & 15, sub = threadIdx.x >> 4;
@@ -523,6 +524,16 @@ __global__ void __launch_bounds__(kJoin, 8) k_combine(const sim_kv kv, const sim
                 const int p = p0 + sl;
                 const int64_t at = p < first.n ? first.at(p, pin) : own.at(p - first.n, in);
                 const float s = at >= 0 ? __ldcg(a.part_lse + at) : -INFINITY;
+                float4 v[4][2];  // a piece that is not there: row 0, with weight 0
+                const auto fetch = [&](int i0) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 *from = reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(mine, at, i0 + e, 16), int64_t(0)) * D);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) v[e][q] = __ldcg(from + (4 * (sl + 16 * q) < D ? sl + 16 * q : 0));
+                    }
+                };
+                fetch(0);  // on their way while the sums are waited for
                 float up = s;
 #pragma unroll
                 for (int d = 8; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(mine, up, d));
@@ -534,13 +545,7 @@ __global__ void __launch_bounds__(kJoin, 8) k_combine(const sim_kv kv, const sim
                 for (int q = 0; q < 2; ++q) acc[q] = make_float4(acc[q].x * f, acc[q].y * f, acc[q].z * f, acc[q].w * f);
 #pragma unroll 1
                 for (int i0 = 0; i0 < min(16, n - p0); i0 += 4) {
-                    float4 v[4][2];  // a piece that is not there: row 0, with weight 0
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float4 *from = reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(mine, at, i0 + e, 16), int64_t(0)) * D);
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) v[e][q] = __ldcg(from + (4 * (sl + 16 * q) < D ? sl + 16 * q : 0));
-                    }
+                    if (i0 > 0) fetch(i0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float we = __shfl_sync(mine, w, i0 + e, 16);
@@ -628,7 +633,7 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
-    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 8));
+    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 6));
     return launch_chained(kv.dtype == SIM_KV_BF16 ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 
