@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_fp16.h>
 
 #include <climits>
 #include <cmath>
@@ -59,7 +60,7 @@ struct alignas(16) Segment {
     int32_t q0, row0, rows, pos0;
     int32_t k0, kv1;         // first key, end of the keys
     int32_t direct;          // results go to the output, not to the workspace
-    int32_t pad;
+    int32_t seq;             // row of the table
     int64_t row;             // row of the partial results
 };
 
@@ -102,6 +103,7 @@ struct Line {
             s.pos0 = it.pos0;
             s.k0 = it.kv0 + t0 * kv_tile(light);
             s.kv1 = it.kv1;
+            s.seq = it.seq;
             s.direct = s.n == it.tiles && !it.partial;
             s.row = piece_row(it, h, c, base, light);
             return;
@@ -345,9 +347,53 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, 
 // Where the results of a segment go.
 template <bool BF>
 struct Sink {
+    const sim_kv &kv;
     const KvAttend &a;
     const Segment &sg;
-    int G, D, q_heads;
+    int G, D, q_heads, end;  // end: of the keys of the segment's tiles
+    // First key of the segment that row y does not see, and whether its tiles have such keys.
+    __device__ int seen(int y) const { return min(sg.kv1, sg.pos0 + int(a.group.div(sg.row0 + y)) + 1); }
+    __device__ bool blind(int y) const { return seen(y) < min(end, sg.kv1); }
+    // A row that does not see all of its tiles' keys has met the values of the others with probability 0, which is not nothing
+    // where they are infinite or not a number.  Where its result is not finite it is computed again here from the keys that it
+    // sees: one warp, a key at a time, a lane for four columns.
+    __device__ void again(int y) const {
+        const int lane = threadIdx.x & 31, P = kv.page_size, d = 4 * lane;
+        const bool in = d < D;
+        const auto wide = [](uint32_t w) {
+            if constexpr (BF) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+            else return make_float2(__half2float(__ushort_as_half(uint16_t(w))), __half2float(__ushort_as_half(uint16_t(w >> 16))));
+        };
+        const int t = a.group.div(sg.row0 + y);
+        const uint16_t *q = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0 + t) * a.qt + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.qh;
+        const float2 q0 = in ? wide(q[d] | uint32_t(q[d + 1]) << 16) : make_float2(0.f, 0.f), q1 = in ? wide(q[d + 2] | uint32_t(q[d + 3]) << 16) : make_float2(0.f, 0.f);
+        const uint16_t *layer = static_cast<const uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv);
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int key = sg.k0; key < min(seen(y), end); ++key) {
+            const int page = kv.table[int64_t(sg.seq) * kv.max_pages + key / P];
+            uint2 k = make_uint2(0, 0), v = k;
+            if (in && unsigned(page) < unsigned(kv.n_pages)) {
+                const uint16_t *at = layer + page * (kv_page_bytes(kv) / 2) + (int64_t(sg.h) * P + key % P) * D + d;
+                k = *reinterpret_cast<const uint2 *>(at);
+                v = *reinterpret_cast<const uint2 *>(at + kv_layer_elems(kv) / 2);
+            }
+            const float2 k0 = wide(k.x), k1 = wide(k.y), v0 = wide(v.x), v1 = wide(v.y);
+            float s = q0.x * k0.x + q0.y * k0.y + q1.x * k1.x + q1.y * k1.y;
+#pragma unroll
+            for (int i = 16; i >= 1; i >>= 1) s += __shfl_xor_sync(FULL, s, i);
+            const float up = fmaxf(m, s * a.scale_log2), f = m == -INFINITY ? 0.f : ex2(m - up), p = ex2(s * a.scale_log2 - up);
+            m = up;
+            l = l * f + p;
+            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+            if (p != 0.f) o = make_float4(fmaf(p, v0.x, o.x), fmaf(p, v0.y, o.y), fmaf(p, v1.x, o.z), fmaf(p, v1.y, o.w));
+        }
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        if (!in) return;
+        if (sg.direct) *reinterpret_cast<uint2 *>(out_row(y) + d) = make_uint2(pack<BF>(o.x * f, o.y * f), pack<BF>(o.z * f, o.w * f));
+        else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+    }
     __device__ uint16_t *out_row(int y) const {  // of row y of the item
         const int t = a.group.div(sg.row0 + y);
         return static_cast<uint16_t *>(a.out) + int64_t(sg.q0 + t) * a.ot + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.oh;
@@ -373,6 +419,7 @@ struct Sink {
             to[q] = (sg.direct ? reinterpret_cast<char *>(out_row(y)) : reinterpret_cast<char *>(a.part + (sg.row + y) * D)) + lane % 4 * 16;
         }
         const int cols = sg.direct ? 32 : 16;
+        float finite = 0.f;  // 0 times every result: not 0 if one is not finite
 #pragma unroll 1
         for (int d0 = 0; d0 < D; d0 += cols) {
             uint32_t x[16];
@@ -381,12 +428,19 @@ struct Sink {
                 tm_ld32(t_o + d0, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
+                for (int y = 0; y < 16; ++y) {
+                    finite = fmaf(__uint_as_float(o[2 * y]), 0.f, finite);
+                    finite = fmaf(__uint_as_float(o[2 * y + 1]), 0.f, finite);
+                    x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
+                }
             } else {
                 tm_ld16(t_o + d0, x);
                 tc_wait_ld();
 #pragma unroll
-                for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
+                for (int y = 0; y < 16; ++y) {
+                    finite = fmaf(__uint_as_float(x[y]), 0.f, finite);
+                    x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
+                }
             }
 #pragma unroll
             for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4 *>(mine + lane * kPitch + y) = make_uint4(x[y], x[y + 1], x[y + 2], x[y + 3]);
@@ -400,6 +454,12 @@ struct Sink {
                 to[q] += 64;
             }
             __syncwarp();
+        }
+        const int row = row0 + lane;
+        unsigned redo = __ballot_sync(FULL, row < rows && finite != 0.f && !empty && blind(row));
+        while (redo) {
+            again(row0 + __ffs(redo) - 1);
+            redo &= redo - 1;
         }
     }
 };

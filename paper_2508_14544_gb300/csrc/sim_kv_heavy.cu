@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             }
             if (!ok) break;
             at += 2 * sg.n;
-            const Sink<BF> sink = {a, sg, G, D, b.q_heads};
+            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + sg.n * kv_tile(0)};
             if (r < sg.rows) sink.lse(r, m, l);
             ok = __all_sync(FULL, bar_wait(o_full(g), x & 1, gave_up));
             if (!ok) break;

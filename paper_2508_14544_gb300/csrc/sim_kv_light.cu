@@ -24,7 +24,8 @@ struct Shape {
     static constexpr int kJoinStage = 2560;          // floats: 4 copies of 32 rows x (16 + 4), or of fewer and longer ones
     static_assert(kJoinStage >= kStage, "stage");
     static constexpr int kOffStat = kOffStage + kJoinStage * 4;
-    static constexpr int kOffSeg = kOffStat + 2 * 128 * 8;
+    static constexpr int kOffAgain = kOffStat + 2 * 128 * 8;  // rows whose results are not finite
+    static constexpr int kOffSeg = kOffAgain + 32 * 4;
     static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
     static constexpr int kBars = 2 * kSlots + 2 * kSegs + 6;
     static constexpr int kBytes = kOffBar + kBars * 8 + 16;
@@ -218,6 +219,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
         const uint32_t t_s = tmem + (uint32_t(w * 32) << 16), t_q = t_s + Sh::kColQ, t_o = t_s + Sh::kColO;
         float *const stage = reinterpret_cast<float *>(base + Sh::kOffStage);
         float2 *const stat = reinterpret_cast<float2 *>(base + Sh::kOffStat);
+        int *const again = reinterpret_cast<int *>(base + Sh::kOffAgain);
         const float c = a.scale_log2;
         uint32_t ns = 0, nj = 0;
         Ring ring;  // of the tile's keys
@@ -313,7 +315,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (next.n > 0) load_q(next);  // every product with this item's queries has been read
             if (!real) continue;
 
-            const Sink<BF> sink = {a, sg, G, D, b.q_heads};
+            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + n * NK};
             if (span == 128) {
                 if (row < rows) sink.lse(row, m, l);
                 ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up));
@@ -333,6 +335,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                     if (st[32 * p + lane].y != 0.f) total += st[32 * p + lane].y * ex2((st[32 * p + lane].x - top) * c);
                 const float f = l == 0.f ? 0.f : ex2((m - top) * c) / total;
                 if (lr < rows) sink.lse(lr, top, total);
+                if (lr < 32) again[lr] = 0;
                 // As many columns at a time as the stage holds of all copies.  No wait is needed after the last ones: the stage is
                 // used again only after the other warps have gone on to another item.
                 int cols = DP, shift = DP == 128 ? 5 : 4;  // log2 of the columns / 4
@@ -375,9 +378,16 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                                                      (v[0].z + v[1].z) + (v[2].z + v[3].z), (v[0].w + v[1].w) + (v[2].w + v[3].w));
                         if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d0 + d) = make_uint2(pack<BF>(t.x, t.y), pack<BF>(t.z, t.w));
                         else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d0 + d) = t;
+                        if (t.x * 0.f + t.y * 0.f + t.z * 0.f + t.w * 0.f != 0.f) again[y] = 1;
                     }
                 }
                 if (!ok) break;
+                if (sink.blind(0)) {  // see Sink::again
+                    join();
+                    if (!ok) break;
+                    for (int y = w; y < rows; y += 4)
+                        if (again[y] && sink.blind(y)) sink.again(y);
+                }
             }
             tc_fence_before();
             give_back(x);

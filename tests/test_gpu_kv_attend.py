@@ -127,6 +127,33 @@ def test_what_lies_past_the_end_is_not_used(rest, group):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("lens,queries,group,dim", [([70, 200], [6, 5], 3, 64), ([300, 65], [30, 40], 2, 80), ([500], [200], 4, 128), ([5000], [7], 2, 128)])
+def test_keys_that_a_query_does_not_see_yet(lens, queries, group, dim, bad, dtype):
+    """The newest tokens' keys and values are infinite or not a number: queries before them are as without them."""
+    c = Case(lens, queries, group=group, dim=dim, dtype=dtype, kv_heads=1, seed=7)
+    torch, P, at = c.torch, c.kv.pool.shape[4], 0
+    out, lse = c.run()
+    c.check(out, lse)
+    keep = torch.zeros(c.n_q, dtype=torch.bool, device="cuda")
+    for i, (n, t) in enumerate(zip(lens, queries)):
+        new = t // 3 + 1  # so many of the last tokens
+        for x in range(n - new, n):
+            page = int(c.table[i, x // P])
+            c.kv.pool[page, :, 1, :, x % P, x % dim] = bad  # one value of each; of the very last also the keys
+            if x == n - 1:
+                c.kv.pool[page, :, 0, :, x % P] = bad
+        keep[at: at + t - new] = True
+        at += t
+    got, glse = c.run()
+    u = ROUND[dtype]
+    assert torch.isfinite(got[keep]).all() and (glse[keep] - lse[keep]).abs().max() <= 1e-5
+    # the probabilities of these rows may have been rounded in one run and not in the other
+    assert ((got[keep].float() - out[keep].float()).abs() <= 2.5 * u * out[keep].float().abs().clamp(min=0.5) + 4 * u).all()
+    assert not torch.isfinite(got[~keep]).all(dim=-1).all(dim=-1).any()
+
+
 @pytest.mark.parametrize("dtype,dim,page,group", [("bfloat16", 128, 16, 8), ("float16", 80, 32, 5), ("bfloat16", 64, 64, 1), ("float16", 128, 128, 3)])
 def test_shared_prefixes(dtype, dim, page, group):
     groups, prefix = [40, 1, 9, 3], 1500
