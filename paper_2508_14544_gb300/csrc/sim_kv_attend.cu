@@ -53,6 +53,8 @@ __device__ __forceinline__ int group_of(const sim_kv_batch &b, int i) {
     return lo >= 0 && i < b.cu_group[lo + 1] ? lo : -1;
 }
 
+constexpr int kAhead = 16;
+
 // A warp for each entry: the pages that its table begins with like that of its group's first entry, all of whose
 // keys each of its queries sees.
 __global__ void __launch_bounds__(256) k_plan_shared(const sim_kv kv, const sim_kv_batch b) {
@@ -72,17 +74,18 @@ __global__ void __launch_bounds__(256) k_plan_shared(const sim_kv kv, const sim_
         const int most = min(max(e.len - e.t + 1, 0), kv.length[s0]) / kv.page_size;
         const int32_t *x = kv.table + int64_t(e.seq) * kv.max_pages, *y = kv.table + int64_t(s0) * kv.max_pages;
         same = most;
-        for (int j0 = 0; j0 < most; j0 += 128) {
-            bool differ[4];
+        for (int j0 = 0; j0 < most; j0 += 32 * kAhead) {  // that many loads of either table in flight
+            int32_t u[kAhead], v[kAhead];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kAhead; ++k) {
                 const int j = j0 + 32 * k + lane;
-                differ[k] = j < most && x[j] != y[j];
+                u[k] = j < most ? x[j] : 0;
+                v[k] = j < most ? y[j] : 0;
             }
             int at = INT_MAX;
 #pragma unroll
-            for (int k = 3; k >= 0; --k) {
-                const unsigned m = __ballot_sync(FULL, differ[k]);
+            for (int k = kAhead - 1; k >= 0; --k) {
+                const unsigned m = __ballot_sync(FULL, u[k] != v[k]);
                 if (m) at = j0 + 32 * k + __ffs(m) - 1;
             }
             if (at != INT_MAX) {

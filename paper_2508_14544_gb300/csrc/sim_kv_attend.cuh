@@ -279,8 +279,9 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_
 // in each of R warps (1 or 4); warp w takes NK / R keys of its rows and leaves zeros for the others.  lim: the last
 // of this thread's keys that its row sees.  m, l: the maximum that P refers to and the sum so far of this
 // thread's keys; DP columns of O from t_o on.
-template <int NK, int R, int DP, bool BF>
-__device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, int lim, bool first, float c, float &m, float &l) {
+// half: called when the first half of P is in place (R = 1, 128 keys).
+template <int NK, int R, int DP, bool BF, typename Half>
+__device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, int lim, bool first, float c, float &m, float &l, Half &&half) {
     constexpr int NC = NK / R;
     static_assert(R == 1 || (R == 4 && NC == 16), "copies");
     const int c0 = R == 4 ? w * NC : 0;
@@ -326,12 +327,19 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, 
         e = make_float2(ex2(e.x), ex2(e.y));
         sum[y / 2 & 3] = add2(sum[y / 2 & 3], e);
         pk[y / 2] = pack<BF>(e.x, e.y);
+        if constexpr (NC == 128) {
+            if (y == NC / 2 - 2) {
+                tm_st32(t_s, pk);
+                tc_wait_st();
+                half();
+            }
+        }
     }
     sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
     l += sum[0].x + sum[0].y;
     if constexpr (R == 1) {
 #pragma unroll
-        for (int q = 0; q < NC / 64; ++q) tm_st32(t_s + 32 * q, pk + 32 * q);
+        for (int q = NC == 128; q < NC / 64; ++q) tm_st32(t_s + 32 * q, pk + 32 * q);
     } else {
 #pragma unroll
         for (int q = 0; q < R; ++q) {

@@ -28,7 +28,7 @@ struct Shape {
     static constexpr int kOffStage = kOffRing + kSlots * kTile;
     static constexpr int kOffSeg = kOffStage + kGroups * kStage * 4;
     static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
-    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 3 * kGroups + 1;
+    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 4 * kGroups + 1;
     static constexpr int kBytes = kOffBar + kBars * 8 + 16;
     static constexpr int kAlloc = kBytes + 1024;                              // the base is rounded up to 1024
     static_assert(kAlloc <= 232448, "shared memory");
@@ -54,7 +54,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
     const auto s_full = [&](int g) { return bars + 8 * (kRest + 2 + g); };
     const auto p_ready = [&](int g) { return bars + 8 * (kRest + 2 + NG + g); };
     const auto o_full = [&](int g) { return bars + 8 * (kRest + 2 + 2 * NG + g); };
-    const uint32_t drained = bars + 8 * (kRest + 2 + 3 * NG);
+    const auto p_half = [&](int g) { return bars + 8 * (kRest + 2 + 3 * NG + g); };
+    const uint32_t drained = bars + 8 * (kRest + 2 + 4 * NG);
     const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31, role = warp - 4 * NG;
 
     if (tid == 0) {
@@ -71,6 +72,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
         for (int g = 0; g < NG; ++g) {
             bar_init(s_full(g), 1);
             bar_init(p_ready(g), 4);
+            bar_init(p_half(g), 4);
             bar_init(o_full(g), 1);
         }
         bar_init(drained, 1);
@@ -193,18 +195,26 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                     ok = wait_full(at + 2 * j + 1);
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
-                        ok = ok && wait(p_ready(g), np & 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint32_t slot = (at + 2 * j + 1) % NS;
+                        const uint32_t slot = (at + 2 * j + 1) % NS;
+                        const auto values = [&](int from) {  // half of the tile's keys
+                            tc_fence_after();
+                            if (elect_one()) {
 #pragma unroll
-                            for (int kk = 0; kk < kv_tile(0) / 16; ++kk)
-                                mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + kk * 8, op_v + ((slot * Sh::kTile + kk * 2048) >> 4), idesc_o, j > 0 || kk > 0);
-                            if (g == NG - 1) tc_commit(empty(at + 2 * j + 1));
-                            if (j + 1 == n) tc_commit(o_full(g));
-                        }
-                        __syncwarp();
+                                for (int kk = 0; kk < kv_tile(0) / 32; ++kk)
+                                    mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + (from + kk) * 8, op_v + ((slot * Sh::kTile + (from + kk) * 2048) >> 4), idesc_o, j > 0 || from + kk > 0);
+                                if (from > 0) {
+                                    if (g == NG - 1) tc_commit(empty(at + 2 * j + 1));
+                                    if (j + 1 == n) tc_commit(o_full(g));
+                                }
+                            }
+                            __syncwarp();
+                        };
+                        ok = ok && wait(p_half(g), np & 1);
+                        if (!ok) break;
+                        values(0);
+                        ok = wait(p_ready(g), np & 1);
+                        if (!ok) break;
+                        values(kv_tile(0) / 32);
                         if (j + 1 < n) {
                             if (g == 0) ok = wait_full(at + 2 * j + 2);
                             if (!ok) break;
@@ -297,7 +307,6 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (!ok) break;
                 ++ns;
                 tc_fence_after();
-                softmax_tile<128, 1, DP, BF>(t_s, t_o, w, last - k0, j == 0, c, m, l);
                 // values past the end of the keys, whatever they are, must not meet their zero probabilities
                 const int valid = sg.kv1 - k0;
                 if (valid < kv_tile(0) && g == 0) {
@@ -310,6 +319,11 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                     }
                     smem_to_async();
                 }
+                softmax_tile<128, 1, DP, BF>(t_s, t_o, w, last - k0, j == 0, c, m, l, [&] {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(p_half(g));
+                });
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_ready(g));

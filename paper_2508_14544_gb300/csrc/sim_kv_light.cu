@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                     if (!ok) return;
                     ++ns;
                     tc_fence_after();
-                    softmax_tile<NK, R, DP, BF>(t_s, t_o, w, last - k0 - c0, j == 0, c, m, l);
+                    softmax_tile<NK, R, DP, BF>(t_s, t_o, w, last - k0 - c0, j == 0, c, m, l, [] {});
                     ring.next();
                     // values past the end of the keys, whatever they are, must not meet their zero probabilities
                     const int valid = kv1 - k0;
