@@ -299,7 +299,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
         Segment sg;
         for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
             const int r = g * 128 + lr;  // the row in this thread's lane
-            const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : -1;  // key position that it sees last
+            // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
+            const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : sg.kv1 - 1;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
                 const int k0 = sg.k0 + j * kv_tile(0);  // first key of the tile

@@ -267,7 +267,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             const int n = real ? sg.n : 0;
             if (real && n == 0) break;
             const int rows = sg.rows, span = span_of(rows), row = lr & (span - 1);
-            const int last = row < rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + row))) : -1;  // key position that it sees last
+            // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
+            const int last = row < rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + row))) : sg.kv1 - 1;
             float m = -INFINITY, l = 0.f;
             const auto tiles = [&](auto copies) {
                 constexpr int R = decltype(copies)::value;
