@@ -146,7 +146,7 @@ int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const 
                   float scale, void *out, int64_t out_token_stride, int64_t out_head_stride, float *lse, void *cuda_stream) {
     if (const char *m = bad_batch(kv, b)) return fail(SIM_E_INVAL, "sim_kv_attend: %s", m);
     if (layer < 0 || layer >= kv->n_layers) return fail(SIM_E_INVAL, "sim_kv_attend: layer %d outside [0, %d)", layer, kv->n_layers);
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(SIM_E_INVAL, "sim_kv_attend: scale must be positive and finite");
+    if (!(scale > 0.f) || !std::isfinite(scale * 1.44269504088896341f)) return fail(SIM_E_INVAL, "sim_kv_attend: scale must be positive and finite");
     if (b->n_q == 0) return SIM_OK;
     if (!q || !out || !aligned(q, 2)) return fail(SIM_E_INVAL, "sim_kv_attend: NULL or odd pointer");
     if (!aligned(out, 16) || out_token_stride % 8 || out_head_stride % 8)
@@ -163,7 +163,6 @@ int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const 
     a.qh = q_head_stride;
     a.ot = out_token_stride;
     a.oh = out_head_stride;
-    a.scale = scale;
     a.scale_log2 = scale * 1.44269504088896341f;
     a.layer = layer;
     a.q_vec = aligned(q, 16) && q_token_stride % 8 == 0 && q_head_stride % 8 == 0;

@@ -8,7 +8,7 @@
 // tokens of one sequence times the heads of its group, or those of all sequences that share a prefix.  Rows of a
 // shared prefix thus meet its keys once, as the rows of one matrix product, and their other keys in items of their own.
 //
-// The plan (k_plan_shared, k_plan_items, made once for all layers) lists the items.  Those of more than 128 rows
+// The plan (k_plan_shared, k_plan_items, made once for all layers) lists the items.  Those of more than 32 rows
 // are heavy, the others light: two kernels (sim_kv_heavy.cu, sim_kv_light.cu), because many rows want the tensor
 // products fed and few rows want bytes in flight.  The tiles of all items and heads of a list lie on one line, and every block
 // takes an equal stretch of it, so that work is even whatever the lengths; an item is split where two stretches meet, and
@@ -23,7 +23,7 @@ namespace {
 
 // ---- plan ---------------------------------------------------------------------------------------------------
 
-constexpr int kShareCost = 4;          // tiles of 128 rows that a second partial result of as many rows costs
+constexpr int kShareCost = 10;         // tiles of 128 rows that a second partial result of as many rows costs
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -128,8 +128,8 @@ __device__ __forceinline__ int tile_rows(int r) {
     const int rem = r % kAttRows;
     return 2 * (r / kAttRows) + (rem > kAttRows / 2 ? 2 : rem > 0);
 }
-__device__ __forceinline__ int heavy_items(int r) { return r / kAttRows + (r % kAttRows > kAttRows / 2); }
-__device__ __forceinline__ int light_items(int r) { return r % kAttRows > 0 && r % kAttRows <= kAttRows / 2; }
+__device__ __forceinline__ int heavy_items(int r) { return r / kAttRows + (r % kAttRows > kLightRows); }
+__device__ __forceinline__ int light_items(int r) { return r % kAttRows > 0 && r % kAttRows <= kLightRows; }
 
 constexpr int kFewSources = 448, kFewItems = 1024;
 
@@ -238,7 +238,6 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             x.pos0 = e.len - e.t;
             x.prefix = shared > 0 ? g : -1;
             x.blind = e.len < e.t;
-
         }
         Two total;
         const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows)) << 32 | heavy_items(x.rows), 0}, sums, total).a;
@@ -273,7 +272,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                 const int s = last_at_most(first, n_src, k);
                 const KvSource x = source[s];
                 it.row0 = (light ? x.n_heavy : k - x.heavy0) * kAttRows;
-                it.rows = min(x.rows - it.row0, light ? kAttRows / 2 : kAttRows);
+                it.rows = min(x.rows - it.row0, kv_rows(light));
                 it.q0 = x.q0;
                 it.seq = x.seq;
                 it.kv0 = x.kv0;
@@ -367,18 +366,17 @@ struct Pieces {
             const int64_t from = unit + int64_t(h) * kv_span(tiles, light) + kv_lead(light);
             const int c0 = share.of(from);
             n = share.of(from + tiles - 1) - c0 + 1;
-            row = base + row_off + int64_t(h) * rows + int64_t(light ? kAttRows / 2 : kAttRows) * c0;
+            row = base + row_off + int64_t(h) * rows + int64_t(kv_rows(light)) * c0;
         }
     }
     // Row `in` of the item in piece i, -1 if there is none.
-    __device__ int64_t at(int i, int in) const { return i >= 0 && i < n ? row + int64_t(light ? kAttRows / 2 : kAttRows) * i + in : -1; }
+    __device__ int64_t at(int i, int in) const { return i >= 0 && i < n ? row + int64_t(kv_rows(light)) * i + in : -1; }
 };
 
 constexpr int kJoin = 128;      // threads
 constexpr int kJoinRows = 8;    // rows of a block at a time, 16 lanes each: as many as a token has heads in a group, often
 constexpr int kJoinHeavy = 16;  // blocks for each cut of a heavy item, of a light one
 constexpr int kJoinLight = 4;
-constexpr int kJoinMany = 12;   // more pieces than this are read by the whole block
 
 // Rows whose keys were divided among items or blocks, or that see none.  A chain of dependent loads bounds it, so it is
 // kept short (what a row needs of its source lies in one record) and every row is a half warp's own: its lanes
@@ -397,64 +395,6 @@ __global__ void __launch_bounds__(kJoin, 6) k_combine(const sim_kv kv, const sim
         for (int q = 0; q < 2; ++q)
             if (4 * (sl + 16 * q) < D) *reinterpret_cast<uint2 *>(o + 4 * (sl + 16 * q)) = make_uint2(pack<BF>(v[q].x, v[q].y), pack<BF>(v[q].z, v[q].w));
         if (sl == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = lse;
-    };
-    // A row in many pieces: every warp takes each fourth of them, up to 32 sums and then eight pieces at once; a lane has
-    // four columns.
-    __shared__ float4 many_acc[kJoin / 32][32];
-    __shared__ float2 many_sum[kJoin / 32];
-    const auto join_many = [&](const Pieces &own, int in, int t, int qh) {
-        constexpr int W = kJoin / 32;
-        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, col = 4 * lane < D ? lane : 0;
-        float top = -INFINITY, total = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-        for (int p0 = w; p0 < own.n; p0 += 32 * W) {
-            const int64_t at = own.at(p0 + W * lane, in);
-            const float s = at >= 0 ? __ldcg(a.part_lse + at) : -INFINITY;
-            float up = s;
-#pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) up = fmaxf(up, __shfl_xor_sync(FULL, up, d));
-            up = fmaxf(up, top);
-            const float wl = s == -INFINITY ? 0.f : ex2(s - up), f = top == -INFINITY ? 0.f : ex2(top - up);
-            top = up;
-            total *= f;
-            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-#pragma unroll 1
-            for (int i0 = 0; i0 < 32 && p0 + W * i0 < own.n; i0 += 8) {
-                float4 v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = __ldcg(reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(FULL, at, i0 + e), int64_t(0)) * D) + col);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float we = __shfl_sync(FULL, wl, i0 + e);
-                    total += we;
-                    acc = we == 0.f ? acc : make_float4(fmaf(v[e].x, we, acc.x), fmaf(v[e].y, we, acc.y), fmaf(v[e].z, we, acc.z), fmaf(v[e].w, we, acc.w));
-                }
-            }
-        }
-        many_acc[w][lane] = acc;
-        if (lane == 0) many_sum[w] = make_float2(top, total);
-        __syncthreads();
-        if (w == 0) {
-            float up = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < W; ++k) up = fmaxf(up, many_sum[k].y == 0.f ? -INFINITY : many_sum[k].x);
-            top = up;
-            total = 0.f;
-            acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < W; ++k) {
-                const float wk = many_sum[k].y == 0.f ? 0.f : ex2(many_sum[k].x - up);
-                const float4 u = many_acc[k][lane];
-                total += wk * many_sum[k].y;
-                acc = make_float4(fmaf(u.x, wk, acc.x), fmaf(u.y, wk, acc.y), fmaf(u.z, wk, acc.z), fmaf(u.w, wk, acc.w));
-            }
-            const float f = total == 0.f ? 0.f : 1.f / total;
-            if (4 * lane < D)
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh + 4 * lane) = make_uint2(pack<BF>(acc.x * f, acc.y * f), pack<BF>(acc.z * f, acc.w * f));
-            if (lane == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
-        }
-        __syncthreads();
     };
     const uint32_t heavy = uint32_t(plan.hdr[7]) * kJoinHeavy, cuts = heavy + uint32_t(plan.hdr[23]) * kJoinLight;
     const uint32_t all = cuts + uint32_t(plan.hdr[17]) * uint32_t(H) * uint32_t(parts);  // at most 2^30 and the cuts
@@ -479,10 +419,6 @@ __global__ void __launch_bounds__(kJoin, 6) k_combine(const sim_kv kv, const sim
             z = cut.row0 + int(nth - c * per) * kJoinRows + sub;
             z1 = cut.row0 + cut.rows;
             step = kJoinRows * int(per);
-            if (own.n > kJoinMany) {  // the whole block for each row
-                for (int r = cut.row0 + int(nth - c * per); r < z1; r += int(per)) join_many(own, r, q0 + int(a.group.div(r)), h * G + r - int(a.group.div(r)) * G);
-                continue;
-            }
         } else {
             const uint32_t pairs = uint32_t(plan.hdr[17]) * uint32_t(H), part = (y - cuts) / pairs, ih = (y - cuts) - part * pairs, i = ih / uint32_t(H);
             h = int(ih - i * H);
@@ -631,7 +567,7 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     if (kv.page_size > kv_tile(1) && !encode_maps(heavy, 0)) return cudaErrorInvalidValue;
     const int64_t rows = int64_t(b.n_q) * b.q_heads;
     cudaError_t e = cudaSuccess;
-    if (rows / kv.n_kv_heads > kAttRows / 2) e = launch_kv_heavy(kv, b, a, heavy, st);  // fewer rows make no heavy item
+    if (rows / kv.n_kv_heads > kLightRows) e = launch_kv_heavy(kv, b, a, heavy, st);  // fewer rows make no heavy item
     if (e == cudaSuccess) e = launch_kv_light(kv, b, a, light, st);
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average

@@ -15,10 +15,8 @@ namespace simgb {
 namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr int kPitch = 20;             // words between rows on the stage, 16 of them used: no bank conflicts
-constexpr int kStage = 128 * kPitch;   // words through which the results of 128 rows pass
-constexpr int kSegs = 4;               // segments that the loading warp may be ahead
-constexpr float kGrow = 8.f;           // log2 of what P may reach before O is rescaled
+constexpr int kSegs = 4;      // segments that the loading warp may be ahead
+constexpr float kGrow = 8.f;  // log2 of what P may reach before O is rescaled
 
 // A list's line (the spans of its items, one after the other) divided among its blocks: [at(c), at(c + 1)) is block c's,
 // each + 1 places for the first `rest` blocks and `each` for the others.
@@ -47,7 +45,7 @@ struct Share {
 
 // First row of the partial results of block c's piece of a list whose rows follow `base` others.
 __device__ __forceinline__ int64_t piece_row(const KvItem &it, int h, int c, int64_t base, int light) {
-    return base + it.row_off + int64_t(h) * it.rows + int64_t(light ? kAttRows / 2 : kAttRows) * c;
+    return base + it.row_off + int64_t(h) * it.rows + int64_t(kv_rows(light)) * c;
 }
 __device__ __forceinline__ int64_t list_base(const KvPlan &p, int light, int sms) {
     return light ? *reinterpret_cast<const int64_t *>(p.hdr + 24) + int64_t(kAttRows) * kv_blocks(sms, 0) : 0;
@@ -279,11 +277,11 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_
 // in each of R warps (1 or 4); warp w takes NK / R keys of its rows and leaves zeros for the others.  lim: the last
 // of this thread's keys that its row sees.  m, l: the maximum that P refers to and the sum so far of this
 // thread's keys; DP columns of O from t_o on.
-// half: called when the first half of P is in place (R = 1, 128 keys).
+// half: called when the first half of P is in place (R = 1).
 template <int NK, int R, int DP, bool BF, typename Half>
 __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, int lim, bool first, float c, float &m, float &l, Half &&half) {
     constexpr int NC = NK / R;
-    static_assert(R == 1 || (R == 4 && NC == 16), "copies");
+    static_assert((R == 1 && NC == 128) || (R == 4 && NC == 16), "copies");
     const int c0 = R == 4 ? w * NC : 0;
     uint32_t s[NC];
     if constexpr (NC == 16) {
@@ -327,7 +325,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, 
         e = make_float2(ex2(e.x), ex2(e.y));
         sum[y / 2 & 3] = add2(sum[y / 2 & 3], e);
         pk[y / 2] = pack<BF>(e.x, e.y);
-        if constexpr (NC == 128) {
+        if constexpr (R == 1) {
             if (y == NC / 2 - 2) {
                 tm_st32(t_s, pk);
                 tc_wait_st();
@@ -338,8 +336,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, 
     sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
     l += sum[0].x + sum[0].y;
     if constexpr (R == 1) {
-#pragma unroll
-        for (int q = NC == 128; q < NC / 64; ++q) tm_st32(t_s + 32 * q, pk + 32 * q);
+        tm_st32(t_s + 32, pk + 32);
     } else {
 #pragma unroll
         for (int q = 0; q < R; ++q) {
@@ -413,61 +410,6 @@ struct Sink {
         } else if (a.lse) {
             const int t = a.group.div(sg.row0 + y);
             a.lse[int64_t(sg.q0 + t) * q_heads + sg.h * G + (sg.row0 + y - t * G)] = e * 0.69314718055994531f;
-        }
-    }
-    // A warp's 32 rows from row0 on, 16 words of each at a time through `mine` (32 x kPitch words), so that stores
-    // fill sectors; f is what the lane's row is multiplied by, empty: it has seen no key.
-    template <int DP>
-    __device__ void warp_rows(uint32_t t_o, uint32_t *mine, int row0, int rows, float f, bool empty) const {
-        const int lane = threadIdx.x & 31;
-        char *to[4];  // this lane's 16 bytes of four rows
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int y = min(row0 + q * 8 + lane / 4, rows - 1);
-            to[q] = (sg.direct ? reinterpret_cast<char *>(out_row(y)) : reinterpret_cast<char *>(a.part + (sg.row + y) * D)) + lane % 4 * 16;
-        }
-        const int cols = sg.direct ? 32 : 16;
-        float finite = 0.f;  // 0 times every result: not 0 if one is not finite
-#pragma unroll 1
-        for (int d0 = 0; d0 < D; d0 += cols) {
-            uint32_t x[16];
-            if (sg.direct) {
-                uint32_t o[32];
-                tm_ld32(t_o + d0, o);
-                tc_wait_ld();
-#pragma unroll
-                for (int y = 0; y < 16; ++y) {
-                    finite = fmaf(__uint_as_float(o[2 * y]), 0.f, finite);
-                    finite = fmaf(__uint_as_float(o[2 * y + 1]), 0.f, finite);
-                    x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
-                }
-            } else {
-                tm_ld16(t_o + d0, x);
-                tc_wait_ld();
-#pragma unroll
-                for (int y = 0; y < 16; ++y) {
-                    finite = fmaf(__uint_as_float(x[y]), 0.f, finite);
-                    x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
-                }
-            }
-#pragma unroll
-            for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4 *>(mine + lane * kPitch + y) = make_uint4(x[y], x[y + 1], x[y + 2], x[y + 3]);
-            __syncwarp();
-            const bool in = d0 + lane % 4 * (cols / 4) < D;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int y = q * 8 + lane / 4;
-                const uint4 v = *reinterpret_cast<const uint4 *>(mine + y * kPitch + lane % 4 * 4);
-                if (in && row0 + y < rows) *reinterpret_cast<uint4 *>(to[q]) = v;
-                to[q] += 64;
-            }
-            __syncwarp();
-        }
-        const int row = row0 + lane;
-        unsigned redo = __ballot_sync(FULL, row < rows && finite != 0.f && !empty && blind(row));
-        while (redo) {
-            again(row0 + __ffs(redo) - 1);
-            redo &= redo - 1;
         }
     }
 };

@@ -1,8 +1,8 @@
-// Attention of heavy items (129 .. 256 query rows; see sim_kv_attend.cu), bound by the tensor products.
+// Attention of heavy items (33 .. 256 query rows; see sim_kv_attend.cu), bound by the tensor products.
 //
 // One block per SM, two groups of four softmax warps with 128 rows each.  Both groups use every tile of 128 keys,
 // so a byte that enters shared memory serves 256 rows; the tensor unit works for one group while the other is in its
-// softmax.  Per tile and group: S = Q K^T (128 x 128 x D, operands in shared memory), P = exp2(c (S - m)) written over
+// softmax (the second group rests while an item has at most 128 rows).  Per tile and group: S = Q K^T (128 x 128 x D, operands in shared memory), P = exp2(c (S - m)) written over
 // S in TMEM as 16 bits, O += P V (128 x D x 128, P from TMEM, V as it lies, the N dimension contiguous).  TMEM is full:
 // 128 columns each for S / P and O of the two groups.
 #include "sim_kv_attend.cuh"
@@ -11,7 +11,65 @@ namespace simgb {
 
 namespace {
 
-// ---- k_attend -----------------------------------------------------------------------------------------------
+constexpr int kPitch = 20;            // words between rows on the stage, 16 of them used: no bank conflicts
+constexpr int kStage = 128 * kPitch;  // words through which the results of 128 rows pass
+
+// The results of a warp's 32 rows from row0 on, 16 words of each at a time through `mine` (32 x kPitch words), so that stores
+// fill sectors; f is what the lane's row is multiplied by, empty: it has seen no key.
+template <int DP, bool BF>
+__device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, uint32_t *mine, int row0, int rows, float f, bool empty) {
+    const Segment &sg = sink.sg;
+    const int lane = threadIdx.x & 31;
+    char *to[4];  // this lane's 16 bytes of four rows
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int y = min(row0 + q * 8 + lane / 4, rows - 1);
+        to[q] = (sg.direct ? reinterpret_cast<char *>(sink.out_row(y)) : reinterpret_cast<char *>(sink.a.part + (sg.row + y) * sink.D)) + lane % 4 * 16;
+    }
+    const int cols = sg.direct ? 32 : 16;
+    float finite = 0.f;  // 0 times every result: not 0 if one is not finite
+#pragma unroll 1
+    for (int d0 = 0; d0 < sink.D; d0 += cols) {
+        uint32_t x[16];
+        if (sg.direct) {
+            uint32_t o[32];
+            tm_ld32(t_o + d0, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                finite = fmaf(__uint_as_float(o[2 * y]), 0.f, finite);
+                finite = fmaf(__uint_as_float(o[2 * y + 1]), 0.f, finite);
+                x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
+            }
+        } else {
+            tm_ld16(t_o + d0, x);
+            tc_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                finite = fmaf(__uint_as_float(x[y]), 0.f, finite);
+                x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4 *>(mine + lane * kPitch + y) = make_uint4(x[y], x[y + 1], x[y + 2], x[y + 3]);
+        __syncwarp();
+        const bool in = d0 + lane % 4 * (cols / 4) < sink.D;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int y = q * 8 + lane / 4;
+            const uint4 v = *reinterpret_cast<const uint4 *>(mine + y * kPitch + lane % 4 * 4);
+            if (in && row0 + y < rows) *reinterpret_cast<uint4 *>(to[q]) = v;
+            to[q] += 64;
+        }
+        __syncwarp();
+    }
+    const int row = row0 + lane;
+    unsigned redo = __ballot_sync(FULL, row < rows && finite != 0.f && !empty && sink.blind(row));
+    while (redo) {
+        sink.again(row0 + __ffs(redo) - 1);
+        redo &= redo - 1;
+    }
+}
 
 template <int DP>
 struct Shape {
@@ -162,13 +220,13 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             const uint32_t idesc_s = 1u << 4 | type | (128 / 8) << 17 | (128 / 16) << 24;
             const uint32_t idesc_o = 1u << 4 | type | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
             const uint64_t op_q = operand(sbase, 16, 1024), op_k = operand(sbase + Sh::kOffRing, 16, 1024), op_v = operand(sbase + Sh::kOffRing, Sh::kHalf, 1024);
-            uint32_t at = 0, np = 0;
+            uint32_t at = 0, np[NG] = {};
             bool ok = true;
             const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, bar_wait(bar, parity, gave_up)) != 0; };
             const auto wait_full = [&](uint32_t y) { return wait(full(y), (y / NS) & 1); };
             Segment sg;
             for (uint32_t x = 0; (ok = take(x, sg)); ++x) {
-                const int n = __shfl_sync(FULL, sg.n, 0);
+                const int n = __shfl_sync(FULL, sg.n, 0), last = __shfl_sync(FULL, sg.rows, 0) > 128;  // group with rows
                 if (n == 0) break;
                 const auto keys = [&](int j, int g) {  // S of group g and tile j
                     if (elect_one()) {
@@ -179,7 +237,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                             mma_ss(tmem + g * 128, op_q + ((g * Sh::kTile + off) >> 4), op_k + ((slot * Sh::kTile + off) >> 4), idesc_s, kk > 0);
                         }
                         tc_commit(s_full(g));
-                        if (g == NG - 1) {
+                        if (g == last) {
                             tc_commit(empty(at + 2 * j));
                             if (j == n - 1) tc_commit(q_empty);
                         }
@@ -190,11 +248,13 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
-                for (int g = 0; g < NG; ++g) keys(0, g);
-                for (int j = 0; j < n && ok; ++j, ++np) {
+                for (int g = 0; g < NG; ++g)
+                    if (g <= last) keys(0, g);
+                for (int j = 0; j < n && ok; ++j) {
                     ok = wait_full(at + 2 * j + 1);
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
+                        if (g > last) break;
                         const uint32_t slot = (at + 2 * j + 1) % NS;
                         const auto values = [&](int from) {  // half of the tile's keys
                             tc_fence_after();
@@ -203,16 +263,16 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                                 for (int kk = 0; kk < kv_tile(0) / 32; ++kk)
                                     mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + (from + kk) * 8, op_v + ((slot * Sh::kTile + (from + kk) * 2048) >> 4), idesc_o, j > 0 || from + kk > 0);
                                 if (from > 0) {
-                                    if (g == NG - 1) tc_commit(empty(at + 2 * j + 1));
+                                    if (g == last) tc_commit(empty(at + 2 * j + 1));
                                     if (j + 1 == n) tc_commit(o_full(g));
                                 }
                             }
                             __syncwarp();
                         };
-                        ok = ok && wait(p_half(g), np & 1);
+                        ok = ok && wait(p_half(g), np[g] & 1);
                         if (!ok) break;
                         values(0);
-                        ok = wait(p_ready(g), np & 1);
+                        ok = wait(p_ready(g), np[g]++ & 1);
                         if (!ok) break;
                         values(kv_tile(0) / 32);
                         if (j + 1 < n) {
@@ -249,8 +309,9 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (maps.q_boxes) {
                     if (lane == 0) {
                         if (role == 2) {
-                            bar_expect(q_full, NG * Sh::kTile);
-                            for (int g = 0; g < NG; ++g)
+                            const int ng = sg.rows > 128 ? NG : 1;
+                            bar_expect(q_full, ng * Sh::kTile);
+                            for (int g = 0; g < ng; ++g)
                                 for (int half = 0; half < DP / 64; ++half)
                                     tma_load3(sbase + g * Sh::kTile + half * Sh::kHalf, &maps.queries, q_full, half * 64, sg.h * G, sg.q0 + a.group.div(sg.row0 + g * 128));
                         } else {
@@ -294,10 +355,11 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
         const uint32_t t_lane = tmem + (uint32_t(w * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + Sh::kOffO + g * 128;
         uint32_t *const stage = reinterpret_cast<uint32_t *>(base + Sh::kOffStage) + g * kStage;
         const float c = a.scale_log2;
-        uint32_t ns = 0, at = 0;
+        uint32_t ns = 0, no = 0, at = 0;
         bool ok = true;
         Segment sg;
         for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
+            if (sg.rows <= g * 128) continue;
             const int r = g * 128 + lr;  // the row in this thread's lane
             // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
             const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : sg.kv1 - 1;
@@ -333,10 +395,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             at += 2 * sg.n;
             const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + sg.n * kv_tile(0)};
             if (r < sg.rows) sink.lse(r, m, l);
-            ok = __all_sync(FULL, bar_wait(o_full(g), x & 1, gave_up));
+            ok = __all_sync(FULL, bar_wait(o_full(g), no++ & 1, gave_up));
             if (!ok) break;
             tc_fence_after();
-            sink.template warp_rows<DP>(t_o, stage + w * 32 * kPitch, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+            store_rows<DP>(sink, t_o, stage + w * 32 * kPitch, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
             tc_fence_before();
         }
     }

@@ -65,8 +65,10 @@ struct KvWrite {
 };
 cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st);
 
-constexpr int kAttRows = 256;  // query rows of an item, at most
-// Items of more than 128 rows are heavy, the others light: two lists, each divided among blocks of its own.
+// Items of more than 32 rows are heavy, the others light: two lists, each divided among blocks of its own.
+constexpr int kAttRows = 256;   // query rows of a heavy item, at most
+constexpr int kLightRows = 32;  // of a light one
+__host__ __device__ constexpr int kv_rows(int light) { return light ? kLightRows : kAttRows; }
 __host__ __device__ constexpr int kv_tile(int light) { return light ? 64 : 128; }  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.
@@ -77,7 +79,7 @@ __host__ __device__ inline int kv_span(int tiles, int light) { return tiles > 0 
 struct alignas(16) KvItem {
     int32_t q0;       // query token of row 0 of its source
     int32_t row0;     // first row within the source
-    int32_t rows;     // 1 .. kAttRows
+    int32_t rows;     // 1 .. kv_rows
     int32_t seq;      // row of the table
     int32_t kv0, kv1; // keys
     int32_t pos0;     // position of token q0: token q0 + t sees the keys up to pos0 + t
@@ -133,7 +135,9 @@ struct KvPlan {
 __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &b) {
     KvPlan p;
     const int64_t G = b.q_heads / kv.n_kv_heads, src = int64_t(b.n_groups) + b.n;
-    p.max_heavy = int32_t(2 * (int64_t(b.n_q) * G / (kAttRows / 2 + 1)) + 1);
+    // each query row is in one group and one entry; a source has one item of fewer than kAttRows rows at most
+    const int64_t whole = 2 * (int64_t(b.n_q) * G / kAttRows) + src, small = 2 * (int64_t(b.n_q) * G / (kLightRows + 1));
+    p.max_heavy = int32_t((whole < small ? whole : small) + 1);
     p.hdr = static_cast<int32_t *>(b.plan);
     p.cut[0] = reinterpret_cast<KvCut *>(p.hdr + 32);
     p.cut[1] = p.cut[0] + kKvMaxSms;
@@ -156,7 +160,7 @@ __host__ __device__ inline int kv_blocks(int sms, int light) { return light ? 2 
 // Partial results: rows of head_dim floats, then a float per row (log2 of the sum of exponentials).  A piece of an
 // item begins at the rows before it plus room for the pieces that blocks have cut off before.
 __host__ __device__ inline int64_t kv_partial_rows(const sim_kv_batch &b, int sms) {
-    return 2 * int64_t(b.n_q) * b.q_heads + int64_t(kAttRows) * kv_blocks(sms, 0) + int64_t(kAttRows / 2) * kv_blocks(sms, 1);
+    return 2 * int64_t(b.n_q) * b.q_heads + int64_t(kAttRows) * kv_blocks(sms, 0) + int64_t(kLightRows) * kv_blocks(sms, 1);
 }
 
 struct KvAttend {
@@ -165,7 +169,7 @@ struct KvAttend {
     float *lse;
     float *part, *part_lse;
     int64_t qt, qh, ot, oh;  // strides in elements
-    float scale, scale_log2;
+    float scale_log2;
     int32_t layer;
     int32_t q_vec;           // q may be read 16 bytes at a time
     int32_t sms;

@@ -1,11 +1,11 @@
-// Attention of light items (up to 128 query rows; see sim_kv_attend.cu): single tokens of one sequence and the
+// Attention of light items (up to 32 query rows; see sim_kv_attend.cu): single tokens of one sequence and the
 // few rows of small groups, bound by the bytes of the keys and values.
 //
 // Two blocks per SM, so that one loads while the other is between two items, and tiles of 64 keys, six (D > 64) or twelve of
 // keys or values in flight in each: about 190 KB per SM.  Queries go to TMEM and are the products' first operand from
 // there: no shared memory is spent on them.  Per tile: S = Q K^T (128 x 64 x D), P = exp2(c (S - m)) over S in TMEM,
 // O += P V (128 x D x 64).  The products always have 128 rows, of which few are in use: the tensor unit has the time.
-// With at most 32 rows, every row lies in TMEM four times, each copy with its own quarter of a tile's keys, so that
+// Every row lies in TMEM four times, each copy with its own quarter of a tile's keys, so that
 // the four warps of the softmax share few rows; the copies are joined at the end of the item.
 #include "sim_kv_attend.cuh"
 
@@ -22,7 +22,6 @@ struct Shape {
     static constexpr int kTmem = 256, kColQ = 64, kColO = 128;  // S / P below
     static constexpr int kOffStage = kSlots * kTile;
     static constexpr int kJoinStage = 2560;          // floats: 4 copies of 32 rows x (16 + 4), or of fewer and longer ones
-    static_assert(kJoinStage >= kStage, "stage");
     static constexpr int kOffStat = kOffStage + kJoinStage * 4;
     static constexpr int kOffAgain = kOffStat + 2 * 128 * 8;  // rows whose results are not finite
     static constexpr int kOffSeg = kOffAgain + 32 * 4;
@@ -229,11 +228,9 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (lane == 0) bar_arrive(joined);
             ok = __all_sync(FULL, bar_wait(joined, nj++ & 1, gave_up)) && ok;
         };
-        // Lanes that hold one copy of the rows.
-        const auto span_of = [](int rows) { return rows > 32 ? 128 : 32; };
         // The query row in this thread's lane.
         const auto q_row = [&](const Segment &s) {
-            const int y = s.row0 + min(lr & (span_of(s.rows) - 1), s.rows - 1), t = a.group.div(y);
+            const int y = s.row0 + min(lane, s.rows - 1), t = a.group.div(y);
             return static_cast<const uint16_t *>(a.q) + int64_t(s.q0 + t) * a.qt + int64_t(s.h * G + y - t * G) * a.qh;
         };
         const auto load_q = [&](const Segment &s) {
@@ -266,129 +263,116 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             const bool real = x != ~0u;
             const int n = real ? sg.n : 0;
             if (real && n == 0) break;
-            const int rows = sg.rows, span = span_of(rows), row = lr & (span - 1);
+            const int rows = sg.rows;
             // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
-            const int last = row < rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + row))) : sg.kv1 - 1;
+            const int last = lane < rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + lane))) : sg.kv1 - 1;
             float m = -INFINITY, l = 0.f;
-            const auto tiles = [&](auto copies) {
-                constexpr int R = decltype(copies)::value;
-                const int c0 = R == 4 ? w * 16 : 0;
-                int k0 = sg.k0;  // first key of the tile
-                const int kv1 = sg.kv1;
-                for (int j = 0; j < n; ++j, k0 += NK) {
-                    if (j == max(n - 2, 0)) {  // the next item's queries come to L1 meanwhile: two lines a row
-                        ok = take(x + 1);
-                        if (!ok) return;
-                        if (next.n > 0 && lr < next.rows) {
-                            const uint16_t *from = q_row(next);
-                            uint16_t v;
-                            asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from));
-                            asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from + D - 1));
-                        }
-                    }
-                    ok = __all_sync(FULL, bar_wait(s_full, ns & 1, gave_up));
-                    if (!ok) return;
-                    ++ns;
-                    tc_fence_after();
-                    softmax_tile<NK, R, DP, BF>(t_s, t_o, w, last - k0 - c0, j == 0, c, m, l, [] {});
-                    ring.next();
-                    // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                    const int valid = kv1 - k0;
-                    if (valid < NK) {
-                        ok = __all_sync(FULL, bar_wait(full(ring.slot), ring.parity, gave_up));
-                        if (lr >= 2 * valid) {  // two threads a row
-                            unsigned char *v = base + ring.slot * Sh::kTile + (lr >> 1) * 128 + (lr & 1) * 64;
-#pragma unroll
-                            for (int z = 0; z < DP / 16; ++z) *reinterpret_cast<uint4 *>(v + (z / 4) * Sh::kHalf + (z % 4) * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        smem_to_async();
-                    }
-                    ring.next();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(p_ready);
-                }
-            };
             if (!real) ok = take(0);
-            else if (span == 128) tiles(std::integral_constant<int, 1>());
-            else tiles(std::integral_constant<int, 4>());
+            int k0 = sg.k0;  // first key of the tile
+            const int kv1 = sg.kv1;
+            for (int j = 0; j < n; ++j, k0 += NK) {
+                if (j == max(n - 2, 0)) {  // the next item's queries come to L1 meanwhile: two lines a row
+                    ok = take(x + 1);
+                    if (!ok) break;
+                    if (next.n > 0 && lr < next.rows) {
+                        const uint16_t *from = q_row(next);
+                        uint16_t v;
+                        asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from));
+                        asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from + D - 1));
+                    }
+                }
+                ok = __all_sync(FULL, bar_wait(s_full, ns & 1, gave_up));
+                if (!ok) break;
+                ++ns;
+                tc_fence_after();
+                softmax_tile<NK, 4, DP, BF>(t_s, t_o, w, last - k0 - w * (NK / 4), j == 0, c, m, l, [] {});
+                ring.next();
+                // values past the end of the keys, whatever they are, must not meet their zero probabilities
+                const int valid = kv1 - k0;
+                if (valid < NK) {
+                    ok = __all_sync(FULL, bar_wait(full(ring.slot), ring.parity, gave_up));
+                    if (lr >= 2 * valid) {  // two threads a row
+                        unsigned char *v = base + ring.slot * Sh::kTile + (lr >> 1) * 128 + (lr & 1) * 64;
+#pragma unroll
+                        for (int z = 0; z < DP / 16; ++z) *reinterpret_cast<uint4 *>(v + (z / 4) * Sh::kHalf + (z % 4) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    smem_to_async();
+                }
+                ring.next();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_ready);
+            }
             if (!ok) break;
             if (next.n > 0) load_q(next);  // every product with this item's queries has been read
             if (!real) continue;
 
             const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + n * NK};
-            if (span == 128) {
-                if (row < rows) sink.lse(row, m, l);
-                ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up));
-                if (!ok) break;
-                tc_fence_after();
-                sink.template warp_rows<DP>(t_o, reinterpret_cast<uint32_t *>(stage) + w * 32 * kPitch, row - lane, rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
-            } else {  // join the four copies of each row: first what each is multiplied by
-                float2 *const st = stat + (x & 1) * 128;
-                st[lr] = make_float2(m, l);
+            // Join the four copies of each row: first what each is multiplied by.
+            float2 *const st = stat + (x & 1) * 128;
+            st[lr] = make_float2(m, l);
+            join();
+            float top = -INFINITY, total = 0.f;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                if (st[32 * p + lane].y != 0.f) top = fmaxf(top, st[32 * p + lane].x);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                if (st[32 * p + lane].y != 0.f) total += st[32 * p + lane].y * ex2((st[32 * p + lane].x - top) * c);
+            const float f = l == 0.f ? 0.f : ex2((m - top) * c) / total;
+            if (lr < rows) sink.lse(lr, top, total);
+            if (lr < 32) again[lr] = 0;
+            // As many columns at a time as the stage holds of all copies.  No wait is needed after the last ones: the stage is
+            // used again only after the other warps have gone on to another item.
+            int cols = DP, shift = DP == 128 ? 5 : 4;  // log2 of the columns / 4
+            while (4 * rows * (cols + 4) > Sh::kJoinStage) {
+                cols /= 2;
+                --shift;
+            }
+            float *const to = stage + (w * rows + lane) * (cols + 4);
+            ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int d0 = 0; d0 < D; d0 += cols) {
+                if (d0 > 0) join();
+#pragma unroll 1
+                for (int d = 0; d < cols; d += 32) {
+                    uint32_t o[32];
+                    if (cols == 16) tm_ld16(t_o + d0, o);
+                    else tm_ld32(t_o + d0 + d, o);
+                    tc_wait_ld();
+                    if (lane < rows) {
+#pragma unroll
+                        for (int y = 0; y < 32; y += 4)
+                            if (y < 16 || cols > 16)
+                                *reinterpret_cast<float4 *>(to + d + y) =
+                                    l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                             : make_float4(__uint_as_float(o[y]) * f, __uint_as_float(o[y + 1]) * f, __uint_as_float(o[y + 2]) * f, __uint_as_float(o[y + 3]) * f);
+                    }
+                }
                 join();
-                float top = -INFINITY, total = 0.f;
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    if (st[32 * p + lane].y != 0.f) top = fmaxf(top, st[32 * p + lane].x);
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    if (st[32 * p + lane].y != 0.f) total += st[32 * p + lane].y * ex2((st[32 * p + lane].x - top) * c);
-                const float f = l == 0.f ? 0.f : ex2((m - top) * c) / total;
-                if (lr < rows) sink.lse(lr, top, total);
-                if (lr < 32) again[lr] = 0;
-                // As many columns at a time as the stage holds of all copies.  No wait is needed after the last ones: the stage is
-                // used again only after the other warps have gone on to another item.
-                int cols = DP, shift = DP == 128 ? 5 : 4;  // log2 of the columns / 4
-                while (4 * rows * (cols + 4) > Sh::kJoinStage) {
-                    cols /= 2;
-                    --shift;
-                }
-                float *const to = stage + (w * rows + lane) * (cols + 4);
-                ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
                 if (!ok) break;
-                tc_fence_after();
 #pragma unroll 1
-                for (int d0 = 0; d0 < D; d0 += cols) {
-                    if (d0 > 0) join();
-#pragma unroll 1
-                    for (int d = 0; d < cols; d += 32) {
-                        uint32_t o[32];
-                        if (cols == 16) tm_ld16(t_o + d0, o);
-                        else tm_ld32(t_o + d0 + d, o);
-                        tc_wait_ld();
-                        if (lane < rows) {
+                for (int e = lr; e < rows << shift; e += 128) {
+                    const int y = e >> shift, d = 4 * (e & ((1 << shift) - 1));
+                    if (d0 + d >= D) continue;
+                    float4 v[4];
 #pragma unroll
-                            for (int y = 0; y < 32; y += 4)
-                                if (y < 16 || cols > 16)
-                                    *reinterpret_cast<float4 *>(to + d + y) =
-                                        l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                 : make_float4(__uint_as_float(o[y]) * f, __uint_as_float(o[y + 1]) * f, __uint_as_float(o[y + 2]) * f, __uint_as_float(o[y + 3]) * f);
-                        }
-                    }
-                    join();
-                    if (!ok) break;
-#pragma unroll 1
-                    for (int e = lr; e < rows << shift; e += 128) {
-                        const int y = e >> shift, d = 4 * (e & ((1 << shift) - 1));
-                        if (d0 + d >= D) continue;
-                        float4 v[4];
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) v[p] = *reinterpret_cast<const float4 *>(stage + (p * rows + y) * (cols + 4) + d);
-                        const float4 t = make_float4((v[0].x + v[1].x) + (v[2].x + v[3].x), (v[0].y + v[1].y) + (v[2].y + v[3].y),
-                                                     (v[0].z + v[1].z) + (v[2].z + v[3].z), (v[0].w + v[1].w) + (v[2].w + v[3].w));
-                        if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d0 + d) = make_uint2(pack<BF>(t.x, t.y), pack<BF>(t.z, t.w));
-                        else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d0 + d) = t;
-                        if (t.x * 0.f + t.y * 0.f + t.z * 0.f + t.w * 0.f != 0.f) again[y] = 1;
-                    }
+                    for (int p = 0; p < 4; ++p) v[p] = *reinterpret_cast<const float4 *>(stage + (p * rows + y) * (cols + 4) + d);
+                    const float4 t = make_float4((v[0].x + v[1].x) + (v[2].x + v[3].x), (v[0].y + v[1].y) + (v[2].y + v[3].y),
+                                                 (v[0].z + v[1].z) + (v[2].z + v[3].z), (v[0].w + v[1].w) + (v[2].w + v[3].w));
+                    if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d0 + d) = make_uint2(pack<BF>(t.x, t.y), pack<BF>(t.z, t.w));
+                    else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d0 + d) = t;
+                    if (t.x * 0.f + t.y * 0.f + t.z * 0.f + t.w * 0.f != 0.f) again[y] = 1;
                 }
+            }
+            if (!ok) break;
+            if (sink.blind(0)) {  // see Sink::again
+                join();
                 if (!ok) break;
-                if (sink.blind(0)) {  // see Sink::again
-                    join();
-                    if (!ok) break;
-                    for (int y = w; y < rows; y += 4)
-                        if (again[y] && sink.blind(y)) sink.again(y);
-                }
+                for (int y = w; y < rows; y += 4)
+                    if (again[y] && sink.blind(y)) sink.again(y);
             }
             tc_fence_before();
             give_back(x);

@@ -111,6 +111,27 @@ def test_many_queries_see_the_keys_up_to_their_own(lens, queries, group, dim):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("group", [1, 3, 4])
+def test_rows_around_the_sizes_of_items(group, dim, dtype):
+    """Up to 32, 128 and 256 rows and just over, whole items and what is left after them, side by side."""
+    rows = [31, 32, 33, 64, 127, 128, 129, 255, 256, 257, 287, 288, 289, 385, 512]
+    queries = [-(-r // group) for r in rows]
+    c = Case([t + 90 for t in queries], queries, group=group, dim=dim, dtype=dtype, kv_heads=3, seed=group)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("groups", [None, [1, 399, 0, 500, 300]])
+def test_more_entries_than_the_plan_keeps_on_chip(groups):
+    rng = np.random.default_rng(5)
+    n, prefix = 1200, 160 if groups else 0
+    lens = (prefix + rng.integers(0, 70, n)).tolist()
+    queries = [int(rng.integers(0, min(x, 3) + 1)) for x in lens]
+    c = Case(lens, queries, kv_heads=1, group=4, groups=groups, prefix=prefix, seed=9)
+    c.check(*c.run())
+
+
 def test_rows_that_see_nothing():
     """More queries than tokens, and sequences without any: zeros and -infinity."""
     for lens, queries in (([0, 3, 0], [2, 5, 1]), ([0], [1]), ([2], [300])):

@@ -83,6 +83,21 @@ def test_a_bad_batch(L, over):
     assert c["plan"]() == INVAL and c["attend"]() == INVAL
 
 
+def test_sizes_whose_products_are_too_large(L):
+    kv = cache(L, n_kv_heads=1 << 10, max_pages=1 << 23)  # 2^27 tokens for each of 2^10 heads
+    assert L.lib().sim_kv_scratch_bytes(ctypes.byref(kv)) == 0
+    kv = cache(L, n_kv_heads=1 << 10, max_seqs=1 << 17)
+    assert L.lib().sim_kv_scratch_bytes(ctypes.byref(kv)) > 0
+    for n, ok in ((1 << 16, True), ((1 << 16) + 1, False)):
+        assert (L.lib().sim_kv_plan_bytes(ctypes.byref(kv), ctypes.byref(batch(L, n=n, q_heads=1 << 10))) > 0) is ok
+
+
+def test_a_scale_that_overflows_as_a_power_of_two(L):
+    """exp(s x) is computed as 2^(s log2(e) x): that product has to be finite too."""
+    lib, p, b, x = L.lib(), ctypes.byref(cache(L)), ctypes.byref(batch(L)), ctypes.c_void_p(1 << 24)
+    assert lib.sim_kv_attend(p, b, 0, x, 128, 64, ctypes.c_float(3e38), x, 128, 64, None, None) == INVAL
+
+
 def test_bad_attention_arguments(L):
     lib, p, b, x = L.lib(), ctypes.byref(cache(L)), ctypes.byref(batch(L)), ctypes.c_void_p(1 << 24)
 
