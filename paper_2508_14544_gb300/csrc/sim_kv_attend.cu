@@ -23,7 +23,12 @@ namespace {
 
 // ---- plan ---------------------------------------------------------------------------------------------------
 
-constexpr int kShareCost = 10;         // tiles of 128 rows that a second partial result of as many rows costs
+// What sharing a prefix costs, in the time that a block needs for 64 keys: for the prefix's own item, for 16 rows that are
+// then joined from two places, and for every block once (a longer chain of kernels).  Measured with and without sharing, 128
+// sequences (8 kv heads, 8 query heads each, up to 64 keys of their own) in groups: 64 groups with a prefix of 512 keys 81-91
+// against 72 us, of 2048 keys 141 against 180 us; 16 groups with 256 keys 60-70 against 55 us, with 1024 keys 78 against 89 us.
+// The rule takes the faster side of these four.
+constexpr int kShareItem = 6, kShareRows = 7, kShareOnce = 5;
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -152,6 +157,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
     constexpr int kPlan = FEW ? 512 : 1024;
     __shared__ Two sums[32];
     __shared__ int32_t counts[3];  // cuts of heavy, of light items, entries to join
+    __shared__ unsigned long long saved;
     __shared__ KvSource few_sources[FEW ? kFewSources : 1];
     __shared__ int32_t few_first[FEW ? 2 : 1][FEW ? kFewSources + 1 : 1], few_used[FEW ? kFewSources : 1], few_alone[FEW ? kFewSources : 1];
     __shared__ int64_t few_units[FEW ? kFewItems : 1];
@@ -163,6 +169,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
     int32_t *const first0 = FEW ? few_first[0] : p.first[0], *const first1 = FEW ? few_first[FEW ? 1 : 0] : p.first[1];
     const int tid = threadIdx.x, ng = b.n_groups, n_src = ng + b.n, G = b.q_heads / kv.n_kv_heads, P = kv.page_size;
     if (tid < 3) counts[tid] = 0;
+    if (tid == 0) saved = 0;
     // Offsets that are not in order: no queries at all, or no groups.
     bool order = true, groups = true, known = true;
 #pragma unroll 1
@@ -199,30 +206,38 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
         }
         __syncthreads();
     }
+    if (ng > 0) {  // share where that saves time: in the group, and in all
+        int64_t net = 0;
+#pragma unroll 1
+        for (int g = tid; g < ng; g += kPlan) {
+            const int a = order && groups ? b.cu_group[g] : 0, z = order && groups ? b.cu_group[g + 1] : 0;
+            KvSource x = {};
+            x.prefix = -1;
+            if (a < z) {
+                x.q0 = b.cu_q[a];
+                const int rows = (b.cu_q[z] - x.q0) * G, found = used[g] != INT_MAX ? used[g] : 0;
+                const int64_t saves = int64_t(found * P / kv_tile(1)) * (alone[g] - tile_rows(rows)) - kShareItem - int64_t(rows) * kShareRows / 16;
+                if (saves > 0) {
+                    net += saves;
+                    x.rows = rows;
+                    x.seq = b.seqs[a];
+                    x.kv1 = found * P;
+                    x.pos0 = 1 << 30;
+                }
+            }
+            source[g] = x;
+        }
+        if (net > 0) atomicAdd(&saved, static_cast<unsigned long long>(net));
+        __syncthreads();
+        if (int64_t(saved) * kv.n_kv_heads < int64_t(kShareOnce) * kv_blocks(sms, 1)) {
+#pragma unroll 1
+            for (int g = tid; g < ng; g += kPlan) source[g].rows = source[g].kv1 = 0;
+            __syncthreads();
+        }
+    }
     int64_t sum = 0;  // heavy items, light ones above
 #pragma unroll 1
     for (int s0 = 0; s0 < n_src; s0 += kPlan) {
-        if (s0 < ng) {  // groups: sharing saves tiles, and costs every row a second partial result
-            const int g = s0 + tid;
-            if (g < ng) {
-                const int a = order && groups ? b.cu_group[g] : 0, z = order && groups ? b.cu_group[g + 1] : 0;
-                KvSource x = {};
-                if (a < z) {
-                    x.q0 = b.cu_q[a];
-                    const int rows = (b.cu_q[z] - x.q0) * G, found = used[g] != INT_MAX ? used[g] : 0;
-                    const int64_t saved = int64_t(found * P / kv_tile(0)) * (alone[g] - tile_rows(rows));
-                    if (saved > kShareCost * int64_t(ceil_div(rows, kAttRows / 2))) {
-                        x.rows = rows;
-                        x.seq = b.seqs[a];
-                        x.kv1 = found * P;
-                        x.pos0 = 1 << 30;
-                    }
-                }
-                x.prefix = -1;
-                source[g] = x;
-            }
-            __syncthreads();
-        }
         const int s = s0 + tid;
         KvSource x = {};
         if (s < ng) {
