@@ -302,8 +302,9 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, 
     const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
     if (first) {
         m = mx;
-    } else if (__any_sync(FULL, (mx - m) * c > kGrow)) {
-        const float up = fmaxf(m, mx), f = up == m ? 1.f : ex2((m - up) * c);
+    } else if (const bool grows = (mx - m) * c > kGrow; __any_sync(FULL, grows)) {
+        // each row for itself: what it becomes does not hang on the rows beside it, nor on what lies in lanes past the rows
+        const float up = grows ? mx : m, f = grows ? ex2((m - up) * c) : 1.f;
         m = up;
         l *= f;
 #pragma unroll 1

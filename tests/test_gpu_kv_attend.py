@@ -202,6 +202,47 @@ def test_shared_prefixes_at_their_edges():
     c.check(*c.run())
 
 
+def shares(c):
+    """Whether a plan of this batch reads prefixes once: entries then have rows to join."""
+    plan = c.kv.plan(c.seqs, c.cu, c.n_q, heads=c.q.shape[1], cu_group=c.bounds)
+    return int(plan._buffer[:128].view(c.torch.int32)[17]) > 0
+
+
+@pytest.mark.parametrize("dtype,dim,page,group", [("bfloat16", 128, 16, 8), ("float16", 80, 32, 5), ("bfloat16", 64, 64, 1), ("float16", 128, 128, 3)])
+@pytest.mark.parametrize("most", [1, 3, 7])
+def test_shared_prefixes_that_are_worth_it(dtype, dim, page, group, most):
+    """Groups of one, few and many; prefixes' rows and entries' own ones in light and in heavy items."""
+    groups, prefix = [30, 1, 9, 2, 12], 2100
+    rng = np.random.default_rng(page + most)
+    queries = [int(rng.integers(1, most + 1)) for _ in range(54)]
+    lens = [prefix + t - 1 + int(rng.integers(0, 200)) for t in queries]
+    c = Case(lens, queries, kv_heads=8, dim=dim, page=page, group=group, dtype=dtype, groups=groups, prefix=prefix, seed=page)
+    assert shares(c)
+    out, lse = c.run()
+    c.check(out, lse)
+    again, again_lse = c.run()
+    assert c.torch.equal(out, again) and c.torch.equal(lse, again_lse)
+
+
+@pytest.mark.parametrize("lens,queries", [
+    ([1600, 1601, 1616, 1660, 1600, 1610, 1605, 1760] * 5, [1, 1, 3, 20, 1, 11, 0, 2] * 5),  # end with the prefix, inside it, after it; no queries
+    ([1600] * 32, [1] * 32),                                                                 # nothing of their own
+    ([1650] * 32, [1] * 32),
+    ([1660] + [1650] * 30, [33] + [5] * 30),
+])
+@pytest.mark.parametrize("rest", [float("nan"), float("inf")])
+def test_edges_of_prefixes_that_are_worth_it(lens, queries, rest):
+    c = Case(lens, queries, kv_heads=8, groups=[len(lens)], prefix=1600, rest=rest)
+    assert shares(c)
+    c.check(*c.run())
+
+
+def test_short_prefixes_are_not_shared():
+    c = Case([70] * 8, [1] * 8, groups=[8], prefix=64)
+    assert not shares(c)
+    c.check(*c.run())
+
+
 def test_a_long_sequence_is_divided():
     c = Case([20011, 3], [1, 1], kv_heads=1, group=8, dim=128, page=128)
     c.check(*c.run())
