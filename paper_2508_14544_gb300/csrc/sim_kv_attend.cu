@@ -23,12 +23,12 @@ namespace {
 
 // ---- plan ---------------------------------------------------------------------------------------------------
 
-// What sharing a prefix costs, in the time that a block needs for 64 keys: for the prefix's own item, for 16 rows that are
+// What sharing a prefix costs, in the time that a block needs for 128 keys: for the prefix's own item, for 32 rows that are
 // then joined from two places, and for every block once (a longer chain of kernels).  Measured with and without sharing, 128
 // sequences (8 kv heads, 8 query heads each, up to 64 keys of their own) in groups: 64 groups with a prefix of 512 keys 81-91
 // against 72 us, of 2048 keys 141 against 180 us; 16 groups with 256 keys 60-70 against 55 us, with 1024 keys 78 against 89 us.
 // The rule takes the faster side of these four.
-constexpr int kShareItem = 6, kShareRows = 7, kShareOnce = 5;
+constexpr int kShareItem = 3, kShareRows = 7, kShareOnce = 3;
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             if (a < z) {
                 x.q0 = b.cu_q[a];
                 const int rows = (b.cu_q[z] - x.q0) * G, found = used[g] != INT_MAX ? used[g] : 0;
-                const int64_t saves = int64_t(found * P / kv_tile(1)) * (alone[g] - tile_rows(rows)) - kShareItem - int64_t(rows) * kShareRows / 16;
+                const int64_t saves = int64_t(found * P / kTileKeys) * (alone[g] - tile_rows(rows)) - kShareItem - int64_t(rows) * kShareRows / 32;
                 if (saves > 0) {
                     net += saves;
                     x.rows = rows;
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                 it.pos0 = x.pos0;
                 it.kv1 = min(x.kv1, x.pos0 + (it.row0 + it.rows - 1) / G + 1);
                 it.partial = s < ng || x.prefix >= 0;
-                it.tiles = ceil_div(max(it.kv1 - it.kv0, 0), kv_tile(light));
+                it.tiles = ceil_div(max(it.kv1 - it.kv0, 0), kTileKeys);
             }
             Two total;
             const Two before = plan_scan<kPlan / 32>({int64_t(kv_span(it.tiles, light)) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
@@ -566,24 +566,18 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
 
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
     if (!encode_fn()) return cudaErrorNotSupported;
-    const auto encode_maps = [&](KvMaps &maps, int light) {
-        for (int v = 0; v < 2; ++v) {
-            uint16_t *at = static_cast<uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + v * (kv_layer_elems(kv) / 2);
-            const uint64_t dim[4] = {uint64_t(kv.head_dim), uint64_t(kv.page_size), uint64_t(kv.n_kv_heads), uint64_t(kv.n_pages)};
-            const uint64_t stride[3] = {uint64_t(kv.head_dim) * 2, uint64_t(kv.head_dim) * 2 * kv.page_size, uint64_t(kv_page_bytes(kv))};
-            const uint32_t box[4] = {64, uint32_t(std::min(kv.page_size, kv_tile(light))), 1, 1};
-            if (!kv_encode_map(kv, v ? &maps.values : &maps.keys, 4, at, dim, stride, box)) return false;
-        }
-        return true;
-    };
-    KvMaps heavy = {}, light = {};
-    if (!encode_maps(light, 1)) return cudaErrorInvalidValue;
-    heavy = light;
-    if (kv.page_size > kv_tile(1) && !encode_maps(heavy, 0)) return cudaErrorInvalidValue;
+    KvMaps maps = {};
+    for (int v = 0; v < 2; ++v) {
+        uint16_t *at = static_cast<uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + v * (kv_layer_elems(kv) / 2);
+        const uint64_t dim[4] = {uint64_t(kv.head_dim), uint64_t(kv.page_size), uint64_t(kv.n_kv_heads), uint64_t(kv.n_pages)};
+        const uint64_t stride[3] = {uint64_t(kv.head_dim) * 2, uint64_t(kv.head_dim) * 2 * kv.page_size, uint64_t(kv_page_bytes(kv))};
+        const uint32_t box[4] = {64, uint32_t(kv.page_size), 1, 1};
+        if (!kv_encode_map(kv, v ? &maps.values : &maps.keys, 4, at, dim, stride, box)) return cudaErrorInvalidValue;
+    }
     const int64_t rows = int64_t(b.n_q) * b.q_heads;
     cudaError_t e = cudaSuccess;
-    if (rows / kv.n_kv_heads > kLightRows) e = launch_kv_heavy(kv, b, a, heavy, st);  // fewer rows make no heavy item
-    if (e == cudaSuccess) e = launch_kv_light(kv, b, a, light, st);
+    if (rows / kv.n_kv_heads > kLightRows) e = launch_kv_heavy(kv, b, a, maps, st);  // fewer rows make no heavy item
+    if (e == cudaSuccess) e = launch_kv_light(kv, b, a, maps, st);
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);

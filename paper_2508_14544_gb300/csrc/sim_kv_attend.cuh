@@ -99,7 +99,7 @@ struct Line {
             s.row0 = it.row0;
             s.rows = it.rows;
             s.pos0 = it.pos0;
-            s.k0 = it.kv0 + t0 * kv_tile(light);
+            s.k0 = it.kv0 + t0 * kTileKeys;
             s.kv1 = it.kv1;
             s.seq = it.seq;
             s.direct = s.n == it.tiles && !it.partial;
@@ -212,6 +212,9 @@ __device__ __forceinline__ void tm_ld16(uint32_t addr, uint32_t *r) {
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
         : REG4(r, 0), REG4(r, 4), REG4(r, 8), REG4(r, 12)
         : "r"(addr));
+}
+__device__ __forceinline__ void tm_ld8(uint32_t addr, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : REG4(r, 0), REG4(r, 4) : "r"(addr));
 }
 __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t *r) {
     asm volatile(
@@ -404,8 +407,8 @@ struct Sink {
         const int t = a.group.div(sg.row0 + y);
         return static_cast<uint16_t *>(a.out) + int64_t(sg.q0 + t) * a.ot + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.oh;
     }
-    __device__ void lse(int y, float top, float total) const {
-        const float e = total == 0.f ? -INFINITY : top * a.scale_log2 + log2f(total);
+    __device__ void lse(int y, float top, float total) const {  // top: log2
+        const float e = total == 0.f ? -INFINITY : top + log2f(total);
         if (!sg.direct) {
             a.part_lse[sg.row + y] = e;
         } else if (a.lse) {
@@ -417,7 +420,7 @@ struct Sink {
 
 }  // namespace
 
-// Tensor maps of one layer's keys and values, [page][head][token][dim], with boxes of up to a tile's tokens of one
+// Tensor maps of one layer's keys and values, [page][head][token][dim], with boxes of the tokens of one
 // page and head and 64 columns; of the queries [token][head][dim], with boxes of 128 rows (if q_boxes).
 struct KvMaps {
     CUtensorMap keys, values, queries;

@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             // ---- the line of work, and loads: lane l brings page l of each tile
             const KvPlan plan = kv_plan(kv, b);
             Line line(plan, kv.n_kv_heads, 0, blockIdx.x, a.sms);
-            const int P = kv.page_size, per = kv_tile(0) / P;
+            const int P = kv.page_size, per = kTileKeys / P;
             uint32_t at = 0;  // tiles loaded
             bool ok = true;
             for (uint32_t x = 0; ok; ++x) {
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                             tc_fence_after();
                             if (elect_one()) {
 #pragma unroll
-                                for (int kk = 0; kk < kv_tile(0) / 32; ++kk)
+                                for (int kk = 0; kk < kTileKeys / 32; ++kk)
                                     mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + (from + kk) * 8, op_v + ((slot * Sh::kTile + (from + kk) * 2048) >> 4), idesc_o, j > 0 || from + kk > 0);
                                 if (from > 0) {
                                     if (g == last) tc_commit(empty(at + 2 * j + 1));
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                         values(0);
                         ok = wait(p_ready(g), np[g]++ & 1);
                         if (!ok) break;
-                        values(kv_tile(0) / 32);
+                        values(kTileKeys / 32);
                         if (j + 1 < n) {
                             if (g == 0) ok = wait_full(at + 2 * j + 2);
                             if (!ok) break;
@@ -365,14 +365,14 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : sg.kv1 - 1;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
-                const int k0 = sg.k0 + j * kv_tile(0);  // first key of the tile
+                const int k0 = sg.k0 + j * kTileKeys;  // first key of the tile
                 ok = __all_sync(FULL, bar_wait(s_full(g), ns & 1, gave_up));
                 if (!ok) break;
                 ++ns;
                 tc_fence_after();
                 // values past the end of the keys, whatever they are, must not meet their zero probabilities
                 const int valid = sg.kv1 - k0;
-                if (valid < kv_tile(0) && g == 0) {
+                if (valid < kTileKeys && g == 0) {
                     const uint32_t y = at + 2 * j + 1;
                     ok = __all_sync(FULL, bar_wait(full(y), (y / NS) & 1, gave_up));
                     if (lr >= valid) {
@@ -393,8 +393,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             }
             if (!ok) break;
             at += 2 * sg.n;
-            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + sg.n * kv_tile(0)};
-            if (r < sg.rows) sink.lse(r, m, l);
+            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + sg.n * kTileKeys};
+            if (r < sg.rows) sink.lse(r, m * c, l);
             ok = __all_sync(FULL, bar_wait(o_full(g), no++ & 1, gave_up));
             if (!ok) break;
             tc_fence_after();

@@ -69,7 +69,7 @@ cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st)
 constexpr int kAttRows = 256;   // query rows of a heavy item, at most
 constexpr int kLightRows = 32;  // of a light one
 __host__ __device__ constexpr int kv_rows(int light) { return light ? kLightRows : kAttRows; }
-__host__ __device__ constexpr int kv_tile(int light) { return light ? 64 : 128; }  // keys of a tile
+constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.
 __host__ __device__ constexpr int kv_lead(int light) { return light ? 3 : 4; }

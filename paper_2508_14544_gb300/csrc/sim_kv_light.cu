@@ -1,12 +1,13 @@
 // Attention of light items (up to 32 query rows; see sim_kv_attend.cu): single tokens of one sequence and the
 // few rows of small groups, bound by the bytes of the keys and values.
 //
-// Two blocks per SM, so that one loads while the other is between two items, and tiles of 64 keys, six (D > 64) or twelve of
-// keys or values in flight in each: about 190 KB per SM.  Queries go to TMEM and are the products' first operand from
-// there: no shared memory is spent on them.  Per tile: S = Q K^T (128 x 64 x D), P = exp2(c (S - m)) over S in TMEM,
-// O += P V (128 x D x 64).  The products always have 128 rows, of which few are in use: the tensor unit has the time.
-// Every row lies in TMEM four times, each copy with its own quarter of a tile's keys, so that
-// the four warps of the softmax share few rows; the copies are joined at the end of the item.
+// Keys take the 128 rows of the tensor products, queries their columns, so that few queries cost little.  Per tile of
+// 128 keys: S' = K Q' (128 x N x D, N = 16 or 32), P' = exp2(c (S' - m)), a thread for each key, O' += V' P' (D x N x 128, V as
+// it lies, its M dimension contiguous).  P goes to shared memory, over the tile's first keys, which are no longer needed.
+// A row's keys lie in all of the block's threads: its sum is joined at the end of the item, its maximum in the item's first
+// tile and then only where a key exceeds it by more than kGrow, which the four warps tell each other in every tile.  Eight
+// rows are in registers at a time, whatever their number; each thread's own sums wait in TMEM.
+// Two blocks per SM, so that one loads while the other is between two items, with 96 KB of keys and values in flight each.
 #include "sim_kv_attend.cuh"
 
 namespace simgb {
@@ -15,36 +16,63 @@ namespace {
 
 template <int DP>
 struct Shape {
-    static constexpr int kThreads = 192;             // four softmax warps, one loads, one issues
-    static constexpr int kTile = DP * 128;           // bytes of 64 keys or values
-    static constexpr int kHalf = 8192;               // 64 rows of 64 columns
-    static constexpr int kSlots = 98304 / kTile;
-    static constexpr int kTmem = 256, kColQ = 64, kColO = 128;  // S / P below
-    static constexpr int kOffStage = kSlots * kTile;
-    static constexpr int kJoinStage = 2560;          // floats: 4 copies of 32 rows x (16 + 4), or of fewer and longer ones
-    static constexpr int kOffStat = kOffStage + kJoinStage * 4;
-    static constexpr int kOffAgain = kOffStat + 2 * 128 * 8;  // rows whose results are not finite
-    static constexpr int kOffSeg = kOffAgain + 32 * 4;
+    static constexpr int kThreads = 192;              // four softmax warps, one loads, one issues
+    static constexpr int kHalves = DP / 64;
+    static constexpr int kSlot = 16384;               // 64 columns of 128 keys or values
+    static constexpr int kSlots = 6;
+    static constexpr int kRowsHalf = kLightRows * 128;  // 64 columns of the queries, or 64 keys of P
+    static constexpr int kTmem = 128, kColO = 32, kColL = 64;  // S below; L: each thread's sums
+    static constexpr int kOffQ = kSlots * kSlot;
+    static constexpr int kOffRed = kOffQ + kHalves * kRowsHalf;  // [2][row][warp]
+    static constexpr int kOffVote = kOffRed + 2 * kLightRows * 16;
+    static constexpr int kOffAgain = kOffVote + 2 * 16;  // rows whose results are not finite
+    static constexpr int kOffSeg = kOffAgain + kLightRows * 4;
     static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
     static constexpr int kBars = 2 * kSlots + 2 * kSegs + 6;
     static constexpr int kBytes = kOffBar + kBars * 8 + 16;
-    static constexpr int kAlloc = kBytes + 1024;     // the base is rounded up to 1024
+    static constexpr int kAlloc = kBytes + 1024;      // the base is rounded up to 1024
     static_assert(kAlloc <= 115712, "two blocks per SM");
+    static_assert(kSlots % (2 * kHalves) % kHalves == 0, "the halves of a tile lie side by side");
 };
+
+// Eight rows' maxima or sums over the warp's lanes: row lane / 4's is returned.
+template <bool SUM>
+__device__ __forceinline__ float over_lanes(const float *x) {
+    const int lane = threadIdx.x & 31;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x[i];
+#pragma unroll
+    for (int d = 16, n = 4; d >= 1; d /= 2, n /= 2) {
+        if (n >= 1) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const bool up = lane & d;
+                const float mine = up ? v[i + n] : v[i], other = __shfl_xor_sync(FULL, up ? v[i] : v[i + n], d);
+                v[i] = SUM ? mine + other : fmaxf(mine, other);
+            }
+        } else {
+            const float other = __shfl_xor_sync(FULL, v[0], d);
+            v[0] = SUM ? v[0] + other : fmaxf(v[0], other);
+        }
+    }
+    return v[0];
+}
 
 template <int DP, bool BF>
 __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
     k_light(const sim_kv kv, const sim_kv_batch b, const KvAttend a, const __grid_constant__ KvMaps maps) {
     using Sh = Shape<DP>;
-    constexpr int NS = Sh::kSlots, NK = kv_tile(1);
+    constexpr int NS = Sh::kSlots, HF = Sh::kHalves, NK = kTileKeys;
     extern __shared__ unsigned char raw[];
     unsigned char *const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
     const uint32_t sbase = smem_addr(base), bars = sbase + Sh::kOffBar;
     volatile int *const gave_up = reinterpret_cast<int *>(base + Sh::kOffBar + Sh::kBars * 8);
     uint32_t *const tmem_at = reinterpret_cast<uint32_t *>(base + Sh::kOffBar + Sh::kBars * 8 + 4);
     Segment *const segs = reinterpret_cast<Segment *>(base + Sh::kOffSeg);
-    const auto full = [&](uint32_t slot) { return bars + 8 * slot; };
-    const auto empty = [&](uint32_t slot) { return bars + 8 * (NS + slot); };
+    const auto full = [&](uint32_t x) { return bars + 8 * (x % NS); };
+    const auto empty = [&](uint32_t x) { return bars + 8 * (NS + x % NS); };
+    const auto slot_at = [&](uint32_t x) { return sbase + (x % NS) * Sh::kSlot; };
     const auto seg_full = [&](uint32_t x) { return bars + 8 * (2 * NS + x % kSegs); };
     const auto seg_empty = [&](uint32_t x) { return bars + 8 * (2 * NS + kSegs + x % kSegs); };
     constexpr int kRest = 2 * NS + 2 * kSegs;
@@ -90,115 +118,102 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
         __syncwarp();
         if (lane == 0) bar_arrive(seg_empty(x));
     };
-    // A slot of the ring and the parity of its current use.
-    struct Ring {
-        uint32_t slot = 0, parity = 0;
-        __device__ void next() {
-            if (++slot == NS) {
-                slot = 0;
-                parity ^= 1;
-            }
-        }
-    };
-
     if (warp == 4) {
         // ---- the line of work, and loads: lane l brings page l of each tile
         const KvPlan plan = kv_plan(kv, b);
         Line line(plan, kv.n_kv_heads, 1, blockIdx.x, a.sms);
-        const int P = kv.page_size, box = min(P, NK), per = NK / box;
-        Ring ring;
-        uint32_t used = 0;
+        const int P = kv.page_size, per = NK / P;
+        uint32_t at = 0;  // slots loaded: for each tile the halves of the keys, of the values
         bool ok = true;
-        for (uint32_t x = 0; ok; ++x) {
-            Segment sg;
-            line.next(sg);
+        const auto tell = [&](uint32_t x, const Segment &sg) {
             ok = __all_sync(FULL, bar_wait(seg_empty(x), (x / kSegs + 1) & 1, gave_up));
-            if (!ok) break;
-            if (lane == 0) {
+            if (ok && lane == 0) {
                 segs[x % kSegs] = sg;
                 bar_arrive(seg_full(x));
             }
-            if (sg.n == 0) break;
-            const int32_t *row = kv.table + int64_t(line.it.seq) * kv.max_pages;
+        };
+        Segment sg, ahead;
+        line.next(sg);
+        tell(0, sg);
+        for (uint32_t x = 0; ok && sg.n > 0; ++x, sg = ahead) {
+            // The next segment is told of before this one is loaded: the softmax asks for it while this one's last tiles wait
+            // for slots that its own work has to free.
+            line.next(ahead);
+            tell(x + 1, ahead);
+            const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
+            const int first = sg.k0 / P + lane;
             const auto page_of = [&](int j) {  // of this lane in tile j; past the keys: none, zeros
-                const int key = sg.k0 + j * NK + lane * box;
-                return lane < per && j < sg.n && key < sg.kv1 ? row[key / P] : -1;
+                const int idx = first + j * per;
+                return lane < per && j < sg.n && idx * P < sg.kv1 ? row[idx] : -1;
             };
             int page = page_of(0);
             for (int j = 0; j < sg.n && ok; ++j) {
-                const int next_page = page_of(j + 1), inside = (sg.k0 + j * NK + lane * box) % P;
+                const int next_page = page_of(j + 1);
                 const int w = unsigned(page) < unsigned(kv.n_pages) ? page : kv.n_pages;
 #pragma unroll
-                for (int v = 0; v < 2; ++v) {  // keys, values
-                    ok = __all_sync(FULL, bar_wait(empty(ring.slot), ring.parity ^ 1, gave_up));
+                for (int y = 0; y < 2 * HF; ++y, ++at) {
+                    ok = __all_sync(FULL, bar_wait(empty(at), (at / NS + 1) & 1, gave_up));
                     if (!ok) break;
-                    if (lane == 0) bar_expect(full(ring.slot), Sh::kTile);
+                    if (lane == 0) bar_expect(full(at), Sh::kSlot);
                     __syncwarp();
-                    if (lane < per) {
-                        const uint32_t dst = sbase + ring.slot * Sh::kTile + lane * box * 128;
-#pragma unroll
-                        for (int half = 0; half < DP / 64; ++half)
-                            tma_load(dst + half * Sh::kHalf, v ? &maps.values : &maps.keys, full(ring.slot), half * 64, inside, sg.h, w);
-                    }
-                    ring.next();
-                    ++used;
+                    if (lane < per) tma_load(slot_at(at) + lane * P * 128, y < HF ? &maps.keys : &maps.values, full(at), y % HF * 64, 0, sg.h, w);
                 }
                 page = next_page;
             }
         }
         if (!ok) {  // let what is on its way arrive
-            for (uint32_t k = used > NS ? used - NS : 0; k < used; ++k)
-                for (int n = 0; n < 1000000 && !bar_try(full(k % NS), (k / NS) & 1); ++n) {
+            for (uint32_t k = at > NS ? at - NS : 0; k < at; ++k)
+                for (int n = 0; n < 1000000 && !bar_try(full(k), (k / NS) & 1); ++n) {
                 }
             if (lane == 0) atomicMin(kv.status, SIM_E_STATE);
         }
     } else if (warp == 5) {
         // ---- tensor products: the whole warp keeps the same (uniform) state, one lane issues
         const uint32_t type = BF ? 1u << 7 | 1u << 10 : 0u;
-        const uint32_t idesc_s = 1u << 4 | type | (NK / 8) << 17 | (128 / 16) << 24;
-        const uint32_t idesc_o = 1u << 4 | type | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
-        const uint64_t op_k = operand(sbase, 16, 1024), op_v = operand(sbase, Sh::kHalf, 1024);
-        Ring ring;
-        uint32_t np = 0;
+        const uint32_t op_q = sbase + Sh::kOffQ;
+        uint32_t at = 0, np = 0;
         bool ok = true;
         const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, bar_wait(bar, parity, gave_up)) != 0; };
-        const auto keys = [&] {  // S of the tile in the ring's slot
-            if (elect_one()) {
+        const auto wait_full = [&](uint32_t x) {
+            bool all = true;
 #pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk)
-                    mma_ts(tmem, tmem + Sh::kColQ + kk * 8, op_k + ((ring.slot * Sh::kTile + (kk / 4) * Sh::kHalf + (kk % 4) * 32) >> 4), idesc_s, kk > 0);
-                tc_commit(s_full);
-                tc_commit(empty(ring.slot));
-            }
-            __syncwarp();
-            ring.next();
+            for (int y = 0; y < HF; ++y) all = all && wait(full(x + y), ((x + y) / NS) & 1);
+            return all;
         };
         for (uint32_t x = 0; (ok = take(x)); ++x) {
-            const int n = __shfl_sync(FULL, segs[x % kSegs].n, 0);
+            const int n = __shfl_sync(FULL, segs[x % kSegs].n, 0), cols = __shfl_sync(FULL, segs[x % kSegs].rows, 0) > 16 ? 32 : 16;
             give_back(x);
             if (n == 0) break;
-            ok = wait(q_full, x & 1) && wait(full(ring.slot), ring.parity);
-            if (!ok) break;
-            tc_fence_after();
-            keys();
-            for (int j = 0; j < n && ok; ++j, ++np) {
-                ok = wait(full(ring.slot), ring.parity) && wait(p_ready, np & 1);
+            const uint32_t idesc_s = 1u << 4 | type | uint32_t(cols / 8) << 17 | (128 / 16) << 24, idesc_o = idesc_s | 1u << 15;
+            ok = wait(q_full, x & 1);
+            for (int j = 0; j < n && ok; ++j, ++np, at += 2 * HF) {
+                ok = wait_full(at);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk)
+                        mma_ss(tmem, operand(slot_at(at + kk / 4) + kk % 4 * 32, 16, 1024), operand(op_q + (kk / 4) * Sh::kRowsHalf + kk % 4 * 32, 16, 1024), idesc_s, kk > 0);
+                    tc_commit(s_full);
+#pragma unroll
+                    for (int y = 1; y < HF; ++y) tc_commit(empty(at + y));  // P takes the first half's place
+                }
+                __syncwarp();
+                ok = wait_full(at + HF) && wait(p_ready, np & 1);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    // D <= 64: rows 64 .. 127 of the product are made of other values (8 keys on) and not used
+#pragma unroll
                     for (int kk = 0; kk < NK / 16; ++kk)
-                        mma_ts(tmem + Sh::kColO, tmem + kk * 8, op_v + ((ring.slot * Sh::kTile + kk * 2048) >> 4), idesc_o, j > 0 || kk > 0);
-                    tc_commit(empty(ring.slot));
+                        mma_ss(tmem + Sh::kColO, operand(slot_at(at + HF) + kk * 2048, HF > 1 ? Sh::kSlot : 1024, 1024),
+                               operand(slot_at(at) + (kk / 4) * Sh::kRowsHalf + kk % 4 * 32, 16, 1024), idesc_o, j > 0 || kk > 0);
+                    tc_commit(empty(at));
+#pragma unroll
+                    for (int y = HF; y < 2 * HF; ++y) tc_commit(empty(at + y));
                     if (j + 1 == n) tc_commit(o_full);
                 }
                 __syncwarp();
-                ring.next();
-                if (j + 1 < n) {
-                    ok = wait(full(ring.slot), ring.parity);
-                    if (!ok) break;
-                    keys();
-                }
             }
             if (!ok) break;
         }
@@ -214,160 +229,238 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
         __syncwarp();
     } else {
         // ---- queries, softmax, results
-        const int w = warp, lr = tid;
-        const uint32_t t_s = tmem + (uint32_t(w * 32) << 16), t_q = t_s + Sh::kColQ, t_o = t_s + Sh::kColO;
-        float *const stage = reinterpret_cast<float *>(base + Sh::kOffStage);
-        float2 *const stat = reinterpret_cast<float2 *>(base + Sh::kOffStat);
+        const int w = warp, lr = tid;  // the key within a tile, the column of the result
+        const uint32_t t_s = tmem + (uint32_t(w * 32) << 16), t_o = t_s + Sh::kColO;
+        float *const red = reinterpret_cast<float *>(base + Sh::kOffRed);
+        int *const vote = reinterpret_cast<int *>(base + Sh::kOffVote);
         int *const again = reinterpret_cast<int *>(base + Sh::kOffAgain);
         const float c = a.scale_log2;
-        uint32_t ns = 0, nj = 0;
-        Ring ring;  // of the tile's keys
+        uint32_t ns = 0, nj = 0, nr = 0, nv = 0, at = 0;
         bool ok = true;
         const auto join = [&] {  // the four warps, by a barrier whose wait ends even if some have given up
             __syncwarp();
             if (lane == 0) bar_arrive(joined);
             ok = __all_sync(FULL, bar_wait(joined, nj++ & 1, gave_up)) && ok;
         };
-        // The query row in this thread's lane.
-        const auto q_row = [&](const Segment &s) {
-            const int y = s.row0 + min(lane, s.rows - 1), t = a.group.div(y);
-            return static_cast<const uint16_t *>(a.q) + int64_t(s.q0 + t) * a.qt + int64_t(s.h * G + y - t * G) * a.qh;
+        // Queries: 16 bytes of a row at a time, the next item's fetched before they can be put in place.
+        constexpr int kVec = DP / 8, kFetch = kLightRows * kVec / 128;
+        uint4 query[kFetch];
+        const auto query_at = [&](const Segment &s, int i) {  // this thread's i-th 16 bytes, NULL if there are none
+            const int r = (lr + 128 * i) / kVec, d = (lr + 128 * i) % kVec * 8, y = s.row0 + r, t = a.group.div(y);
+            return r < s.rows && d < D ? static_cast<const uint16_t *>(a.q) + int64_t(s.q0 + t) * a.qt + int64_t(s.h * G + y - t * G) * a.qh + d : nullptr;
         };
-        const auto load_q = [&](const Segment &s) {
-            const uint16_t *from = q_row(s);
+        const auto fetch = [&](const Segment &s) {
+#pragma unroll
+            for (int i = 0; i < kFetch; ++i) {
+                const uint16_t *from = a.q_vec ? query_at(s, i) : nullptr;
+                query[i] = from ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0, 0, 0, 0);  // columns past the head's: zeros
+            }
+        };
+        const auto place = [&](const Segment &s) {
+            const auto put = [&](int i, uint4 v) {
+                const int r = (lr + 128 * i) / kVec, e = (lr + 128 * i) % kVec;
+                if (r < s.rows) *reinterpret_cast<uint4 *>(base + Sh::kOffQ + (e / 8) * Sh::kRowsHalf + r * 128 + ((e % 8 ^ (r & 7)) << 4)) = v;
+            };
             if (a.q_vec) {
 #pragma unroll
-                for (int half = 0; half < DP / 64; ++half) {
-                    uint4 q[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[j] = half * 64 + j * 8 < D ? *reinterpret_cast<const uint4 *>(from + half * 64 + j * 8) : make_uint4(0, 0, 0, 0);
-                    tm_st32(t_q + 32 * half, reinterpret_cast<const uint32_t *>(q));
-                }
+                for (int i = 0; i < kFetch; ++i) put(i, query[i]);
             } else {
 #pragma unroll 1
-                for (int d = 0; d < DP; d += 16) {
-                    uint32_t q[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[j] = d + 2 * j < D ? from[d + 2 * j] | uint32_t(from[d + 2 * j + 1]) << 16 : 0;
-                    tm_st8(t_q + d / 2, q);
+                for (int i = 0; i < kFetch; ++i) {
+                    const uint16_t *from = query_at(s, i);
+                    put(i, from ? make_uint4(from[0] | uint32_t(from[1]) << 16, from[2] | uint32_t(from[3]) << 16, from[4] | uint32_t(from[5]) << 16,
+                                             from[6] | uint32_t(from[7]) << 16)
+                                : make_uint4(0, 0, 0, 0));
                 }
             }
-            tc_wait_st();
+            smem_to_async();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(q_full);
         };
-        // Before segment 0 comes one without tiles, so that the code that takes up the next segment is there once.
-        for (uint32_t x = ~0u; ok; ++x) {
+        ok = take(0);
+        if (ok && segs[0].n > 0) {
+            fetch(segs[0]);
+            place(segs[0]);
+        }
+        for (uint32_t x = 0; ok; ++x) {
             const Segment &sg = segs[x % kSegs], &next = segs[(x + 1) % kSegs];
-            const bool real = x != ~0u;
-            const int n = real ? sg.n : 0;
-            if (real && n == 0) break;
-            const int rows = sg.rows;
-            // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
-            const int last = lane < rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + lane))) : sg.kv1 - 1;
-            float m = -INFINITY, l = 0.f;
-            if (!real) ok = take(0);
+            const int n = sg.n, rows = sg.rows, kv1 = sg.kv1;
+            if (n == 0) break;
+            const int t0 = a.group.div(sg.row0), h0 = sg.row0 - t0 * G, sees = sg.pos0 + t0 + 1;  // of the first row: token, head, keys
             int k0 = sg.k0;  // first key of the tile
-            const int kv1 = sg.kv1;
-            for (int j = 0; j < n; ++j, k0 += NK) {
-                if (j == max(n - 2, 0)) {  // the next item's queries come to L1 meanwhile: two lines a row
+            // Eight rows' scores of this thread's key, -infinity where they do not see it.
+            const auto scores = [&](int r0, float *s) {
+                uint32_t u[8];
+                tm_ld8(t_s + r0, u);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = __uint_as_float(u[i]);
+                if (k0 + NK > min(kv1, sees)) {
+                    int to = sees + int(a.group.div(h0 + r0)), h = h0 + r0 - int(a.group.div(h0 + r0)) * G;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (k0 + lr >= min(kv1, to)) s[i] = -INFINITY;
+                        if (++h == G) {
+                            h = 0;
+                            ++to;
+                        }
+                    }
+                }
+            };
+            // A row's maximum or sum over all of the block's keys, for the lane of that number.  Between two uses of one half
+            // of `red` lies a third one.
+            const auto joined_rows = [&](auto sum) {
+                constexpr bool SUM = decltype(sum)::value;
+                float *const to = red + (++nr & 1) * kLightRows * 4;
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += 8) {
+                    float s[8];
+                    if constexpr (SUM) {
+                        uint32_t u[8];
+                        tm_ld8(t_s + Sh::kColL + r0, u);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) s[i] = __uint_as_float(u[i]);
+                    } else {
+                        scores(r0, s);
+                    }
+                    const float v = over_lanes<SUM>(s);
+                    if (lane % 4 == 0) to[(r0 + lane / 4) * 4 + w] = v;
+                }
+                join();
+                const float4 v = *reinterpret_cast<const float4 *>(to + lane * 4);
+                return SUM ? (v.x + v.y) + (v.z + v.w) : fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
+            };
+            float m = -INFINITY;  // of row `lane`: log2, times c
+#pragma unroll 1
+            for (int j = 0; j < n; ++j, k0 += NK, at += 2 * HF) {
+                if (j == max(n - 2, 0)) {
                     ok = take(x + 1);
                     if (!ok) break;
-                    if (next.n > 0 && lr < next.rows) {
-                        const uint16_t *from = q_row(next);
-                        uint16_t v;
-                        asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from));
-                        asm volatile("ld.global.ca.u16 %0, [%1];" : "=h"(v) : "l"(from + D - 1));
-                    }
+                    if (next.n > 0) fetch(next);
                 }
-                ok = __all_sync(FULL, bar_wait(s_full, ns & 1, gave_up));
+                ok = __all_sync(FULL, bar_wait(s_full, ns++ & 1, gave_up));
                 if (!ok) break;
-                ++ns;
                 tc_fence_after();
-                softmax_tile<NK, 4, DP, BF>(t_s, t_o, w, last - k0 - w * (NK / 4), j == 0, c, m, l, [] {});
-                ring.next();
-                // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                const int valid = kv1 - k0;
-                if (valid < NK) {
-                    ok = __all_sync(FULL, bar_wait(full(ring.slot), ring.parity, gave_up));
-                    if (lr >= 2 * valid) {  // two threads a row
-                        unsigned char *v = base + ring.slot * Sh::kTile + (lr >> 1) * 128 + (lr & 1) * 64;
+                bool grows = j == 0;
+                if (j > 0) {
+#pragma unroll 1
+                    for (int r0 = 0; r0 < rows; r0 += 8) {
+                        float s[8];
+                        scores(r0, s);
 #pragma unroll
-                        for (int z = 0; z < DP / 16; ++z) *reinterpret_cast<uint4 *>(v + (z / 4) * Sh::kHalf + (z % 4) * 16) = make_uint4(0, 0, 0, 0);
+                        for (int i = 0; i < 8; ++i) {
+                            const float over = fmaf(s[i], c, -__shfl_sync(FULL, m, r0 + i));
+                            grows |= r0 + i < rows && over > kGrow;
+                        }
                     }
-                    smem_to_async();
+                    grows = __any_sync(FULL, grows);
+                    int *const to = vote + (nv++ & 1) * 4;
+                    if (lane == 0) to[w] = grows;
+                    join();
+                    if (!ok) break;
+                    const int4 v = *reinterpret_cast<const int4 *>(to);
+                    grows = v.x | v.y | v.z | v.w;
                 }
-                ring.next();
+                if (grows) {
+                    const float top = joined_rows(std::false_type()) * c;
+                    if (!ok) break;
+                    // each row for itself: what it becomes does not hang on the rows beside it
+                    const bool up = j == 0 || top - m > kGrow;
+                    const float f = up ? ex2(m - top) : 1.f;
+                    if (up) m = top;
+#pragma unroll 1
+                    for (int r0 = 0; r0 < rows && j > 0; r0 += 8) {  // O: the product before has ended, this tile's first came after it
+                        uint32_t o[8], l[8];
+                        tm_ld8(t_o + r0, o);
+                        tm_ld8(t_s + Sh::kColL + r0, l);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float fi = __shfl_sync(FULL, f, r0 + i);
+                            o[i] = __float_as_uint(__uint_as_float(o[i]) * fi);
+                            l[i] = __float_as_uint(__uint_as_float(l[i]) * fi);
+                        }
+                        tm_st8(t_o + r0, o);
+                        tm_st8(t_s + Sh::kColL + r0, l);
+                        tc_wait_st();
+                    }
+                }
+                unsigned char *const p = base + (at % NS) * Sh::kSlot + lr / 64 * Sh::kRowsHalf + lr % 8 * 2;
+                const float off = m == -INFINITY ? 0.f : -m;
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += 8) {
+                    float s[8];
+                    uint32_t l[8] = {};
+                    if (j > 0) tm_ld8(t_s + Sh::kColL + r0, l);
+                    scores(r0, s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        s[i] = ex2(fmaf(s[i], c, __shfl_sync(FULL, off, r0 + i)));
+                        l[i] = __float_as_uint(__uint_as_float(l[i]) + s[i]);
+                    }
+                    tm_st8(t_s + Sh::kColL + r0, l);
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        const uint32_t both = pack<BF>(s[i], s[i + 1]);
+                        *reinterpret_cast<uint16_t *>(p + (r0 + i) * 128 + ((lr % 64 / 8 ^ i) << 4)) = uint16_t(both);
+                        *reinterpret_cast<uint16_t *>(p + (r0 + i + 1) * 128 + ((lr % 64 / 8 ^ (i + 1)) << 4)) = uint16_t(both >> 16);
+                    }
+                }
+                // values past the end of the keys, whatever they are, must not meet their zero probabilities
+                if (kv1 - k0 < NK) {
+#pragma unroll
+                    for (int y = HF; y < 2 * HF; ++y) {
+                        ok = __all_sync(FULL, bar_wait(full(at + y), ((at + y) / NS) & 1, gave_up)) && ok;
+                        if (lr >= kv1 - k0) {
+                            uint4 *const v = reinterpret_cast<uint4 *>(base + ((at + y) % NS) * Sh::kSlot + lr * 128);
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) v[z] = make_uint4(0, 0, 0, 0);
+                        }
+                    }
+                    if (!ok) break;
+                }
+                tc_wait_st();
+                smem_to_async();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_ready);
             }
             if (!ok) break;
-            if (next.n > 0) load_q(next);  // every product with this item's queries has been read
-            if (!real) continue;
+            if (next.n > 0) place(next);  // every product with this item's queries has ended
 
             const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + n * NK};
-            // Join the four copies of each row: first what each is multiplied by.
-            float2 *const st = stat + (x & 1) * 128;
-            st[lr] = make_float2(m, l);
-            join();
-            float top = -INFINITY, total = 0.f;
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-                if (st[32 * p + lane].y != 0.f) top = fmaxf(top, st[32 * p + lane].x);
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-                if (st[32 * p + lane].y != 0.f) total += st[32 * p + lane].y * ex2((st[32 * p + lane].x - top) * c);
-            const float f = l == 0.f ? 0.f : ex2((m - top) * c) / total;
-            if (lr < rows) sink.lse(lr, top, total);
-            if (lr < 32) again[lr] = 0;
-            // As many columns at a time as the stage holds of all copies.  No wait is needed after the last ones: the stage is
-            // used again only after the other warps have gone on to another item.
-            int cols = DP, shift = DP == 128 ? 5 : 4;  // log2 of the columns / 4
-            while (4 * rows * (cols + 4) > Sh::kJoinStage) {
-                cols /= 2;
-                --shift;
-            }
-            float *const to = stage + (w * rows + lane) * (cols + 4);
+            if (lr < kLightRows) again[lr] = 0;
+            const float total = joined_rows(std::true_type()), inv = total == 0.f ? 0.f : 1.f / total;
             ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
             if (!ok) break;
             tc_fence_after();
+            if (lr < rows) sink.lse(lr, m, total);
+            int h = h0;
+            uint16_t *out = sink.out_row(0) + lr;
+            float *part = a.part + sg.row * D + lr;
 #pragma unroll 1
-            for (int d0 = 0; d0 < D; d0 += cols) {
-                if (d0 > 0) join();
-#pragma unroll 1
-                for (int d = 0; d < cols; d += 32) {
-                    uint32_t o[32];
-                    if (cols == 16) tm_ld16(t_o + d0, o);
-                    else tm_ld32(t_o + d0 + d, o);
-                    tc_wait_ld();
-                    if (lane < rows) {
+            for (int r0 = 0; r0 < rows; r0 += 8) {
+                uint32_t o[8];
+                tm_ld8(t_o + r0, o);
+                tc_wait_ld();
 #pragma unroll
-                        for (int y = 0; y < 32; y += 4)
-                            if (y < 16 || cols > 16)
-                                *reinterpret_cast<float4 *>(to + d + y) =
-                                    l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                             : make_float4(__uint_as_float(o[y]) * f, __uint_as_float(o[y + 1]) * f, __uint_as_float(o[y + 2]) * f, __uint_as_float(o[y + 3]) * f);
+                for (int i = 0; i < 8; ++i) {
+                    const float f = __shfl_sync(FULL, inv, r0 + i), v = f == 0.f ? 0.f : __uint_as_float(o[i]) * f;
+                    if (r0 + i < rows && lr < D) {
+                        if (sg.direct) *out = uint16_t(pack<BF>(v, v));
+                        else *part = v;
+                        if (v * 0.f != 0.f) again[r0 + i] = 1;
+                    }
+                    part += D;
+                    out += a.oh;
+                    if (++h == G) {
+                        h = 0;
+                        out += a.ot - G * a.oh;
                     }
                 }
-                join();
-                if (!ok) break;
-#pragma unroll 1
-                for (int e = lr; e < rows << shift; e += 128) {
-                    const int y = e >> shift, d = 4 * (e & ((1 << shift) - 1));
-                    if (d0 + d >= D) continue;
-                    float4 v[4];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) v[p] = *reinterpret_cast<const float4 *>(stage + (p * rows + y) * (cols + 4) + d);
-                    const float4 t = make_float4((v[0].x + v[1].x) + (v[2].x + v[3].x), (v[0].y + v[1].y) + (v[2].y + v[3].y),
-                                                 (v[0].z + v[1].z) + (v[2].z + v[3].z), (v[0].w + v[1].w) + (v[2].w + v[3].w));
-                    if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d0 + d) = make_uint2(pack<BF>(t.x, t.y), pack<BF>(t.z, t.w));
-                    else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d0 + d) = t;
-                    if (t.x * 0.f + t.y * 0.f + t.z * 0.f + t.w * 0.f != 0.f) again[y] = 1;
-                }
             }
-            if (!ok) break;
             if (sink.blind(0)) {  // see Sink::again
                 join();
                 if (!ok) break;
