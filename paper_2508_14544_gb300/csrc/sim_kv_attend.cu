@@ -28,7 +28,7 @@ namespace {
 // sequences (8 kv heads, 8 query heads each, up to 64 keys of their own) in groups: 64 groups with a prefix of 512 keys 81-91
 // against 72 us, of 2048 keys 141 against 180 us; 16 groups with 256 keys 60-70 against 55 us, with 1024 keys 78 against 89 us.
 // The rule takes the faster side of these four.
-constexpr int kShareItem = 3, kShareRows = 7, kShareOnce = 3;
+constexpr int kShareItem = 3, kShareRows = 7, kShareOnce = 2;
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 

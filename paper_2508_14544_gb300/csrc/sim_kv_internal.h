@@ -72,7 +72,7 @@ __host__ __device__ constexpr int kv_rows(int light) { return light ? kLightRows
 constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.
-__host__ __device__ constexpr int kv_lead(int light) { return light ? 3 : 4; }
+__host__ __device__ constexpr int kv_lead(int light) { return light ? 1 : 4; }
 __host__ __device__ inline int kv_span(int tiles, int light) { return tiles > 0 ? tiles + kv_lead(light) : 0; }
 
 // A run of query rows (token x head of the group, for every kv head alike) against a range of one table's keys.

@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             const Segment &sg = segs[x % kSegs], &next = segs[(x + 1) % kSegs];
             const int n = sg.n, rows = sg.rows, kv1 = sg.kv1;
             if (n == 0) break;
-            const int t0 = a.group.div(sg.row0), h0 = sg.row0 - t0 * G, sees = sg.pos0 + t0 + 1;  // of the first row: token, head, keys
+            // The first key that row `lane` does not see; that row 0 does not.
+            const int blind = min(kv1, sg.pos0 + int(a.group.div(sg.row0 + lane)) + 1), all = __shfl_sync(FULL, blind, 0);
             int k0 = sg.k0;  // first key of the tile
             // Eight rows' scores of this thread's key, -infinity where they do not see it.
             const auto scores = [&](int r0, float *s) {
@@ -296,16 +297,9 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                 tc_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s[i] = __uint_as_float(u[i]);
-                if (k0 + NK > min(kv1, sees)) {
-                    int to = sees + int(a.group.div(h0 + r0)), h = h0 + r0 - int(a.group.div(h0 + r0)) * G;
+                if (k0 + NK > all) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (k0 + lr >= min(kv1, to)) s[i] = -INFINITY;
-                        if (++h == G) {
-                            h = 0;
-                            ++to;
-                        }
-                    }
+                    for (int i = 0; i < 8; ++i) s[i] = k0 + lr >= __shfl_sync(FULL, blind, r0 + i) ? -INFINITY : s[i];
                 }
             };
             // A row's maximum or sum over all of the block's keys, for the lane of that number.  Between two uses of one half
@@ -437,7 +431,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (!ok) break;
             tc_fence_after();
             if (lr < rows) sink.lse(lr, m, total);
-            int h = h0;
+            int h = sg.row0 - int(a.group.div(sg.row0)) * G;  // head of the row in its group
             uint16_t *out = sink.out_row(0) + lr;
             float *part = a.part + sg.row * D + lr;
 #pragma unroll 1
