@@ -399,7 +399,7 @@ constexpr int kJoinLight = 4;
 // goes over what there is to join: items without a prefix that blocks' stretches cut, then entries with a shared prefix
 // and rows without keys, by kv head (`parts` blocks for each).
 template <bool BF>
-__global__ void __launch_bounds__(kJoin, 6) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
+__global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
     const int H = kv.n_kv_heads, G = b.q_heads / H, D = kv.head_dim, sl = threadIdx.x & 15, sub = threadIdx.x >> 4;
@@ -476,13 +476,15 @@ __global__ void __launch_bounds__(kJoin, 6) k_combine(const sim_kv kv, const sim
 #pragma unroll 1
             for (int p0 = 0; p0 < n; p0 += 16) {
                 const int p = p0 + sl;
-                const int64_t at = p < first.n ? first.at(p, pin) : own.at(p - first.n, in);
+                int64_t at = p < first.n ? first.at(p, pin) : own.at(p - first.n, in);
                 const float s = at >= 0 ? __ldcg(a.part_lse + at) : -INFINITY;
-                float4 v[4][2];  // a piece that is not there: row 0, with weight 0
+                const int64_t some = __shfl_sync(mine, at, 0, 16);
+                at = at >= 0 ? at : some;  // a piece that is not there: another, with weight 0
+                float4 v[4][2];
                 const auto fetch = [&](int i0) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float4 *from = reinterpret_cast<const float4 *>(a.part + max(__shfl_sync(mine, at, i0 + e, 16), int64_t(0)) * D);
+                        const float4 *from = reinterpret_cast<const float4 *>(a.part + __shfl_sync(mine, at, i0 + e, 16) * D);
 #pragma unroll
                         for (int q = 0; q < 2; ++q) v[e][q] = __ldcg(from + (4 * (sl + 16 * q) < D ? sl + 16 * q : 0));
                     }
@@ -581,7 +583,7 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
-    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 6));
+    const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 5));
     return launch_chained(kv.dtype == SIM_KV_BF16 ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 
