@@ -105,8 +105,8 @@ int sim_kv_compact(const sim_kv *kv, int32_t *to, void *cuda_stream);
 /* The queries of one batch: entry i has the query tokens cu_q[i] .. cu_q[i + 1] - 1, which are the last
  * tokens of sequence seqs[i] (already in the cache); a query sees the keys up to its own position. */
 typedef struct {
-    int32_t n;                /* entries, 0 .. max_seqs (an entry may have no queries, a sequence may repeat) */
-    int32_t n_q;              /* query tokens in all */
+    int32_t n;                /* entries, 0 .. 2^17, n * n_kv_heads <= 2^26 (an entry may have no queries, a sequence may repeat) */
+    int32_t n_q;              /* query tokens in all, n_q * q_heads <= 2^30 */
     int32_t q_heads;          /* a multiple of n_kv_heads: query head h reads kv head h / (q_heads / n_kv_heads) */
     int32_t n_groups;         /* 0: none */
     const int32_t *seqs;      /* DEVICE [n] */
@@ -134,7 +134,7 @@ int sim_kv_plan(const sim_kv *kv, const sim_kv_batch *b, void *cuda_stream);
  *   q        DEVICE [n_q][q_heads][head_dim] of kv->dtype, strides in elements, last dimension contiguous.
  *   out      the same shape and type, strides multiples of 8, 16-byte aligned.
  *   lse      DEVICE float [n_q][q_heads], or NULL: log of the sum of the exponentials.
- *   scale    > 0, finite.
+ *   scale    > 0, finite, also times log2(e).
  * A query that sees no key gets zeros, and -infinity for lse.  Cached values past a sequence's length are
  * never used, whatever they are.  Sums and the softmax are in 32 bits; the probabilities are rounded to
  * kv->dtype for the product with the values.

@@ -274,85 +274,6 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_
     return uint64_t((addr >> 4) & 0x3fff) | uint64_t(lbo >> 4) << 16 | uint64_t(sbo >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 
-// ---- softmax ------------------------------------------------------------------------------------------------
-
-// A tile of NK keys: S (columns t_s on) becomes P in 16 bits, in the same columns.  Every row lies in R lanes, one
-// in each of R warps (1 or 4); warp w takes NK / R keys of its rows and leaves zeros for the others.  lim: the last
-// of this thread's keys that its row sees.  m, l: the maximum that P refers to and the sum so far of this
-// thread's keys; DP columns of O from t_o on.
-// half: called when the first half of P is in place (R = 1).
-template <int NK, int R, int DP, bool BF, typename Half>
-__device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int w, int lim, bool first, float c, float &m, float &l, Half &&half) {
-    constexpr int NC = NK / R;
-    static_assert((R == 1 && NC == 128) || (R == 4 && NC == 16), "copies");
-    const int c0 = R == 4 ? w * NC : 0;
-    uint32_t s[NC];
-    if constexpr (NC == 16) {
-        tm_ld16(t_s + c0, s);
-    } else {
-#pragma unroll
-        for (int q = 0; q < NC / 32; ++q) tm_ld32(t_s + c0 + 32 * q, s + 32 * q);
-    }
-    tc_wait_ld();
-    if (__any_sync(FULL, lim < NC - 1)) {
-#pragma unroll
-        for (int y = 0; y < NC; ++y)
-            if (y > lim) s[y] = 0xff800000u;
-    }
-    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-    for (int y = 0; y < NC; y += 2) top[y / 2 & 3] = max3(top[y / 2 & 3], __uint_as_float(s[y]), __uint_as_float(s[y + 1]));
-    const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-    if (first) {
-        m = mx;
-    } else if (const bool grows = (mx - m) * c > kGrow; __any_sync(FULL, grows)) {
-        // each row for itself: what it becomes does not hang on the rows beside it, nor on what lies in lanes past the rows
-        const float up = grows ? mx : m, f = grows ? ex2((m - up) * c) : 1.f;
-        m = up;
-        l *= f;
-#pragma unroll 1
-        for (int q = 0; q < DP / 32; ++q) {
-            uint32_t o[32];
-            tm_ld32(t_o + 32 * q, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
-            tm_st32(t_o + 32 * q, o);
-        }
-    }
-    const float off = m == -INFINITY ? 0.f : m * c;
-    float2 sum[4] = {};
-    uint32_t pk[NC / 2];
-#pragma unroll
-    for (int y = 0; y < NC; y += 2) {
-        float2 e = fma2(make_float2(__uint_as_float(s[y]), __uint_as_float(s[y + 1])), make_float2(c, c), make_float2(-off, -off));
-        e = make_float2(ex2(e.x), ex2(e.y));
-        sum[y / 2 & 3] = add2(sum[y / 2 & 3], e);
-        pk[y / 2] = pack<BF>(e.x, e.y);
-        if constexpr (R == 1) {
-            if (y == NC / 2 - 2) {
-                tm_st32(t_s, pk);
-                tc_wait_st();
-                half();
-            }
-        }
-    }
-    sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-    l += sum[0].x + sum[0].y;
-    if constexpr (R == 1) {
-        tm_st32(t_s + 32, pk + 32);
-    } else {
-#pragma unroll
-        for (int q = 0; q < R; ++q) {
-            uint32_t z[NC / 2];
-#pragma unroll
-            for (int y = 0; y < NC / 2; ++y) z[y] = q == w ? pk[y] : 0;
-            tm_st8(t_s + 8 * q, z);
-        }
-    }
-    tc_wait_st();
-}
-
 // Where the results of a segment go.
 template <bool BF>
 struct Sink {

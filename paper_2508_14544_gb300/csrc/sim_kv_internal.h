@@ -1,4 +1,5 @@
-// Declarations shared by the C ABI of the paged cache (sim_kv_api.cpp) and its kernels (sim_kv.cu, sim_kv_attend.cu).
+// Declarations shared by the C ABI of the paged cache (sim_kv_api.cpp) and its kernels (sim_kv.cu, sim_kv_attend.cu,
+// sim_kv_heavy.cu, sim_kv_light.cu).
 #pragma once
 
 #include <cuda_runtime.h>
