@@ -137,8 +137,10 @@ __device__ __forceinline__ int tile_rows(int r) {
     const int rem = r % kAttRows;
     return 2 * (r / kAttRows) + (rem > kAttRows / 2 ? 2 : rem > 0);
 }
-__device__ __forceinline__ int heavy_items(int r) { return r / kAttRows + (r % kAttRows > kLightRows); }
-__device__ __forceinline__ int light_items(int r) { return r % kAttRows > 0 && r % kAttRows <= kLightRows; }
+__device__ __forceinline__ int heavy_items(int r, bool only) { return only ? 0 : r / kAttRows + (r % kAttRows > kLightRows); }
+__device__ __forceinline__ int light_items(int r, bool only) {
+    return only ? ceil_div(r, kLightRows) : r % kAttRows > 0 && r % kAttRows <= kLightRows;
+}
 
 constexpr int kFewSources = 448, kFewItems = 1024;
 
@@ -174,6 +176,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
     int32_t *const used = FEW ? few_used : p.used, *const alone = FEW ? few_alone : p.alone;
     int32_t *const first0 = FEW ? few_first[0] : p.first[0], *const first1 = FEW ? few_first[FEW ? 1 : 0] : p.first[1];
     const int tid = threadIdx.x, ng = b.n_groups, n_src = ng + b.n, G = b.q_heads / kv.n_kv_heads, P = kv.page_size;
+    const bool only = kv_light_only(kv, b);
     if (tid < 3) counts[tid] = 0;
     if (tid == 0) saved = 0;
     // Offsets that are not in order: no queries at all, or no groups.
@@ -261,12 +264,12 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             x.blind = e.len < e.t;
         }
         Two total;
-        const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows)) << 32 | heavy_items(x.rows), 0}, sums, total).a;
+        const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows, only)) << 32 | heavy_items(x.rows, only), 0}, sums, total).a;
         sum += total.a;
         if (s < n_src) {
             x.heavy0 = first0[s] = int(before & 0xffffffff);
             x.light0 = first1[s] = int(before >> 32);
-            x.n_heavy = heavy_items(x.rows);
+            x.n_heavy = heavy_items(x.rows, only);
             source[s] = x;
             if (FEW) p.source[s] = x;
             if (x.rows > 0 && (x.prefix >= 0 || x.blind)) p.join[atomicAdd(&counts[2], 1)] = s - ng;
@@ -289,10 +292,11 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
         for (int k0 = 0; k0 < n_items; k0 += kPlan) {
             const int k = k0 + tid;
             KvItem it = {};
+            int of = -1;  // source whose (first) light item this is
             if (k < n_items) {
                 const int s = last_at_most(first, n_src, k);
                 const KvSource x = source[s];
-                it.row0 = (light ? x.n_heavy : k - x.heavy0) * kAttRows;
+                it.row0 = only ? (k - x.light0) * kLightRows : (light ? x.n_heavy : k - x.heavy0) * kAttRows;
                 it.rows = min(x.rows - it.row0, kv_rows(light));
                 it.q0 = x.q0;
                 it.seq = x.seq;
@@ -301,6 +305,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                 it.kv1 = min(x.kv1, x.pos0 + (it.row0 + it.rows - 1) / G + 1);
                 it.partial = s < ng || x.prefix >= 0;
                 it.tiles = ceil_div(max(it.kv1 - it.kv0, 0), kTileKeys);
+                if (light && it.row0 == x.n_heavy * kAttRows) of = s;
             }
             Two total;
             const Two before = plan_scan<kPlan / 32>({int64_t(kv_span(it.tiles, light)) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
@@ -313,8 +318,8 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                     few_units[k] = it.unit;
                     few_tiles[k] = it.partial ? -1 : it.tiles;
                 }
-                if (light) {
-                    KvSource *const to = p.source + last_at_most(first, n_src, k);
+                if (of >= 0) {
+                    KvSource *const to = p.source + of;
                     to->tiles = it.tiles;
                     to->unit = it.unit;
                     to->row_off = it.row_off;
@@ -422,6 +427,7 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
     const uint32_t heavy = uint32_t(plan.hdr[7]) * kJoinHeavy, cuts = heavy + uint32_t(plan.hdr[23]) * kJoinLight;
     const uint32_t all = cuts + uint32_t(plan.hdr[17]) * uint32_t(H) * uint32_t(parts);  // at most 2^30 and the cuts
     const Share share0(plan, 0), share1(plan, 1);
+    const int per_item = kv_rows(kv_light_only(kv, b));
     const int64_t base1 = list_base(plan, 1, a.sms);
 #pragma unroll 1
     for (uint32_t y = blockIdx.x; y < all; y += gridDim.x) {
@@ -456,17 +462,18 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
             const int dt = a.group.div(z), t = q0 + dt, qh = h * G + z - dt * G;
             int in = z, pin = 0;
             if (!by_cut) {
-                const int nth = z / kAttRows;
-                in = z % kAttRows;
-                if (nth >= x.n_heavy) {
-                    own = Pieces(share1, base1, x.unit, x.tiles, x.row_off, min(x.rows - nth * kAttRows, kAttRows), h, 1);
-                    if (x.prefix < 0 && x.tiles > 0) continue;  // only rows without keys
+                if (x.prefix < 0) {  // only rows of items without keys: the item's last row sees the most
+                    const int end = min(z / per_item * per_item + per_item, x.rows);
+                    if (min(x.kv1, x.pos0 + int(a.group.div(end - 1)) + 1) > 0) continue;
                 } else {
-                    const KvItem it = plan.items[0][x.heavy0 + nth];
-                    own = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
-                    if (x.prefix < 0 && it.tiles > 0) continue;
-                }
-                if (x.prefix >= 0) {
+                    const int nth = z / kAttRows;
+                    in = z % kAttRows;
+                    if (nth >= x.n_heavy) {
+                        own = Pieces(share1, base1, x.unit, x.tiles, x.row_off, min(x.rows - nth * kAttRows, kAttRows), h, 1);
+                    } else {
+                        const KvItem it = plan.items[0][x.heavy0 + nth];
+                        own = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
+                    }
                     const KvSource px = plan.source[x.prefix];
                     const int row = (q0 - px.q0) * G + z, pth = row / kAttRows;
                     pin = row % kAttRows;
@@ -586,7 +593,7 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     }
     const int64_t rows = int64_t(b.n_q) * b.q_heads;
     cudaError_t e = cudaSuccess;
-    if (rows / kv.n_kv_heads > kLightRows) e = launch_kv_heavy(kv, b, a, maps, st);  // fewer rows make no heavy item
+    if (!kv_light_only(kv, b)) e = launch_kv_heavy(kv, b, a, maps, st);
     if (e == cudaSuccess) e = launch_kv_light(kv, b, a, maps, st);
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average

@@ -21,10 +21,15 @@ def _dtypes():
 class AttentionPlan:
     """How the attention of one batch is divided (``KVCache.plan``); holds what the calls with it read."""
 
-    def __init__(self, cache, batch, seqs, cu_q, cu_group, buffer):
+    def __init__(self, cache, batch, seqs, cu_q, cu_group, buffer, stream):
         self.cache, self.batch, self.seqs, self.cu_q, self.cu_group, self._buffer = cache, batch, seqs, cu_q, cu_group, buffer
         self._ref = ctypes.byref(batch)
         self.n_q, self.heads = batch.n_q, batch.q_heads
+        self._stream = stream  # whose next plan may have the buffer, None: no other plan
+
+    def __del__(self):
+        if self._stream is not None and len(self.cache._spare) < 2:
+            self.cache._spare.append((self._stream, self._buffer))
 
 
 class KVCache:
@@ -71,6 +76,7 @@ class KVCache:
         self._index, self._dim, self._heads, self._n_pages = pool.device.index, dim, heads, n_pages
         self._torch, self._i32 = torch, torch.int32
         self._sizes = {}  # bytes of a plan and its workspace by the batch's sizes
+        self._spare = []  # streams and buffers of plans that are gone: the workspace of the next ones
         torch.cuda.current_stream(self.device).synchronize()  # the first call may be on any stream
 
     def _empty(self, stream, shape, dtype):
@@ -185,10 +191,18 @@ class KVCache:
             if len(self._sizes) > 1000:
                 self._sizes.clear()
             self._sizes[n, n_q, heads, ng] = sizes
-        buffer = self._empty(stream, (sizes[0] + sizes[1] + 16,), self._torch.uint8)
+        size, buffer, mine = sizes[0] + sizes[1] + 16, None, None
+        if stream is None and not self._torch.cuda.is_current_stream_capturing():  # a graph's buffers are its own
+            mine = st
+            while buffer is None and self._spare:
+                of, buffer = self._spare.pop()
+                if of != st or buffer.shape[0] < size:
+                    buffer = None
+        if buffer is None:
+            buffer = self._empty(stream, (size,), self._torch.uint8)
         b.plan = buffer.data_ptr()
         b.workspace = b.plan + sizes[0]
-        plan = AttentionPlan(self, b, seqs, cu_q, cu_group, buffer)
+        plan = AttentionPlan(self, b, seqs, cu_q, cu_group, buffer, mine)
         rc = self._lib.sim_kv_plan(self._ref, plan._ref, st)
         if rc:
             self._fail(rc)
@@ -200,6 +214,8 @@ class KVCache:
         torch, st, dim = self._torch, self._stream(stream), self._dim
         if plan.cache is not self:
             raise ValueError("the plan is another cache's")
+        if plan._stream is not None and (plan._stream != st or torch.cuda.is_current_stream_capturing()):  # read where no next plan waits
+            plan._stream = None
         rows = self._rows("q", q, plan.n_q, plan.heads)
         if out is None:
             out = self._empty(stream, (plan.n_q, plan.heads, dim), self.dtype)

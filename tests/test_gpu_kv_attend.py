@@ -132,6 +132,54 @@ def test_more_entries_than_the_plan_keeps_on_chip(groups):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("group", [1, 4, 32])
+@pytest.mark.parametrize("queries,lens", [
+    ([20, 0, 0, 3, 0, 17] + [0, 1] * 3 + [0] * 34, [300, 5, 0, 3, 70, 30] + [200] * 40),   # as many tokens as entries at most, unevenly
+    ([0] * 29 + [30], [9] * 29 + [10]),                                       # rows of the first tokens see nothing
+    ([40] + [0] * 60, [35] + [1] * 60),
+    ([33] + [0] * 40, [1500] + [0] * 40),
+])
+def test_no_more_tokens_than_entries(queries, lens, group):
+    assert sum(queries) <= len(queries)
+    c = Case(lens, queries, group=group, dim=128 if group == 4 else 72, seed=group)
+    c.check(*c.run())
+
+
+def test_plans_that_are_gone_leave_their_room_to_the_next():
+    a, b = Case([900, 40], [1, 1], seed=1), Case([300] * 30, [3] * 30, seed=2)
+    for c in (a, b, a, b):
+        for _ in range(3):
+            c.check(*c.run())
+    torch = a.torch
+    want = a.run()
+    plan = a.kv.plan(a.seqs, a.cu, a.n_q, heads=a.q.shape[1])
+    other = a.kv.plan(a.seqs, a.cu, a.n_q, heads=a.q.shape[1])
+    assert plan._buffer.data_ptr() != other._buffer.data_ptr()
+    assert torch.equal(a.kv.attend(a.q, plan)[0], want[0]) and torch.equal(a.kv.attend(a.q, other)[0], want[0])
+    room = other._buffer.data_ptr()
+    del other
+    third = a.kv.plan(a.seqs, a.cu, a.n_q, heads=a.q.shape[1])
+    assert third._buffer.data_ptr() == room != plan._buffer.data_ptr()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):  # read on another stream: not the next one's
+        out = a.kv.attend(a.q, third)[0]
+    torch.cuda.current_stream().wait_stream(side)
+    del third
+    assert a.kv._spare == [] and torch.equal(out, want[0])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured = a.kv.attend(a.q, plan)
+        own = a.run()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(own[0], want[0]) and torch.equal(captured[0], want[0])
+    del plan  # the graph may be replayed: its plan's room is no other's
+    assert a.kv._spare == []
+    a.kv.check()
+
+
 def test_rows_that_see_nothing():
     """More queries than tokens, and sequences without any: zeros and -infinity."""
     for lens, queries in (([0, 3, 0], [2, 5, 1]), ([0], [1]), ([2], [300])):
