@@ -9,12 +9,13 @@
 //                40 entries, 11 us for 250 entries and 16000 new pages, most of it chains of loads from L2.
 //   k_move     - puts the pages into the tables, and makes the slots of the new tokens and the copies that k_extend
 //                listed, whole pages of all layers.  Every byte read once and written once, 16 bytes a load, eight in
-//                flight a thread, past L1: 84 us for 0.53 GB moved, 6.3 TB/s.
+//                flight a thread, past L1 and L2: 80 us for 0.53 GB moved, 6.6 TB/s.
 //   k_free, k_fork - a warp for each entry; `ref` changes by atomics whose order does not matter.  7 and 6 us for 256 entries.
 //   k_compact  - one block: with N pages in use, the i-th used page at or above N goes to the i-th free one below N.  6 us for
-//                4600 pages; k_compact_move makes the copies, 84 us for 0.52 GB, 6.1 TB/s.
-//   k_write    - a thread for each 16 bytes of a token's keys and of its values, both loads before both stores: 312 us for
-//                2.02 GB, 6.5 TB/s.  Sources that are not 16-byte aligned are read 2 bytes at a time, as they must be.
+//                4600 pages; k_compact_move makes the copies, 78 us for 0.52 GB, 6.6 TB/s.
+//   k_write    - a thread for each 16 bytes of a token's keys and of its values, both loads before both stores, no thread with
+//                more than one of each and stores that L2 need not keep: 286 us for 2.02 GB, 7.1 TB/s (312 us with 16 blocks
+//                per SM that stay).  Sources that are not 16-byte aligned are read 2 bytes at a time, as they must be.
 #include <algorithm>
 #include <climits>
 
@@ -30,6 +31,9 @@ constexpr int kMeta = 1024;   // threads of the one-block kernels
 constexpr int kMove = 256;    // threads of the moving kernels
 constexpr int kUnroll = 8;    // 16-byte loads in flight per thread
 constexpr int kChunk = kMove * kUnroll * 16;
+// Blocks per SM of the moving kernels, many more than fit: blocks that come as others end keep HBM busier than as many as fit,
+// each with its share (0.53 GB in all: 101 us with 4, 96 with 8, 93 with 32).
+constexpr int kMoveWaves = 32;
 // Sums over the entries of a call: pages in the low bits (at most n_pages + 1 <= 2^28 + 1 counted for an entry, 2^17
 // entries), copies of shared pages above.
 constexpr int kCowShift = 46;
@@ -461,8 +465,8 @@ __global__ void __launch_bounds__(kMove) k_write(const sim_kv kv, const KvWrite 
             x = make_uint4(xs[0], xs[1], xs[2], xs[3]);
             y = make_uint4(ys[0], ys[1], ys[2], ys[3]);
         }
-        *reinterpret_cast<uint4 *>(to) = x;
-        *reinterpret_cast<uint4 *>(to + values) = y;
+        __stcs(reinterpret_cast<uint4 *>(to), x);
+        __stcs(reinterpret_cast<uint4 *>(to + values), y);
     }
 }
 
@@ -491,14 +495,14 @@ cudaError_t launch_kv_extend(const sim_kv &kv, int32_t n, const int32_t *seqs, c
     if (e != cudaSuccess) return e;
     // at most one page copied for each entry
     const int64_t chunks = (kv_page_bytes(kv) + kChunk - 1) / kChunk * n;
-    const int blocks = std::max(blocks_for(chunks, 1, 4), blocks_for(n_new, kMove, 8));
+    const int blocks = std::max(blocks_for(chunks, 1, kMoveWaves), blocks_for(n_new, kMove, 8));
     return launch_chained(k_move, blocks, kMove, 0, st, kv, n, seqs, cu_new, n_new, slots);
 }
 
 cudaError_t launch_kv_copy(const sim_kv &kv, int32_t n, const int32_t *src, const int32_t *dst, cudaStream_t st) {
     cudaError_t e = launch_chained(k_extend<true>, 1, kMeta, set_bytes(kv), st, kv, n, dst, static_cast<const int32_t *>(nullptr), 0, src);
     if (e != cudaSuccess) return e;
-    return launch_chained(k_move, kv_sm_count() * 4, kMove, 0, st, kv, n, dst, static_cast<const int32_t *>(nullptr), 0, static_cast<int64_t *>(nullptr));
+    return launch_chained(k_move, kv_sm_count() * kMoveWaves, kMove, 0, st, kv, n, dst, static_cast<const int32_t *>(nullptr), 0, static_cast<int64_t *>(nullptr));
 }
 
 cudaError_t launch_kv_fork(const sim_kv &kv, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *tokens, cudaStream_t st) {
@@ -512,14 +516,14 @@ cudaError_t launch_kv_free(const sim_kv &kv, int32_t n, const int32_t *seqs, con
 cudaError_t launch_kv_compact(const sim_kv &kv, int32_t *to, cudaStream_t st) {
     cudaError_t e = launch_chained(k_compact, 1, kMeta, 0, st, kv, to);
     if (e != cudaSuccess) return e;
-    return launch_chained(k_compact_move, kv_sm_count() * 4, kMove, 0, st, kv, static_cast<const int32_t *>(to));
+    return launch_chained(k_compact_move, kv_sm_count() * kMoveWaves, kMove, 0, st, kv, static_cast<const int32_t *>(to));
 }
 
 cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st) {
     const int per_head = kv.head_dim / 8, per_token = per_head * kv.n_kv_heads;
     const auto aligned = [](const void *p, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && a % 8 == 0 && b % 8 == 0; };
     const bool vec = aligned(w.k, w.kt, w.kh) && aligned(w.v, w.vt, w.vh);
-    const int blocks = blocks_for(int64_t(w.n_new) * per_token, kMove, 16);
+    const int blocks = blocks_for(int64_t(w.n_new) * per_token, kMove, 4096);
     return launch_chained(vec ? k_write<true> : k_write<false>, blocks, kMove, 0, st, kv, w, FastDiv(per_token), FastDiv(per_head));
 }
 
