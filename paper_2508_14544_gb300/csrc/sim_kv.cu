@@ -14,8 +14,8 @@
 //   k_compact  - one block: with N pages in use, the i-th used page at or above N goes to the i-th free one below N.  6 us for
 //                4600 pages; k_compact_move makes the copies, 78 us for 0.52 GB, 6.6 TB/s.
 //   k_write    - a thread for each 16 bytes of a token's keys and of its values, both loads before both stores, no thread with
-//                more than one of each and stores that L2 need not keep: 286 us for 2.02 GB, 7.1 TB/s (312 us with 16 blocks
-//                per SM that stay).  Sources that are not 16-byte aligned are read 2 bytes at a time, as they must be.
+//                more than one of each and stores that L2 need not keep: 286 us for 2.02 GB, 7.1 TB/s, the last writes still in
+//                L2 (312 us with 16 blocks per SM that stay).  Sources that are not 16-byte aligned are read 2 bytes at a time, as they must be.
 #include <algorithm>
 #include <climits>
 

@@ -11,8 +11,9 @@
 // behind the row's maximum by a factor of 2^kGrow before O is rescaled, which float16 holds with room to spare.
 //
 // 16 prompts' own 300 - 512 tokens on 4096 + 600 keys each, 64 heads, D = 128: 464 us, 1.66 PFLOP/s, 86 % of cuBLAS's
-// burst rate.  A tile takes both groups about 2600 cycles of the 2048 of its products: what is left is the way from a product
-// through the softmax to the next one.  The first half of P is multiplied while the second is made (602 -> 591 us for the whole
+// burst rate.  A tile takes both groups about 2600 cycles, its products alone 2048.  In these, operands and loads ask shared
+// memory for 256 KB (S 128, P V 64, the tile's arrival 64), which at 128 bytes a cycle is all that it can give; the rest is the
+// way from a product through the softmax to the next one.  The first half of P is multiplied while the second is made (602 -> 591 us for the whole
 // call); split three to one it is slower (447 -> 477 us).
 #include "sim_kv_attend.cuh"
 
