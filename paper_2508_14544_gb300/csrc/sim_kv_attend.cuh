@@ -274,55 +274,90 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_
     return uint64_t((addr >> 4) & 0x3fff) | uint64_t(lbo >> 4) << 16 | uint64_t(sbo >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 
+// A row meets the values of a tile's keys that it does not see with probability 0, which is not nothing where they are infinite
+// or not a number.  In tiles that some rows do not see whole (Sink::blind_from), each key's values (`row`, and `half` bytes on
+// the next 64 columns) are looked at before the product, one fused multiply-add for two, and those that are not finite become
+// zeros; Sink::spoil gives the rows that do see them their due.  True if the key has such values.  An item of 256 rows has three
+// of these tiles at most, a single token none.
+constexpr int kBlindTiles = 3;
+template <int DP, bool BF>
+__device__ __forceinline__ bool clean_row(unsigned char *row, int half) {
+    const int turn = threadIdx.x & 7;  // 8 lanes, 8 places of 16 bytes: no bank conflicts
+    uint32_t sum[4] = {};              // of 0 times the values: not 0 if one is not finite
+    const auto fma0 = [](uint32_t x, uint32_t &y) {
+        if (BF) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(y) : "r"(x), "r"(0));
+        else asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(y) : "r"(x), "r"(0));
+    };
+#pragma unroll
+    for (int z = 0; z < DP / 8; ++z) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(row + z / 8 * half + (z % 8 ^ turn) * 16);
+        fma0(v.x, sum[0]);
+        fma0(v.y, sum[1]);
+        fma0(v.z, sum[2]);
+        fma0(v.w, sum[3]);
+    }
+    if (!((sum[0] | sum[1] | sum[2] | sum[3]) & 0x7fff7fffu)) return false;
+    constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
+#pragma unroll 1
+    for (int z = 0; z < DP / 2; ++z) {
+        uint32_t *const at = reinterpret_cast<uint32_t *>(row + z / 32 * half) + z % 32;
+        uint32_t w = *at;
+        if ((w & kExp) == kExp) w &= 0xffff0000u;
+        if ((w >> 16 & kExp) == kExp) w &= 0xffffu;
+        *at = w;
+    }
+    return true;
+}
+
 // Where the results of a segment go.
 template <bool BF>
 struct Sink {
     const sim_kv &kv;
     const KvAttend &a;
     const Segment &sg;
-    int G, D, q_heads, end;  // end: of the keys of the segment's tiles
-    // First key of the segment that row y does not see, and whether its tiles have such keys.
+    int G, D, q_heads;
+    // First key of the segment that row y does not see.
     __device__ int seen(int y) const { return min(sg.kv1, sg.pos0 + int(a.group.div(sg.row0 + y)) + 1); }
-    __device__ bool blind(int y) const { return seen(y) < min(end, sg.kv1); }
-    // A row that does not see all of its tiles' keys has met the values of the others with probability 0, which is not nothing
-    // where they are infinite or not a number.  Where its result is not finite it is computed again here from the keys that it
-    // sees: one warp, a key at a time, a lane for four columns.
-    __device__ void again(int y) const {
-        const int lane = threadIdx.x & 31, P = kv.page_size, d = 4 * lane;
-        const bool in = d < D;
-        const auto wide = [](uint32_t w) {
-            if constexpr (BF) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-            else return make_float2(__half2float(__ushort_as_half(uint16_t(w))), __half2float(__ushort_as_half(uint16_t(w >> 16))));
-        };
-        const int t = a.group.div(sg.row0 + y);
-        const uint16_t *q = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0 + t) * a.qt + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.qh;
-        const float2 q0 = in ? wide(q[d] | uint32_t(q[d + 1]) << 16) : make_float2(0.f, 0.f), q1 = in ? wide(q[d + 2] | uint32_t(q[d + 3]) << 16) : make_float2(0.f, 0.f);
-        const uint16_t *layer = static_cast<const uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv);
-        float m = -INFINITY, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    // The first tile that row 0, which sees the fewest keys, does not see as far as the item's keys go; sg.n: none.
+    __device__ int blind_from() const {
+        const int none = seen(0);
+        return none < min(sg.kv1, sg.k0 + sg.n * kTileKeys) ? max(none - sg.k0, 0) / kTileKeys : sg.n;
+    }
+    // The first tile whose values are looked at before the product: a blind one, or one past the end of the keys; sg.n: none.
+    __device__ int clean_from() const { return min(blind_from(), sg.kv1 - (sg.k0 + (sg.n - 1) * kTileKeys) < kTileKeys ? sg.n - 1 : sg.n); }
+    // A row that sees values which clean_row took for zeros: its result in their columns is what they alone add up to, infinite
+    // or not a number.  bad: a bit for each key of the tiles from blind_from on.  By one warp, a lane for four columns.
+    __device__ void spoil(int y, const uint32_t *bad) const {
+        const int lane = threadIdx.x & 31, P = kv.page_size, d = 4 * lane, from = blind_from(), stop = seen(y);
+        const uint16_t *values = static_cast<const uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + kv_layer_elems(kv) / 2;
+        float o[4] = {};
 #pragma unroll 1
-        for (int key = sg.k0; key < min(seen(y), end); ++key) {
-            const int page = kv.table[int64_t(sg.seq) * kv.max_pages + key / P];
-            uint2 k = make_uint2(0, 0), v = k;
-            if (in && unsigned(page) < unsigned(kv.n_pages)) {
-                const uint16_t *at = layer + page * (kv_page_bytes(kv) / 2) + (int64_t(sg.h) * P + key % P) * D + d;
-                k = *reinterpret_cast<const uint2 *>(at);
-                v = *reinterpret_cast<const uint2 *>(at + kv_layer_elems(kv) / 2);
+        for (int z = 0; z < 4 * (sg.n - from); ++z) {
+            const int key = sg.k0 + from * kTileKeys + z * 32 + lane;
+            int64_t at = -1;
+            if ((bad[z] >> lane & 1) && key < stop) {
+                const int page = kv.table[int64_t(sg.seq) * kv.max_pages + key / P];
+                if (unsigned(page) < unsigned(kv.n_pages)) at = page * (kv_page_bytes(kv) / 2) + (int64_t(sg.h) * P + key % P) * D;
             }
-            const float2 k0 = wide(k.x), k1 = wide(k.y), v0 = wide(v.x), v1 = wide(v.y);
-            float s = q0.x * k0.x + q0.y * k0.y + q1.x * k1.x + q1.y * k1.y;
+            if (!__any_sync(FULL, at >= 0)) continue;
+#pragma unroll 4
+            for (int k = 0; k < 32; ++k) {
+                const int64_t ak = __shfl_sync(FULL, at, k);
+                const uint2 v = ak >= 0 && d < D ? *reinterpret_cast<const uint2 *>(values + ak + d) : make_uint2(0, 0);
 #pragma unroll
-            for (int i = 16; i >= 1; i >>= 1) s += __shfl_xor_sync(FULL, s, i);
-            const float up = fmaxf(m, s * a.scale_log2), f = m == -INFINITY ? 0.f : ex2(m - up), p = ex2(s * a.scale_log2 - up);
-            m = up;
-            l = l * f + p;
-            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-            if (p != 0.f) o = make_float4(fmaf(p, v0.x, o.x), fmaf(p, v0.y, o.y), fmaf(p, v1.x, o.z), fmaf(p, v1.y, o.w));
+                for (int i = 0; i < 4; ++i) {
+                    const uint16_t bits = uint16_t((i < 2 ? v.x : v.y) >> i % 2 * 16);
+                    const float x = BF ? __uint_as_float(uint32_t(bits) << 16) : __half2float(__ushort_as_half(bits));
+                    if (x * 0.f != 0.f) o[i] += x;
+                }
+            }
         }
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        if (!in) return;
-        if (sg.direct) *reinterpret_cast<uint2 *>(out_row(y) + d) = make_uint2(pack<BF>(o.x * f, o.y * f), pack<BF>(o.z * f, o.w * f));
-        else *reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (o[i] == 0.f) continue;
+            if (sg.direct) out_row(y)[d + i] = uint16_t(pack<BF>(o[i], o[i]));
+            else a.part[(sg.row + y) * D + d + i] = o[i];
+        }
     }
     __device__ uint16_t *out_row(int y) const {  // of row y of the item
         const int t = a.group.div(sg.row0 + y);

@@ -37,7 +37,6 @@ __device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, u
         to[q] = (sg.direct ? reinterpret_cast<char *>(sink.out_row(y)) : reinterpret_cast<char *>(sink.a.part + (sg.row + y) * sink.D)) + lane % 4 * 16;
     }
     const int cols = sg.direct ? 32 : 16;
-    float finite = 0.f;  // 0 times every result: not 0 if one is not finite
 #pragma unroll 1
     for (int d0 = 0; d0 < sink.D; d0 += cols) {
         uint32_t x[16];
@@ -46,19 +45,12 @@ __device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, u
             tm_ld32(t_o + d0, o);
             tc_wait_ld();
 #pragma unroll
-            for (int y = 0; y < 16; ++y) {
-                finite = fmaf(__uint_as_float(o[2 * y]), 0.f, finite);
-                finite = fmaf(__uint_as_float(o[2 * y + 1]), 0.f, finite);
-                x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
-            }
+            for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
         } else {
             tm_ld16(t_o + d0, x);
             tc_wait_ld();
 #pragma unroll
-            for (int y = 0; y < 16; ++y) {
-                finite = fmaf(__uint_as_float(x[y]), 0.f, finite);
-                x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
-            }
+            for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
         }
 #pragma unroll
         for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4 *>(mine + lane * kPitch + y) = make_uint4(x[y], x[y + 1], x[y + 2], x[y + 3]);
@@ -72,12 +64,6 @@ __device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, u
             to[q] += 64;
         }
         __syncwarp();
-    }
-    const int row = row0 + lane;
-    unsigned redo = __ballot_sync(FULL, row < rows && finite != 0.f && !empty && sink.blind(row));
-    while (redo) {
-        sink.again(row0 + __ffs(redo) - 1);
-        redo &= redo - 1;
     }
 }
 
@@ -95,8 +81,11 @@ struct Shape {
     static constexpr int kOffRing = kGroups * kTile;
     static constexpr int kOffStage = kOffRing + kSlots * kTile;
     static constexpr int kOffSeg = kOffStage + kGroups * kStage * 4;
-    static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
-    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 4 * kGroups + 1;
+    // Keys with values that are not finite, in tiles that not all rows see whole, of segment x at x modulo twice kSegs: the warp
+    // that finds them is less than that ahead of the softmax, without which no segment is told of kSegs later.
+    static constexpr int kOffBad = kOffSeg + kSegs * int(sizeof(Segment));
+    static constexpr int kOffBar = kOffBad + 2 * kSegs * kBlindTiles * 16;
+    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 4 * kGroups + 1 + kSlots;
     static constexpr int kBytes = kOffBar + kBars * 8 + 16;
     static constexpr int kAlloc = kBytes + 1024;                              // the base is rounded up to 1024
     static_assert(kAlloc <= 232448, "shared memory");
@@ -180,6 +169,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
     const auto o_full = [&](int g) { return bars + 8 * (kRest + 2 + 2 * NG + g); };
     const auto p_half = [&](int g) { return bars + 8 * (kRest + 2 + 3 * NG + g); };
     const uint32_t drained = bars + 8 * (kRest + 2 + 4 * NG);
+    // The x-th tile of values that is looked at is being loaded (only from then on can one wait for it to be there); has been looked
+    // at.  No more than NS / 2 are loaded that are not yet multiplied.
+    const auto look_at = [&](uint32_t x) { return bars + 8 * (kRest + 3 + 4 * NG + x % (NS / 2)); };
+    const auto clean = [&](uint32_t x) { return bars + 8 * (kRest + 3 + 4 * NG + NS / 2 + x % (NS / 2)); };
     const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31, role = warp - 4 * NG;
 
     if (tid == 0) {
@@ -197,9 +190,13 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             bar_init(s_full(g), 1);
             bar_init(p_ready(g), 4);
             bar_init(p_half(g), 4);
-            bar_init(o_full(g), 1);
+            bar_init(o_full(g), 2);
         }
         bar_init(drained, 1);
+        for (int x = 0; x < NS / 2; ++x) {
+            bar_init(look_at(x), 1);
+            bar_init(clean(x), 2);
+        }
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -236,7 +233,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             const KvPlan plan = kv_plan(kv, b);
             Line line(plan, kv.n_kv_heads, 0, blockIdx.x, a.sms);
             const int P = kv.page_size, per = kTileKeys / P;
-            uint32_t at = 0;  // tiles loaded
+            uint32_t at = 0, nc = 0;  // tiles loaded, those looked at
             bool ok = true;
             for (uint32_t x = 0; ok; ++x) {
                 Segment sg;
@@ -248,6 +245,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                     bar_arrive(seg_full(x));
                 }
                 if (sg.n == 0) break;
+                const int clean_from = Sink<BF>{kv, a, sg, G, D, b.q_heads}.clean_from();
                 const int32_t *row = kv.table + int64_t(line.it.seq) * kv.max_pages;
                 const int first = sg.k0 / P + lane;
                 const auto page_of = [&](int j) {  // of this lane in tile j; past the keys: none, zeros
@@ -271,6 +269,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                                 tma_load(dst + half * Sh::kHalf, v ? &maps.values : &maps.keys, full(at), half * 64, 0, sg.h, w);
                         }
                     }
+                    if (ok && j >= clean_from) {
+                        if (lane == 0) bar_arrive(look_at(nc));
+                        ++nc;
+                    }
                     page = next_page;
                 }
             }
@@ -286,7 +288,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             const uint32_t idesc_s = 1u << 4 | type | (128 / 8) << 17 | (128 / 16) << 24;
             const uint32_t idesc_o = 1u << 4 | type | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
             const uint64_t op_q = operand(sbase, 16, 1024), op_k = operand(sbase + Sh::kOffRing, 16, 1024), op_v = operand(sbase + Sh::kOffRing, Sh::kHalf, 1024);
-            uint32_t at = 0, np[NG] = {};
+            uint32_t at = 0, nc = 0, np[NG] = {};
             bool ok = true;
             const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, bar_wait(bar, parity, gave_up)) != 0; };
             const auto wait_full = [&](uint32_t y) { return wait(full(y), (y / NS) & 1); };
@@ -294,6 +296,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             for (uint32_t x = 0; (ok = take(x, sg)); ++x) {
                 const int n = __shfl_sync(FULL, sg.n, 0), last = __shfl_sync(FULL, sg.rows, 0) > 128;  // group with rows
                 if (n == 0) break;
+                const int clean_from = __shfl_sync(FULL, Sink<BF>{kv, a, sg, G, D, b.q_heads}.clean_from(), 0);
                 const auto keys = [&](int j, int g) {  // S of group g and tile j
                     if (elect_one()) {
                         const uint32_t slot = (at + 2 * j) % NS;
@@ -318,6 +321,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                     if (g <= last) keys(0, g);
                 for (int j = 0; j < n && ok; ++j) {
                     ok = wait_full(at + 2 * j + 1);
+                    if (ok && j >= clean_from) ok = wait(clean(nc), nc / (NS / 2) & 1), ++nc;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
                         if (g > last) break;
@@ -330,7 +334,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                                     mma_ts(tmem + Sh::kOffO + g * 128, tmem + g * 128 + (from + kk) * 8, op_v + ((slot * Sh::kTile + (from + kk) * 2048) >> 4), idesc_o, j > 0 || from + kk > 0);
                                 if (from > 0) {
                                     if (g == last) tc_commit(empty(at + 2 * j + 1));
-                                    if (j + 1 == n) tc_commit(o_full(g));
+                                    if (j + 1 == n) {
+                                        tc_commit(o_full(g));
+                                        bar_arrive(o_full(g));  // what the look at the values has found is in shared memory
+                                    }
                                 }
                             }
                             __syncwarp();
@@ -365,11 +372,40 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             // ---- query rows, by TMA where heads and tokens make boxes of 128 rows (rows of other entries, past the item's,
             // come with them); else two warps, 16 bytes a lane, the lanes of a row side by side (all that prefill 527 instead of
             // 509 us).  What rows past the item's hold meets no other row and is not used.
+            // They then look at the values of the item's last tiles, before they are multiplied: those past the end of
+            // the keys, whatever they are, must not meet their zero probabilities, nor those that are not finite the rows that do not
+            // see them.
             constexpr int kVec = DP / 8, kStep = 64 / kVec;
             const int j = (tid & 63) % kVec;
             const bool has = j * 8 < D;
+            const auto look = [&](const Segment &s, uint32_t x, uint32_t at, uint32_t &nc) {
+                const Sink<BF> sink = {kv, a, s, G, D, b.q_heads};
+                const int blind_from = sink.blind_from();
+                uint32_t *const bad = reinterpret_cast<uint32_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 4;
+                for (int t = sink.clean_from(); t < s.n; ++t, ++nc) {
+                    const uint32_t y = at + 2 * t + 1;
+                    if (!__all_sync(FULL, bar_wait(look_at(nc), nc / (NS / 2) & 1, gave_up) && bar_wait(full(y), (y / NS) & 1, gave_up))) return false;
+#pragma unroll 1
+                    for (int r = (role - 2) * 64 + lane; r < (role - 1) * 64; r += 32) {
+                        unsigned char *const v = base + Sh::kOffRing + (y % NS) * Sh::kTile + r * 128;
+                        bool found = false;
+                        if (r >= s.kv1 - s.k0 - t * kTileKeys) {
+#pragma unroll
+                            for (int z = 0; z < DP / 8; ++z) *reinterpret_cast<uint4 *>(v + (z / 8) * Sh::kHalf + (z % 8) * 16) = make_uint4(0, 0, 0, 0);
+                        } else if (t >= blind_from) {
+                            found = clean_row<DP, BF>(v, Sh::kHalf);
+                        }
+                        const unsigned keys = __ballot_sync(FULL, found);
+                        if (t >= blind_from && lane == 0) bad[(t - blind_from) * 4 + r / 32] = keys;
+                    }
+                    smem_to_async();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(clean(nc));
+                }
+                return true;
+            };
             Segment sg;
-            uint32_t x = 0;
+            uint32_t x = 0, at = 0, nc = 0;
             for (; take(x, sg) && sg.n > 0; ++x) {
                 if (!__all_sync(FULL, bar_wait(q_empty, (x + 1) & 1, gave_up))) break;
                 if (maps.q_boxes) {
@@ -385,6 +421,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                         }
                     }
                     __syncwarp();
+                    if (!look(sg, x, at, nc)) break;
+                    at += 2 * sg.n;
                     continue;
                 }
                 const uint16_t *const from0 = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0) * a.qt + int64_t(sg.h * G) * a.qh + (has ? j * 8 : 0);
@@ -408,6 +446,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 smem_to_async();
                 __syncwarp();
                 if (lane == 0) bar_arrive(q_full);
+                if (!look(sg, x, at, nc)) break;
+                at += 2 * sg.n;
             }
             // after a wait that gave up: the last boxes may be on their way
             if (maps.q_boxes && x > 0)
@@ -421,7 +461,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
         const uint32_t t_lane = tmem + (uint32_t(w * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + Sh::kOffO + g * 128;
         uint32_t *const stage = reinterpret_cast<uint32_t *>(base + Sh::kOffStage) + g * kStage;
         const float c = a.scale_log2;
-        uint32_t ns = 0, no = 0, at = 0;
+        uint32_t ns = 0, no = 0;
         bool ok = true;
         Segment sg;
         for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
@@ -429,6 +469,9 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             const int r = g * 128 + lr;  // the row in this thread's lane
             // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
             const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : sg.kv1 - 1;
+            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
+            const int blind_from = sink.blind_from();
+            const uint32_t *const bad = reinterpret_cast<const uint32_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 4;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
                 const int k0 = sg.k0 + j * kTileKeys;  // first key of the tile
@@ -436,18 +479,6 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (!ok) break;
                 ++ns;
                 tc_fence_after();
-                // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                const int valid = sg.kv1 - k0;
-                if (valid < kTileKeys && g == 0) {
-                    const uint32_t y = at + 2 * j + 1;
-                    ok = __all_sync(FULL, bar_wait(full(y), (y / NS) & 1, gave_up));
-                    if (lr >= valid) {
-                        unsigned char *v = base + Sh::kOffRing + (y % NS) * Sh::kTile + lr * 128;
-#pragma unroll
-                        for (int z = 0; z < DP / 8; ++z) *reinterpret_cast<uint4 *>(v + (z / 8) * Sh::kHalf + (z % 8) * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    smem_to_async();
-                }
                 softmax_tile<DP, BF>(t_s, t_o, last - k0, j == 0, c, m, l, [&] {
                     tc_fence_before();
                     __syncwarp();
@@ -458,13 +489,16 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (lane == 0) bar_arrive(p_ready(g));
             }
             if (!ok) break;
-            at += 2 * sg.n;
-            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + sg.n * kTileKeys};
             if (r < sg.rows) sink.lse(r, m * c, l);
             ok = __all_sync(FULL, bar_wait(o_full(g), no++ & 1, gave_up));
             if (!ok) break;
             tc_fence_after();
             store_rows<DP>(sink, t_o, stage + w * 32 * kPitch, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+            uint32_t some = 0;
+#pragma unroll 1
+            for (int z = 0; z < 4 * (sg.n - blind_from); ++z) some |= bad[z];
+            if (some)
+                for (int y = r - lane; y < min(r - lane + 32, sg.rows); ++y) sink.spoil(y, bad);
             tc_fence_before();
         }
     }

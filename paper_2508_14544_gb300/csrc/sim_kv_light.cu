@@ -30,8 +30,8 @@ struct Shape {
     static constexpr int kOffQ = kSlots * kSlot;
     static constexpr int kOffRed = kOffQ + kHalves * kRowsHalf;  // [2][row][warp]
     static constexpr int kOffVote = kOffRed + 2 * kLightRows * 16;
-    static constexpr int kOffAgain = kOffVote + 2 * 16;  // rows whose results are not finite
-    static constexpr int kOffSeg = kOffAgain + kLightRows * 4;
+    static constexpr int kOffBad = kOffVote + 2 * 16;  // keys with values that are not finite, in tiles that not all rows see whole
+    static constexpr int kOffSeg = kOffBad + kBlindTiles * 16;
     static constexpr int kOffBar = kOffSeg + kSegs * int(sizeof(Segment));
     static constexpr int kBars = 2 * kSlots + 2 * kSegs + 6;
     static constexpr int kBytes = kOffBar + kBars * 8 + 16;
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
         bar_init(q_full, 4);
         bar_init(s_full, 1);
         bar_init(p_ready, 4);
-        bar_init(o_full, 1);
+        bar_init(o_full, 2);
         bar_init(drained, 1);
         bar_init(joined, 4);
         *gave_up = 0;
@@ -216,7 +216,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                     tc_commit(empty(at));
 #pragma unroll
                     for (int y = HF; y < 2 * HF; ++y) tc_commit(empty(at + y));
-                    if (j + 1 == n) tc_commit(o_full);
+                    if (j + 1 == n) {
+                        tc_commit(o_full);
+                        bar_arrive(o_full);  // what the warps have told each other in shared memory is there as well
+                    }
                 }
                 __syncwarp();
             }
@@ -238,7 +241,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
         const uint32_t t_s = tmem + (uint32_t(w * 32) << 16), t_o = t_s + Sh::kColO;
         float *const red = reinterpret_cast<float *>(base + Sh::kOffRed);
         int *const vote = reinterpret_cast<int *>(base + Sh::kOffVote);
-        int *const again = reinterpret_cast<int *>(base + Sh::kOffAgain);
+        uint32_t *const bad = reinterpret_cast<uint32_t *>(base + Sh::kOffBad);
         const float c = a.scale_log2;
         uint32_t ns = 0, nj = 0, nr = 0, nv = 0, at = 0;
         bool ok = true;
@@ -331,6 +334,8 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                 const float4 v = *reinterpret_cast<const float4 *>(to + lane * 4);
                 return SUM ? (v.x + v.y) + (v.z + v.w) : fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
             };
+            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
+            const int blind_from = sink.blind_from();
             float m = -INFINITY;  // of row `lane`: log2, times c
 #pragma unroll 1
             for (int j = 0; j < n; ++j, k0 += NK, at += 2 * HF) {
@@ -407,18 +412,24 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                         *reinterpret_cast<uint16_t *>(p + (r0 + i + 1) * 128 + ((lr % 64 / 8 ^ (i + 1)) << 4)) = uint16_t(both >> 16);
                     }
                 }
-                // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                if (kv1 - k0 < NK) {
+                // values past the end of the keys, whatever they are, must not meet their zero probabilities, nor those that are
+                // not finite the rows that do not see them
+                if (kv1 - k0 < NK || j >= blind_from) {
 #pragma unroll
-                    for (int y = HF; y < 2 * HF; ++y) {
-                        ok = __all_sync(FULL, bar_wait(full(at + y), ((at + y) / NS) & 1, gave_up)) && ok;
-                        if (lr >= kv1 - k0) {
-                            uint4 *const v = reinterpret_cast<uint4 *>(base + ((at + y) % NS) * Sh::kSlot + lr * 128);
-#pragma unroll
-                            for (int z = 0; z < 8; ++z) v[z] = make_uint4(0, 0, 0, 0);
-                        }
-                    }
+                    for (int y = HF; y < 2 * HF; ++y) ok = __all_sync(FULL, bar_wait(full(at + y), ((at + y) / NS) & 1, gave_up)) && ok;
                     if (!ok) break;
+                    unsigned char *const v = base + ((at + HF) % NS) * Sh::kSlot + lr * 128;
+                    bool found = false;
+                    if (lr >= kv1 - k0) {
+#pragma unroll
+                        for (int z = 0; z < DP / 8; ++z) *reinterpret_cast<uint4 *>(v + z / 8 * Sh::kSlot + z % 8 * 16) = make_uint4(0, 0, 0, 0);
+                    } else if (j >= blind_from) {
+                        found = clean_row<DP, BF>(v, Sh::kSlot);
+                    }
+                    if (j >= blind_from) {
+                        const unsigned keys = __ballot_sync(FULL, found);
+                        if (lane == 0) bad[(j - blind_from) * 4 + w] = keys;
+                    }
                 }
                 tc_wait_st();
                 smem_to_async();
@@ -429,8 +440,6 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (!ok) break;
             if (next.n > 0) place(next);  // every product with this item's queries has ended
 
-            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads, sg.k0 + n * NK};
-            if (lr < kLightRows) again[lr] = 0;
             const float total = joined_rows(std::true_type()), inv = total == 0.f ? 0.f : 1.f / total;
             ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
             if (!ok) break;
@@ -450,7 +459,6 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                     if (r0 + i < rows && lr < D) {
                         if (sg.direct) *out = uint16_t(pack<BF>(v, v));
                         else *part = v;
-                        if (v * 0.f != 0.f) again[r0 + i] = 1;
                     }
                     part += D;
                     out += a.oh;
@@ -460,11 +468,13 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                     }
                 }
             }
-            if (sink.blind(0)) {  // see Sink::again
-                join();
+            uint32_t some = 0;
+#pragma unroll 1
+            for (int z = 0; z < 4 * (n - blind_from); ++z) some |= bad[z];
+            if (some) {
+                join();  // after the results
                 if (!ok) break;
-                for (int y = w; y < rows; y += 4)
-                    if (again[y] && sink.blind(y)) sink.again(y);
+                for (int y = w; y < rows; y += 4) sink.spoil(y, bad);
             }
             tc_fence_before();
             give_back(x);
