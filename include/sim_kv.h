@@ -22,8 +22,9 @@
  * negative code until the caller clears it: an entry that is out of range, repeated or refused
  * (SIM_E_INVAL) is left out and the other entries take effect; a sim_kv_extend or sim_kv_copy that needs
  * more free pages than there are (SIM_E_NOMEM), or whose offsets are not in order (SIM_E_INVAL), changes
- * nothing.  Calls on one cache belong on one
- * stream at a time (they share kv->scratch).
+ * nothing.  SIM_E_STATE: a block of sim_kv_attend gave up a wait (nothing moved for a second, which no input should
+ * cause); results that it had not written yet are left as they were.  Calls on one cache belong on one stream at a time
+ * (they share kv->scratch).
  */
 #ifndef SIM_KV_H_
 #define SIM_KV_H_
@@ -136,8 +137,9 @@ int sim_kv_plan(const sim_kv *kv, const sim_kv_batch *b, void *cuda_stream);
  *   lse      DEVICE float [n_q][q_heads], or NULL: log of the sum of the exponentials.
  *   scale    > 0, finite, also times log2(e).
  * A query that sees no key gets zeros, and -infinity for lse.  Cached values past a sequence's length are
- * never used, whatever they are.  Sums and the softmax are in 32 bits; the probabilities are rounded to
- * kv->dtype for the product with the values.
+ * never used, whatever they are, nor are those that a query does not see.  Sums and the softmax are in 32 bits, those
+ * of the products (which cut off what does not fit) over 2^15 keys at most; the probabilities are rounded to kv->dtype for
+ * the product with the values.
  */
 int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const void *q, int64_t q_token_stride,
                   int64_t q_head_stride, float scale, void *out, int64_t out_token_stride, int64_t out_head_stride,

@@ -16,6 +16,11 @@ namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int kSegs = 4;      // segments that the loading warp may be ahead
+// Tiles that a segment has at most; longer stretches of an item are several segments, each of which adds to what the last has left
+// in the workspace.  The tensor products' sums are cut off, not rounded, after every 16 keys: sums of one sign lose 2^-24 of
+// themselves each time, 2^-13 in all over 256 tiles (over 10^6 keys, 0.6 %; the joining is rounded).  It also bounds how long the
+// warps of a block wait for each other.  Taking up a segment costs some 4 tiles.
+constexpr int kMostTiles = 256;
 constexpr float kGrow = 8.f;  // log2 of what P may reach before O is rescaled
 
 // A list's line (the spans of its items, one after the other) divided among its blocks: [at(c), at(c + 1)) is block c's,
@@ -57,8 +62,9 @@ struct alignas(16) Segment {
     int32_t h;
     int32_t q0, row0, rows, pos0;
     int32_t k0, kv1;         // first key, end of the keys
-    int32_t direct;          // results go to the output, not to the workspace
     int32_t seq;             // row of the table
+    bool direct;             // results go to the output, not to the workspace
+    bool joins;              // what the workspace has in that place is part of them
     int64_t row;             // row of the partial results
 };
 
@@ -68,6 +74,7 @@ struct Line {
     KvItem it;
     int64_t u, u1, base;
     int n_items, heads, k, h, c, light;
+    int t, t_end, whole;  // tiles of the item and head that are left, and whether all of them are this block's
     __device__ Line(const KvPlan &p, int heads_, int light_, int c_, int sms) : items(p.items[light_]), heads(heads_), c(c_), light(light_) {
         n_items = p.hdr[16 * light];
         const Share share(p, light);
@@ -76,10 +83,12 @@ struct Line {
         base = list_base(p, light, sms);
         k = p.start[light][c];
         h = -1;
+        t = t_end = whole = 0;
     }
     // The next item and head with work for this block; s.n = 0 at the end.
     __device__ void next(Segment &s) {
         s.n = 0;
+        if (t < t_end) return part(s, true);
         while (u < u1 && k < n_items) {
             if (h < 0) it = items[k];
             const int span = kv_span(it.tiles, light);
@@ -90,22 +99,27 @@ struct Line {
             }
             h = h < 0 ? int(uint32_t(u - it.unit) / uint32_t(span)) : h + 1;
             const int64_t a = it.unit + int64_t(h) * span, tile0 = a + kv_lead(light);
-            const int t0 = int(max(u - tile0, int64_t(0))), t1 = int(min(u1 - tile0, int64_t(it.tiles)));
+            t = int(max(u - tile0, int64_t(0)));
+            t_end = int(min(u1 - tile0, int64_t(it.tiles)));
+            whole = t_end - t == it.tiles && !it.partial;
             u = a + span;
-            if (t0 >= t1) continue;
-            s.n = t1 - t0;
-            s.h = h;
-            s.q0 = it.q0;
-            s.row0 = it.row0;
-            s.rows = it.rows;
-            s.pos0 = it.pos0;
-            s.k0 = it.kv0 + t0 * kTileKeys;
-            s.kv1 = it.kv1;
-            s.seq = it.seq;
-            s.direct = s.n == it.tiles && !it.partial;
-            s.row = piece_row(it, h, c, base, light);
-            return;
+            if (t < t_end) return part(s, false);
         }
+    }
+    __device__ void part(Segment &s, bool joins) {
+        s.n = min(t_end - t, kMostTiles);
+        s.h = h;
+        s.q0 = it.q0;
+        s.row0 = it.row0;
+        s.rows = it.rows;
+        s.pos0 = it.pos0;
+        s.k0 = it.kv0 + t * kTileKeys;
+        s.kv1 = it.kv1;
+        s.seq = it.seq;
+        t += s.n;
+        s.direct = whole && t == t_end;
+        s.joins = joins;
+        s.row = piece_row(it, h, c, base, light);
     }
 };
 
@@ -363,8 +377,21 @@ struct Sink {
         const int t = a.group.div(sg.row0 + y);
         return static_cast<uint16_t *>(a.out) + int64_t(sg.q0 + t) * a.ot + int64_t(sg.h * G + (sg.row0 + y - t * G)) * a.oh;
     }
-    __device__ void lse(int y, float top, float total) const {  // top: log2
-        const float e = total == 0.f ? -INFINITY : top + log2f(total);
+    // What row y's result over this segment, before the division by `total`, and the one in the workspace are multiplied by to
+    // make up the joint one; log2 of the joint sum of exponentials, where `top` is log2 of what `total` is in units of.
+    struct Joint {
+        float mine, before, e;
+    };
+    __device__ float before(int y) const { return sg.joins ? a.part_lse[sg.row + y] : -INFINITY; }  // log2 of the sum so far
+    __device__ Joint joint(float top, float total, float before) const {
+        Joint x = {total == 0.f ? 0.f : 1.f / total, 0.f, total == 0.f ? -INFINITY : top + log2f(total)};
+        if (before != -INFINITY) {
+            const float up = fmaxf(x.e, before), mine = x.e == -INFINITY ? 0.f : ex2(x.e - up), old = ex2(before - up), f = 1.f / (mine + old);
+            x = {x.mine * mine * f, old * f, up + log2f(mine + old)};
+        }
+        return x;
+    }
+    __device__ void lse(int y, float e) const {  // log2
         if (!sg.direct) {
             a.part_lse[sg.row + y] = e;
         } else if (a.lse) {

@@ -15,6 +15,8 @@
 // memory for 256 KB (S 128, P V 64, the tile's arrival 64), which at 128 bytes a cycle is all that it can give; the rest is the
 // way from a product through the softmax to the next one.  The first half of P is multiplied while the second is made (602 -> 591 us for the whole
 // call); split three to one it is slower (447 -> 477 us).
+#include <type_traits>
+
 #include "sim_kv_attend.cuh"
 
 namespace simgb {
@@ -25,9 +27,9 @@ constexpr int kPitch = 20;            // words between rows on the stage, 16 of 
 constexpr int kStage = 128 * kPitch;  // words through which the results of 128 rows pass
 
 // The results of a warp's 32 rows from row0 on, 16 words of each at a time through `mine` (32 x kPitch words), so that stores
-// fill sectors; f is what the lane's row is multiplied by, empty: it has seen no key.
+// fill sectors; what the lane's row is multiplied by, and what it has in the workspace (Sink::joint).
 template <int DP, bool BF>
-__device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, uint32_t *mine, int row0, int rows, float f, bool empty) {
+__device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, uint32_t *mine, int row0, int rows, float f, float fb) {
     const Segment &sg = sink.sg;
     const int lane = threadIdx.x & 31;
     char *to[4];  // this lane's 16 bytes of four rows
@@ -37,6 +39,18 @@ __device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, u
         to[q] = (sg.direct ? reinterpret_cast<char *>(sink.out_row(y)) : reinterpret_cast<char *>(sink.a.part + (sg.row + y) * sink.D)) + lane % 4 * 16;
     }
     const int cols = sg.direct ? 32 : 16;
+    const float *const old = sink.a.part + (sg.row + min(row0 + lane, rows - 1)) * sink.D;
+    const auto add = [&](uint32_t *o, auto n, int d0) {
+#pragma unroll
+        for (int y = 0; y < decltype(n)::value; y += 4) {
+            if (fb == 0.f || d0 + y >= sink.D) continue;
+            const float4 v = *reinterpret_cast<const float4 *>(old + d0 + y);
+            o[y] = __float_as_uint(fmaf(v.x, fb, __uint_as_float(o[y])));
+            o[y + 1] = __float_as_uint(fmaf(v.y, fb, __uint_as_float(o[y + 1])));
+            o[y + 2] = __float_as_uint(fmaf(v.z, fb, __uint_as_float(o[y + 2])));
+            o[y + 3] = __float_as_uint(fmaf(v.w, fb, __uint_as_float(o[y + 3])));
+        }
+    };
 #pragma unroll 1
     for (int d0 = 0; d0 < sink.D; d0 += cols) {
         uint32_t x[16];
@@ -45,12 +59,16 @@ __device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, u
             tm_ld32(t_o + d0, o);
             tc_wait_ld();
 #pragma unroll
-            for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : pack<BF>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
+            for (int y = 0; y < 32; ++y) o[y] = f == 0.f ? 0 : __float_as_uint(__uint_as_float(o[y]) * f);
+            if (sg.joins) add(o, std::integral_constant<int, 32>(), d0);
+#pragma unroll
+            for (int y = 0; y < 16; ++y) x[y] = pack<BF>(__uint_as_float(o[2 * y]), __uint_as_float(o[2 * y + 1]));
         } else {
             tm_ld16(t_o + d0, x);
             tc_wait_ld();
 #pragma unroll
-            for (int y = 0; y < 16; ++y) x[y] = empty ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
+            for (int y = 0; y < 16; ++y) x[y] = f == 0.f ? 0 : __float_as_uint(__uint_as_float(x[y]) * f);
+            if (sg.joins) add(x, std::integral_constant<int, 16>(), d0);
         }
 #pragma unroll
         for (int y = 0; y < 16; y += 4) *reinterpret_cast<uint4 *>(mine + lane * kPitch + y) = make_uint4(x[y], x[y + 1], x[y + 2], x[y + 3]);
@@ -246,7 +264,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 }
                 if (sg.n == 0) break;
                 const int clean_from = Sink<BF>{kv, a, sg, G, D, b.q_heads}.clean_from();
-                const int32_t *row = kv.table + int64_t(line.it.seq) * kv.max_pages;
+                const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
                 const int first = sg.k0 / P + lane;
                 const auto page_of = [&](int j) {  // of this lane in tile j; past the keys: none, zeros
                     const int idx = first + j * per;
@@ -489,11 +507,12 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (lane == 0) bar_arrive(p_ready(g));
             }
             if (!ok) break;
-            if (r < sg.rows) sink.lse(r, m * c, l);
+            const typename Sink<BF>::Joint joint = sink.joint(m * c, l, r < sg.rows ? sink.before(r) : -INFINITY);
+            if (r < sg.rows) sink.lse(r, joint.e);
             ok = __all_sync(FULL, bar_wait(o_full(g), no++ & 1, gave_up));
             if (!ok) break;
             tc_fence_after();
-            store_rows<DP>(sink, t_o, stage + w * 32 * kPitch, r - lane, sg.rows, l == 0.f ? 0.f : 1.f / l, l == 0.f);
+            store_rows<DP>(sink, t_o, stage + w * 32 * kPitch, r - lane, sg.rows, joint.mine, joint.before);
             uint32_t some = 0;
 #pragma unroll 1
             for (int z = 0; z < 4 * (sg.n - blind_from); ++z) some |= bad[z];

@@ -440,11 +440,12 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (!ok) break;
             if (next.n > 0) place(next);  // every product with this item's queries has ended
 
-            const float total = joined_rows(std::true_type()), inv = total == 0.f ? 0.f : 1.f / total;
+            const float before = lane < rows ? sink.before(lane) : -INFINITY;  // written anew only after the next join
+            const typename Sink<BF>::Joint joint = sink.joint(m, joined_rows(std::true_type()), before);
             ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
             if (!ok) break;
             tc_fence_after();
-            if (lr < rows) sink.lse(lr, m, total);
+            if (lr < rows) sink.lse(lr, joint.e);
             int h = sg.row0 - int(a.group.div(sg.row0)) * G;  // head of the row in its group
             uint16_t *out = sink.out_row(0) + lr;
             float *part = a.part + sg.row * D + lr;
@@ -455,8 +456,10 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                 tc_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float f = __shfl_sync(FULL, inv, r0 + i), v = f == 0.f ? 0.f : __uint_as_float(o[i]) * f;
+                    const float f = __shfl_sync(FULL, joint.mine, r0 + i), fb = __shfl_sync(FULL, joint.before, r0 + i);
+                    float v = f == 0.f ? 0.f : __uint_as_float(o[i]) * f;
                     if (r0 + i < rows && lr < D) {
+                        if (fb != 0.f) v = fmaf(*part, fb, v);
                         if (sg.direct) *out = uint16_t(pack<BF>(v, v));
                         else *part = v;
                     }
