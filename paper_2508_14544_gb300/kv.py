@@ -21,11 +21,25 @@ def _dtypes():
 class AttentionPlan:
     """How the attention of one batch is divided (``KVCache.plan``); holds what the calls with it read."""
 
-    def __init__(self, cache, batch, seqs, cu_q, cu_group, buffer, stream):
+    def __init__(self, cache, batch, seqs, cu_q, cu_group, buffer, made_on, stream, captured):
         self.cache, self.batch, self.seqs, self.cu_q, self.cu_group, self._buffer = cache, batch, seqs, cu_q, cu_group, buffer
         self._ref = ctypes.byref(batch)
         self.n_q, self.heads = batch.n_q, batch.q_heads
-        self._stream = stream  # whose next plan may have the buffer, None: no other plan
+        self._stream = stream       # whose next plan may have the buffer, None: no other plan
+        self._read_on = {made_on}   # streams that the allocator knows of
+        self._captured = captured   # what it reads lives as long as the graph that reads it
+
+    def _read_elsewhere(self, stream, capturing):
+        """Before it is read on a stream that is not the one it was made on, or in a graph: what it reads outlives the plan."""
+        self._stream = None
+        held = [x for x in (self._buffer, self.seqs, self.cu_q, self.cu_group) if x is not None]
+        if capturing:
+            if not self._captured:
+                self.cache._in_graphs.append(held)
+                self._captured = True
+        elif stream not in self._read_on:
+            self.cache._record(stream, held)
+            self._read_on.add(stream)
 
     def __del__(self):
         if self._stream is not None and len(self.cache._spare) < 2:
@@ -77,6 +91,7 @@ class KVCache:
         self._torch, self._i32 = torch, torch.int32
         self._sizes = {}  # bytes of a plan and its workspace by the batch's sizes
         self._spare = []  # streams and buffers of plans that are gone: the workspace of the next ones
+        self._in_graphs = []  # what plans made outside of a graph have left to its replays
         torch.cuda.current_stream(self.device).synchronize()  # the first call may be on any stream
 
     def _empty(self, stream, shape, dtype):
@@ -92,6 +107,19 @@ class KVCache:
         if torch._C._cuda_getDevice() != self._index:
             raise ValueError(f"the cache is on {self.device}, which is not the current device")
         return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else int(stream)
+
+    def _capturing(self, stream):
+        torch = self._torch
+        if stream is None:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=self.device)):
+            return torch.cuda.is_current_stream_capturing()
+
+    def _record(self, stream, tensors):
+        """Their memory is used on that stream: the allocator gives it to others only after the work enqueued there."""
+        on = self._torch.cuda.ExternalStream(stream, device=self.device)
+        for x in tensors:
+            x.record_stream(on)
 
     def _fail(self, rc):
         raise L.SimError(rc, L.sim_last_error(None))
@@ -179,7 +207,8 @@ class KVCache:
     def plan(self, seqs, cu_q, n_q: int, heads: int, cu_group=None, stream: int | None = None) -> AttentionPlan:
         """Divide a batch's attention: entry i has the query tokens cu_q[i] .. cu_q[i + 1] - 1 (``n_q`` in all), the
         last ones of sequence seqs[i].  Entries cu_group[g] .. cu_group[g + 1] - 1 may share a prefix: pages that
-        all of them begin with are read once.  Valid until lengths or tables change."""
+        all of them begin with are read once.  Valid until lengths or tables change; what a captured ``attend`` reads of
+        it is kept as long as the cache."""
         n, st = seqs.shape[0], self._stream(stream)
         ng = 0 if cu_group is None else max(cu_group.shape[0] - 1, 0)
         b = L.sim_kv_batch(n, n_q, heads, ng, self._ints("seqs", seqs, n), self._ints("cu_q", cu_q, n + 1),
@@ -192,7 +221,8 @@ class KVCache:
                 self._sizes.clear()
             self._sizes[n, n_q, heads, ng] = sizes
         size, buffer, mine = sizes[0] + sizes[1] + 16, None, None
-        if stream is None and not self._torch.cuda.is_current_stream_capturing():  # a graph's buffers are its own
+        capturing = self._capturing(stream)
+        if stream is None and not capturing:  # a graph's buffers are its own
             mine = st
             while buffer is None and self._spare:
                 of, buffer = self._spare.pop()
@@ -202,7 +232,7 @@ class KVCache:
             buffer = self._empty(stream, (size,), self._torch.uint8)
         b.plan = buffer.data_ptr()
         b.workspace = b.plan + sizes[0]
-        plan = AttentionPlan(self, b, seqs, cu_q, cu_group, buffer, mine)
+        plan = AttentionPlan(self, b, seqs, cu_q, cu_group, buffer, st, mine, capturing)
         rc = self._lib.sim_kv_plan(self._ref, plan._ref, st)
         if rc:
             self._fail(rc)
@@ -214,8 +244,8 @@ class KVCache:
         torch, st, dim = self._torch, self._stream(stream), self._dim
         if plan.cache is not self:
             raise ValueError("the plan is another cache's")
-        if plan._stream is not None and (plan._stream != st or torch.cuda.is_current_stream_capturing()):  # read where no next plan waits
-            plan._stream = None
+        if plan._stream != st or torch.cuda.is_current_stream_capturing():
+            plan._read_elsewhere(st, self._capturing(stream))
         rows = self._rows("q", q, plan.n_q, plan.heads)
         if out is None:
             out = self._empty(stream, (plan.n_q, plan.heads, dim), self.dtype)
