@@ -1,7 +1,8 @@
 """A paged key/value cache on the GPU and attention over it (``include/sim_kv.h``): one ``KVCache`` per pool.
 
 The tensors are torch's; every step runs in the library's CUDA kernels.  Calls are enqueued on torch's current
-stream, or on ``stream`` (a cudaStream_t as an int); one cache is used on one stream at a time.  Lists of
+stream, or on ``stream`` (a cudaStream_t as an int); one cache is used on one stream at a time.  The cache, its plans and the
+tensors given to a call on ``stream`` may be dropped while work on them is still to come.  Lists of
 sequences and offsets are int32 CUDA tensors.  What only the device can see (an unknown sequence, no page left)
 is reported by ``check()``.
 """
@@ -91,6 +92,7 @@ class KVCache:
         self._torch, self._i32 = torch, torch.int32
         self._sizes = {}  # bytes of a plan and its workspace by the batch's sizes
         self._spare = []  # streams and buffers of plans that are gone: the workspace of the next ones
+        self._streams = set()  # where the cache has been used
         self._in_graphs = []  # what plans made outside of a graph have left to its replays
         torch.cuda.current_stream(self.device).synchronize()  # the first call may be on any stream
 
@@ -106,7 +108,15 @@ class KVCache:
         torch = self._torch
         if torch._C._cuda_getDevice() != self._index:
             raise ValueError(f"the cache is on {self.device}, which is not the current device")
-        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else int(stream)
+        st = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else int(stream)
+        if st not in self._streams:
+            self._record(st, (self.pool, self.table, self.length, self.ref, self.status, self._scratch))
+            self._streams.add(st)
+        return st
+
+    def _lend(self, stream, *tensors):
+        if stream is not None:
+            self._record(int(stream), [x for x in tensors if x is not None])
 
     def _capturing(self, stream):
         torch = self._torch
@@ -157,6 +167,7 @@ class KVCache:
                                      slots.data_ptr(), st)
         if rc:
             self._fail(rc)
+        self._lend(stream, seqs, cu_new)
         return slots
 
     def write(self, slots, k, v, layer: int = 0, stream: int | None = None) -> None:
@@ -169,6 +180,7 @@ class KVCache:
                                     *self._rows("v", v, n, self._heads), st)
         if rc:
             self._fail(rc)
+        self._lend(stream, slots, k, v)
 
     def fork(self, src, dst, tokens=None, stream: int | None = None) -> None:
         """dst[i] (empty) becomes the first tokens[i] tokens of src[i], on the same pages."""
@@ -177,6 +189,7 @@ class KVCache:
                                    None if tokens is None else self._ints("tokens", tokens, n), st)
         if rc:
             self._fail(rc)
+        self._lend(stream, src, dst, tokens)
 
     def copy(self, src, dst, stream: int | None = None) -> None:
         """dst[i] (empty) becomes src[i], on pages of its own."""
@@ -184,6 +197,7 @@ class KVCache:
         rc = self._lib.sim_kv_copy(self._ref, n, self._ints("src", src, n), self._ints("dst", dst, n), st)
         if rc:
             self._fail(rc)
+        self._lend(stream, src, dst)
 
     def free(self, seqs, keep=None, stream: int | None = None) -> None:
         """seqs[i] keeps its first keep[i] tokens (none by default) and gives the other pages back."""
@@ -192,6 +206,7 @@ class KVCache:
                                    None if keep is None else self._ints("keep", keep, n), st)
         if rc:
             self._fail(rc)
+        self._lend(stream, seqs, keep)
 
     def compact(self, stream: int | None = None):
         """Move the pages in use to the lowest numbers; returns each page's new number (int32, -1: was free)."""
@@ -236,6 +251,7 @@ class KVCache:
         rc = self._lib.sim_kv_plan(self._ref, plan._ref, st)
         if rc:
             self._fail(rc)
+        self._lend(stream, seqs, cu_q, cu_group)
         return plan
 
     def attend(self, q, plan: AttentionPlan, layer: int = 0, scale: float | None = None, out=None, lse=None, stream: int | None = None):
@@ -260,4 +276,5 @@ class KVCache:
                                      *to, lse.data_ptr(), st)
         if rc:
             self._fail(rc)
+        self._lend(stream, q, out, lse)
         return out, lse

@@ -68,3 +68,66 @@ def test_a_plan_that_another_stream_reads_outlives_its_object(explicit):
     side.synchronize()
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     c.kv.check()
+
+
+def life(torch, kv, x, **on):
+    """Every call that takes lists or values, on 40 sequences of one token."""
+    slots = kv.extend(x["seqs"], x["cu"], 40, **on)
+    kv.write(slots, x["k"], x["v"], **on)
+    kv.attend(x["q"], kv.plan(x["seqs"], x["cu"], 40, heads=2, **on), out=x["out"], lse=x["lse"], **on)
+    kv.fork(x["src"], x["dst"], x["tokens"], **on)
+    kv.free(x["some"], x["keep"], **on)
+
+
+def things(torch):
+    from paper_2508_14544_gb300 import KVCache
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    k, v, q, out = (torch.randn(40, 2, 16, device="cuda").bfloat16() for _ in range(4))
+    return KVCache(64, 16, 2, 16, 41, 8), dict(seqs=ints(range(40)), cu=ints(range(41)), k=k, v=v, q=q, out=out, lse=torch.empty(40, 2, device="cuda"), src=ints([3]),
+                                               dst=ints([40]), tokens=ints([1]), some=ints([5]), keep=ints([0]))
+
+
+@pytest.mark.parametrize("explicit", [False, True])
+def test_a_cache_that_another_stream_uses_outlives_its_object(explicit):
+    import torch
+    life(torch, *things(torch))  # kernels that are loaded at their first launch wait for the GPU
+    kv, x = things(torch)
+    held = [kv.pool, kv.table, kv.length, kv.ref, kv.status, kv._scratch]
+    like, at = [torch.empty_like(y, device="cpu") for y in held], [y.data_ptr() for y in held]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    if explicit:
+        life(torch, kv, x, stream=side.cuda_stream)
+    else:
+        with torch.cuda.stream(side):
+            life(torch, kv, x)
+    del kv, held
+    gc.collect()
+    assert all(z.data_ptr() != old for y, old in zip(like, at) for z in others_like(torch, y))
+    assert not side.query()  # the above was in time
+    side.synchronize()
+    assert torch.equal(x["out"], x["v"])  # sequences of one token: its value
+
+
+def test_tensors_given_to_a_call_on_a_stream_may_be_dropped():
+    import torch
+    life(torch, *things(torch))
+    kv, x = things(torch)
+    want = x["v"].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    life(torch, kv, x, stream=side.cuda_stream)
+    out = x.pop("out")
+    like, at = [torch.empty_like(y, device="cpu") for y in x.values()], [y.data_ptr() for y in x.values()]
+    x.clear()
+    gc.collect()
+    assert all(z.data_ptr() != old for y, old in zip(like, at) for z in others_like(torch, y))
+    assert not side.query()
+    side.synchronize()
+    assert torch.equal(out, want)
+    assert kv.length.tolist() == [1] * 5 + [0] + [1] * 35
+    kv.check()
