@@ -146,9 +146,13 @@ class KVCache:
         return x.data_ptr(), token, head
 
     def check(self) -> None:
-        """Raise if a call has been refused, in part or as a whole, since the last check (waits for the device)."""
+        """Raise if a call has been refused, in part or as a whole, since the last check.  Waits for the device, calls on
+        all streams and in replayed graphs included."""
+        self._torch.cuda.synchronize(self.device)
         code = int(self.status.item())
-        self.status.zero_()
+        if code != L.SIM_OK:
+            self.status.zero_()
+            self._torch.cuda.current_stream(self.device).synchronize()  # later calls may be on any stream
         if code == L.SIM_E_NOMEM:
             raise L.SimError(code, "too few free pages: that call changed nothing")
         if code == L.SIM_E_INVAL:

@@ -131,3 +131,31 @@ def test_tensors_given_to_a_call_on_a_stream_may_be_dropped():
     assert torch.equal(out, want)
     assert kv.length.tolist() == [1] * 5 + [0] + [1] * 35
     kv.check()
+
+
+@pytest.mark.parametrize("how", ["current", "named", "graph"])
+def test_a_check_sees_calls_on_other_streams(how):
+    import torch
+
+    from paper_2508_14544_gb300 import SimError
+    kv, x = things(torch)
+    life(torch, kv, x)
+    kv.check()
+    wrong = torch.tensor([77], dtype=torch.int32, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    if how == "graph":
+        with torch.cuda.graph(graph):
+            kv.free(wrong)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        if how == "current":
+            kv.free(wrong)
+        elif how == "graph":
+            graph.replay()
+    if how == "named":
+        kv.free(wrong, stream=side.cuda_stream)
+    with pytest.raises(SimError) as e:
+        kv.check()
+    assert e.value.code == -1
+    kv.check()
