@@ -94,6 +94,7 @@ int sim_kv_extend(const sim_kv *kv, int32_t n, const int32_t *seqs, const int32_
     if (const char *m = bad_entries(kv, n, seqs, cu_new)) return fail(SIM_E_INVAL, "sim_kv_extend: %s", m);
     if (n_new < 0 || (n_new > 0 && !slots)) return fail(SIM_E_INVAL, "sim_kv_extend: n_new < 0 or NULL slots");
     if (n == 0 && n_new == 0) return SIM_OK;
+    if (!cu_new) return fail(SIM_E_INVAL, "sim_kv_extend: NULL offsets");
     return done(simgb::launch_kv_extend(*kv, n, seqs, cu_new, n_new, slots, static_cast<cudaStream_t>(cuda_stream)), "sim_kv_extend");
 }
 

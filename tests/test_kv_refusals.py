@@ -128,3 +128,10 @@ def test_python_refuses_other_tensors():
                     ("table", torch.zeros(3, 4)), ("length", torch.zeros(4, dtype=torch.int32)), ("ref", torch.zeros(3, dtype=torch.int32))):
         with pytest.raises(ValueError):
             KVCache.wrap(**{**good, name: x})
+
+
+def test_tokens_without_entries_need_their_offsets(L):
+    """n_new slots are to be written, as of no entry: not without the one offset that there is."""
+    lib, p, x = L.lib(), ctypes.byref(cache(L)), ctypes.c_void_p(1 << 24)
+    assert lib.sim_kv_extend(p, 0, None, None, 3, x, None) == INVAL
+    assert L.sim_last_error(None).startswith("sim_kv_extend")
