@@ -143,6 +143,8 @@ class KVCache:
         token, head, last = x.stride() if x.dim() == 3 else (0, 0, 0)
         if last != 1 or x.dtype is not self.dtype or x.shape != (n, heads, self._dim) or x.get_device() != self._index:
             raise ValueError(f"{name} must be {self.dtype} [{n}, {heads}, {self._dim}] on {self.device}, the last dimension contiguous")
+        if x.requires_grad and self._torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which these calls do not have: detach it, or call under torch.no_grad()")
         return x.data_ptr(), token, head
 
     def check(self) -> None:
@@ -260,7 +262,8 @@ class KVCache:
 
     def attend(self, q, plan: AttentionPlan, layer: int = 0, scale: float | None = None, out=None, lse=None, stream: int | None = None):
         """softmax(scale q k^T) v of queries [n_q, heads, head_dim] over the keys that each sees, and the log of the
-        sum of exponentials [n_q, heads] (float32); scale is head_dim ** -0.5 by default."""
+        sum of exponentials [n_q, heads] (float32); scale is head_dim ** -0.5 by default.  There is no backward pass:
+        tensors that require a gradient are refused, here and in ``write``, unless gradients are switched off."""
         torch, st, dim = self._torch, self._stream(stream), self._dim
         if plan.cache is not self:
             raise ValueError("the plan is another cache's")
