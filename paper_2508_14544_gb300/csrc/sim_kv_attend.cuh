@@ -22,6 +22,10 @@ constexpr int kSegs = 4;      // segments that the loading warp may be ahead
 // warps of a block wait for each other.  Taking up a segment costs some 4 tiles.
 constexpr int kMostTiles = 256;
 constexpr float kGrow = 8.f;  // log2 of what P may reach before O is rescaled
+// log2 of what P, and the sum that its product is divided by, are multiplied by: up to 2^15, float16 has room, and below 2^-14 it
+// has fewer and fewer bits.  So a key keeps all of its bits of P down to 2^-21 of the largest one's, and some down to 2^-32; many
+// small weights beside a large one are not lost (32767 of 2^-25 are 2^-10 in all).
+__host__ __device__ constexpr float kv_lift(bool bf) { return bf ? 0.f : 7.f; }
 
 // A list's line (the spans of its items, one after the other) divided among its blocks: [at(c), at(c + 1)) is block c's,
 // each + 1 places for the first `rest` blocks and `each` for the others.

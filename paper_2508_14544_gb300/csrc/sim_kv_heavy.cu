@@ -7,8 +7,8 @@
 // S in TMEM as 16 bits, O += P V (128 x D x 128, P from TMEM, V as it lies, the N dimension contiguous).  TMEM is full:
 // 128 columns each for S / P and O of the two groups.
 //
-// P is rounded to the cache's type (its relative error, 2^-9 or 2^-12, is that of the values it meets), its sum is not; m may lag
-// behind the row's maximum by a factor of 2^kGrow before O is rescaled, which float16 holds with room to spare.
+// P is rounded to the cache's type (its relative error, 2^-9 or 2^-12, is that of the values it meets; in float16 with steps of
+// 2^-31 below 2^-21, see kv_lift), its sum is not; m may lag behind the row's maximum by a factor of 2^kGrow before O is rescaled.
 //
 // 16 prompts' own 300 - 512 tokens on 4096 + 600 keys each, 64 heads, D = 128: 464 us, 1.66 PFLOP/s, 86 % of cuBLAS's
 // burst rate.  A tile takes both groups about 2600 cycles, its products alone 2048.  In these, operands and loads ask shared
@@ -144,7 +144,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int lim
             tm_st32(t_o + 32 * q, o);
         }
     }
-    const float off = m == -INFINITY ? 0.f : m * c;
+    const float off = m == -INFINITY ? 0.f : m * c - kv_lift(BF);
     float2 sum[4] = {};
     uint32_t pk[kTileKeys / 2];
 #pragma unroll
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 if (lane == 0) bar_arrive(p_ready(g));
             }
             if (!ok) break;
-            const typename Sink<BF>::Joint joint = sink.joint(m * c, l, r < sg.rows ? sink.before(r) : -INFINITY);
+            const typename Sink<BF>::Joint joint = sink.joint(m * c - kv_lift(BF), l, r < sg.rows ? sink.before(r) : -INFINITY);
             if (r < sg.rows) sink.lse(r, joint.e);
             ok = __all_sync(FULL, bar_wait(o_full(g), no++ & 1, gave_up));
             if (!ok) break;

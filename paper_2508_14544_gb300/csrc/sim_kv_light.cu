@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
                     }
                 }
                 unsigned char *const p = base + (at % NS) * Sh::kSlot + lr / 64 * Sh::kRowsHalf + lr % 8 * 2;
-                const float off = m == -INFINITY ? 0.f : -m;
+                const float off = m == -INFINITY ? 0.f : kv_lift(BF) - m;
 #pragma unroll 1
                 for (int r0 = 0; r0 < rows; r0 += 8) {
                     float s[8];
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 2)
             if (next.n > 0) place(next);  // every product with this item's queries has ended
 
             const float before = lane < rows ? sink.before(lane) : -INFINITY;  // written anew only after the next join
-            const typename Sink<BF>::Joint joint = sink.joint(m, joined_rows(std::true_type()), before);
+            const typename Sink<BF>::Joint joint = sink.joint(m - kv_lift(BF), joined_rows(std::true_type()), before);
             ok = __all_sync(FULL, bar_wait(o_full, x & 1, gave_up)) && ok;
             if (!ok) break;
             tc_fence_after();
