@@ -2,7 +2,8 @@
 
 The tensors are torch's; every step runs in the library's CUDA kernels.  Calls are enqueued on torch's current
 stream, or on ``stream`` (a cudaStream_t as an int); one cache is used on one stream at a time.  The cache, its plans and the
-tensors given to a call on ``stream`` may be dropped while work on them is still to come.  Lists of
+tensors given to a call on ``stream`` may be dropped while work on them is still to come; the stream has to exist until they are.
+Lists of
 sequences and offsets are int32 CUDA tensors.  What only the device can see (an unknown sequence, no page left)
 is reported by ``check()``.
 """
