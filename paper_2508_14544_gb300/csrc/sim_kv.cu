@@ -6,7 +6,7 @@
 //                page is shared and has room; an exclusive scan over the entries places each entry's pages in the list of
 //                the sum(n_i) lowest free ones, which 32 warps find by counting zeros of `ref` in a run of pages each,
 //                a scan over the warps and a second walk.  Nothing is changed before the sum is known to fit.  6 us for
-//                40 entries, 11 us for 250 entries and 16000 new pages, most of it chains of loads from L2.
+//                40 entries, 10 us for 250 entries and 16000 new pages, most of it chains of loads from L2.
 //   k_move     - puts the pages into the tables, and makes the slots of the new tokens and the copies that k_extend
 //                listed, whole pages of all layers.  Every byte read once and written once, 16 bytes a load, eight in
 //                flight a thread, past L1 and L2: 80 us for 0.53 GB moved, 6.6 TB/s.
@@ -14,8 +14,8 @@
 //   k_compact  - one block: with N pages in use, the i-th used page at or above N goes to the i-th free one below N.  6 us for
 //                4600 pages; k_compact_move makes the copies, 78 us for 0.52 GB, 6.6 TB/s.
 //   k_write    - a thread for each 16 bytes of a token's keys and of its values, both loads before both stores, no thread with
-//                more than one of each and stores that L2 need not keep: 286 us for 2.02 GB, 7.1 TB/s, the last writes still in
-//                L2 (312 us with 16 blocks per SM that stay).  Sources that are not 16-byte aligned are read 2 bytes at a time, as they must be.
+//                more than one of each and stores that L2 need not keep: 285 us for 2.02 GB, 7.1 TB/s, the last writes still in
+//                L2 (26 us more with 16 blocks per SM that stay).  Sources that are not 16-byte aligned are read 2 bytes at a time, as they must be.
 #include <algorithm>
 #include <climits>
 
@@ -32,7 +32,7 @@ constexpr int kMove = 256;    // threads of the moving kernels
 constexpr int kUnroll = 8;    // 16-byte loads in flight per thread
 constexpr int kChunk = kMove * kUnroll * 16;
 // Blocks per SM of the moving kernels, many more than fit: blocks that come as others end keep HBM busier than as many as fit,
-// each with its share (0.53 GB in all: 101 us with 4, 96 with 8, 93 with 32).
+// each with its share (0.53 GB, the free list included: 108 us with 4, 106 with 8, 103 with 32).
 constexpr int kMoveWaves = 32;
 // Sums over the entries of a call: pages in the low bits (at most n_pages + 1 <= 2^28 + 1 counted for an entry, 2^17
 // entries), copies of shared pages above.

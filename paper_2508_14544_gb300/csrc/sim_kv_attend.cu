@@ -10,12 +10,12 @@
 //
 // The plan (k_plan_shared, k_plan_items, made once for all layers) lists the items.  Those of more than 32 rows
 // are heavy, the others light: two kernels (sim_kv_heavy.cu, sim_kv_light.cu), because many rows want the tensor
-// products fed and few rows want bytes in flight.  Measured either way, 8 kv heads: 200 sequences of up to 2600 keys with 16
-// rows take 208 us light and 224 us heavy, 64 sequences of 2048 keys with 32 rows 124 us both; a light item has no room for
-// more.  The tiles of all items and heads of a list lie on one line, and every block takes an equal stretch of it, so that work
+// products fed and few rows want bytes in flight.  Measured either way, 8 kv heads (these and the figures below: plan and
+// attention as a captured graph, caches flushed): 200 sequences of up to 2600 keys with 16 rows take 206 us light and 222 us
+// heavy, 64 sequences of 2048 keys with 32 rows 124 and 126 us; a light item has no room for more.  The tiles of all items and heads of a list lie on one line, and every block takes an equal stretch of it, so that work
 // is even whatever the lengths; an item is split where two stretches meet, and k_combine joins the pieces.  What taking up an
-// item costs lies on the line too (kv_lead): left out, a step of 64 short sequences takes 38 instead of 34 us and one of 256
-// on a prefix 159 instead of 151 us.
+// item costs lies on the line too (kv_lead): left out, a step of 384 sequences takes 360 instead of 347 us and one of 256
+// on a prefix 162 instead of 149 us.
 #include <algorithm>
 
 #include "sim_kv_attend.cuh"
@@ -28,9 +28,10 @@ namespace {
 
 // What sharing a prefix costs, in the time that a block needs for 128 keys: for the prefix's own item, for 32 rows that are
 // then joined from two places, and for every block once (a longer chain of kernels).  Measured with and without sharing, 128
-// sequences (8 kv heads, 8 query heads each, up to 64 keys of their own) in groups: 64 groups with a prefix of 512 keys 85
-// against 71 us, of 2048 keys 142 against 171 us; 16 groups with 256 keys 73 against 52 us, with 1024 keys 76 against 81 us.
-// The rule takes the faster side of these four.
+// sequences (8 kv heads, 8 query heads each, up to 64 keys of their own) in groups: 64 groups with a prefix of 512 keys 93
+// against 71 us, of 2048 keys 140 against 170 us; 16 groups with 256 keys 72 against 52 us, with 1024 keys 75 against 81 us.
+// The rule takes the faster side of these four.  With 2 kv heads of 4 query heads and D = 64 it shares a little early: 64 groups with
+// 2048 keys 59 against 50 us (8192: 88 against 102), 16 groups with 1024 keys 48 against 42 us (4096: 59 against 63).
 constexpr int kShareItem = 3, kShareRows = 7, kShareOnce = 2;
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -61,7 +62,7 @@ __device__ __forceinline__ int group_of(const sim_kv_batch &b, int i) {
     return lo >= 0 && i < b.cu_group[lo + 1] ? lo : -1;
 }
 
-constexpr int kAhead = 16;  // 256 tables of 540 pages: the whole call takes 4 us less than with 2
+constexpr int kAhead = 16;  // 256 tables of 540 pages: the whole call takes 5 us less than with 2
 
 // A warp for each entry: the pages that its table begins with like that of its group's first entry, all of whose
 // keys each of its queries sees.  Bound by the latency of loads, so kAhead of either table are in flight: 5 us for 256 tables of
@@ -158,8 +159,8 @@ __device__ __forceinline__ int last_at_most(const T *x, int n, T v) {
 
 // One block: which prefixes are shared, the sources and items, and where each begins on its list's line of work.
 // Bound by its chain of dependent loads and barriers, not by bytes: 7 us for 40 entries, 12 us for 256 and their group.
-// FEW: what the searches read is in shared memory, as far as that goes without asking for more than 48 KB; steps of 40, 64 and
-// 256 sequences take 28, 34 and 149 us in all, and 32, 38 and 154 us without.
+// FEW: what the searches read is in shared memory, as far as that goes without asking for more than 48 KB; steps of 40, 64,
+// 256 (on a prefix) and 440 sequences take 26, 33, 149 and 96 us in all, and 30, 36, 155 and 100 us without.
 template <bool FEW>
 __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv, const sim_kv_batch b, int sms) {
     constexpr int kPlan = FEW ? 512 : 1024;
@@ -409,7 +410,7 @@ constexpr int kJoinLight = 4;
 // read the sums of 16 pieces at once and, four at a time without waiting in between, the pieces.  One wave of blocks
 // goes over what there is to join: items without a prefix that blocks' stretches cut, then entries with a shared prefix
 // and rows without keys, by kv head (`parts` blocks for each).  Loads of pieces that are not there are made all the same, from
-// another piece's row: asked for only where there is one, they wait for each other (11 -> 30 us for 64 rows in 38 pieces).
+// another piece's row, so that the four of a lane need not be told apart (64 rows in 38 pieces: 118 us the whole call either way).
 // 18 us for 16384 rows with a prefix in 3 or 4 pieces and their own keys, 15 us for the cuts of 152 heavy stretches.
 template <bool BF>
 __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {

@@ -2,7 +2,7 @@
 //
 // One block per SM, two groups of four softmax warps with 128 rows each.  Both groups use every tile of 128 keys,
 // so a byte that enters shared memory serves 256 rows; the tensor unit works for one group while the other is in its
-// softmax (the second group rests while an item has at most 128 rows: 132 instead of 138 us for 64 sequences of 2048 keys with 128
+// softmax (the second group rests while an item has at most 128 rows: 132 instead of 134 us for 64 sequences of 2048 keys with 128
 // rows).  Per tile and group: S = Q K^T (128 x 128 x D, operands in shared memory), P = exp2(c (S - m)) written over
 // S in TMEM as 16 bits, O += P V (128 x D x 128, P from TMEM, V as it lies, the N dimension contiguous).  TMEM is full:
 // 128 columns each for S / P and O of the two groups.
@@ -10,11 +10,11 @@
 // P is rounded to the cache's type (its relative error, 2^-9 or 2^-12, is that of the values it meets; in float16 with steps of
 // 2^-31 below 2^-21, see kv_lift), its sum is not; m may lag behind the row's maximum by a factor of 2^kGrow before O is rescaled.
 //
-// 16 prompts' own 300 - 512 tokens on 4096 + 600 keys each, 64 heads, D = 128: 464 us, 1.66 PFLOP/s, 86 % of cuBLAS's
-// burst rate.  A tile takes both groups about 2600 cycles, its products alone 2048.  In these, operands and loads ask shared
+// 16 prompts' own 300 - 512 tokens on 4096 + 600 keys each, 64 heads, D = 128: 456 us, 1.69 PFLOP/s, 87 % of cuBLAS's
+// burst rate.  A tile takes both groups about 2550 cycles, its products alone 2048.  In these, operands and loads ask shared
 // memory for 256 KB (S 128, P V 64, the tile's arrival 64), which at 128 bytes a cycle is all that it can give; the rest is the
-// way from a product through the softmax to the next one.  The first half of P is multiplied while the second is made (602 -> 591 us for the whole
-// call); split three to one it is slower (447 -> 477 us).
+// way from a product through the softmax to the next one.  The first half of P is multiplied while the second is made (508 instead of 544 us, plan,
+// light items and join included).
 #include <type_traits>
 
 #include "sim_kv_attend.cuh"
@@ -388,11 +388,11 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             __syncwarp();
         } else {
             // ---- query rows, by TMA where heads and tokens make boxes of 128 rows (rows of other entries, past the item's,
-            // come with them); else two warps, 16 bytes a lane, the lanes of a row side by side (all that prefill 527 instead of
-            // 509 us).  What rows past the item's hold meets no other row and is not used.
+            // come with them); else two warps, 16 bytes a lane, the lanes of a row side by side (all that prefill 532 instead of
+            // 508 us).  What rows past the item's hold meets no other row and is not used.
             // They then look at the values of the item's last tiles, before they are multiplied: those past the end of
             // the keys, whatever they are, must not meet their zero probabilities, nor those that are not finite the rows that do not
-            // see them.
+            // see them (by the softmax's warps instead: 531 us).
             constexpr int kVec = DP / 8, kStep = 64 / kVec;
             const int j = (tid & 63) % kVec;
             const bool has = j * 8 < D;

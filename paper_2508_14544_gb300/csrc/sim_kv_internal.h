@@ -72,7 +72,7 @@ constexpr int kLightRows = 32;  // of a light one
 __host__ __device__ constexpr int kv_rows(int light) { return light ? kLightRows : kAttRows; }
 // Batches that look like single tokens (no more of them than entries, no groups): all rows are light items, more than one
 // if an entry has more than kLightRows after all, and the heavy kernel is not launched: over an empty list it costs the
-// host 1.6 us and the GPU 1 to 4 us of a step that takes 25.
+// host 1.6 us and the GPU 2 to 3 us of a step that takes 26.
 __host__ __device__ inline bool kv_light_only(const sim_kv &kv, const sim_kv_batch &b) {
     const int64_t G = b.q_heads / kv.n_kv_heads;
     return b.n_q * G <= kLightRows || (b.n_groups == 0 && G <= kLightRows && b.n_q <= b.n);

@@ -10,9 +10,9 @@
 // Two blocks per SM, so that one loads while the other is between two items, with 96 KB of keys and values in flight each.
 // Rows of P are rounded as in sim_kv_heavy.cu.
 //
-// 384 sequences of up to 2600 keys, 8 query heads on each of 8 kv heads, D = 128: 315 us for 2.10 GB, 6.66 TB/s; one sequence
-// of 131071 keys 79 us for 0.54 GB, 6.76 TB/s: what a copy reaches.  With queries on the rows (each four times, for four
-// quarters of the keys) these took 330 and 85 us.  D <= 64 has half the columns: 196 us for the first with D = 64, 218 us as D = 128.
+// 384 sequences of up to 2600 keys, 8 query heads on each of 8 kv heads, D = 128: 316 us for 2.10 GB, 6.64 TB/s; one sequence
+// of 131071 keys 80 us for 0.54 GB, 6.7 TB/s: what a copy reaches.  With queries on the rows (each four times, for four
+// quarters of the keys) these took 330 and 85 us.  D <= 64 has half the columns: the first with D = 64 takes 197 us with the plan, 223 us as D = 128.
 #include "sim_kv_attend.cuh"
 
 namespace simgb {
