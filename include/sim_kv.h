@@ -7,7 +7,8 @@
  * batches of a schedule can be run and timed (the coefficients of sim_batch_time are the caller's).
  *
  * Layout.  A cache is four arrays of the caller in DEVICE memory:
- *   pool    [n_pages][n_layers][2: keys, values][n_kv_heads][page_size][head_dim], 16-bit floats,
+ *   pool    [n_pages][n_layers][2: keys, values][n_kv_heads][page_size][head_dim], 16-bit floats, or, in a cache of
+ *           4 bits, strips of 16 tokens (below),
  *   table   int32 [max_seqs][max_pages]: the pages of each sequence in order, -1 where there is none,
  *   length  int32 [max_seqs]: tokens of each sequence (0: none),
  *   ref     int32 [n_pages]: sequences that hold the page; 0 means free.
@@ -35,7 +36,25 @@
 extern "C" {
 #endif
 
-typedef enum { SIM_KV_BF16 = 0, SIM_KV_F16 = 1 } sim_kv_dtype;
+/* The type of keys, values, queries and results, and how the pool holds keys and values: as they are, or in 4 bits. */
+typedef enum { SIM_KV_BF16 = 0, SIM_KV_F16 = 1, SIM_KV_BF16_4BIT = 16, SIM_KV_F16_4BIT = 17 } sim_kv_dtype;
+
+/*
+ * Caches in 4 bits.  The keys (values) x of a token and head are cut into groups of 32, the last one shorter:
+ *   lo    their lowest,  hi  their highest,
+ *   step  the largest 16-bit float of the type that is not above (hi - lo) / 15; the smallest positive one where
+ *         that is 0 and hi > lo,
+ *   code  the nearest of 0 .. 15 to (x - lo) / step, ties to even (0 where step is 0),
+ * and in x's place the cache holds the 16-bit float nearest to lo + code step: |held - x| is at most step / 2 (or 15
+ * times the smallest positive float, if that is more) and a rounding.  If one of the group is infinite or not a number, all of it is held as not a number.  Everything below goes
+ * by the values held.  The pool is [n_pages][n_layers][2][n_kv_heads][page_size / 16] strips of 16 tokens, each, with
+ * G = ceil(head_dim / 32) groups, 320 G bytes (5 bits a value), in the order in which the matrix instructions of sim_kv_attend take
+ * them.  With token T (0 .. 15) of the strip and group g, whose dimension d is 32 g + d:
+ *   keys    32-bit word at 16 G T + 4 G (d / 8) + 4 g: code of d at bit 4 (d % 8 / 2) + 16 (d % 2); step and lo, 16 bits each, from
+ *           256 G + 4 G T + 4 g on;
+ *   values  16-bit word at 128 G (T / 8) + 4 G (4 (d / 4) + T % 8 / 2) + 4 g + 2 (T % 2): code of d at bit 4 (d % 4); step at
+ *           256 G + 8 G (T / 2) + 8 g + 2 (T % 2), lo 4 bytes behind it.
+ */
 
 typedef struct {
     void *pool;       /* DEVICE, 16-byte aligned */
@@ -57,6 +76,9 @@ typedef struct {
 /* sim_kv_scratch_bytes: size of kv->scratch (the pointers of *kv are not read); 0 for bad sizes. */
 int64_t sim_kv_scratch_bytes(const sim_kv *kv);
 
+/* sim_kv_pool_bytes: size of kv->pool (the pointers of *kv are not read); 0 for bad sizes. */
+int64_t sim_kv_pool_bytes(const sim_kv *kv);
+
 /*
  * sim_kv_extend: room for new tokens at the end of sequences.
  *   n        entries, 0 .. max_seqs;  seqs  DEVICE int32 [n], distinct.
@@ -74,7 +96,8 @@ int sim_kv_extend(const sim_kv *kv, int32_t n, const int32_t *seqs, const int32_
  * sim_kv_write: keys and values of one layer into the slots of sim_kv_extend.
  *   k, v     DEVICE [n_new][n_kv_heads][head_dim] of kv->dtype; strides in elements between tokens and
  *            between heads, the last dimension contiguous; any alignment of the type.
- * Slots outside the pool are skipped.
+ * Slots outside the pool are skipped.  In a cache of 4 bits they are quantised as they are written.  A slot that is named twice
+ * gets one or the other, in a cache of 4 bits codes of one and steps of the other.
  */
 int sim_kv_write(const sim_kv *kv, int32_t layer, int32_t n_new, const int64_t *slots, const void *k,
                  int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
@@ -102,6 +125,20 @@ int sim_kv_free(const sim_kv *kv, int32_t n, const int32_t *seqs, const int32_t 
  *   to       DEVICE int32 [n_pages]: the new number of each page, -1 where it was free.
  */
 int sim_kv_compact(const sim_kv *kv, int32_t *to, void *cuda_stream);
+
+/*
+ * sim_kv_read: cached keys and values of one layer, in order.
+ *   n        entries, 0 .. 2^17;  seqs  DEVICE int32 [n] (a sequence may repeat).
+ *   cu       DEVICE int32 [n + 1], non-decreasing, 0 .. total: entry i has the rows cu[i] .. cu[i + 1] - 1.
+ *   first    DEVICE int32 [n]: token of sequence seqs[i] that is entry i's first row, or NULL (0).
+ *   k, v     DEVICE [total][n_kv_heads][head_dim] of the type of kv->dtype; strides in elements, multiples of 8, the last
+ *            dimension contiguous, 16-byte aligned.
+ * Rows of an entry whose sequence is out of range or does not have its tokens (SIM_E_INVAL in kv->status) are zeros, as are
+ * tokens of pages that the pool does not have and rows of no entry.  With offsets that are not in order (SIM_E_INVAL) all rows are.
+ */
+int sim_kv_read(const sim_kv *kv, int32_t layer, int32_t n, const int32_t *seqs, const int32_t *cu, const int32_t *first,
+                int32_t total, void *k, int64_t k_token_stride, int64_t k_head_stride, void *v, int64_t v_token_stride,
+                int64_t v_head_stride, void *cuda_stream);
 
 /* The queries of one batch: entry i has the query tokens cu_q[i] .. cu_q[i + 1] - 1, which are the last
  * tokens of sequence seqs[i] (already in the cache); a query sees the keys up to its own position. */
@@ -132,13 +169,13 @@ int sim_kv_plan(const sim_kv *kv, const sim_kv_batch *b, void *cuda_stream);
 
 /*
  * sim_kv_attend: softmax(scale q k^T) v over the cached keys that each query sees, for one layer.
- *   q        DEVICE [n_q][q_heads][head_dim] of kv->dtype, strides in elements, last dimension contiguous.
+ *   q        DEVICE [n_q][q_heads][head_dim] of the type of kv->dtype, strides in elements, last dimension contiguous.
  *   out      the same shape and type, strides multiples of 8, 16-byte aligned.
  *   lse      DEVICE float [n_q][q_heads], or NULL: log of the sum of the exponentials.
  *   scale    > 0, finite, also times log2(e).
  * A query that sees no key gets zeros, and -infinity for lse.  Cached values past a sequence's length are
  * never used, whatever they are, nor are those that a query does not see.  Sums and the softmax are in 32 bits, those
- * of the products (which cut off what does not fit) over 2^15 keys at most; the probabilities are rounded to kv->dtype for
+ * of the products (which cut off what does not fit) over 2^15 keys at most; the probabilities are rounded to that type for
  * the product with the values.
  */
 int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const void *q, int64_t q_token_stride,

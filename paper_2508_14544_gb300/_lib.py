@@ -24,6 +24,8 @@ SIM_OPT_COUNT_WORK = 9
 SIM_OPT_BATCH_TIME = 10
 SIM_OPT_DENSE_RESIDENCY = 11
 
+SIM_KV_4BIT = 16  # of a cache's dtype: SIM_KV_BF16_4BIT, SIM_KV_F16_4BIT
+
 STATUS_NAMES = {0: "SIM_OK", -1: "SIM_E_INVAL", -2: "SIM_E_INFEASIBLE", -3: "SIM_E_STEPCAP", -4: "SIM_E_CUDA",
                 -5: "SIM_E_STATE", -6: "SIM_E_NOMEM"}
 
@@ -55,7 +57,7 @@ EXPORTS = ("sim_create", "sim_load", "sim_load_csr", "sim_load_ranked_csr", "sim
            "sim_set_option", "sim_set_tie_seeds", "sim_get_work_counts", "sim_batch_time",
            "sim_get_batch_time_sums", "sim_last_error", "sim_destroy", "sim_kernel_launches", "sim_run_noalloc",
            "sim_cr_amin_lemma", "sim_cr_amin_rho", "sim_measure_peaks",
-           "sim_kv_scratch_bytes", "sim_kv_extend", "sim_kv_write", "sim_kv_fork", "sim_kv_copy", "sim_kv_free",
+           "sim_kv_scratch_bytes", "sim_kv_pool_bytes", "sim_kv_extend", "sim_kv_write", "sim_kv_read", "sim_kv_fork", "sim_kv_copy", "sim_kv_free",
            "sim_kv_compact", "sim_kv_plan_bytes", "sim_kv_workspace_bytes", "sim_kv_plan", "sim_kv_attend")
 
 _lib = None
@@ -123,8 +125,10 @@ def lib() -> ctypes.CDLL:
     L.sim_measure_peaks.restype = ctypes.c_int
     kv, batch, i32, i64 = ctypes.POINTER(sim_kv), ctypes.POINTER(sim_kv_batch), ctypes.c_int32, ctypes.c_int64
     for name, res, args in (("sim_kv_scratch_bytes", i64, [kv]),
+                            ("sim_kv_pool_bytes", i64, [kv]),
                             ("sim_kv_extend", ctypes.c_int, [kv, i32, vp, vp, i32, vp, vp]),
                             ("sim_kv_write", ctypes.c_int, [kv, i32, i32, vp, vp, i64, i64, vp, i64, i64, vp]),
+                            ("sim_kv_read", ctypes.c_int, [kv, i32, i32, vp, vp, vp, i32, vp, i64, i64, vp, i64, i64, vp]),
                             ("sim_kv_fork", ctypes.c_int, [kv, i32, vp, vp, vp, vp]),
                             ("sim_kv_copy", ctypes.c_int, [kv, i32, vp, vp, vp]),
                             ("sim_kv_free", ctypes.c_int, [kv, i32, vp, vp, vp]),

@@ -15,7 +15,8 @@ INCLUDE = ROOT / "include"
 BUILD = PKG / "_build"
 LIB = BUILD / "libsim.so"
 SOURCES = ["sim_kernels.cu", "sim_stage.cu", "sim_api.cpp", "sim_noalloc.cu", "sim_analytic.cu", "sim_peaks.cu", "sim_kv.cu",
-           "sim_kv_attend.cu", "sim_kv_heavy.cu", "sim_kv_light.cu", "sim_kv_api.cpp"]
+           "sim_kv_attend.cu", "sim_kv_heavy.cu", "sim_kv_light.cu", "sim_kv_4bit.cu",
+           "sim_kv_4bit_light.cu", "sim_kv_api.cpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

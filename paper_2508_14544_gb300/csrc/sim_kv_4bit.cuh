@@ -1,0 +1,68 @@
+// Device code shared by the kernels of 4-bit caches: what a strip of 16 tokens holds (include/sim_kv.h) as 16-bit floats.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "sim_kv_internal.h"
+
+namespace simgb {
+
+namespace {
+
+// N 32-bit words that lie N words apart from the neighbours', so aligned as far as N allows.
+template <int N>
+__device__ __forceinline__ void words(const void *from, uint32_t *w) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 v = static_cast<const uint4 *>(from)[i / 4];
+            w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+        }
+    } else if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const uint2 v = static_cast<const uint2 *>(from)[i / 2];
+            w[i] = v.x, w[i + 1] = v.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = static_cast<const uint32_t *>(from)[i];
+    }
+}
+
+template <bool BF>
+__device__ __forceinline__ uint32_t fma16(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    if (BF) asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    else asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+template <bool BF>
+__device__ __forceinline__ uint32_t add16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if (BF) asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// Codes at bits 4 I and 16 + 4 I of w, as the values that they stand for: a code is put under the exponent whose unit it is
+// (128 + code, 1024 + code), which is then taken away, exactly; lo + code step is rounded once.
+template <bool BF, int I>
+__device__ __forceinline__ uint32_t values(uint32_t w, uint32_t step, uint32_t lo) {
+    const uint32_t code = (w >> (4 * I) & 0x000f000fu) | (BF ? 0x43004300u : 0x64006400u);
+    return fma16<BF>(add16<BF>(code, BF ? 0xc300c300u : 0xe400e400u), step, lo);
+}
+template <bool BF>
+__device__ __forceinline__ void values4(uint32_t w, uint32_t step, uint32_t lo, uint32_t *x) {
+    x[0] = values<BF, 0>(w, step, lo);
+    x[1] = values<BF, 1>(w, step, lo);
+    x[2] = values<BF, 2>(w, step, lo);
+    x[3] = values<BF, 3>(w, step, lo);
+}
+__device__ __forceinline__ uint32_t low_twice(uint32_t x) { return __byte_perm(x, 0, 0x1010); }
+__device__ __forceinline__ uint32_t high_twice(uint32_t x) { return __byte_perm(x, 0, 0x3232); }
+
+}  // namespace
+
+}  // namespace simgb

@@ -1,0 +1,475 @@
+// Attention over a 4-bit cache (see sim_kv_attend.cu for the plan, the lines of work and the joining of pieces).
+//
+// Keys and values become 16-bit floats in registers, in the very places that the matrix instructions take their first operand
+// from: the strips are laid out for that (include/sim_kv.h), so that a byte goes from HBM through shared memory into a register and no
+// further.  Per warp and strip of 16 keys: S' = K Q' (16 keys x 8 query rows at a time, D / 16 products), P' = exp2(c (S' - m)), whose
+// 8 x 8 parts are turned over between the lanes, and O' += V' P' (D x 8, one product for each 16 columns).  Each warp keeps its own
+// running maximum, sum and O; the warps' shares are joined at the end of the segment.
+#include <algorithm>
+
+#include "sim_kv_4bit.cuh"
+#include "sim_kv_attend.cuh"
+
+namespace simgb {
+
+namespace {
+
+constexpr int kStrips = kTileKeys / kStrip;  // of a tile
+
+// DG groups of 32 columns, NT times 8 query rows in a pass, W warps that compute and one that loads.
+template <int DG, int NT, int W>
+struct Shape {
+    static constexpr int kThreads = 32 * (W + 1);
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kBytesStrip = 320 * DG;
+    static constexpr int kStage = 2 * kStrips * kBytesStrip;  // a tile's keys, then its values
+    static constexpr int kPart = NT > 2 ? 2 : NT;             // times 8 rows of O that are joined at a time
+    static constexpr int kPitch = 32 * DG + 4;                // floats between rows of the warps' O
+    static constexpr int kOffQ = 0;                           // queries: [NT][DG][lane] 16 bytes
+    static constexpr int kOffO = kOffQ + NT * DG * 512;       // [W][8 kPart][kPitch]
+    static constexpr int kOffM = kOffO + W * 8 * kPart * kPitch * 4;  // [W][kRows] maximum and sum
+    static constexpr int kOffSeg = kOffM + W * kRows * 8;
+    static constexpr int kFixed = kOffSeg + kSegs * int(sizeof(Segment)) + 256;
+    static constexpr int kStages = (114000 - kFixed) / kStage < 4 ? (114000 - kFixed) / kStage : 4;
+    static constexpr int kOffRing = (kOffSeg + kSegs * int(sizeof(Segment)) + 127) / 128 * 128;
+    static constexpr int kOffBar = kOffRing + kStages * kStage;
+    static constexpr int kBars = 2 * kStages + 2 * kSegs + 1;
+    static constexpr int kOffGone = kOffBar + kBars * 8;      // per stage: strips on pages that the pool does not have
+    static constexpr int kBytes = kOffGone + kStages * 4 + 16;
+    static_assert(kStages >= 2 && kBytes <= 115712, "two blocks per SM");
+};
+
+// 16 x 8 += 16 x 16 times 16 x 8.
+template <bool BF>
+__device__ __forceinline__ void product(float *d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (BF)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The 8 x 8 matrix of which a lane has two values of row lane / 4, turned over.
+__device__ __forceinline__ uint32_t turned(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from), "r"(bytes),
+                 "r"(bar)
+                 : "memory");
+}
+
+template <int DG, int NT, int W, bool BF>
+__global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
+    k_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int light) {
+    using Sh = Shape<DG, NT, W>;
+    constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip;
+    extern __shared__ __align__(128) unsigned char base[];
+    const uint32_t sbase = smem_addr(base), bars = sbase + Sh::kOffBar;
+    volatile int *const gave_up = reinterpret_cast<int *>(base + Sh::kOffGone + NS * 4);
+    uint32_t *const gone = reinterpret_cast<uint32_t *>(base + Sh::kOffGone);
+    Segment *const segs = reinterpret_cast<Segment *>(base + Sh::kOffSeg);
+    const auto full = [&](uint32_t x) { return bars + 8 * (x % NS); };
+    const auto empty = [&](uint32_t x) { return bars + 8 * (NS + x % NS); };
+    const auto seg_full = [&](uint32_t x) { return bars + 8 * (2 * NS + x % kSegs); };
+    const auto seg_empty = [&](uint32_t x) { return bars + 8 * (2 * NS + kSegs + x % kSegs); };
+    const uint32_t joined = bars + 8 * (2 * NS + 2 * kSegs);
+    const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < NS; ++s) {
+            bar_init(full(s), 1);
+            bar_init(empty(s), W);
+        }
+        for (int s = 0; s < kSegs; ++s) {
+            bar_init(seg_full(s), 1);
+            bar_init(seg_empty(s), W);
+        }
+        bar_init(joined, W);
+        *gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    kv_wait_previous();
+    const int G = b.q_heads / kv.n_kv_heads, D = kv.head_dim;
+
+    if (warp == W) {
+        // ---- the line of work, and loads: lane l brings the keys of strip l, lane 8 + l its values
+        const KvPlan plan = kv_plan(kv, b);
+        Line line(plan, kv.n_kv_heads, light, blockIdx.x, a.sms);
+        const int P = kv.page_size, strip = lane % kStrips;
+        const int64_t head_bytes = kv_head_bytes(kv), page_bytes = kv_page_bytes(kv);
+        const unsigned char *const layer = static_cast<const unsigned char *>(kv.pool) + int64_t(a.layer) * 2 * kv.n_kv_heads * head_bytes;
+        uint32_t at = 0, x = 0;  // tiles loaded, segments told of
+        bool ok = true;
+        const auto tell = [&](const Segment &sg) {
+            ok = __all_sync(FULL, bar_wait(seg_empty(x), (x / kSegs + 1) & 1, gave_up));
+            if (ok && lane == 0) {
+                segs[x % kSegs] = sg;
+                bar_arrive(seg_full(x));
+            }
+            ++x;
+        };
+        Segment all;
+        for (line.next(all); ok && all.n > 0; line.next(all)) {
+            for (int r0 = 0; ok && r0 < all.rows; r0 += R) {  // as many rows as a pass has room for
+                Segment sg = all;
+                sg.row0 = all.row0 + r0;
+                sg.rows = min(all.rows - r0, R);
+                sg.row = all.row + r0;
+                // no key that none of them sees
+                sg.kv1 = min(all.kv1, sg.pos0 + int(a.group.div(sg.row0 + sg.rows - 1)) + 1);
+                sg.n = min(all.n, max((sg.kv1 - sg.k0 + kTileKeys - 1) / kTileKeys, 1));
+                tell(sg);
+                const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
+                const auto page_of = [&](int j) {  // of this lane's strip in tile j, -1 past the keys
+                    const int key = sg.k0 + j * kTileKeys + strip * kStrip;
+                    return j < sg.n && key < sg.kv1 ? row[key / P] : -1;
+                };
+                int page = page_of(0);
+                for (int j = 0; j < sg.n && ok; ++j, ++at) {
+                    const int next_page = page_of(j + 1), key = sg.k0 + j * kTileKeys + strip * kStrip;
+                    const bool in = key < sg.kv1, there = in && unsigned(page) < unsigned(kv.n_pages);
+                    ok = __all_sync(FULL, bar_wait(empty(at), (at / NS + 1) & 1, gave_up));
+                    if (!ok) break;
+                    const unsigned none = __ballot_sync(FULL, lane < kStrips && in && !there), some = __ballot_sync(FULL, lane < 2 * kStrips && there);
+                    if (lane == 0) {
+                        gone[at % NS] = none;
+                        bar_expect(full(at), __popc(some) * KS);
+                    }
+                    __syncwarp();
+                    if (lane < 2 * kStrips && there)
+                        bulk_load(sbase + Sh::kOffRing + (at % NS) * Sh::kStage + lane * KS,
+                                  layer + page * page_bytes + ((lane / kStrips) * kv.n_kv_heads + sg.h) * head_bytes + key % P / kStrip * KS, KS, full(at));
+                    page = next_page;
+                }
+            }
+        }
+        all.n = 0;
+        if (ok) tell(all);
+        if (!ok) {  // let what is on its way arrive
+            for (uint32_t k = at > NS ? at - NS : 0; k < at; ++k)
+                for (int n = 0; n < 1000000 && !bar_try(full(k), (k / NS) & 1); ++n) {
+                }
+            if (lane == 0) atomicMin(kv.status, SIM_E_STATE);
+        }
+        return;
+    }
+
+    // ---- products, softmax, results: lane 4 g + t
+    const int g = lane >> 2, t = lane & 3;
+    const float c = a.scale_log2;
+    float *const all_o = reinterpret_cast<float *>(base + Sh::kOffO);
+    float2 *const all_m = reinterpret_cast<float2 *>(base + Sh::kOffM);
+    uint4 *const qs = reinterpret_cast<uint4 *>(base + Sh::kOffQ);
+    uint32_t at = 0, nj = 0;
+    bool ok = true;
+    const auto join = [&] {  // the warps, by a barrier whose wait ends even if some have given up
+        __syncwarp();
+        if (lane == 0) bar_arrive(joined);
+        ok = __all_sync(FULL, bar_wait(joined, nj++ & 1, gave_up)) && ok;
+    };
+    for (uint32_t x = 0; ok; ++x) {
+        ok = __all_sync(FULL, bar_wait(seg_full(x), (x / kSegs) & 1, gave_up)) != 0;
+        if (!ok) break;
+        const Segment &sg = segs[x % kSegs];
+        const int n = sg.n, rows = sg.rows, kv1 = sg.kv1;
+        if (n == 0) break;
+        const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
+        // Queries, 8 columns of a row at a time: the second operand of two products; rows and columns that are not there are zeros.
+        for (int i = tid; i < NT * DG * 32; i += 32 * W) {
+            const int l = i % 32, j = i / 32 % DG, y = i / 32 / DG * 8 + l / 4, d = 32 * j + 8 * (l % 4);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (y < rows && d < D) {
+                const int z = sg.row0 + y, tok = a.group.div(z);
+                const uint16_t *from = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0 + tok) * a.qt + int64_t(sg.h * G + z - tok * G) * a.qh + d;
+                if (a.q_vec) v = *reinterpret_cast<const uint4 *>(from);
+                else v = make_uint4(from[0] | uint32_t(from[1]) << 16, from[2] | uint32_t(from[3]) << 16, from[4] | uint32_t(from[5]) << 16,
+                                    from[6] | uint32_t(from[7]) << 16);
+            }
+            qs[i] = v;
+        }
+        join();
+        if (!ok) break;
+        uint4 q1[NT == 1 ? DG : 1];  // 8 rows: in registers
+        if constexpr (NT == 1)
+#pragma unroll
+            for (int j = 0; j < DG; ++j) q1[j] = qs[j * 32 + lane];
+        const int all_see = sink.seen(0);  // keys that every row sees: rows are in the order of their tokens
+        float o[NT][2 * DG][4], m[NT][2], sum[NT][2];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+#pragma unroll
+            for (int z = 0; z < 2 * DG; ++z) o[i][z][0] = o[i][z][1] = o[i][z][2] = o[i][z][3] = 0.f;
+            m[i][0] = m[i][1] = -INFINITY;
+            sum[i][0] = sum[i][1] = 0.f;
+        }
+#pragma unroll 1
+        for (int tile = 0; tile < n; ++tile, ++at) {
+            ok = __all_sync(FULL, bar_wait(full(at), (at / NS) & 1, gave_up));
+            if (!ok) break;
+            const uint32_t no_page = gone[at % NS];
+#pragma unroll 1
+            for (int strip = warp; strip < kStrips; strip += W) {
+                const int key0 = sg.k0 + tile * kTileKeys + strip * kStrip;
+                if (key0 >= kv1) break;
+                const unsigned char *const ks = base + Sh::kOffRing + (at % NS) * Sh::kStage + strip * KS, *const vs = ks + kStrips * KS;
+                const uint32_t there = no_page >> strip & 1 ? 0u : FULL;
+                // S': lane has keys g and g + 8, rows 2 t and 2 t + 1 of each 8
+                float s[NT][4];
+#pragma unroll
+                for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+                {
+                    uint32_t k0[DG], k1[DG], e0[DG], e1[DG];
+                    words<DG>(ks + 16 * DG * g + 4 * DG * t, k0);
+                    words<DG>(ks + 16 * DG * (g + 8) + 4 * DG * t, k1);
+                    words<DG>(ks + 256 * DG + 4 * DG * g, e0);
+                    words<DG>(ks + 256 * DG + 4 * DG * (g + 8), e1);
+#pragma unroll
+                    for (int j = 0; j < DG; ++j) {
+                        uint32_t u[4], v[4];
+                        values4<BF>(k0[j], low_twice(e0[j] & there), high_twice(e0[j] & there), u);
+                        values4<BF>(k1[j], low_twice(e1[j] & there), high_twice(e1[j] & there), v);
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            uint4 q;
+                            if constexpr (NT == 1) q = q1[j];
+                            else q = qs[(i * DG + j) * 32 + lane];
+                            product<BF>(s[i], u[0], v[0], u[1], v[1], q.x, q.y);
+                            product<BF>(s[i], u[2], v[2], u[3], v[3], q.z, q.w);
+                        }
+                    }
+                }
+                const bool blind = key0 + kStrip > all_see;
+                if (blind) {
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int lim = sink.seen(8 * i + 2 * t + z);
+                            if (key0 + g >= lim) s[i][z] = -INFINITY;
+                            if (key0 + g + 8 >= lim) s[i][2 + z] = -INFINITY;
+                        }
+                }
+                bool grows = false;
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) grows |= fmaf(s[i][z], c, -m[i][z & 1]) > kGrow;
+                if (__any_sync(FULL, grows)) {
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            float top = fmaxf(s[i][z], s[i][2 + z]);
+#pragma unroll
+                            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
+                            top *= c;
+                            if (top - m[i][z] > kGrow) {  // each row for itself: what it becomes does not hang on the rows beside it
+                                const float f = ex2(m[i][z] - top);
+                                m[i][z] = top;
+                                sum[i][z] *= f;
+#pragma unroll
+                                for (int y = 0; y < 2 * DG; ++y) {
+                                    o[i][y][z] *= f;
+                                    o[i][y][2 + z] *= f;
+                                }
+                            }
+                        }
+                }
+                uint32_t p[NT][2];
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const float mz = m[i][z & 1];
+                        s[i][z] = ex2(fmaf(s[i][z], c, mz == -INFINITY ? 0.f : kv_lift(BF) - mz));
+                        sum[i][z & 1] += s[i][z];
+                    }
+                    p[i][0] = turned(pack<BF>(s[i][0], s[i][1]));
+                    p[i][1] = turned(pack<BF>(s[i][2], s[i][3]));
+                }
+                uint32_t v0[DG], v1[DG], f0[2 * DG], f1[2 * DG];
+                words<DG>(vs + 4 * DG * lane, v0);
+                words<DG>(vs + 128 * DG + 4 * DG * lane, v1);
+                words<2 * DG>(vs + 256 * DG + 8 * DG * t, f0);
+                words<2 * DG>(vs + 256 * DG + 8 * DG * (t + 4), f1);
+                if (blind || !there) {  // values past the end of the keys, whatever they are, must not meet their zero probabilities
+                    const auto kept = [&](int key) { return (key < kv1 ? 0xffffu : 0u) & there; };
+                    const uint32_t m0 = kept(key0 + 2 * t) | kept(key0 + 2 * t + 1) << 16, m1 = kept(key0 + 8 + 2 * t) | kept(key0 + 9 + 2 * t) << 16;
+#pragma unroll
+                    for (int j = 0; j < DG; ++j) {
+                        f0[2 * j] &= m0, f0[2 * j + 1] &= m0;
+                        f1[2 * j] &= m1, f1[2 * j + 1] &= m1;
+                        // Nor may a group that is not a number meet rows that do not see it: it is left out, and those that do are spoilt.
+                        constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
+                        const auto odd = [&](const uint32_t *f, int half) {
+                            const uint32_t st = f[2 * j] >> (16 * half), lo = f[2 * j + 1] >> (16 * half);
+                            return (st & kExp) == kExp || (lo & kExp) == kExp;
+                        };
+                        const bool b0 = odd(f0, 0), b1 = odd(f0, 1), b2 = odd(f1, 0), b3 = odd(f1, 1);
+                        if (__any_sync(FULL, b0 || b1 || b2 || b3)) {
+                            int first = INT_MAX;  // of such keys
+                            if (b3) first = key0 + 9 + 2 * t;
+                            if (b2) first = key0 + 8 + 2 * t;
+                            if (b1) first = key0 + 1 + 2 * t;
+                            if (b0) first = key0 + 2 * t;
+                            first = __reduce_min_sync(FULL, first);
+                            const uint32_t n0 = (b0 ? 0u : 0xffffu) | (b1 ? 0u : 0xffff0000u), n1 = (b2 ? 0u : 0xffffu) | (b3 ? 0u : 0xffff0000u);
+                            f0[2 * j] &= n0, f0[2 * j + 1] &= n0;
+                            f1[2 * j] &= n1, f1[2 * j + 1] &= n1;
+#pragma unroll
+                            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                                for (int z = 0; z < 2; ++z)
+                                    if (first < sink.seen(8 * i + 2 * t + z)) {
+                                        o[i][2 * j][z] = o[i][2 * j][2 + z] = NAN;
+                                        o[i][2 * j + 1][z] = o[i][2 * j + 1][2 + z] = NAN;
+                                    }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < DG; ++j) {
+                    uint32_t u[4], v[4];
+                    values4<BF>(v0[j], f0[2 * j], f0[2 * j + 1], u);
+                    values4<BF>(v1[j], f1[2 * j], f1[2 * j + 1], v);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        product<BF>(o[i][2 * j], u[0], u[1], v[0], v[1], p[i][0], p[i][1]);
+                        product<BF>(o[i][2 * j + 1], u[2], u[3], v[2], v[3], p[i][0], p[i][1]);
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(empty(at));
+        }
+        if (!ok) break;
+        // The warps' shares: columns 32 j + 4 g + (0 .. 3) of rows 2 t and 2 t + 1 of each 8.
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                float l = sum[i][z];
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) l += __shfl_xor_sync(FULL, l, d);
+                if (g == 0) all_m[warp * R + 8 * i + 2 * t + z] = make_float2(m[i][z], l);
+            }
+        // What warp w's share of row y is multiplied by, in units of the highest maximum.
+        const auto top_of = [&](int y) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < W; ++w) top = fmaxf(top, all_m[w * R + y].x);
+            return top;
+        };
+        const auto factor = [&](int w, int y, float top) {
+            const float2 ml = all_m[w * R + y];
+            return ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2(ml.x - top);  // a sum without a maximum is not a number
+        };
+        const auto total_of = [&](int y, float top) {
+            float total = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float f = factor(w, y, top);
+                if (f != 0.f) total = fmaf(all_m[w * R + y].y, f, total);
+            }
+            return total;
+        };
+#pragma unroll
+        for (int i0 = 0; i0 < NT; i0 += Sh::kPart) {
+            if (i0 > 0) {
+                if (8 * i0 >= rows) break;
+                join();  // the part before has been read
+                if (!ok) break;
+            }
+#pragma unroll
+            for (int i = 0; i < Sh::kPart; ++i)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    float *const to = all_o + (warp * 8 * Sh::kPart + 8 * i + 2 * t + z) * Sh::kPitch + 4 * g;
+                    const auto &x4 = o[i0 + i];
+#pragma unroll
+                    for (int j = 0; j < DG; ++j)
+                        *reinterpret_cast<float4 *>(to + 32 * j) = make_float4(x4[2 * j][z], x4[2 * j][2 + z], x4[2 * j + 1][z], x4[2 * j + 1][2 + z]);
+                }
+            join();
+            if (!ok) break;
+            for (int e = tid; e < min(rows - 8 * i0, 8 * Sh::kPart) * 8 * DG; e += 32 * W) {
+                const int in = e / (8 * DG), y = 8 * i0 + in, d = e % (8 * DG) * 4;
+                if (d >= D) continue;
+                const float top = top_of(y), total = total_of(y, top);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float f = factor(w, y, top);
+                    const float4 u = *reinterpret_cast<const float4 *>(all_o + (w * 8 * Sh::kPart + in) * Sh::kPitch + d);
+                    if (f != 0.f) v = make_float4(fmaf(u.x, f, v.x), fmaf(u.y, f, v.y), fmaf(u.z, f, v.z), fmaf(u.w, f, v.w));
+                }
+                const typename Sink<BF>::Joint joint = sink.joint(top - kv_lift(BF), total, sink.before(y));
+                const float f = joint.mine, fb = joint.before;
+                v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+                float4 *const part = reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d);
+                if (fb != 0.f) {
+                    const float4 u = *part;
+                    v = make_float4(fmaf(u.x, fb, v.x), fmaf(u.y, fb, v.y), fmaf(u.z, fb, v.z), fmaf(u.w, fb, v.w));
+                }
+                if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d) = make_uint2(pack<BF>(v.x, v.y), pack<BF>(v.z, v.w));
+                else *part = v;
+            }
+        }
+        if (!ok) break;
+        // the joint sums, once all have read the ones before
+        if (sg.joins) join();
+        if (!ok) break;
+        for (int y = tid; y < rows; y += 32 * W) {
+            const float top = top_of(y);
+            sink.lse(y, sink.joint(top - kv_lift(BF), total_of(y, top), sink.before(y)).e);
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(seg_empty(x));
+    }
+    if (!ok && lane == 0) atomicMin(kv.status, SIM_E_STATE);
+}
+
+template <int DG, int NT, bool BF>
+cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+    constexpr int W = NT == 1 ? 8 : 4;
+    using Sh = Shape<DG, NT, W>;
+    static thread_local int ready = -1;  // the device on which the kernel has its shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev != ready) {
+        e = cudaFuncSetAttribute((const void *)k_4bit<DG, NT, W, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
+        if (e == cudaSuccess) ready = dev;
+    }
+    return e == cudaSuccess ? launch_chained(k_4bit<DG, NT, W, BF>, kv_blocks(a.sms, light), Sh::kThreads, Sh::kBytes, st, kv, b, a, light) : e;
+}
+
+template <int DG, bool BF>
+cudaError_t launch_rows(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+    // Rows of a pass by what entries have on average; items with more are gone over again.
+    const int64_t G = b.q_heads / kv.n_kv_heads, rows = light ? (int64_t(b.n_q) * G + std::max(b.n, 1) - 1) / std::max(b.n, 1) : kAttRows;
+    if (rows <= 8) return launch<DG, 1, BF>(kv, b, a, light, st);
+    return rows <= 16 ? launch<DG, 2, BF>(kv, b, a, light, st) : launch<DG, 4, BF>(kv, b, a, light, st);
+}
+
+template <bool BF>
+cudaError_t launch_dims(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+    switch (kv_dim_groups(kv)) {
+        case 1: return launch_rows<1, BF>(kv, b, a, light, st);
+        case 2: return launch_rows<2, BF>(kv, b, a, light, st);
+        case 3: return launch_rows<3, BF>(kv, b, a, light, st);
+        default: return launch_rows<4, BF>(kv, b, a, light, st);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_kv_4bit(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+    return kv_bf(kv) ? launch_dims<true>(kv, b, a, light, st) : launch_dims<false>(kv, b, a, light, st);
+}
+
+}  // namespace simgb

@@ -39,7 +39,7 @@ bool aligned(const void *p, unsigned a) { return reinterpret_cast<uintptr_t>(p) 
 // Null, or what is wrong with the sizes.
 const char *bad_sizes(const sim_kv *kv) {
     if (!kv) return "NULL cache";
-    if (kv->dtype != SIM_KV_BF16 && kv->dtype != SIM_KV_F16) return "dtype must be SIM_KV_BF16 or SIM_KV_F16";
+    if (kv->dtype != SIM_KV_BF16 && kv->dtype != SIM_KV_F16 && !simgb::kv_4bit(*kv)) return "dtype must be a sim_kv_dtype";
     if (kv->n_pages < 1 || kv->n_pages > 1 << 28) return "n_pages outside [1, 2^28]";
     if (kv->n_layers < 1 || kv->n_layers > 1 << 16 || kv->n_kv_heads < 1 || kv->n_kv_heads > 1 << 16) return "n_layers and n_kv_heads must be in [1, 2^16]";
     if (kv->page_size != 16 && kv->page_size != 32 && kv->page_size != 64 && kv->page_size != 128) return "page_size must be 16, 32, 64 or 128";
@@ -89,6 +89,8 @@ extern "C" {
 
 int64_t sim_kv_scratch_bytes(const sim_kv *kv) { return bad_sizes(kv) ? 0 : simgb::kv_scratch_ints(*kv) * 4; }
 
+int64_t sim_kv_pool_bytes(const sim_kv *kv) { return bad_sizes(kv) ? 0 : kv->n_pages * simgb::kv_page_bytes(*kv); }
+
 int sim_kv_extend(const sim_kv *kv, int32_t n, const int32_t *seqs, const int32_t *cu_new, int32_t n_new, int64_t *slots,
                   void *cuda_stream) {
     if (const char *m = bad_entries(kv, n, seqs, cu_new)) return fail(SIM_E_INVAL, "sim_kv_extend: %s", m);
@@ -105,7 +107,21 @@ int sim_kv_write(const sim_kv *kv, int32_t layer, int32_t n_new, const int64_t *
     if (n_new == 0) return SIM_OK;
     if (!slots || !k || !v || !aligned(k, 2) || !aligned(v, 2)) return fail(SIM_E_INVAL, "sim_kv_write: NULL or odd pointer");
     const simgb::KvWrite w = {k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride, slots, layer, n_new};
-    return done(simgb::launch_kv_write(*kv, w, static_cast<cudaStream_t>(cuda_stream)), "sim_kv_write");
+    const auto launch = simgb::kv_4bit(*kv) ? simgb::launch_kv_write_4bit : simgb::launch_kv_write;
+    return done(launch(*kv, w, static_cast<cudaStream_t>(cuda_stream)), "sim_kv_write");
+}
+
+int sim_kv_read(const sim_kv *kv, int32_t layer, int32_t n, const int32_t *seqs, const int32_t *cu, const int32_t *first, int32_t total, void *k,
+                int64_t k_token_stride, int64_t k_head_stride, void *v, int64_t v_token_stride, int64_t v_head_stride, void *cuda_stream) {
+    if (const char *m = bad_cache(kv)) return fail(SIM_E_INVAL, "sim_kv_read: %s", m);
+    if (layer < 0 || layer >= kv->n_layers) return fail(SIM_E_INVAL, "sim_kv_read: layer %d outside [0, %d)", layer, kv->n_layers);
+    if (n < 0 || n > simgb::kKvMaxSeqs || total < 0) return fail(SIM_E_INVAL, "sim_kv_read: n outside [0, 2^17] or total < 0");
+    if (!cu || (n > 0 && !seqs)) return fail(SIM_E_INVAL, "sim_kv_read: NULL list of entries");
+    if (total == 0) return SIM_OK;
+    if (!k || !v || !aligned(k, 16) || !aligned(v, 16) || k_token_stride % 8 || k_head_stride % 8 || v_token_stride % 8 || v_head_stride % 8)
+        return fail(SIM_E_INVAL, "sim_kv_read: k and v must be 16-byte aligned with strides that are multiples of 8");
+    const simgb::KvRead r = {seqs, cu, first, k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride, layer, n, total};
+    return done(simgb::launch_kv_read(*kv, r, static_cast<cudaStream_t>(cuda_stream)), "sim_kv_read");
 }
 
 int sim_kv_fork(const sim_kv *kv, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *tokens, void *cuda_stream) {

@@ -585,7 +585,8 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
 cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
     if (!encode_fn()) return cudaErrorNotSupported;
     KvMaps maps = {};
-    for (int v = 0; v < 2; ++v) {
+    const bool packed = kv_4bit(kv);
+    for (int v = 0; v < 2 && !packed; ++v) {
         uint16_t *at = static_cast<uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + v * (kv_layer_elems(kv) / 2);
         const uint64_t dim[4] = {uint64_t(kv.head_dim), uint64_t(kv.page_size), uint64_t(kv.n_kv_heads), uint64_t(kv.n_pages)};
         const uint64_t stride[3] = {uint64_t(kv.head_dim) * 2, uint64_t(kv.head_dim) * 2 * kv.page_size, uint64_t(kv_page_bytes(kv))};
@@ -594,13 +595,13 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     }
     const int64_t rows = int64_t(b.n_q) * b.q_heads;
     cudaError_t e = cudaSuccess;
-    if (!kv_light_only(kv, b)) e = launch_kv_heavy(kv, b, a, maps, st);
-    if (e == cudaSuccess) e = launch_kv_light(kv, b, a, maps, st);
+    if (!kv_light_only(kv, b)) e = packed ? launch_kv_4bit(kv, b, a, 0, st) : launch_kv_heavy(kv, b, a, maps, st);
+    if (e == cudaSuccess) e = packed ? launch_kv_4bit(kv, b, a, 1, st) : launch_kv_light(kv, b, a, maps, st);
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
     const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 5));
-    return launch_chained(kv.dtype == SIM_KV_BF16 ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
+    return launch_chained(kv_bf(kv) ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 
 }  // namespace simgb

@@ -417,5 +417,7 @@ struct KvMaps {
 bool kv_encode_map(const sim_kv &kv, CUtensorMap *map, int rank, const void *at, const uint64_t *dim, const uint64_t *stride, const uint32_t *box);
 cudaError_t launch_kv_heavy(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
 cudaError_t launch_kv_light(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
+// Of a 4-bit cache: one list, the heavy (0) or the light (1).
+cudaError_t launch_kv_4bit(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st);
 
 }  // namespace simgb

@@ -1,5 +1,5 @@
 // Declarations shared by the C ABI of the paged cache (sim_kv_api.cpp) and its kernels (sim_kv.cu, sim_kv_attend.cu,
-// sim_kv_heavy.cu, sim_kv_light.cu).
+// sim_kv_heavy.cu, sim_kv_light.cu; of 4-bit caches sim_kv_4bit.cu, sim_kv_4bit_light.cu).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -30,8 +30,17 @@ __host__ __device__ inline KvScratch kv_scratch(const sim_kv &kv) {
     return s;
 }
 
-__host__ __device__ inline int64_t kv_layer_elems(const sim_kv &kv) { return 2 * int64_t(kv.n_kv_heads) * kv.page_size * kv.head_dim; }
-__host__ __device__ inline int64_t kv_page_bytes(const sim_kv &kv) { return 2 * kv.n_layers * kv_layer_elems(kv); }
+__host__ __device__ inline bool kv_bf(const sim_kv &kv) { return kv.dtype == SIM_KV_BF16 || kv.dtype == SIM_KV_BF16_4BIT; }
+__host__ __device__ inline bool kv_4bit(const sim_kv &kv) { return kv.dtype == SIM_KV_BF16_4BIT || kv.dtype == SIM_KV_F16_4BIT; }
+// A 4-bit cache: groups of 32 values of a token's head, the last one shorter; strips of 16 tokens of a head, 20 bytes a token and group.
+constexpr int kStrip = 16;
+__host__ __device__ inline int kv_dim_groups(const sim_kv &kv) { return (kv.head_dim + 31) / 32; }
+__host__ __device__ inline int64_t kv_strip_bytes(const sim_kv &kv) { return 20 * kStrip * kv_dim_groups(kv); }
+__host__ __device__ inline int64_t kv_layer_elems(const sim_kv &kv) { return 2 * int64_t(kv.n_kv_heads) * kv.page_size * kv.head_dim; }  // 16-bit caches
+__host__ __device__ inline int64_t kv_head_bytes(const sim_kv &kv) {  // a page's keys, or values, of one head
+    return kv.page_size * (kv_4bit(kv) ? 20 * int64_t(kv_dim_groups(kv)) : 2 * int64_t(kv.head_dim));
+}
+__host__ __device__ inline int64_t kv_page_bytes(const sim_kv &kv) { return kv.n_layers * (2 * int64_t(kv.n_kv_heads)) * kv_head_bytes(kv); }
 
 // n / d for 0 <= n < 2^31 and 1 <= d < 2^31 by a multiplication: with 2^(k-1) < d <= 2^k, m = ceil(2^(31+k) / d)
 // < 2^32 gives floor(n m / 2^(31+k)), since n (m d - 2^(31+k)) < n 2^k <= 2^(31+k).
@@ -65,6 +74,15 @@ struct KvWrite {
     int32_t layer, n_new;
 };
 cudaError_t launch_kv_write(const sim_kv &kv, const KvWrite &w, cudaStream_t st);
+
+struct KvRead {
+    const int32_t *seqs, *cu, *first;
+    void *k, *v;
+    int64_t kt, kh, vt, vh;  // strides in elements
+    int32_t layer, n, total;
+};
+cudaError_t launch_kv_read(const sim_kv &kv, const KvRead &r, cudaStream_t st);
+cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_t st);
 
 // Items of more than 32 rows are heavy, the others light: two lists, each divided among blocks of its own.
 constexpr int kAttRows = 256;   // query rows of a heavy item, at most

@@ -51,37 +51,58 @@ class AttentionPlan:
 class KVCache:
     """``n_pages`` pages of ``page_size`` tokens, each with the keys and values of all layers and kv heads; up to
     ``max_seqs`` sequences of up to ``max_pages`` pages.  ``pool`` [n_pages, n_layers, 2, n_kv_heads, page_size,
-    head_dim], ``table`` [max_seqs, max_pages], ``length`` [max_seqs] and ``ref`` [n_pages] are its state."""
+    head_dim], ``table`` [max_seqs, max_pages], ``length`` [max_seqs] and ``ref`` [n_pages] are its state.
+
+    With ``bits=4`` keys and values of the type ``dtype`` are quantised as they are written: each 32 of a token's head (the last ones:
+    fewer) are held as their lowest, a step and 4 bits each, 5 bits a value in all; ``pool`` is then uint8 [n_pages, n_layers, 2,
+    n_kv_heads, page_size, 20 ceil(head_dim / 32)], in strips of 16 tokens (``include/sim_kv.h``).  A value read back, or attended to, is
+    the 16-bit float nearest to lowest + code step, within half a step (a 30th of the distance from the lowest of its 32 to the highest, at most) of
+    the one written."""
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, max_seqs: int, max_pages: int,
-                 n_layers: int = 1, dtype=None, device="cuda"):
+                 n_layers: int = 1, dtype=None, device="cuda", bits: int = 16):
         import torch
+        if bits not in (4, 16):
+            raise ValueError("bits must be 4 or 16")
         ints = dict(dtype=torch.int32, device=device)
-        self._set(torch.empty(n_pages, n_layers, 2, n_kv_heads, page_size, head_dim, dtype=dtype or torch.bfloat16, device=device),
-                  torch.full((max_seqs, max_pages), -1, **ints), torch.zeros(max_seqs, **ints), torch.zeros(n_pages, **ints))
+        dtype = dtype or torch.bfloat16
+        kind, last = (dtype, head_dim) if bits == 16 else (torch.uint8, 20 * -(-head_dim // 32))
+        self._set(torch.empty(n_pages, n_layers, 2, n_kv_heads, page_size, last, dtype=kind, device=device),
+                  torch.full((max_seqs, max_pages), -1, **ints), torch.zeros(max_seqs, **ints), torch.zeros(n_pages, **ints), head_dim, dtype)
 
     @classmethod
-    def wrap(cls, pool, table, length, ref) -> "KVCache":
-        """A cache over tensors that exist (laid out as above, on one CUDA device); nothing is copied."""
+    def wrap(cls, pool, table, length, ref, head_dim: int | None = None, dtype=None) -> "KVCache":
+        """A cache over tensors that exist (laid out as above, on one CUDA device); nothing is copied.  A uint8 pool is
+        one of 4 bits, which does not say its ``head_dim`` and ``dtype``."""
         self = cls.__new__(cls)
-        self._set(pool, table, length, ref)
+        self._set(pool, table, length, ref, head_dim, dtype)
         return self
 
-    def _set(self, pool, table, length, ref):
+    def _set(self, pool, table, length, ref, head_dim=None, dtype=None):
         import torch
-        if pool.dim() != 6 or pool.shape[2] != 2 or pool.dtype not in _dtypes() or not pool.is_cuda:
-            raise ValueError("pool must be a CUDA tensor [n_pages, n_layers, 2, n_kv_heads, page_size, head_dim] of bfloat16 or float16")
+        packed = pool.dtype == torch.uint8
+        if pool.dim() != 6 or pool.shape[2] != 2 or (not packed and pool.dtype not in _dtypes()) or not pool.is_cuda:
+            raise ValueError("pool must be a CUDA tensor [n_pages, n_layers, 2, n_kv_heads, page_size, head_dim] of bfloat16 or float16, "
+                             "or of uint8 for 4 bits")
         n_pages, n_layers, _, heads, page, dim = pool.shape
+        if packed:
+            if head_dim is None or dtype not in _dtypes() or dim != 20 * -(-head_dim // 32):
+                raise ValueError("a pool of 4 bits needs its dtype, bfloat16 or float16, and a head_dim with 20 ceil(head_dim / 32) bytes a token")
+            dim = head_dim
+        elif head_dim not in (None, dim) or dtype not in (None, pool.dtype):
+            raise ValueError(f"the pool is {pool.dtype} with head_dim {dim}")
+        else:
+            dtype = pool.dtype
         if table.dim() != 2 or length.shape != table.shape[:1] or ref.shape != (n_pages,):
             raise ValueError("table must be [max_seqs, max_pages], length [max_seqs] and ref [n_pages]")
         for x in (pool, table, length, ref):
             if not x.is_contiguous() or x.device != pool.device or (x is not pool and x.dtype != torch.int32):
                 raise ValueError("pool, table, length and ref must be contiguous, on one device, the last three int32")
         self.pool, self.table, self.length, self.ref = pool, table, length, ref
-        self.device, self.dtype = pool.device, pool.dtype
+        self.device, self.dtype, self.bits = pool.device, dtype, 4 if packed else 16
         self.status = torch.zeros(1, dtype=torch.int32, device=pool.device)
         self._kv = L.sim_kv(pool.data_ptr(), table.data_ptr(), length.data_ptr(), ref.data_ptr(), self.status.data_ptr(), None,
-                            _dtypes()[pool.dtype], n_pages, n_layers, heads, page, dim, table.shape[0], table.shape[1])
+                            _dtypes()[dtype] | (L.SIM_KV_4BIT if packed else 0), n_pages, n_layers, heads, page, dim, table.shape[0], table.shape[1])
         self._ref = ctypes.byref(self._kv)
         self._lib = L.lib()
         size = self._lib.sim_kv_scratch_bytes(self._ref)
@@ -178,7 +199,7 @@ class KVCache:
         return slots
 
     def write(self, slots, k, v, layer: int = 0, stream: int | None = None) -> None:
-        """Keys and values [n_new, n_kv_heads, head_dim] of one layer into their slots."""
+        """Keys and values [n_new, n_kv_heads, head_dim] of one layer into their slots; quantised in a cache of 4 bits."""
         n = slots.shape[0]
         if slots.dtype is not self._torch.int64 or slots.get_device() != self._index or slots.dim() != 1 or not slots.is_contiguous():
             raise ValueError(f"slots must be a contiguous int64 tensor on {self.device}")
@@ -188,6 +209,19 @@ class KVCache:
         if rc:
             self._fail(rc)
         self._lend(stream, slots, k, v)
+
+    def read(self, seqs, cu, n: int, layer: int = 0, first=None, stream: int | None = None):
+        """Cached keys and values of one layer, each [n, n_kv_heads, head_dim], in order: rows cu[i] .. cu[i + 1] - 1 are the
+        tokens of seqs[i] from first[i] on (0 by default).  Rows of an entry that is refused are zeros."""
+        m, st, torch = seqs.shape[0], self._stream(stream), self._torch
+        k, v = (self._empty(stream, (n, self._heads, self._dim), self.dtype) for _ in range(2))
+        at = self._heads * self._dim, self._dim
+        rc = self._lib.sim_kv_read(self._ref, layer, m, self._ints("seqs", seqs, m), self._ints("cu", cu, m + 1),
+                                   None if first is None else self._ints("first", first, m), n, k.data_ptr(), *at, v.data_ptr(), *at, st)
+        if rc:
+            self._fail(rc)
+        self._lend(stream, seqs, cu, first)
+        return k, v
 
     def fork(self, src, dst, tokens=None, stream: int | None = None) -> None:
         """dst[i] (empty) becomes the first tokens[i] tokens of src[i], on the same pages."""
