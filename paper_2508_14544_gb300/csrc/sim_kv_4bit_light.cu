@@ -57,15 +57,9 @@ __device__ __forceinline__ uint32_t turned(uint32_t x) {
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *from, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from), "r"(bytes),
-                 "r"(bar)
-                 : "memory");
-}
-
 template <int DG, int NT, int W, bool BF>
 __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
-    k_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int light) {
+    k_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a) {
     using Sh = Shape<DG, NT, W>;
     constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip;
     extern __shared__ __align__(128) unsigned char base[];
@@ -99,7 +93,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
     if (warp == W) {
         // ---- the line of work, and loads: lane l brings the keys of strip l, lane 8 + l its values
         const KvPlan plan = kv_plan(kv, b);
-        Line line(plan, kv.n_kv_heads, light, blockIdx.x, a.sms);
+        Line line(plan, kv.n_kv_heads, 1, blockIdx.x, a.sms);
         const int P = kv.page_size, strip = lane % kStrips;
         const int64_t head_bytes = kv_head_bytes(kv), page_bytes = kv_page_bytes(kv);
         const unsigned char *const layer = static_cast<const unsigned char *>(kv.pool) + int64_t(a.layer) * 2 * kv.n_kv_heads * head_bytes;
@@ -435,7 +429,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
 }
 
 template <int DG, int NT, bool BF>
-cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
     constexpr int W = NT == 1 ? 8 : 4;
     using Sh = Shape<DG, NT, W>;
     static thread_local int ready = -1;  // the device on which the kernel has its shared memory
@@ -445,31 +439,31 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, i
         e = cudaFuncSetAttribute((const void *)k_4bit<DG, NT, W, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
         if (e == cudaSuccess) ready = dev;
     }
-    return e == cudaSuccess ? launch_chained(k_4bit<DG, NT, W, BF>, kv_blocks(a.sms, light), Sh::kThreads, Sh::kBytes, st, kv, b, a, light) : e;
+    return e == cudaSuccess ? launch_chained(k_4bit<DG, NT, W, BF>, kv_blocks(a.sms, 1), Sh::kThreads, Sh::kBytes, st, kv, b, a) : e;
 }
 
 template <int DG, bool BF>
-cudaError_t launch_rows(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+cudaError_t launch_rows(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
     // Rows of a pass by what entries have on average; items with more are gone over again.
-    const int64_t G = b.q_heads / kv.n_kv_heads, rows = light ? (int64_t(b.n_q) * G + std::max(b.n, 1) - 1) / std::max(b.n, 1) : kAttRows;
-    if (rows <= 8) return launch<DG, 1, BF>(kv, b, a, light, st);
-    return rows <= 16 ? launch<DG, 2, BF>(kv, b, a, light, st) : launch<DG, 4, BF>(kv, b, a, light, st);
+    const int64_t G = b.q_heads / kv.n_kv_heads, rows = (int64_t(b.n_q) * G + std::max(b.n, 1) - 1) / std::max(b.n, 1);
+    if (rows <= 8) return launch<DG, 1, BF>(kv, b, a, st);
+    return rows <= 16 ? launch<DG, 2, BF>(kv, b, a, st) : launch<DG, 4, BF>(kv, b, a, st);
 }
 
 template <bool BF>
-cudaError_t launch_dims(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
+cudaError_t launch_dims(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
     switch (kv_dim_groups(kv)) {
-        case 1: return launch_rows<1, BF>(kv, b, a, light, st);
-        case 2: return launch_rows<2, BF>(kv, b, a, light, st);
-        case 3: return launch_rows<3, BF>(kv, b, a, light, st);
-        default: return launch_rows<4, BF>(kv, b, a, light, st);
+        case 1: return launch_rows<1, BF>(kv, b, a, st);
+        case 2: return launch_rows<2, BF>(kv, b, a, st);
+        case 3: return launch_rows<3, BF>(kv, b, a, st);
+        default: return launch_rows<4, BF>(kv, b, a, st);
     }
 }
 
 }  // namespace
 
-cudaError_t launch_kv_4bit(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st) {
-    return kv_bf(kv) ? launch_dims<true>(kv, b, a, light, st) : launch_dims<false>(kv, b, a, light, st);
+cudaError_t launch_kv_light_4bit(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
+    return kv_bf(kv) ? launch_dims<true>(kv, b, a, st) : launch_dims<false>(kv, b, a, st);
 }
 
 }  // namespace simgb

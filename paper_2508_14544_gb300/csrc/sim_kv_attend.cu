@@ -595,8 +595,8 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     }
     const int64_t rows = int64_t(b.n_q) * b.q_heads;
     cudaError_t e = cudaSuccess;
-    if (!kv_light_only(kv, b)) e = packed ? launch_kv_4bit(kv, b, a, 0, st) : launch_kv_heavy(kv, b, a, maps, st);
-    if (e == cudaSuccess) e = packed ? launch_kv_4bit(kv, b, a, 1, st) : launch_kv_light(kv, b, a, maps, st);
+    if (!kv_light_only(kv, b)) e = launch_kv_heavy(kv, b, a, maps, st);
+    if (e == cudaSuccess) e = packed ? launch_kv_light_4bit(kv, b, a, st) : launch_kv_light(kv, b, a, maps, st);
     if (e != cudaSuccess) return e;
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);

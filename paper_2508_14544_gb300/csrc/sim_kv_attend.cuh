@@ -189,6 +189,13 @@ __device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap *map, 
         : "memory");
 }
 
+// 16-byte aligned addresses and size.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from), "r"(bytes),
+                 "r"(bar)
+                 : "memory");
+}
+
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -347,6 +354,7 @@ struct Sink {
     // or not a number.  bad: a bit for each key of the tiles from blind_from on.  By one warp, a lane for four columns.
     __device__ void spoil(int y, const uint32_t *bad) const {
         const int lane = threadIdx.x & 31, P = kv.page_size, d = 4 * lane, from = blind_from(), stop = seen(y);
+        if (kv_4bit(kv)) return spoil_4bit(y, bad);
         const uint16_t *values = static_cast<const uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + kv_layer_elems(kv) / 2;
         float o[4] = {};
 #pragma unroll 1
@@ -375,6 +383,31 @@ struct Sink {
             if (o[i] == 0.f) continue;
             if (sg.direct) out_row(y)[d + i] = uint16_t(pack<BF>(o[i], o[i]));
             else a.part[(sg.row + y) * D + d + i] = o[i];
+        }
+    }
+    // The same of a 4-bit cache, where groups of 32 columns are not numbers.
+    __device__ void spoil_4bit(int y, const uint32_t *bad) const {
+        const int lane = threadIdx.x & 31, P = kv.page_size, d = 4 * lane, from = blind_from(), stop = seen(y), groups = kv_dim_groups(kv);
+        const unsigned char *values = static_cast<const unsigned char *>(kv.pool) + ((int64_t(a.layer) * 2 + 1) * kv.n_kv_heads + sg.h) * kv_head_bytes(kv);
+        bool odd = false;
+#pragma unroll 1
+        for (int z = 0; z < 4 * (sg.n - from); ++z)
+#pragma unroll 1
+            for (uint32_t left = bad[z]; left; left &= left - 1) {
+                const int key = sg.k0 + from * kTileKeys + z * 32 + __ffs(left) - 1;
+                if (key >= stop || d >= D) break;
+                const int page = kv.table[int64_t(sg.seq) * kv.max_pages + key / P], T = key % kStrip;
+                if (unsigned(page) >= unsigned(kv.n_pages)) continue;
+                const uint16_t *at = reinterpret_cast<const uint16_t *>(values + page * kv_page_bytes(kv) + key % P / kStrip * kv_strip_bytes(kv) + 256 * groups +
+                                                                        8 * groups * (T / 2) + 8 * (d / 32) + 2 * (T % 2));
+                constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
+                odd |= (at[0] & kExp) == kExp || (at[2] & kExp) == kExp;
+            }
+        if (!odd) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (sg.direct) out_row(y)[d + i] = 0x7fff;
+            else a.part[(sg.row + y) * D + d + i] = NAN;
         }
     }
     __device__ uint16_t *out_row(int y) const {  // of row y of the item
@@ -417,7 +450,6 @@ struct KvMaps {
 bool kv_encode_map(const sim_kv &kv, CUtensorMap *map, int rank, const void *at, const uint64_t *dim, const uint64_t *stride, const uint32_t *box);
 cudaError_t launch_kv_heavy(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
 cudaError_t launch_kv_light(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st);
-// Of a 4-bit cache: one list, the heavy (0) or the light (1).
-cudaError_t launch_kv_4bit(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, int light, cudaStream_t st);
+cudaError_t launch_kv_light_4bit(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st);
 
 }  // namespace simgb

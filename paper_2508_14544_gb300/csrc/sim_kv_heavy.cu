@@ -17,6 +17,7 @@
 // light items and join included).
 #include <type_traits>
 
+#include "sim_kv_4bit.cuh"
 #include "sim_kv_attend.cuh"
 
 namespace simgb {
@@ -85,26 +86,31 @@ __device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, u
     }
 }
 
-template <int DP>
+// DG: groups of 32 columns of a 4-bit cache, whose strips four more warps turn into tiles of 16-bit floats; 0: a 16-bit cache.
+template <int DP, int DG>
 struct Shape {
     static constexpr int kGroups = 2;
-    static constexpr int kThreads = kGroups * 128 + 128;
+    static constexpr int kThreads = kGroups * 128 + 128 + (DG ? 128 : 0);
     static constexpr int kTile = DP * 256;                                    // bytes of 128 query rows, or of a tile of keys or values
     static constexpr int kHalf = 16384;                                       // 128 rows of 64 columns
-    static constexpr int kSlots = 131072 / kTile;                             // tiles of keys or values in flight
+    static constexpr int kSlots = (DG ? 98304 : 131072) / kTile;              // tiles of keys or values in flight
+    static constexpr int kPacks = 2, kPack = 2 * kTileKeys / kStrip * 320 * DG;  // strips of a tile's keys and values in flight
     static constexpr int kTmem = 512;
     static constexpr int kOffO = kGroups * 128;                               // TMEM column of the first group's O
-    static constexpr int kSoftRegs = 208, kOtherRegs = 88;
-    static_assert(kGroups * kSoftRegs + kOtherRegs <= (kGroups + 1) * 168, "the launch gives 168 registers a thread: no more are handed out");
+    static constexpr int kSoftRegs = DG ? 192 : 208, kOtherRegs = DG ? 64 : 88;
+    static_assert(DG ? kGroups * kSoftRegs + 2 * kOtherRegs <= 4 * 128 : kGroups * kSoftRegs + kOtherRegs <= (kGroups + 1) * 168,
+                  "the launch gives 128 or 168 registers a thread: no more are handed out");
     static constexpr int kOffRing = kGroups * kTile;
-    static constexpr int kOffStage = kOffRing + kSlots * kTile;
+    static constexpr int kOffPack = kOffRing + kSlots * kTile;
+    static constexpr int kOffStage = kOffPack + kPacks * kPack;
     static constexpr int kOffSeg = kOffStage + kGroups * kStage * 4;
     // Keys with values that are not finite, in tiles that not all rows see whole, of segment x at x modulo twice kSegs: the warp
     // that finds them is less than that ahead of the softmax, without which no segment is told of kSegs later.
     static constexpr int kOffBad = kOffSeg + kSegs * int(sizeof(Segment));
     static constexpr int kOffBar = kOffBad + 2 * kSegs * kBlindTiles * 16;
-    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 4 * kGroups + 1 + kSlots;
-    static constexpr int kBytes = kOffBar + kBars * 8 + 16;
+    static constexpr int kBars = 2 * kSlots + 2 * kSegs + 2 + 4 * kGroups + 1 + (DG ? 2 * kPacks : kSlots);
+    static constexpr int kOffGone = kOffBar + kBars * 8 + 16;                 // of each kPack: strips on pages that the pool does not have
+    static constexpr int kBytes = kOffGone + (DG ? kPacks * 4 : 0);
     static constexpr int kAlloc = kBytes + 1024;                              // the base is rounded up to 1024
     static_assert(kAlloc <= 232448, "shared memory");
 };
@@ -165,10 +171,69 @@ __device__ __forceinline__ void softmax_tile(uint32_t t_s, uint32_t t_o, int lim
     tc_wait_st();
 }
 
-template <int DP, bool BF>
-__global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
+// The strips of a tile's keys, and those of its values, of a 4-bit cache, by four warps, two of each a warp: as 16-bit floats in
+// the places where TMA puts those of a 16-bit cache, without bank conflicts but two-way ones for the keys' codes.
+template <int DG, bool BF>
+__device__ __forceinline__ void unpack_keys(const unsigned char *strip, unsigned char *tile, int row0, int half, bool there) {
+    const int lane = threadIdx.x & 31, t = lane & 3;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int y = 8 * e + (lane >> 2 & 1) * 4 + (lane >> 3), r = row0 + y;  // 8 lanes write rows that differ in the swizzle's highest bit
+        uint32_t w[DG], q[DG];
+        words<DG>(strip + 16 * DG * y + 4 * DG * t, w);
+        words<DG>(strip + 256 * DG + 4 * DG * y, q);
+#pragma unroll
+        for (int j = 0; j < DG; ++j) {
+            uint32_t x[4];
+            const uint32_t f = there ? q[j] : 0;
+            values4<BF>(w[j], low_twice(f), high_twice(f), x);
+            *reinterpret_cast<uint4 *>(tile + j / 2 * half + r * 128 + ((j % 2 * 4 + t ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+    }
+}
+// keys: of the strip, the others' values are zeros; blind: so are those of keys with a group that is not a number, which are returned as bits.
+template <int DG, bool BF>
+__device__ __forceinline__ uint32_t unpack_values(const unsigned char *strip, unsigned char *tile, int row0, int half, int keys, bool blind) {
+    const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int y = 8 * e + 2 * t, r = row0 + y;
+        uint32_t w[DG], f[2 * DG];
+        words<DG>(strip + 128 * DG * e + 4 * DG * lane, w);
+        words<2 * DG>(strip + 256 * DG + 8 * DG * (t + 4 * e), f);
+        if (keys < kStrip || blind) {
+            const uint32_t kept = (y < keys ? 0xffffu : 0u) | (y + 1 < keys ? 0xffff0000u : 0u);
+            uint32_t odd = 0;
+            constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
+#pragma unroll
+            for (int j = 0; j < 2 * DG; ++j) {
+                f[j] &= kept;
+                odd |= ((f[j] & kExp) == kExp ? 0xffffu : 0u) | ((f[j] >> 16 & kExp) == kExp ? 0xffff0000u : 0u);
+            }
+            if (blind) {
+                bad |= (odd & 1) << y | (odd >> 31) << (y + 1);
+#pragma unroll
+                for (int j = 0; j < 2 * DG; ++j) f[j] &= ~odd;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < DG; ++j) {
+            uint32_t x[4];
+            values4<BF>(w[j], f[2 * j], f[2 * j + 1], x);
+            unsigned char *const to = tile + j / 2 * half + r * 128 + (g & 1) * 8;
+            const int c = j % 2 * 4 + g / 2;
+            *reinterpret_cast<uint2 *>(to + ((c ^ (r & 7)) << 4)) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
+            *reinterpret_cast<uint2 *>(to + 128 + ((c ^ (r + 1 & 7)) << 4)) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+        }
+    }
+    return blind ? __reduce_or_sync(FULL, bad) : 0;
+}
+
+template <int DP, bool BF, int DG>
+__global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
     k_heavy(const sim_kv kv, const sim_kv_batch b, const KvAttend a, const __grid_constant__ KvMaps maps) {
-    using Sh = Shape<DP>;
+    using Sh = Shape<DP, DG>;
     constexpr int NS = Sh::kSlots, NG = Sh::kGroups;
     extern __shared__ unsigned char raw[];
     unsigned char *const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
@@ -191,16 +256,19 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
     // at.  No more than NS / 2 are loaded that are not yet multiplied.
     const auto look_at = [&](uint32_t x) { return bars + 8 * (kRest + 3 + 4 * NG + x % (NS / 2)); };
     const auto clean = [&](uint32_t x) { return bars + 8 * (kRest + 3 + 4 * NG + NS / 2 + x % (NS / 2)); };
+    const auto pack_full = [&](uint32_t x) { return bars + 8 * (kRest + 3 + 4 * NG + x % Sh::kPacks); };
+    const auto pack_empty = [&](uint32_t x) { return bars + 8 * (kRest + 3 + 4 * NG + Sh::kPacks + x % Sh::kPacks); };
+    uint32_t *const gone = reinterpret_cast<uint32_t *>(base + Sh::kOffGone);
     const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31, role = warp - 4 * NG;
 
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) {
-            bar_init(full(s), 1);
+            bar_init(full(s), DG ? 4 : 1);
             bar_init(empty(s), 1);
         }
         for (int s = 0; s < kSegs; ++s) {
             bar_init(seg_full(s), 1);
-            bar_init(seg_empty(s), 4 * NG + 3);
+            bar_init(seg_empty(s), 4 * NG + 3 + (DG ? 4 : 0));
         }
         bar_init(q_full, 2);
         bar_init(q_empty, 1);
@@ -211,21 +279,32 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             bar_init(o_full(g), 2);
         }
         bar_init(drained, 1);
-        for (int x = 0; x < NS / 2; ++x) {
+        for (int x = 0; x < NS / 2 && !DG; ++x) {
             bar_init(look_at(x), 1);
             bar_init(clean(x), 2);
+        }
+        for (int x = 0; x < Sh::kPacks && DG; ++x) {
+            bar_init(pack_full(x), 1);
+            bar_init(pack_empty(x), 4);
         }
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid == 128 * NG) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.keys) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.values) : "memory");
+        if (!DG) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.keys) : "memory");
+        if (!DG) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.values) : "memory");
         if (maps.q_boxes) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.queries) : "memory");
     }
     if (role == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)), "n"(Sh::kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if constexpr (DG % 2 == 1) {  // columns that no group has, which meet zeros: no numbers that are not finite
+        for (int i = tid; i < NS * kTileKeys * 4; i += Sh::kThreads) {
+            const int r = i / 4 % kTileKeys, c = 4 + i % 4;
+            *reinterpret_cast<uint4 *>(base + Sh::kOffRing + i / 4 / kTileKeys * Sh::kTile + (DP / 64 - 1) * Sh::kHalf + r * 128 + ((c ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+        }
+        smem_to_async();
     }
     tc_fence_before();
     __syncthreads();
@@ -263,6 +342,28 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                     bar_arrive(seg_full(x));
                 }
                 if (sg.n == 0) break;
+                if constexpr (DG > 0) {  // lane l brings the keys of strip l, lane 8 + l its values
+                    constexpr int kStrips = kTileKeys / kStrip, KS = 320 * DG;
+                    const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
+                    const int strip = lane % kStrips;
+                    const int64_t head_bytes = kv_head_bytes(kv), page_bytes = kv_page_bytes(kv);
+                    const unsigned char *const from = static_cast<const unsigned char *>(kv.pool) + ((int64_t(a.layer) * 2 + (lane / kStrips & 1)) * kv.n_kv_heads + sg.h) * head_bytes;
+                    for (int j = 0; j < sg.n && ok; ++j, ++at) {
+                        const int key = sg.k0 + j * kTileKeys + strip * kStrip, page = key < sg.kv1 ? row[key / P] : -1;
+                        const bool in = key < sg.kv1, there = in && unsigned(page) < unsigned(kv.n_pages);
+                        ok = __all_sync(FULL, bar_wait(pack_empty(at), (at / Sh::kPacks + 1) & 1, gave_up));
+                        if (!ok) break;
+                        const unsigned none = __ballot_sync(FULL, lane < kStrips && in && !there), some = __ballot_sync(FULL, lane < 2 * kStrips && there);
+                        if (lane == 0) {
+                            gone[at % Sh::kPacks] = none;
+                            bar_expect(pack_full(at), __popc(some) * KS);
+                        }
+                        __syncwarp();
+                        if (lane < 2 * kStrips && there)
+                            bulk_load(sbase + Sh::kOffPack + (at % Sh::kPacks) * Sh::kPack + lane * KS, from + page * page_bytes + key % P / kStrip * KS, KS, pack_full(at));
+                    }
+                    continue;
+                }
                 const int clean_from = Sink<BF>{kv, a, sg, G, D, b.q_heads}.clean_from();
                 const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
                 const int first = sg.k0 / P + lane;
@@ -295,10 +396,52 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                 }
             }
             if (!ok) {  // let what is on its way arrive
-                for (uint32_t k = at > NS ? at - NS : 0; k < at; ++k)
-                    for (int n = 0; n < 1000000 && !bar_try(full(k), (k / NS) & 1); ++n) {
+                constexpr uint32_t kRing = DG ? Sh::kPacks : NS;
+                for (uint32_t k = at > kRing ? at - kRing : 0; k < at; ++k)
+                    for (int n = 0; n < 1000000 && !bar_try(DG ? pack_full(k) : full(k), (k / kRing) & 1); ++n) {
                     }
                 if (lane == 0) atomicMin(kv.status, SIM_E_STATE);
+            }
+        } else if (DG > 0 && role >= 4) {
+            // ---- strips of a 4-bit cache: two of the keys', then two of the values', of each tile, a warp
+            if constexpr (DG > 0) {
+                Segment sg;
+                uint32_t at = 0, np = 0;
+                bool ok = true;
+                for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
+                    const int blind_from = Sink<BF>{kv, a, sg, G, D, b.q_heads}.blind_from();
+                    uint16_t *const bad = reinterpret_cast<uint16_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 8;
+                    for (int j = 0; j < sg.n && ok; ++j, ++np) {
+                        const unsigned char *const pack = base + Sh::kOffPack + (np % Sh::kPacks) * Sh::kPack;
+                        ok = __all_sync(FULL, bar_wait(pack_full(np), (np / Sh::kPacks) & 1, gave_up));
+                        if (!ok) break;
+                        const uint32_t none = gone[np % Sh::kPacks];
+#pragma unroll
+                        for (int v = 0; v < 2; ++v, ++at) {
+                            ok = __all_sync(FULL, bar_wait(empty(at), (at / NS + 1) & 1, gave_up));
+                            if (!ok) break;
+                            unsigned char *const tile = base + Sh::kOffRing + (at % NS) * Sh::kTile;
+#pragma unroll 1
+                            for (int z = 2 * (role - 4); z < 2 * (role - 4) + 2; ++z) {
+                                const int left = sg.kv1 - (sg.k0 + j * kTileKeys + z * kStrip);  // keys from the strip's first on
+                                const bool there = !(none >> z & 1);
+                                const unsigned char *const strip = pack + (v * (kTileKeys / kStrip) + z) * (320 * DG);
+                                if (v == 0) {
+                                    if (left > 0) unpack_keys<DG, BF>(strip, tile, z * kStrip, Sh::kHalf, there);
+                                } else {
+                                    const uint32_t found = unpack_values<DG, BF>(strip, tile, z * kStrip, Sh::kHalf, there ? max(left, 0) : 0, j >= blind_from);
+                                    if (j >= blind_from && lane == 0) bad[(j - blind_from) * 8 + z] = uint16_t(found);
+                                }
+                            }
+                            smem_to_async();
+                            __syncwarp();
+                            if (lane == 0) {
+                                bar_arrive(full(at));
+                                if (v) bar_arrive(pack_empty(np));
+                            }
+                        }
+                    }
+                }
             }
         } else if (role == 1) {
             // ---- tensor products: the whole warp keeps the same (uniform) state, one lane issues
@@ -339,7 +482,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
                     if (g <= last) keys(0, g);
                 for (int j = 0; j < n && ok; ++j) {
                     ok = wait_full(at + 2 * j + 1);
-                    if (ok && j >= clean_from) ok = wait(clean(nc), nc / (NS / 2) & 1), ++nc;
+                    if (!DG && ok && j >= clean_from) ok = wait(clean(nc), nc / (NS / 2) & 1), ++nc;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
                         if (g > last) break;
@@ -397,6 +540,7 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
             const int j = (tid & 63) % kVec;
             const bool has = j * 8 < D;
             const auto look = [&](const Segment &s, uint32_t x, uint32_t at, uint32_t &nc) {
+                if (DG) return true;
                 const Sink<BF> sink = {kv, a, s, G, D, b.q_heads};
                 const int blind_from = sink.blind_from();
                 uint32_t *const bad = reinterpret_cast<uint32_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 4;
@@ -529,13 +673,13 @@ __global__ void __launch_bounds__(Shape<DP>::kThreads, 1)
     }
 }
 
-template <int DP, bool BF>
+template <int DP, bool BF, int DG = 0>
 cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st) {
     static thread_local int ready = -1;  // the device on which the kernel has its shared memory
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && dev != ready) {
-        e = cudaFuncSetAttribute((const void *)k_heavy<DP, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kAlloc);
+        e = cudaFuncSetAttribute((const void *)k_heavy<DP, BF, DG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP, DG>::kAlloc);
         if (e == cudaSuccess) ready = dev;
     }
     // queries by TMA: 128 rows are 128 / G tokens of G heads
@@ -546,12 +690,20 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
         const uint32_t box[3] = {64, G, 128 / G};
         m.q_boxes = kv_encode_map(kv, &m.queries, 3, a.q, dim, stride, box);
     }
-    return e == cudaSuccess ? launch_chained(k_heavy<DP, BF>, kv_blocks(a.sms, 0), Shape<DP>::kThreads, Shape<DP>::kAlloc, st, kv, b, a, m) : e;
+    return e == cudaSuccess ? launch_chained(k_heavy<DP, BF, DG>, kv_blocks(a.sms, 0), Shape<DP, DG>::kThreads, Shape<DP, DG>::kAlloc, st, kv, b, a, m) : e;
 }
 
 }  // namespace
 
 cudaError_t launch_kv_heavy(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, const KvMaps &maps, cudaStream_t st) {
+    if (kv_4bit(kv)) {
+        switch (kv_dim_groups(kv)) {
+            case 1: return kv_bf(kv) ? launch<64, true, 1>(kv, b, a, maps, st) : launch<64, false, 1>(kv, b, a, maps, st);
+            case 2: return kv_bf(kv) ? launch<64, true, 2>(kv, b, a, maps, st) : launch<64, false, 2>(kv, b, a, maps, st);
+            case 3: return kv_bf(kv) ? launch<128, true, 3>(kv, b, a, maps, st) : launch<128, false, 3>(kv, b, a, maps, st);
+            default: return kv_bf(kv) ? launch<128, true, 4>(kv, b, a, maps, st) : launch<128, false, 4>(kv, b, a, maps, st);
+        }
+    }
     if (kv.dtype == SIM_KV_BF16) return kv.head_dim > 64 ? launch<128, true>(kv, b, a, maps, st) : launch<64, true>(kv, b, a, maps, st);
     return kv.head_dim > 64 ? launch<128, false>(kv, b, a, maps, st) : launch<64, false>(kv, b, a, maps, st);
 }
