@@ -46,12 +46,21 @@ __device__ __forceinline__ uint32_t add16(uint32_t a, uint32_t b) {
     return d;
 }
 
+// (a & b) | c, in one instruction.
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+
 // Codes at bits 4 I and 16 + 4 I of w, as the values that they stand for: a code is put under the exponent whose unit it is
 // (128 + code, 1024 + code), which is then taken away, exactly; lo + code step is rounded once.
 template <bool BF, int I>
 __device__ __forceinline__ uint32_t values(uint32_t w, uint32_t step, uint32_t lo) {
-    const uint32_t code = (w >> (4 * I) & 0x000f000fu) | (BF ? 0x43004300u : 0x64006400u);
-    return fma16<BF>(add16<BF>(code, BF ? 0xc300c300u : 0xe400e400u), step, lo);
+    // float16 has room for a code four bits further up, as 1024 + 16 code: two of the three shifts are not needed
+    constexpr bool kUp = !BF && I % 2 == 1;
+    const uint32_t code = and_or(I < (BF ? 1 : 2) ? w : w >> (BF ? 4 * I : 8), kUp ? 0x00f000f0u : 0x000f000fu, BF ? 0x43004300u : 0x64006400u);
+    return fma16<BF>(kUp ? fma16<BF>(code, 0x2c002c00u, 0xd400d400u) : add16<BF>(code, BF ? 0xc300c300u : 0xe400e400u), step, lo);
 }
 template <bool BF>
 __device__ __forceinline__ void values4(uint32_t w, uint32_t step, uint32_t lo, uint32_t *x) {

@@ -4,8 +4,9 @@
 // from: the strips are laid out for that (include/sim_kv.h), so that a byte goes from HBM through shared memory into a register and no
 // further.  Per warp and strip of 16 keys: S' = K Q' (16 keys x 8 query rows at a time, D / 16 products), P' = exp2(c (S' - m)), whose
 // 8 x 8 parts are turned over between the lanes, and O' += V' P' (D x 8, one product for each 16 columns).  Each warp keeps its own
-// running maximum, sum and O; the warps' shares are joined at the end of the segment.
+// running maximum (as off), sum and O; the warps' shares are joined at the end of the segment.
 #include <algorithm>
+#include <cfloat>
 
 #include "sim_kv_4bit.cuh"
 #include "sim_kv_attend.cuh"
@@ -19,16 +20,19 @@ constexpr int kStrips = kTileKeys / kStrip;  // of a tile
 // DG groups of 32 columns, NT times 8 query rows in a pass, W warps that compute and one that loads.
 template <int DG, int NT, int W>
 struct Shape {
+    static constexpr int kSteps = NT > 2 ? 1 : kStrips / W;  // strips that a warp takes at a time
     static constexpr int kThreads = 32 * (W + 1);
     static constexpr int kRows = 8 * NT;
     static constexpr int kBytesStrip = 320 * DG;
     static constexpr int kStage = 2 * kStrips * kBytesStrip;  // a tile's keys, then its values
-    static constexpr int kPart = NT > 2 ? 2 : NT;             // times 8 rows of O that are joined at a time
+    static constexpr int kPart = 1;                           // times 8 rows of O that are joined at a time
     static constexpr int kPitch = 32 * DG + 4;                // floats between rows of the warps' O
+    // All of these twice, so that one barrier for each segment, or part of it, is enough.
+    static constexpr int kSizeQ = NT * DG * 512, kSizeO = W * 8 * kPart * kPitch * 4, kSizeM = W * kRows * 8;
     static constexpr int kOffQ = 0;                           // queries: [NT][DG][lane] 16 bytes
-    static constexpr int kOffO = kOffQ + NT * DG * 512;       // [W][8 kPart][kPitch]
-    static constexpr int kOffM = kOffO + W * 8 * kPart * kPitch * 4;  // [W][kRows] maximum and sum
-    static constexpr int kOffSeg = kOffM + W * kRows * 8;
+    static constexpr int kOffO = kOffQ + 2 * kSizeQ;          // [W][8 kPart][kPitch]
+    static constexpr int kOffM = kOffO + 2 * kSizeO;          // [W][kRows] off and sum
+    static constexpr int kOffSeg = kOffM + 2 * kSizeM;
     static constexpr int kFixed = kOffSeg + kSegs * int(sizeof(Segment)) + 256;
     static constexpr int kStages = (114000 - kFixed) / kStage < 4 ? (114000 - kFixed) / kStage : 4;
     static constexpr int kOffRing = (kOffSeg + kSegs * int(sizeof(Segment)) + 127) / 128 * 128;
@@ -61,7 +65,7 @@ template <int DG, int NT, int W, bool BF>
 __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
     k_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a) {
     using Sh = Shape<DG, NT, W>;
-    constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip;
+    constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip, SP = Sh::kSteps;
     extern __shared__ __align__(128) unsigned char base[];
     const uint32_t sbase = smem_addr(base), bars = sbase + Sh::kOffBar;
     volatile int *const gave_up = reinterpret_cast<int *>(base + Sh::kOffGone + NS * 4);
@@ -156,115 +160,143 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
     // ---- products, softmax, results: lane 4 g + t
     const int g = lane >> 2, t = lane & 3;
     const float c = a.scale_log2;
-    float *const all_o = reinterpret_cast<float *>(base + Sh::kOffO);
-    float2 *const all_m = reinterpret_cast<float2 *>(base + Sh::kOffM);
-    uint4 *const qs = reinterpret_cast<uint4 *>(base + Sh::kOffQ);
-    uint32_t at = 0, nj = 0;
+    uint32_t at = 0, nj = 0, no = 0;
     bool ok = true;
     const auto join = [&] {  // the warps, by a barrier whose wait ends even if some have given up
         __syncwarp();
         if (lane == 0) bar_arrive(joined);
         ok = __all_sync(FULL, bar_wait(joined, nj++ & 1, gave_up)) && ok;
     };
-    for (uint32_t x = 0; ok; ++x) {
-        ok = __all_sync(FULL, bar_wait(seg_full(x), (x / kSegs) & 1, gave_up)) != 0;
-        if (!ok) break;
-        const Segment &sg = segs[x % kSegs];
-        const int n = sg.n, rows = sg.rows, kv1 = sg.kv1;
-        if (n == 0) break;
-        const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
-        // Queries, 8 columns of a row at a time: the second operand of two products; rows and columns that are not there are zeros.
-        for (int i = tid; i < NT * DG * 32; i += 32 * W) {
-            const int l = i % 32, j = i / 32 % DG, y = i / 32 / DG * 8 + l / 4, d = 32 * j + 8 * (l % 4);
+    const auto take = [&](uint32_t x) { return __all_sync(FULL, bar_wait(seg_full(x), (x / kSegs) & 1, gave_up)) != 0; };
+    // Queries, 8 columns of a row at a time: the second operand of two products; rows and columns that are not there are zeros.
+    constexpr int kFetch = (NT * DG + W - 1) / W;
+    uint4 query[kFetch];
+    const auto fetch = [&](const Segment &s) {
+#pragma unroll
+        for (int e = 0; e < kFetch; ++e) {
+            const int i = warp + W * e, j = i % DG, y = i / DG * 8 + g, d = 32 * j + 8 * t;
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (y < rows && d < D) {
-                const int z = sg.row0 + y, tok = a.group.div(z);
-                const uint16_t *from = static_cast<const uint16_t *>(a.q) + int64_t(sg.q0 + tok) * a.qt + int64_t(sg.h * G + z - tok * G) * a.qh + d;
+            if (y < s.rows && d < D) {
+                const int z = s.row0 + y, tok = a.group.div(z);
+                const uint16_t *from = static_cast<const uint16_t *>(a.q) + int64_t(s.q0 + tok) * a.qt + int64_t(s.h * G + z - tok * G) * a.qh + d;
                 if (a.q_vec) v = *reinterpret_cast<const uint4 *>(from);
                 else v = make_uint4(from[0] | uint32_t(from[1]) << 16, from[2] | uint32_t(from[3]) << 16, from[4] | uint32_t(from[5]) << 16,
                                     from[6] | uint32_t(from[7]) << 16);
             }
-            qs[i] = v;
+            query[e] = v;
         }
+    };
+    const auto queries = [&](uint32_t x) { return reinterpret_cast<uint4 *>(base + Sh::kOffQ + (x & 1) * Sh::kSizeQ); };
+    const auto place = [&](uint32_t x) {
+#pragma unroll
+        for (int e = 0; e < kFetch; ++e)
+            if (warp + W * e < NT * DG) queries(x)[(warp + W * e) * 32 + lane] = query[e];
+    };
+    ok = take(0);
+    if (ok && segs[0].n > 0) {
+        fetch(segs[0]);
+        place(0);
         join();
-        if (!ok) break;
+    }
+    for (uint32_t x = 0; ok; ++x) {
+        const Segment &sg = segs[x % kSegs], &next = segs[(x + 1) % kSegs];
+        const int n = sg.n, rows = sg.rows, kv1 = sg.kv1;
+        if (n == 0) break;
+        const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
+        const uint4 *const qs = queries(x);
         uint4 q1[NT == 1 ? DG : 1];  // 8 rows: in registers
         if constexpr (NT == 1)
 #pragma unroll
             for (int j = 0; j < DG; ++j) q1[j] = qs[j * 32 + lane];
         const int all_see = sink.seen(0);  // keys that every row sees: rows are in the order of their tokens
-        float o[NT][2 * DG][4], m[NT][2], sum[NT][2];
+        // off: what is added to a score, so that its power of two is its weight: 2^off is above one over the highest one's
+        float o[NT][2 * DG][4], off[NT][2], sum[NT][2];
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
 #pragma unroll
             for (int z = 0; z < 2 * DG; ++z) o[i][z][0] = o[i][z][1] = o[i][z][2] = o[i][z][3] = 0.f;
-            m[i][0] = m[i][1] = -INFINITY;
+            off[i][0] = off[i][1] = FLT_MAX;
             sum[i][0] = sum[i][1] = 0.f;
         }
 #pragma unroll 1
         for (int tile = 0; tile < n; ++tile, ++at) {
+            if (tile == n - 1) {  // the next segment's queries are on their way while this one ends
+                ok = take(x + 1);
+                if (!ok) break;
+                if (next.n > 0) fetch(next);
+            }
             ok = __all_sync(FULL, bar_wait(full(at), (at / NS) & 1, gave_up));
             if (!ok) break;
-            const uint32_t no_page = gone[at % NS];
+            const unsigned char *const stage = base + Sh::kOffRing + (at % NS) * Sh::kStage;
 #pragma unroll 1
-            for (int strip = warp; strip < kStrips; strip += W) {
-                const int key0 = sg.k0 + tile * kTileKeys + strip * kStrip;
+            for (int step = 0; step < kStrips / W; step += SP) {
+                const int strip0 = warp * (kStrips / W) + step, key0 = sg.k0 + tile * kTileKeys + strip0 * kStrip;
                 if (key0 >= kv1) break;
-                const unsigned char *const ks = base + Sh::kOffRing + (at % NS) * Sh::kStage + strip * KS, *const vs = ks + kStrips * KS;
-                const uint32_t there = no_page >> strip & 1 ? 0u : FULL;
+                const unsigned char *const ks = stage + strip0 * KS, *const vs = ks + kStrips * KS;
+                const uint32_t none = gone[at % NS] >> strip0;  // strips on pages that the pool does not have: zeros
                 // S': lane has keys g and g + 8, rows 2 t and 2 t + 1 of each 8
-                float s[NT][4];
+                float s[SP][NT][4];
 #pragma unroll
-                for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-                {
+                for (int y = 0; y < SP; ++y) {
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) s[y][i][0] = s[y][i][1] = s[y][i][2] = s[y][i][3] = 0.f;
                     uint32_t k0[DG], k1[DG], e0[DG], e1[DG];
-                    words<DG>(ks + 16 * DG * g + 4 * DG * t, k0);
-                    words<DG>(ks + 16 * DG * (g + 8) + 4 * DG * t, k1);
-                    words<DG>(ks + 256 * DG + 4 * DG * g, e0);
-                    words<DG>(ks + 256 * DG + 4 * DG * (g + 8), e1);
+                    words<DG>(ks + y * KS + 16 * DG * g + 4 * DG * t, k0);
+                    words<DG>(ks + y * KS + 16 * DG * (g + 8) + 4 * DG * t, k1);
+                    words<DG>(ks + y * KS + 256 * DG + 4 * DG * g, e0);
+                    words<DG>(ks + y * KS + 256 * DG + 4 * DG * (g + 8), e1);
+                    if (none >> y & 1) {
+#pragma unroll
+                        for (int j = 0; j < DG; ++j) e0[j] = e1[j] = 0;
+                    }
 #pragma unroll
                     for (int j = 0; j < DG; ++j) {
                         uint32_t u[4], v[4];
-                        values4<BF>(k0[j], low_twice(e0[j] & there), high_twice(e0[j] & there), u);
-                        values4<BF>(k1[j], low_twice(e1[j] & there), high_twice(e1[j] & there), v);
+                        values4<BF>(k0[j], low_twice(e0[j]), high_twice(e0[j]), u);
+                        values4<BF>(k1[j], low_twice(e1[j]), high_twice(e1[j]), v);
 #pragma unroll
                         for (int i = 0; i < NT; ++i) {
                             uint4 q;
                             if constexpr (NT == 1) q = q1[j];
                             else q = qs[(i * DG + j) * 32 + lane];
-                            product<BF>(s[i], u[0], v[0], u[1], v[1], q.x, q.y);
-                            product<BF>(s[i], u[2], v[2], u[3], v[3], q.z, q.w);
+                            product<BF>(s[y][i], u[0], v[0], u[1], v[1], q.x, q.y);
+                            product<BF>(s[y][i], u[2], v[2], u[3], v[3], q.z, q.w);
                         }
                     }
                 }
-                const bool blind = key0 + kStrip > all_see;
+                const bool blind = key0 + SP * kStrip > all_see;
                 if (blind) {
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
-                            const int lim = sink.seen(8 * i + 2 * t + z);
-                            if (key0 + g >= lim) s[i][z] = -INFINITY;
-                            if (key0 + g + 8 >= lim) s[i][2 + z] = -INFINITY;
+                            const int lim = sink.seen(8 * i + 2 * t + z) - key0 - g;
+#pragma unroll
+                            for (int y = 0; y < 2 * SP; ++y)
+                                if (8 * y >= lim) s[y / 2][i][y % 2 * 2 + z] = -INFINITY;
                         }
                 }
-                bool grows = false;
+                float over = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) grows |= fmaf(s[i][z], c, -m[i][z & 1]) > kGrow;
-                if (__any_sync(FULL, grows)) {
+                    for (int y = 0; y < SP; ++y) {
+                        over = max3(over, fmaf(s[y][i][0], c, off[i][0]), fmaf(s[y][i][1], c, off[i][1]));
+                        over = max3(over, fmaf(s[y][i][2], c, off[i][0]), fmaf(s[y][i][3], c, off[i][1]));
+                    }
+                if (__any_sync(FULL, over > kv_lift(BF) + kGrow)) {
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
-                            float top = fmaxf(s[i][z], s[i][2 + z]);
+                            float top = fmaxf(s[0][i][z], s[0][i][2 + z]);
+#pragma unroll
+                            for (int y = 1; y < SP; ++y) top = max3(top, s[y][i][z], s[y][i][2 + z]);
 #pragma unroll
                             for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
-                            top *= c;
-                            if (top - m[i][z] > kGrow) {  // each row for itself: what it becomes does not hang on the rows beside it
-                                const float f = ex2(m[i][z] - top);
-                                m[i][z] = top;
+                            if (fmaf(top, c, off[i][z]) > kv_lift(BF) + kGrow) {  // each row for itself: what it becomes does not hang on the rows beside it
+                                const float to = kv_lift(BF) - top * c, f = ex2(to - off[i][z]);
+                                off[i][z] = to;
                                 sum[i][z] *= f;
 #pragma unroll
                                 for (int y = 0; y < 2 * DG; ++y) {
@@ -274,67 +306,66 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
                             }
                         }
                 }
-                uint32_t p[NT][2];
+                uint32_t p[SP][NT][2];
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        const float mz = m[i][z & 1];
-                        s[i][z] = ex2(fmaf(s[i][z], c, mz == -INFINITY ? 0.f : kv_lift(BF) - mz));
-                        sum[i][z & 1] += s[i][z];
-                    }
-                    p[i][0] = turned(pack<BF>(s[i][0], s[i][1]));
-                    p[i][1] = turned(pack<BF>(s[i][2], s[i][3]));
-                }
-                uint32_t v0[DG], v1[DG], f0[2 * DG], f1[2 * DG];
-                words<DG>(vs + 4 * DG * lane, v0);
-                words<DG>(vs + 128 * DG + 4 * DG * lane, v1);
-                words<2 * DG>(vs + 256 * DG + 8 * DG * t, f0);
-                words<2 * DG>(vs + 256 * DG + 8 * DG * (t + 4), f1);
-                if (blind || !there) {  // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                    const auto kept = [&](int key) { return (key < kv1 ? 0xffffu : 0u) & there; };
-                    const uint32_t m0 = kept(key0 + 2 * t) | kept(key0 + 2 * t + 1) << 16, m1 = kept(key0 + 8 + 2 * t) | kept(key0 + 9 + 2 * t) << 16;
-#pragma unroll
-                    for (int j = 0; j < DG; ++j) {
-                        f0[2 * j] &= m0, f0[2 * j + 1] &= m0;
-                        f1[2 * j] &= m1, f1[2 * j + 1] &= m1;
-                        // Nor may a group that is not a number meet rows that do not see it: it is left out, and those that do are spoilt.
-                        constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
-                        const auto odd = [&](const uint32_t *f, int half) {
-                            const uint32_t st = f[2 * j] >> (16 * half), lo = f[2 * j + 1] >> (16 * half);
-                            return (st & kExp) == kExp || (lo & kExp) == kExp;
-                        };
-                        const bool b0 = odd(f0, 0), b1 = odd(f0, 1), b2 = odd(f1, 0), b3 = odd(f1, 1);
-                        if (__any_sync(FULL, b0 || b1 || b2 || b3)) {
-                            int first = INT_MAX;  // of such keys
-                            if (b3) first = key0 + 9 + 2 * t;
-                            if (b2) first = key0 + 8 + 2 * t;
-                            if (b1) first = key0 + 1 + 2 * t;
-                            if (b0) first = key0 + 2 * t;
-                            first = __reduce_min_sync(FULL, first);
-                            const uint32_t n0 = (b0 ? 0u : 0xffffu) | (b1 ? 0u : 0xffff0000u), n1 = (b2 ? 0u : 0xffffu) | (b3 ? 0u : 0xffff0000u);
-                            f0[2 * j] &= n0, f0[2 * j + 1] &= n0;
-                            f1[2 * j] &= n1, f1[2 * j + 1] &= n1;
-#pragma unroll
-                            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                                for (int z = 0; z < 2; ++z)
-                                    if (first < sink.seen(8 * i + 2 * t + z)) {
-                                        o[i][2 * j][z] = o[i][2 * j][2 + z] = NAN;
-                                        o[i][2 * j + 1][z] = o[i][2 * j + 1][2 + z] = NAN;
-                                    }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < DG; ++j) {
-                    uint32_t u[4], v[4];
-                    values4<BF>(v0[j], f0[2 * j], f0[2 * j + 1], u);
-                    values4<BF>(v1[j], f1[2 * j], f1[2 * j + 1], v);
+                for (int y = 0; y < SP; ++y)
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
-                        product<BF>(o[i][2 * j], u[0], u[1], v[0], v[1], p[i][0], p[i][1]);
-                        product<BF>(o[i][2 * j + 1], u[2], u[3], v[2], v[3], p[i][0], p[i][1]);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) s[y][i][z] = ex2(fmaf(s[y][i][z], c, off[i][z & 1]));
+                        sum[i][0] += s[y][i][0] + s[y][i][2];
+                        sum[i][1] += s[y][i][1] + s[y][i][3];
+                        p[y][i][0] = turned(pack<BF>(s[y][i][0], s[y][i][1]));
+                        p[y][i][1] = turned(pack<BF>(s[y][i][2], s[y][i][3]));
+                    }
+#pragma unroll
+                for (int y = 0; y < SP; ++y) {
+                    uint32_t v0[DG], v1[DG], f0[2 * DG], f1[2 * DG];
+                    words<DG>(vs + y * KS + 4 * DG * lane, v0);
+                    words<DG>(vs + y * KS + 128 * DG + 4 * DG * lane, v1);
+                    words<2 * DG>(vs + y * KS + 256 * DG + 8 * DG * t, f0);
+                    words<2 * DG>(vs + y * KS + 256 * DG + 8 * DG * (t + 4), f1);
+                    if (blind || none) {  // values past the end of the keys, whatever they are, must not meet their zero probabilities
+                        const int key = key0 + y * kStrip + 2 * t, end = none >> y & 1 ? 0 : kv1;
+                        const uint32_t m0 = (key < end ? 0xffffu : 0u) | (key + 1 < end ? 0xffff0000u : 0u);
+                        const uint32_t m1 = (key + 8 < end ? 0xffffu : 0u) | (key + 9 < end ? 0xffff0000u : 0u);
+#pragma unroll
+                        for (int j = 0; j < DG; ++j) {
+                            f0[2 * j] &= m0, f0[2 * j + 1] &= m0;
+                            f1[2 * j] &= m1, f1[2 * j + 1] &= m1;
+                            // Nor may a group that is not a number meet rows that do not see it: it is left out, and those that do are spoilt.
+                            constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
+                            const auto odd = [&](const uint32_t *f, int half) {
+                                const uint32_t st = f[2 * j] >> (16 * half), lo = f[2 * j + 1] >> (16 * half);
+                                return (st & kExp) == kExp || (lo & kExp) == kExp;
+                            };
+                            const bool b0 = odd(f0, 0), b1 = odd(f0, 1), b2 = odd(f1, 0), b3 = odd(f1, 1);
+                            if (__any_sync(FULL, b0 || b1 || b2 || b3)) {
+                                const int first = __reduce_min_sync(FULL, b0 ? key : b1 ? key + 1 : b2 ? key + 8 : b3 ? key + 9 : INT_MAX);  // of such keys
+                                const uint32_t n0 = (b0 ? 0u : 0xffffu) | (b1 ? 0u : 0xffff0000u), n1 = (b2 ? 0u : 0xffffu) | (b3 ? 0u : 0xffff0000u);
+                                f0[2 * j] &= n0, f0[2 * j + 1] &= n0;
+                                f1[2 * j] &= n1, f1[2 * j + 1] &= n1;
+#pragma unroll
+                                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                                    for (int z = 0; z < 2; ++z)
+                                        if (first < sink.seen(8 * i + 2 * t + z)) {
+                                            o[i][2 * j][z] = o[i][2 * j][2 + z] = NAN;
+                                            o[i][2 * j + 1][z] = o[i][2 * j + 1][2 + z] = NAN;
+                                        }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < DG; ++j) {
+                        uint32_t u[4], v[4];
+                        values4<BF>(v0[j], f0[2 * j], f0[2 * j + 1], u);
+                        values4<BF>(v1[j], f1[2 * j], f1[2 * j + 1], v);
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            product<BF>(o[i][2 * j], u[0], u[1], v[0], v[1], p[y][i][0], p[y][i][1]);
+                            product<BF>(o[i][2 * j + 1], u[2], u[3], v[2], v[3], p[y][i][0], p[y][i][1]);
+                        }
                     }
                 }
             }
@@ -342,6 +373,8 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
             if (lane == 0) bar_arrive(empty(at));
         }
         if (!ok) break;
+        place(x + 1);
+        float2 *const all_m = reinterpret_cast<float2 *>(base + Sh::kOffM + (x & 1) * Sh::kSizeM);
         // The warps' shares: columns 32 j + 4 g + (0 .. 3) of rows 2 t and 2 t + 1 of each 8.
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -350,35 +383,26 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
                 float l = sum[i][z];
 #pragma unroll
                 for (int d = 4; d < 32; d *= 2) l += __shfl_xor_sync(FULL, l, d);
-                if (g == 0) all_m[warp * R + 8 * i + 2 * t + z] = make_float2(m[i][z], l);
+                if (g == 0) all_m[warp * R + 8 * i + 2 * t + z] = make_float2(off[i][z], l);
             }
-        // What warp w's share of row y is multiplied by, in units of the highest maximum.
-        const auto top_of = [&](int y) {
-            float top = -INFINITY;
+        // What warp w's share of row y is multiplied by, in units of the one with the highest scores; the joint sum.
+        const auto least = [&](int y) {
+            float off = FLT_MAX;
 #pragma unroll
-            for (int w = 0; w < W; ++w) top = fmaxf(top, all_m[w * R + y].x);
-            return top;
+            for (int w = 0; w < W; ++w) off = fminf(off, all_m[w * R + y].x);
+            return off;
         };
-        const auto factor = [&](int w, int y, float top) {
-            const float2 ml = all_m[w * R + y];
-            return ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2(ml.x - top);  // a sum without a maximum is not a number
-        };
-        const auto total_of = [&](int y, float top) {
+        const auto factor = [&](int w, int y, float off) { return ex2(off - all_m[w * R + y].x); };
+        const auto total_of = [&](int y, float off) {
             float total = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float f = factor(w, y, top);
-                if (f != 0.f) total = fmaf(all_m[w * R + y].y, f, total);
-            }
+            for (int w = 0; w < W; ++w) total = fmaf(all_m[w * R + y].y, factor(w, y, off), total);
             return total;
         };
 #pragma unroll
         for (int i0 = 0; i0 < NT; i0 += Sh::kPart) {
-            if (i0 > 0) {
-                if (8 * i0 >= rows) break;
-                join();  // the part before has been read
-                if (!ok) break;
-            }
+            if (i0 > 0 && 8 * i0 >= rows) break;
+            float *const all_o = reinterpret_cast<float *>(base + Sh::kOffO + (no++ & 1) * Sh::kSizeO);
 #pragma unroll
             for (int i = 0; i < Sh::kPart; ++i)
 #pragma unroll
@@ -394,15 +418,15 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
             for (int e = tid; e < min(rows - 8 * i0, 8 * Sh::kPart) * 8 * DG; e += 32 * W) {
                 const int in = e / (8 * DG), y = 8 * i0 + in, d = e % (8 * DG) * 4;
                 if (d >= D) continue;
-                const float top = top_of(y), total = total_of(y, top);
+                const float off0 = least(y), total = total_of(y, off0);
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const float f = factor(w, y, top);
+                    const float f = factor(w, y, off0);
                     const float4 u = *reinterpret_cast<const float4 *>(all_o + (w * 8 * Sh::kPart + in) * Sh::kPitch + d);
-                    if (f != 0.f) v = make_float4(fmaf(u.x, f, v.x), fmaf(u.y, f, v.y), fmaf(u.z, f, v.z), fmaf(u.w, f, v.w));
+                    v = make_float4(fmaf(u.x, f, v.x), fmaf(u.y, f, v.y), fmaf(u.z, f, v.z), fmaf(u.w, f, v.w));
                 }
-                const typename Sink<BF>::Joint joint = sink.joint(top - kv_lift(BF), total, sink.before(y));
+                const typename Sink<BF>::Joint joint = sink.joint(-off0, total, sink.before(y));
                 const float f = joint.mine, fb = joint.before;
                 v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
                 float4 *const part = reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d);
@@ -419,8 +443,8 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
         if (sg.joins) join();
         if (!ok) break;
         for (int y = tid; y < rows; y += 32 * W) {
-            const float top = top_of(y);
-            sink.lse(y, sink.joint(top - kv_lift(BF), total_of(y, top), sink.before(y)).e);
+            const float off0 = least(y);
+            sink.lse(y, sink.joint(-off0, total_of(y, off0), sink.before(y)).e);
         }
         __syncwarp();
         if (lane == 0) bar_arrive(seg_empty(x));
@@ -430,7 +454,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
 
 template <int DG, int NT, bool BF>
 cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
-    constexpr int W = NT == 1 ? 8 : 4;
+    constexpr int W = 4;
     using Sh = Shape<DG, NT, W>;
     static thread_local int ready = -1;  // the device on which the kernel has its shared memory
     int dev = 0;

@@ -288,6 +288,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
         const int n_items = light ? n_light : n_heavy, blocks = kv_blocks(sms, light);
         const int32_t *first = light ? first1 : first0;
         KvItem *const items = light ? p.items[1] : p.items[0];
+        const int lead = kv_lead(kv, light);
         Two done = {0, 0};  // spans, rows
 #pragma unroll 1
         for (int k0 = 0; k0 < n_items; k0 += kPlan) {
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                 if (light && it.row0 == x.n_heavy * kAttRows) of = s;
             }
             Two total;
-            const Two before = plan_scan<kPlan / 32>({int64_t(kv_span(it.tiles, light)) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
+            const Two before = plan_scan<kPlan / 32>({int64_t(kv_span(it.tiles, lead)) * kv.n_kv_heads, int64_t(it.rows) * kv.n_kv_heads}, sums, total);
             it.unit = done.a + before.a;
             it.row_off = done.b + before.b;
             done = {done.a + total.a, done.b + total.b};
@@ -327,12 +328,13 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
                 }
             }
         }
-        const Share share(done.a, blocks);
+        const Share share(done.a, blocks, lead);
         if (tid == 0) {
             int32_t *h = p.hdr + 16 * light;
             *reinterpret_cast<int64_t *>(h + 2) = done.a;
             *reinterpret_cast<int64_t *>(h + 4) = share.each;
             h[6] = share.rest;
+            h[10] = lead;
             if (!light) *reinterpret_cast<int64_t *>(p.hdr + 24) = done.b;
         }
         __syncthreads();
@@ -356,8 +358,8 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             (light ? p.start[1] : p.start[0])[c] = k;
             if (u < done.a && c > 0 && (!FEW || (few_tiles[k] > 0 && few_units[k] != u))) {
                 const KvItem it = items[k];
-                const int span = kv_span(it.tiles, light), h = span > 0 ? int(uint32_t(u - it.unit) / uint32_t(span)) : 0;
-                const int64_t from = it.unit + int64_t(h) * span + kv_lead(light), before = share.at(c - 1);  // tile 0
+                const int span = kv_span(it.tiles, lead), h = span > 0 ? int(uint32_t(u - it.unit) / uint32_t(span)) : 0;
+                const int64_t from = it.unit + int64_t(h) * span + lead, before = share.at(c - 1);  // tile 0
                 if (u > from && u < from + it.tiles && before <= from && !it.partial) {
                     KvCut cut;
                     cut.h = h;
@@ -390,7 +392,7 @@ struct Pieces {
     // unit, tiles, row_off, rows: of the item
     __device__ Pieces(const Share &share, int64_t base, int64_t unit, int tiles, int64_t row_off, int rows, int h, int light_) : row(0), n(0), light(light_) {
         if (tiles > 0) {
-            const int64_t from = unit + int64_t(h) * kv_span(tiles, light) + kv_lead(light);
+            const int64_t from = unit + int64_t(h) * kv_span(tiles, share.lead) + share.lead;
             const int c0 = share.of(from);
             n = share.of(from + tiles - 1) - c0 + 1;
             row = base + row_off + int64_t(h) * rows + int64_t(kv_rows(light)) * c0;

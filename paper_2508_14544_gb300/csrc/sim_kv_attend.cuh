@@ -31,8 +31,8 @@ __host__ __device__ constexpr float kv_lift(bool bf) { return bf ? 0.f : 7.f; }
 // each + 1 places for the first `rest` blocks and `each` for the others.
 struct Share {
     int64_t units, each;
-    int rest;
-    __device__ Share(int64_t units_, int blocks) : units(units_) {
+    int rest, lead;
+    __device__ Share(int64_t units_, int blocks, int lead_) : units(units_), lead(lead_) {
         each = units_ <= INT_MAX ? int64_t(uint32_t(units_) / uint32_t(blocks)) : units_ / blocks;
         rest = int(units - each * blocks);
     }
@@ -41,6 +41,7 @@ struct Share {
         units = *reinterpret_cast<const int64_t *>(h + 2);
         each = *reinterpret_cast<const int64_t *>(h + 4);
         rest = h[6];
+        lead = h[10];
     }
     __device__ int64_t at(int c) const { return each * c + min(c, rest); }
     __device__ int of(int64_t u) const {  // the block that has place u < units
@@ -77,11 +78,12 @@ struct Line {
     const KvItem *items;
     KvItem it;
     int64_t u, u1, base;
-    int n_items, heads, k, h, c, light;
+    int n_items, heads, k, h, c, light, lead;
     int t, t_end, whole;  // tiles of the item and head that are left, and whether all of them are this block's
     __device__ Line(const KvPlan &p, int heads_, int light_, int c_, int sms) : items(p.items[light_]), heads(heads_), c(c_), light(light_) {
         n_items = p.hdr[16 * light];
         const Share share(p, light);
+        lead = share.lead;
         u = share.at(c);
         u1 = share.at(c + 1);
         base = list_base(p, light, sms);
@@ -95,14 +97,14 @@ struct Line {
         if (t < t_end) return part(s, true);
         while (u < u1 && k < n_items) {
             if (h < 0) it = items[k];
-            const int span = kv_span(it.tiles, light);
+            const int span = kv_span(it.tiles, lead);
             if (span == 0 || h + 1 == heads) {
                 ++k;
                 h = -1;
                 continue;
             }
             h = h < 0 ? int(uint32_t(u - it.unit) / uint32_t(span)) : h + 1;
-            const int64_t a = it.unit + int64_t(h) * span, tile0 = a + kv_lead(light);
+            const int64_t a = it.unit + int64_t(h) * span, tile0 = a + lead;
             t = int(max(u - tile0, int64_t(0)));
             t_end = int(min(u1 - tile0, int64_t(it.tiles)));
             whole = t_end - t == it.tiles && !it.partial;

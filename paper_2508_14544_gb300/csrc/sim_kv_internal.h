@@ -98,8 +98,12 @@ __host__ __device__ inline bool kv_light_only(const sim_kv &kv, const sim_kv_bat
 constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.
-__host__ __device__ constexpr int kv_lead(int light) { return light ? 1 : 4; }
-__host__ __device__ inline int kv_span(int tiles, int light) { return tiles > 0 ? tiles + kv_lead(light) : 0; }
+#ifndef KLEAD4
+#define KLEAD4 2
+#endif
+constexpr int kLead4 = KLEAD4;
+__host__ __device__ inline int kv_lead(const sim_kv &kv, int light) { return light ? (kv_4bit(kv) ? kLead4 : 1) : 4; }
+__host__ __device__ inline int kv_span(int tiles, int lead) { return tiles > 0 ? tiles + lead : 0; }
 
 // A run of query rows (token x head of the group, for every kv head alike) against a range of one table's keys.
 struct alignas(16) KvItem {
@@ -145,7 +149,7 @@ static_assert(sizeof(KvCut) == 32, "KvCut");
 constexpr int kKvMaxSms = 256;
 struct KvPlan {
     int32_t *hdr;       // heavy, and 16 further light: [0] items, [2..3] spans in all, [4..5] of each block, [6] left over,
-                        // [7] cuts; [1] offsets in order, [17] entries to join, [24..25] rows of the heavy items
+                        // [7] cuts, [10] lead; [1] offsets in order, [17] entries to join, [24..25] rows of the heavy items
     KvCut *cut[2];      // as many as there are, in any order
     KvSource *source;   // [n_groups + n]
     KvItem *items[2];
