@@ -37,106 +37,129 @@ __device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
     return d;
 }
 
-// The largest 16-bit float that is not above (hi - lo) / 15, as bits.  Each step is cut off, and 15 times a 16-bit float is a
-// 32-bit one, so that a float t <= (hi - lo) / 15 is never above what the 32-bit steps leave: the result is that of the exact quotient.
+// The largest 16-bit float that is not above (hi - lo) / 15, as bits.  A product with slightly less than 1 / 15, cut off, gives it or the
+// one below; 15 times a 16-bit float is a 32-bit one, so that comparing it with the difference, cut off too, is exact.
 template <bool BF>
 __device__ __forceinline__ uint32_t step_of(float lo, float hi) {
-    uint32_t step;
+    // a difference past the largest float: of an eighth of both, which is exact but for what is far below the last place
+    const bool large = BF && (hi > 1e38f || lo < -1e38f);
+    const float span = large ? __fsub_rz(hi * 0.125f, lo * 0.125f) : __fsub_rz(hi, lo), q = __fmul_rz(span, 0x1.11111p-4f);
+    uint32_t step, up;
     if (BF) {
-        // a difference past the largest float: of an eighth of both, which is exact but for what is far below the last place
-        const bool large = hi > 1e38f || lo < -1e38f;
-        const float q = large ? __fdiv_rz(__fsub_rz(hi * 0.125f, lo * 0.125f), 15.f) * 8.f : __fdiv_rz(__fsub_rz(hi, lo), 15.f);
         step = __float_as_uint(q) >> 16;
+        up = step + 1;
+        step = 15.f * __uint_as_float(up << 16) <= span ? up : step;
+        if (large) step += 3 << 7;
     } else {
-        step = __half_as_ushort(__float2half_rz(__fdiv_rz(__fsub_rz(hi, lo), 15.f)));
+        step = __half_as_ushort(__float2half_rz(q));
+        up = step + 1;
+        step = 15.f * __half2float(__ushort_as_half(uint16_t(up))) <= span ? up : step;
     }
     return step == 0 && hi > lo ? 1 : step;
 }
 
-// Next to a border between two codes, (k + 1/2) step, r decides only which one: then x - lo, as a 32-bit float and the rest, is
-// compared with the border, which is exact.
+// Next to a border between two codes, (k + 1/2) s, r = (x - lo) / s decides only which one: then t = x - lo, as a 32-bit float, and
+// the rest are compared with the border, which is exact.
 __device__ __forceinline__ float code_at_border(float x, float lo, float t, float r, float s) {
     const float k = floorf(r), border = fmaf(k, s, 0.5f * s);
     // t + rest = x - lo exactly (a sum of two floats and its rounding error)
     const float y = t - x, rest = (x - (t - y)) + (-lo - y);
     const bool tie = t == border && rest == 0.f;
-    const bool up = tie ? fmodf(k, 2.f) != 0.f : t == border ? rest > 0.f : t > border;
+    const bool up = tie ? int(k) & 1 : t == border ? rest > 0.f : t > border;
     return k + (up ? 1.f : 0.f);
 }
 
-// Codes of the N16 pairs of values in x, 0 .. 15, given to put(i, code) one after the other.
-template <bool BF, int N, typename Put>
-__device__ __forceinline__ void codes_of(const uint32_t *x, float lo, float s, Put &&put) {
-    // tiny steps, whose reciprocals overflow, and large ones, whose differences do, after a multiplication by a power of two
-    const float more = BF && s > 0.f && s < 0x1p-60f ? 0x1p60f : BF && s > 0x1p110f ? 0x1p-8f : 1.f;
-    s *= more;
-    lo *= more;
-    const float inv = s > 0.f ? 1.f / s : 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float v = wide<BF>(x[i / 2], i % 2), t = fmaf(v, more, -lo);
-        const float r = t * inv;  // within 2^-20 of the quotient (r < 32)
-        float code = rintf(r);
-        if (fabsf(r - code) > 0.5f - 0x1p-18f) code = code_at_border(v * more, lo, t, r, s);
-        put(i, uint32_t(fminf(code, 15.f)));
-    }
-}
-
-// A thread for each group of a token's keys or values.  VEC: the sources are 16-byte aligned.
+// A lane has 8 of a group's values at columns 8 u and 8 more at 16 + 8 u, the other half of them is its neighbour's.
+// VEC: the sources are 16-byte aligned.
 template <bool BF, bool VEC>
-__global__ void __launch_bounds__(kWrite) k_write_4bit(const sim_kv kv, const KvWrite a) {
+__global__ void __launch_bounds__(kWrite) k_write_4bit(const sim_kv kv, const KvWrite a, const FastDiv per_row, const FastDiv groups) {
     kv_wait_previous();
-    const int P = kv.page_size, D = kv.head_dim, G = kv_dim_groups(kv), H = kv.n_kv_heads, shift = __ffs(P) - 1;
-    const int64_t all = int64_t(a.n_new) * 2 * H * G, head_bytes = kv_head_bytes(kv);
-    for (int64_t i = int64_t(blockIdx.x) * kWrite + threadIdx.x; i < all; i += int64_t(gridDim.x) * kWrite) {
-        const int j = int(i % G), h = int(i / G % H), v = int(i / (int64_t(G) * H) & 1);
-        const int64_t tok = i / (2 * int64_t(G) * H), slot = a.slots[tok], page = slot >> shift;
-        if (slot < 0 || page >= kv.n_pages) continue;
-        const uint16_t *from = static_cast<const uint16_t *>(v ? a.v : a.k) + tok * (v ? a.vt : a.kt) + h * (v ? a.vh : a.kh) + 32 * j;
-        const int n = min(32, D - 32 * j);  // a multiple of 8
-        uint32_t x[16];
+    const int P = kv.page_size, D = kv.head_dim, G = int(groups.d), H = kv.n_kv_heads, shift = __ffs(P) - 1;
+    const int64_t all = int64_t(a.n_new) * 2 * per_row.d;
+    for (int64_t i0 = int64_t(blockIdx.x) * kWrite; i0 < all; i0 += int64_t(gridDim.x) * kWrite) {
+        const int64_t i = min(i0 + threadIdx.x, all - 1);  // lanes past the end (of all, an even number) make the last one's pair again, or its neighbour's
+        int row, r;
+        if (all <= INT_MAX) {
+            row = int(per_row.div(uint32_t(i)));
+            r = int(i - int64_t(row) * per_row.d);
+        } else {
+            row = int(i / per_row.d);
+            r = int(i % per_row.d);
+        }
+        const int tok = row >> 1, v = row & 1, u = r & 1, h = int(groups.div(uint32_t(r >> 1))), j = (r >> 1) - h * G;
+        const int64_t slot = a.slots[tok], page = slot >> shift;
+        const bool there = slot >= 0 && page < kv.n_pages && i0 + threadIdx.x < all;
+        const uint16_t *const from = static_cast<const uint16_t *>(v ? a.v : a.k) + tok * (v ? a.vt : a.kt) + h * (v ? a.vh : a.kh) + 32 * j + 8 * u;
+        const int left = D - 32 * j - 8 * u;  // columns from the first of this lane's on
+        uint32_t x[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (8 * e >= n) {  // as the first ones: neither lowest nor highest is changed
-                x[4 * e] = x[0], x[4 * e + 1] = x[0], x[4 * e + 2] = x[0], x[4 * e + 3] = x[0];
+        for (int e = 0; e < 2; ++e) {
+            if (16 * e >= left) {  // none: as others of the group, so that neither lowest nor highest is changed
+                x[4 * e] = x[4 * e + 1] = x[4 * e + 2] = x[4 * e + 3] = e > 0 ? x[0] : 0;
             } else if (VEC) {
-                const uint4 y = __ldcs(reinterpret_cast<const uint4 *>(from + 8 * e));
+                const uint4 y = __ldcs(reinterpret_cast<const uint4 *>(from + 16 * e));
                 x[4 * e] = y.x, x[4 * e + 1] = y.y, x[4 * e + 2] = y.z, x[4 * e + 3] = y.w;
             } else {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[4 * e + q] = from[8 * e + 2 * q] | uint32_t(from[8 * e + 2 * q + 1]) << 16;
+                for (int q = 0; q < 4; ++q) x[4 * e + q] = from[16 * e + 2 * q] | uint32_t(from[16 * e + 2 * q + 1]) << 16;
             }
         }
         uint32_t least = x[0], most = x[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) {
+        for (int e = 1; e < 8; ++e) {
             least = min16<BF>(least, x[e]);
             most = max16<BF>(most, x[e]);
         }
-        least = min16<BF>(least, least >> 16 | least << 16) & 0xffffu;
-        most = max16<BF>(most, most >> 16 | most << 16) & 0xffffu;
-        const float lo = wide16<BF>(least), hi = wide16<BF>(most);
+        least = min16<BF>(least, least >> 16 | least << 16);
+        most = max16<BF>(most, most >> 16 | most << 16);
+        const uint32_t mine = __byte_perm(least, most, 0x5410), other = __shfl_xor_sync(FULL, mine, 1);
+        const bool both = D - 32 * j > 8;  // the group has columns for the second lane
+        least = both ? min16<BF>(mine, other) & 0xffffu : (u ? other : mine) & 0xffffu;
+        most = both ? max16<BF>(mine, other) >> 16 : (u ? other : mine) >> 16;
+        float lo = wide16<BF>(least);
+        const float hi = wide16<BF>(most);
         const bool finite = lo * 0.f == 0.f && hi * 0.f == 0.f;
         const uint32_t step = finite ? step_of<BF>(lo, hi) : 0x7fffu, base = finite ? least : 0x7fffu;
-        const float s = finite ? wide16<BF>(step) : 0.f;
+        float s = finite ? wide16<BF>(step) : 0.f;
+        // Tiny steps, whose reciprocals overflow, and large ones, whose differences do, after a multiplication by a power of two.
+        const float more = BF && s > 0.f && s < 0x1p-60f ? 0x1p60f : BF && s > 0x1p110f ? 0x1p-8f : 1.f;
+        s *= more;
+        lo = finite ? lo * more : 0.f;
+        float inv = 0.f;
+        if (s > 0.f) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));  // f16's least is 2^-24
+        uint32_t w[4];  // of columns 2 q and 2 q + 1 at bits 4 q of two halves, for 8 columns; or of four and four
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float part[2] = {0.f, 0.f};  // four codes each, below 2^16: exact
+            constexpr float kScale[4] = {1.f, 16.f, 256.f, 4096.f};
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float val = wide<BF>(x[4 * e + q / 2], q % 2), t = fmaf(val, more, -lo), near = fmaf(t, inv, 0x1.8p23f) - 0x1.8p23f;
+                float code = near;  // the quotient, within 2^-18 where it is below 16, to the nearest
+                if (fabsf(fmaf(t, inv, -near)) > 0.5f - 0x1p-17f) code = code_at_border(val * more, lo, t, t * inv, s);
+                code = fminf(code, 15.f);
+                part[v ? q / 4 : q % 2] = fmaf(code, kScale[v ? q % 4 : q / 2], part[v ? q / 4 : q % 2]);
+            }
+            w[2 * e] = finite ? uint32_t(part[0]) : 0;
+            w[2 * e + 1] = finite ? uint32_t(part[1]) : 0;
+        }
+        if (!there) continue;
         unsigned char *const strip = static_cast<unsigned char *>(kv.pool) + page * kv_page_bytes(kv) +
-                                     ((int64_t(a.layer) * 2 + v) * H + h) * head_bytes + (slot & (P - 1)) / kStrip * kv_strip_bytes(kv);
+                                     ((int64_t(a.layer) * 2 + v) * H + h) * kv_head_bytes(kv) + int(slot & (P - 1)) / kStrip * kv_strip_bytes(kv);
         const int T = int(slot & (kStrip - 1));
-        uint32_t w[4] = {};
         if (v == 0) {
-            codes_of<BF, 32>(x, finite ? lo : 0.f, s, [&](int i2, uint32_t c) { w[i2 / 8] |= c << (i2 % 8 / 2 * 4 + i2 % 2 * 16); });
-            uint32_t *const to = reinterpret_cast<uint32_t *>(strip + 16 * G * T + 4 * j);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) to[t * G] = finite ? w[t] : 0;
-            *reinterpret_cast<uint32_t *>(strip + 256 * G + 4 * G * T + 4 * j) = step | base << 16;
+            uint32_t *const to = reinterpret_cast<uint32_t *>(strip + 16 * G * T + 4 * G * u + 4 * j);
+            to[0] = w[0] | w[1] << 16;
+            to[2 * G] = w[2] | w[3] << 16;
+            if (u == 0) *reinterpret_cast<uint32_t *>(strip + 256 * G + 4 * G * T + 4 * j) = step | base << 16;
         } else {
-            codes_of<BF, 32>(x, finite ? lo : 0.f, s, [&](int i2, uint32_t c) { w[i2 / 8] |= c << (i2 % 8 * 4); });
-            unsigned char *const to = strip + 128 * G * (T / 8) + 4 * G * (T % 8 / 2) + 4 * j + 2 * (T % 2);
-#pragma unroll
-            for (int g = 0; g < 8; ++g) *reinterpret_cast<uint16_t *>(to + 16 * G * g) = finite ? uint16_t(w[g / 2] >> (g % 2 * 16)) : 0;
+            uint16_t *const to = reinterpret_cast<uint16_t *>(strip + 128 * G * (T / 8) + 4 * G * (T % 8 / 2) + 32 * G * u + 4 * j + 2 * (T % 2));
+            to[0] = uint16_t(w[0]);
+            to[8 * G] = uint16_t(w[1]);
+            to[32 * G] = uint16_t(w[2]);
+            to[40 * G] = uint16_t(w[3]);
             uint16_t *const sc = reinterpret_cast<uint16_t *>(strip + 256 * G + 8 * G * (T / 2) + 8 * j + 2 * (T % 2));
-            sc[0] = uint16_t(step);
-            sc[2] = uint16_t(base);
+            sc[2 * u] = uint16_t(u ? base : step);
         }
     }
 }
@@ -273,8 +296,9 @@ cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_
     const auto aligned = [](const void *p, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && a % 8 == 0 && b % 8 == 0; };
     const bool vec = aligned(w.k, w.kt, w.kh) && aligned(w.v, w.vt, w.vh);
     const auto k = kv_bf(kv) ? (vec ? k_write_4bit<true, true> : k_write_4bit<true, false>) : vec ? k_write_4bit<false, true> : k_write_4bit<false, false>;
-    const int blocks = blocks_for(int64_t(w.n_new) * 2 * kv.n_kv_heads * kv_dim_groups(kv), kWrite, 4096);
-    return launch_chained(k, blocks, kWrite, 0, st, kv, w);
+    const int G = kv_dim_groups(kv), per_row = 2 * G * kv.n_kv_heads;  // lanes for a token's keys, or its values
+    const int blocks = blocks_for(int64_t(w.n_new) * 2 * per_row, kWrite, 4096);
+    return launch_chained(k, blocks, kWrite, 0, st, kv, w, FastDiv(per_row), FastDiv(G));
 }
 
 cudaError_t launch_kv_read(const sim_kv &kv, const KvRead &r, cudaStream_t st) {

@@ -25,22 +25,23 @@ struct Shape {
     static constexpr int kRows = 8 * NT;
     static constexpr int kBytesStrip = 320 * DG;
     static constexpr int kStage = 2 * kStrips * kBytesStrip;  // a tile's keys, then its values
-    static constexpr int kPart = 1;                           // times 8 rows of O that are joined at a time
     static constexpr int kPitch = 32 * DG + 4;                // floats between rows of the warps' O
-    // All of these twice, so that one barrier for each segment, or part of it, is enough.
-    static constexpr int kSizeQ = NT * DG * 512, kSizeO = W * 8 * kPart * kPitch * 4, kSizeM = W * kRows * 8;
+    static constexpr int kPerSm = NT == 1 ? 3 : 2;            // blocks, as in kv_per_sm
+    static constexpr int kRoom = kPerSm == 3 ? 76800 : 115712;
+    // Queries and sums twice, so that one barrier for each part of a segment is enough.
+    static constexpr int kSizeQ = NT * DG * 512, kSizeO = W * 8 * kPitch * 4, kSizeM = W * kRows * 8;
     static constexpr int kOffQ = 0;                           // queries: [NT][DG][lane] 16 bytes
-    static constexpr int kOffO = kOffQ + 2 * kSizeQ;          // [W][8 kPart][kPitch]
-    static constexpr int kOffM = kOffO + 2 * kSizeO;          // [W][kRows] off and sum
+    static constexpr int kOffO = kOffQ + 2 * kSizeQ;          // [W][8][kPitch]
+    static constexpr int kOffM = kOffO + kSizeO;              // [W][kRows] off and sum
     static constexpr int kOffSeg = kOffM + 2 * kSizeM;
     static constexpr int kFixed = kOffSeg + kSegs * int(sizeof(Segment)) + 256;
-    static constexpr int kStages = (114000 - kFixed) / kStage < 4 ? (114000 - kFixed) / kStage : 4;
+    static constexpr int kStages = (kRoom - kFixed) / kStage < 4 ? (kRoom - kFixed) / kStage : 4;
     static constexpr int kOffRing = (kOffSeg + kSegs * int(sizeof(Segment)) + 127) / 128 * 128;
     static constexpr int kOffBar = kOffRing + kStages * kStage;
-    static constexpr int kBars = 2 * kStages + 2 * kSegs + 1;
+    static constexpr int kBars = 2 * kStages + 2 * kSegs + 2;
     static constexpr int kOffGone = kOffBar + kBars * 8;      // per stage: strips on pages that the pool does not have
     static constexpr int kBytes = kOffGone + kStages * 4 + 16;
-    static_assert(kStages >= 2 && kBytes <= 115712, "two blocks per SM");
+    static_assert(kStages >= 2 && kBytes <= kRoom, "shared memory");
 };
 
 // 16 x 8 += 16 x 16 times 16 x 8.
@@ -62,7 +63,7 @@ __device__ __forceinline__ uint32_t turned(uint32_t x) {
     return y;
 }
 template <int DG, int NT, int W, bool BF>
-__global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
+__global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::kPerSm)
     k_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a) {
     using Sh = Shape<DG, NT, W>;
     constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip, SP = Sh::kSteps;
@@ -75,7 +76,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
     const auto empty = [&](uint32_t x) { return bars + 8 * (NS + x % NS); };
     const auto seg_full = [&](uint32_t x) { return bars + 8 * (2 * NS + x % kSegs); };
     const auto seg_empty = [&](uint32_t x) { return bars + 8 * (2 * NS + kSegs + x % kSegs); };
-    const uint32_t joined = bars + 8 * (2 * NS + 2 * kSegs);
+    const uint32_t joined = bars + 8 * (2 * NS + 2 * kSegs), cleared = joined + 8;
     const int tid = threadIdx.x, warp = __shfl_sync(FULL, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int s = 0; s < NS; ++s) {
@@ -87,6 +88,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
             bar_init(seg_empty(s), W);
         }
         bar_init(joined, W);
+        bar_init(cleared, W);
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -399,31 +401,31 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
             for (int w = 0; w < W; ++w) total = fmaf(all_m[w * R + y].y, factor(w, y, off), total);
             return total;
         };
+        float *const all_o = reinterpret_cast<float *>(base + Sh::kOffO);
 #pragma unroll
-        for (int i0 = 0; i0 < NT; i0 += Sh::kPart) {
-            if (i0 > 0 && 8 * i0 >= rows) break;
-            float *const all_o = reinterpret_cast<float *>(base + Sh::kOffO + (no++ & 1) * Sh::kSizeO);
+        for (int i = 0; i < NT; ++i) {  // 8 rows at a time
+            if (i > 0 && 8 * i >= rows) break;
+            if (no > 0) ok = __all_sync(FULL, bar_wait(cleared, (no - 1) & 1, gave_up));  // the rows before have been read
+            if (!ok) break;
+            ++no;
 #pragma unroll
-            for (int i = 0; i < Sh::kPart; ++i)
+            for (int z = 0; z < 2; ++z) {
+                float *const to = all_o + (warp * 8 + 2 * t + z) * Sh::kPitch + 4 * g;
 #pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                    float *const to = all_o + (warp * 8 * Sh::kPart + 8 * i + 2 * t + z) * Sh::kPitch + 4 * g;
-                    const auto &x4 = o[i0 + i];
-#pragma unroll
-                    for (int j = 0; j < DG; ++j)
-                        *reinterpret_cast<float4 *>(to + 32 * j) = make_float4(x4[2 * j][z], x4[2 * j][2 + z], x4[2 * j + 1][z], x4[2 * j + 1][2 + z]);
-                }
+                for (int j = 0; j < DG; ++j)
+                    *reinterpret_cast<float4 *>(to + 32 * j) = make_float4(o[i][2 * j][z], o[i][2 * j][2 + z], o[i][2 * j + 1][z], o[i][2 * j + 1][2 + z]);
+            }
             join();
             if (!ok) break;
-            for (int e = tid; e < min(rows - 8 * i0, 8 * Sh::kPart) * 8 * DG; e += 32 * W) {
-                const int in = e / (8 * DG), y = 8 * i0 + in, d = e % (8 * DG) * 4;
+            for (int e = tid; e < min(rows - 8 * i, 8) * 8 * DG; e += 32 * W) {
+                const int in = e / (8 * DG), y = 8 * i + in, d = e % (8 * DG) * 4;
                 if (d >= D) continue;
                 const float off0 = least(y), total = total_of(y, off0);
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     const float f = factor(w, y, off0);
-                    const float4 u = *reinterpret_cast<const float4 *>(all_o + (w * 8 * Sh::kPart + in) * Sh::kPitch + d);
+                    const float4 u = *reinterpret_cast<const float4 *>(all_o + (w * 8 + in) * Sh::kPitch + d);
                     v = make_float4(fmaf(u.x, f, v.x), fmaf(u.y, f, v.y), fmaf(u.z, f, v.z), fmaf(u.w, f, v.w));
                 }
                 const typename Sink<BF>::Joint joint = sink.joint(-off0, total, sink.before(y));
@@ -437,6 +439,8 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, 2)
                 if (sg.direct) *reinterpret_cast<uint2 *>(sink.out_row(y) + d) = make_uint2(pack<BF>(v.x, v.y), pack<BF>(v.z, v.w));
                 else *part = v;
             }
+            __syncwarp();
+            if (lane == 0) bar_arrive(cleared);
         }
         if (!ok) break;
         // the joint sums, once all have read the ones before
@@ -463,15 +467,16 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
         e = cudaFuncSetAttribute((const void *)k_4bit<DG, NT, W, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
         if (e == cudaSuccess) ready = dev;
     }
-    return e == cudaSuccess ? launch_chained(k_4bit<DG, NT, W, BF>, kv_blocks(a.sms, 1), Sh::kThreads, Sh::kBytes, st, kv, b, a) : e;
+    return e == cudaSuccess ? launch_chained(k_4bit<DG, NT, W, BF>, kv_blocks(a.sms, 1, Sh::kPerSm), Sh::kThreads, Sh::kBytes, st, kv, b, a) : e;
 }
 
 template <int DG, bool BF>
 cudaError_t launch_rows(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
-    // Rows of a pass by what entries have on average; items with more are gone over again.
-    const int64_t G = b.q_heads / kv.n_kv_heads, rows = (int64_t(b.n_q) * G + std::max(b.n, 1) - 1) / std::max(b.n, 1);
-    if (rows <= 8) return launch<DG, 1, BF>(kv, b, a, st);
-    return rows <= 16 ? launch<DG, 2, BF>(kv, b, a, st) : launch<DG, 4, BF>(kv, b, a, st);
+    switch (kv_pass_rows(kv, b)) {
+        case 8: return launch<DG, 1, BF>(kv, b, a, st);
+        case 16: return launch<DG, 2, BF>(kv, b, a, st);
+        default: return launch<DG, 4, BF>(kv, b, a, st);
+    }
 }
 
 template <bool BF>

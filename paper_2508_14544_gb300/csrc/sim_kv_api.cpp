@@ -151,7 +151,7 @@ int sim_kv_compact(const sim_kv *kv, int32_t *to, void *cuda_stream) {
 int64_t sim_kv_plan_bytes(const sim_kv *kv, const sim_kv_batch *b) { return bad_batch_sizes(kv, b) ? 0 : (simgb::kv_plan(*kv, *b).bytes + 15) / 16 * 16; }
 
 int64_t sim_kv_workspace_bytes(const sim_kv *kv, const sim_kv_batch *b) {
-    return bad_batch_sizes(kv, b) ? 0 : simgb::kv_partial_rows(*b, simgb::kv_sm_count()) * (kv->head_dim + 1) * 4;
+    return bad_batch_sizes(kv, b) ? 0 : simgb::kv_partial_rows(*kv, *b, simgb::kv_sm_count()) * (kv->head_dim + 1) * 4;
 }
 
 int sim_kv_plan(const sim_kv *kv, const sim_kv_batch *b, void *cuda_stream) {
@@ -175,7 +175,7 @@ int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const 
     a.sms = simgb::kv_sm_count();
     a.group = simgb::FastDiv(uint32_t(b->q_heads / kv->n_kv_heads));
     a.part = static_cast<float *>(b->workspace);
-    a.part_lse = a.part + simgb::kv_partial_rows(*b, a.sms) * kv->head_dim;
+    a.part_lse = a.part + simgb::kv_partial_rows(*kv, *b, a.sms) * kv->head_dim;
     a.qt = q_token_stride;
     a.qh = q_head_stride;
     a.ot = out_token_stride;

@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
     __syncthreads();
 #pragma unroll 1
     for (int light = 0; light < 2; ++light) {
-        const int n_items = light ? n_light : n_heavy, blocks = kv_blocks(sms, light);
+        const int n_items = light ? n_light : n_heavy, blocks = kv_blocks(sms, light, kv_per_sm(kv, b));
         const int32_t *first = light ? first1 : first0;
         KvItem *const items = light ? p.items[1] : p.items[0];
         const int lead = kv_lead(kv, light);

@@ -95,6 +95,13 @@ __host__ __device__ inline bool kv_light_only(const sim_kv &kv, const sim_kv_bat
     const int64_t G = b.q_heads / kv.n_kv_heads;
     return b.n_q * G <= kLightRows || (b.n_groups == 0 && G <= kLightRows && b.n_q <= b.n);
 }
+// Rows of a pass over a light item of a 4-bit cache, by what entries have on average: an item with more is gone over again.
+__host__ __device__ inline int kv_pass_rows(const sim_kv &kv, const sim_kv_batch &b) {
+    const int64_t rows = (int64_t(b.n_q) * (b.q_heads / kv.n_kv_heads) + b.n - 1) / (b.n > 0 ? b.n : 1);
+    return rows <= 8 ? 8 : rows <= 16 ? 16 : kLightRows;
+}
+// Blocks of the light list on an SM.
+__host__ __device__ inline int kv_per_sm(const sim_kv &kv, const sim_kv_batch &b) { return kv_4bit(kv) && kv_pass_rows(kv, b) == 8 ? 3 : 2; }
 constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.
@@ -171,12 +178,12 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     p.hdr = static_cast<int32_t *>(b.plan);
     p.cut[0] = reinterpret_cast<KvCut *>(p.hdr + 32);
     p.cut[1] = p.cut[0] + kKvMaxSms;
-    p.source = reinterpret_cast<KvSource *>(p.cut[1] + 2 * kKvMaxSms);
+    p.source = reinterpret_cast<KvSource *>(p.cut[1] + 3 * kKvMaxSms);
     p.items[0] = reinterpret_cast<KvItem *>(p.source + src);
     p.items[1] = p.items[0] + p.max_heavy;
     p.start[0] = reinterpret_cast<int32_t *>(p.items[1] + src + (kv_light_only(kv, b) ? int64_t(b.n_q) * G / kLightRows : 0));
     p.start[1] = p.start[0] + kKvMaxSms;
-    p.first[0] = p.start[1] + 2 * kKvMaxSms;
+    p.first[0] = p.start[1] + 3 * kKvMaxSms;
     p.first[1] = p.first[0] + src + 1;
     p.used = p.first[1] + src + 1;
     p.alone = p.used + b.n_groups;
@@ -186,11 +193,11 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     return p;
 }
 // Blocks of the two lists for a number of SMs.
-__host__ __device__ inline int kv_blocks(int sms, int light) { return light ? 2 * sms : sms; }
+__host__ __device__ inline int kv_blocks(int sms, int light, int per_sm = 2) { return light ? per_sm * sms : sms; }
 // Partial results: rows of head_dim floats, then a float per row (log2 of the sum of exponentials).  A piece of an
 // item begins at the rows before it plus room for the pieces that blocks have cut off before.
-__host__ __device__ inline int64_t kv_partial_rows(const sim_kv_batch &b, int sms) {
-    return 2 * int64_t(b.n_q) * b.q_heads + int64_t(kAttRows) * kv_blocks(sms, 0) + int64_t(kLightRows) * kv_blocks(sms, 1);
+__host__ __device__ inline int64_t kv_partial_rows(const sim_kv &kv, const sim_kv_batch &b, int sms) {
+    return 2 * int64_t(b.n_q) * b.q_heads + int64_t(kAttRows) * kv_blocks(sms, 0) + int64_t(kLightRows) * kv_blocks(sms, 1, kv_per_sm(kv, b));
 }
 
 struct KvAttend {
