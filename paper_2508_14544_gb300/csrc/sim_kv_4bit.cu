@@ -1,6 +1,7 @@
 // Keys and values of a 4-bit cache: quantised as they are written, and read back (16-bit caches are read here too).
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "sim.h"
 #include "sim_kv_4bit.cuh"
@@ -69,97 +70,184 @@ __device__ __forceinline__ float code_at_border(float x, float lo, float t, floa
     return k + (up ? 1.f : 0.f);
 }
 
-// A lane has 8 of a group's values at columns 8 u and 8 more at 16 + 8 u, the other half of them is its neighbour's.
+// Codes of eight values, place q of them at the bits that the powers of two in `at` give: any values of the type, lo the lowest of
+// the group and s its step.
+template <bool BF>
+__device__ __noinline__ uint32_t codes_exactly(uint4 x, float lo, float s, bool by_column) {
+    // Tiny steps, whose reciprocals overflow, and large ones, whose differences do, after a multiplication by a power of two.
+    const float more = BF && s < 0x1p-60f ? 0x1p60f : BF && s > 0x1p110f ? 0x1p-8f : 1.f;
+    s *= more;
+    lo *= more;
+    const float inv = 1.f / s;
+    uint32_t w = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const uint32_t pair = q < 2 ? x.x : q < 4 ? x.y : q < 6 ? x.z : x.w;
+        const float val = wide<BF>(pair, q % 2) * more, t = val - lo, r = t * inv;  // r: within 2^-20 of the quotient, where it is below 16
+        float code = rintf(r);
+        if (fabsf(r - code) > 0.5f - 0x1p-18f) code = code_at_border(val, lo, t, r, s);
+        w |= uint32_t(fminf(code, 15.f)) << (by_column ? 4 * q : 4 * (q / 2) + 16 * (q % 2));
+    }
+    return w;
+}
+
+// A warp for 16 tokens' keys, or values, of one head; lane 4 g + t has columns 8 t .. 8 t + 7 of each group of tokens g and g + 8.
+// Where 16 tokens of the list fill a strip, it is put together in shared memory and stored by 16 bytes; others' pieces are stored
+// each for itself (a list's tokens lie on strips in any way, but those of a prompt fill most that they touch).
 // VEC: the sources are 16-byte aligned.
-template <bool BF, bool VEC>
-__global__ void __launch_bounds__(kWrite) k_write_4bit(const sim_kv kv, const KvWrite a, const FastDiv per_row, const FastDiv groups) {
+template <int DG, bool BF, bool VEC>
+__global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const KvWrite a, int each) {
+    __shared__ __align__(16) unsigned char images[kWrite / 32][320 * DG];
     kv_wait_previous();
-    const int P = kv.page_size, D = kv.head_dim, G = int(groups.d), H = kv.n_kv_heads, shift = __ffs(P) - 1;
-    const int64_t all = int64_t(a.n_new) * 2 * per_row.d;
-    for (int64_t i0 = int64_t(blockIdx.x) * kWrite; i0 < all; i0 += int64_t(gridDim.x) * kWrite) {
-        const int64_t i = min(i0 + threadIdx.x, all - 1);  // lanes past the end (of all, an even number) make the last one's pair again, or its neighbour's
-        int row, r;
-        if (all <= INT_MAX) {
-            row = int(per_row.div(uint32_t(i)));
-            r = int(i - int64_t(row) * per_row.d);
-        } else {
-            row = int(i / per_row.d);
-            r = int(i % per_row.d);
-        }
-        const int tok = row >> 1, v = row & 1, u = r & 1, h = int(groups.div(uint32_t(r >> 1))), j = (r >> 1) - h * G;
-        const int64_t slot = a.slots[tok], page = slot >> shift;
-        const bool there = slot >= 0 && page < kv.n_pages && i0 + threadIdx.x < all;
-        const uint16_t *const from = static_cast<const uint16_t *>(v ? a.v : a.k) + tok * (v ? a.vt : a.kt) + h * (v ? a.vh : a.kh) + 32 * j + 8 * u;
-        const int left = D - 32 * j - 8 * u;  // columns from the first of this lane's on
-        uint32_t x[8];
+    const int P = kv.page_size, D = kv.head_dim, H = kv.n_kv_heads, shift = __ffs(P) - 1, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    unsigned char *const image = images[threadIdx.x >> 5];
+    const int parts = (2 * H + each - 1) / each;  // of a chunk's heads: `each` for a warp
+    const int64_t jobs = (int64_t(a.n_new) + kStrip - 1) / kStrip * parts;
+    for (int64_t job = int64_t(blockIdx.x) * (kWrite / 32) + (threadIdx.x >> 5); job < jobs; job += int64_t(gridDim.x) * (kWrite / 32)) {
+        const int64_t chunk = job / parts;
+        const int first = int(chunk) * kStrip - kStrip, hv0 = int(job - chunk * parts) * each;  // first: of a window of 48 tokens
+        const auto slot_of = [&](int64_t i) -> int64_t {
+            const int64_t slot = i >= 0 && i < a.n_new ? a.slots[i] : -1;
+            return (slot >> shift) < kv.n_pages ? slot : -1;
+        };
+        const int64_t s0 = slot_of(int64_t(first) + lane), s1 = lane < kStrip ? slot_of(int64_t(first) + 32 + lane) : -1;
+        // Tokens whose slot begins a strip that they and the 15 behind them fill; bit i: the window's token i.
+        int64_t n0 = __shfl_down_sync(FULL, s0, 1);
+        const int64_t n1 = __shfl_down_sync(FULL, s1, 1), s32 = __shfl_sync(FULL, s1, 0);
+        if (lane == 31) n0 = s32;
+        uint64_t run = __ballot_sync(FULL, s0 >= 0 && n0 == s0 + 1) | uint64_t(__ballot_sync(FULL, lane < kStrip - 1 && s1 >= 0 && n1 == s1 + 1)) << 32;
+        run &= run >> 1;
+        run &= run >> 2;
+        run &= run >> 4;
+        run &= run >> 7;  // 15 in a row
+        const uint32_t fills = uint32_t(run) & __ballot_sync(FULL, s0 >= 0 && s0 % kStrip == 0);
+        const uint32_t before = fills & 0xfffeu, here = fills >> 16;  // at most one each that reaches into the chunk
+        const int done = before ? 32 - __clz(before) - 1 + kStrip : kStrip, own = here ? __ffs(here) - 1 + kStrip : 2 * kStrip;
+#pragma unroll 1
+        for (int hw = 2 * hv0; hw < 2 * min(hv0 + each, 2 * H); ++hw) {  // the chunk's tokens that fill no strip; the strip that begins in it
+        const int hv = hw >> 1, whole = hw & 1, v = hv >= H, h = hv - v * H;
+        if (whole ? own == 2 * kStrip : done >= own) continue;
+        const uint16_t *const source = static_cast<const uint16_t *>(v ? a.v : a.k) + h * (v ? a.vh : a.kh) + 8 * t;
+        const int64_t stride = v ? a.vt : a.kt;
+        unsigned char *const heads = static_cast<unsigned char *>(kv.pool) + ((int64_t(a.layer) * 2 + v) * H + h) * kv_head_bytes(kv);
+        const auto strip_at = [&](int64_t slot) {
+            return heads + (slot >> shift) * kv_page_bytes(kv) + int(slot & (P - 1)) / kStrip * kv_strip_bytes(kv);
+        };
+#pragma unroll 1
+            for (int e = 0; e < 2; ++e) {
+                const int at = (whole ? own : kStrip) + g + 8 * e;  // in the window
+                const int64_t lo_slot = __shfl_sync(FULL, s0, at & 31), hi_slot = __shfl_sync(FULL, s1, at & 31), slot = at < 32 ? lo_slot : hi_slot;
+                const bool in = whole || (at >= done && at < own && slot >= 0);
+                const uint16_t *from = source + (int64_t(first) + at) * stride;
+                uint4 x[DG];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (16 * e >= left) {  // none: as others of the group, so that neither lowest nor highest is changed
-                x[4 * e] = x[4 * e + 1] = x[4 * e + 2] = x[4 * e + 3] = e > 0 ? x[0] : 0;
-            } else if (VEC) {
-                const uint4 y = __ldcs(reinterpret_cast<const uint4 *>(from + 16 * e));
-                x[4 * e] = y.x, x[4 * e + 1] = y.y, x[4 * e + 2] = y.z, x[4 * e + 3] = y.w;
-            } else {
+                for (int j = 0; j < DG; ++j) {
+                    x[j] = make_uint4(0, 0, 0, 0);
+                    if (!in || 32 * j + 8 * t >= D) continue;
+                    if (VEC) {
+                        x[j] = __ldcs(reinterpret_cast<const uint4 *>(from + 32 * j));
+                    } else {
+                        const uint16_t *y = from + 32 * j;
+                        x[j] = make_uint4(y[0] | uint32_t(y[1]) << 16, y[2] | uint32_t(y[3]) << 16, y[4] | uint32_t(y[5]) << 16, y[6] | uint32_t(y[7]) << 16);
+                    }
+                }
+                // Each lane's lowest, and highest with its sign turned, so that the lower of both is taken at once; then those of group t.
+                uint32_t ends[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[4 * e + q] = from[16 * e + 2 * q] | uint32_t(from[16 * e + 2 * q + 1]) << 16;
+                for (int j = 0; j < 4; ++j) {
+                    ends[j] = BF ? 0x7f807f80u : 0x7c007c00u;  // none: above all
+                    if (j < DG && 32 * j + 8 * t < D) {
+                        const uint4 y = x[j < DG ? j : 0];
+                        const uint32_t least = min16<BF>(min16<BF>(y.x, y.y), min16<BF>(y.z, y.w)), most = max16<BF>(max16<BF>(y.x, y.y), max16<BF>(y.z, y.w)) ^ 0x80008000u;
+                        ends[j] = min16<BF>(__byte_perm(least, most, 0x5410), __byte_perm(least, most, 0x7632));
+                    }
+                }
+                const bool odd = t & 1, high = t & 2;
+                const uint32_t l0 = min16<BF>(odd ? ends[1] : ends[0], __shfl_xor_sync(FULL, odd ? ends[0] : ends[1], 1));
+                const uint32_t l1 = min16<BF>(odd ? ends[3] : ends[2], __shfl_xor_sync(FULL, odd ? ends[2] : ends[3], 1));
+                const uint32_t mine = min16<BF>(high ? l1 : l0, __shfl_xor_sync(FULL, high ? l0 : l1, 2));
+                const float low = wide<BF>(mine, 0), up = -wide<BF>(mine, 1);
+                const bool finite = low * 0.f == 0.f && up * 0.f == 0.f;
+                const uint32_t step = finite ? step_of<BF>(low, up) : 0x7fffu, scale = step | (finite ? mine << 16 : 0x7fff0000u);
+                // One over the step, to the nearest float; 0 where that, or the quotients by the step, may leave the range, where the step
+                // leaves more than 15.5 of them, and where there is none.
+                const float of = wide<BF>(scale, 0);
+                float over;
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(over) : "f"(of));
+                over = fmaf(fmaf(-of, over, 1.f), over, over);
+                if (!(of > (BF ? 0x1p-100f : 0x1p-18f) && of < (BF ? 0x1p100f : 0x1p14f))) over = 0.f;
+                // bfloat16: a difference that is not exact is one of numbers more than 15 powers of two apart, and is rounded to a border (13
+                // bits) only if the larger is one.  So where the step's borders miss -lo, and lo is 0 or not small, it does not matter.
+                if (BF) {
+                    const float q0 = -low * over, q1 = fmaf(fmaf(-q0, of, -low), over, q0);
+                    const bool on = fabsf(q1 - (q1 + 0x1.8p23f - 0x1.8p23f)) == 0.5f, small = low != 0.f && fabsf(low) < up * 0x1p-14f;
+                    over = on || small ? -over : over;
+                }
+                uint32_t code[DG];
+                const auto quantise = [&](auto values, int j) {  // the codes' places in a word: those of values or of keys
+                    constexpr bool V = decltype(values)::value;
+                    const uint32_t sc = __shfl_sync(FULL, scale, j, 4);
+                    const float in1 = __shfl_sync(FULL, over, j, 4), inv = fabsf(in1), s = wide<BF>(sc, 0), lo = wide<BF>(sc, 1);
+                    const uint4 y = x[j];
+                    // The difference where it is exact, its quotient by the step to the nearest float, and that to the nearest whole number,
+                    // ties to even.  A quotient on a border is a float; one next to it is more than half of a float's unit away, as
+                    // the difference is a float too.
+                    uint32_t cut = 0, w = 0u - 0x4b400000u * 0x11111111u;
+                    const auto value = [&](int q) { return wide<BF>(q < 2 ? y.x : q < 4 ? y.y : q < 6 ? y.z : y.w, q % 2); };
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float d = BF ? value(q) - lo : __fsub_rz(value(q), lo), q0 = d * inv, q1 = fmaf(fmaf(-q0, s, d), inv, q0);
+                        if (!BF) cut |= __float_as_uint(d) ^ __float_as_uint(__fsub_ru(value(q), lo));
+                        w += __float_as_uint(q1 + 0x1.8p23f) << (V ? 4 * q : 4 * (q / 2) + 16 * (q % 2));
+                    }
+                    if (BF ? !(in1 > 0.f) : cut || in1 == 0.f) {
+                        if (BF && in1 < 0.f) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) cut |= __float_as_uint(__fsub_rz(value(q), lo)) ^ __float_as_uint(__fsub_ru(value(q), lo));
+                        }
+                        if (cut || in1 == 0.f) w = s > 0.f && 32 * j + 8 * t < D ? codes_exactly<BF>(y, lo, s, V) : 0;
+                    }
+                    code[j] = w;
+                };
+                if (v) {
+#pragma unroll
+                    for (int j = 0; j < DG; ++j) quantise(std::true_type(), j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < DG; ++j) quantise(std::false_type(), j);
+                }
+                const auto store = [&](unsigned char *to, int T) {
+                    if (v == 0) {
+                        uint32_t *const c = reinterpret_cast<uint32_t *>(to + 16 * DG * T + 4 * DG * t), *const sc = reinterpret_cast<uint32_t *>(to + 256 * DG + 4 * DG * T);
+                        if constexpr (DG == 4) *reinterpret_cast<uint4 *>(c) = make_uint4(code[0], code[1], code[2], code[3]);
+#pragma unroll
+                        for (int j = 0; j < DG && DG != 4; ++j) c[j] = code[j];
+                        if (t < DG) sc[t] = scale;
+                    } else {
+                        unsigned char *const c = to + 128 * DG * (T / 8) + 4 * DG * (8 * t + T % 8 / 2) + 2 * (T % 2);
+                        uint16_t *const sc = reinterpret_cast<uint16_t *>(to + 256 * DG + 8 * DG * (T / 2) + 2 * (T % 2) + 8 * t);
+#pragma unroll
+                        for (int j = 0; j < DG; ++j) {
+                            *reinterpret_cast<uint16_t *>(c + 4 * j) = uint16_t(code[j]);
+                            *reinterpret_cast<uint16_t *>(c + 16 * DG + 4 * j) = uint16_t(code[j] >> 16);
+                        }
+                        if (t < DG) {
+                            sc[0] = uint16_t(scale);
+                            sc[2] = uint16_t(scale >> 16);
+                        }
+                    }
+                };
+                if (whole) store(image, g + 8 * e);
+                else if (in) store(strip_at(slot), int(slot & (kStrip - 1)));
             }
-        }
-        uint32_t least = x[0], most = x[0];
+            if (whole) {
+                __syncwarp();
+                uint4 *const to = reinterpret_cast<uint4 *>(strip_at(__shfl_sync(FULL, s0, own)));
 #pragma unroll
-        for (int e = 1; e < 8; ++e) {
-            least = min16<BF>(least, x[e]);
-            most = max16<BF>(most, x[e]);
-        }
-        least = min16<BF>(least, least >> 16 | least << 16);
-        most = max16<BF>(most, most >> 16 | most << 16);
-        const uint32_t mine = __byte_perm(least, most, 0x5410), other = __shfl_xor_sync(FULL, mine, 1);
-        const bool both = D - 32 * j > 8;  // the group has columns for the second lane
-        least = both ? min16<BF>(mine, other) & 0xffffu : (u ? other : mine) & 0xffffu;
-        most = both ? max16<BF>(mine, other) >> 16 : (u ? other : mine) >> 16;
-        float lo = wide16<BF>(least);
-        const float hi = wide16<BF>(most);
-        const bool finite = lo * 0.f == 0.f && hi * 0.f == 0.f;
-        const uint32_t step = finite ? step_of<BF>(lo, hi) : 0x7fffu, base = finite ? least : 0x7fffu;
-        float s = finite ? wide16<BF>(step) : 0.f;
-        // Tiny steps, whose reciprocals overflow, and large ones, whose differences do, after a multiplication by a power of two.
-        const float more = BF && s > 0.f && s < 0x1p-60f ? 0x1p60f : BF && s > 0x1p110f ? 0x1p-8f : 1.f;
-        s *= more;
-        lo = finite ? lo * more : 0.f;
-        float inv = 0.f;
-        if (s > 0.f) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));  // f16's least is 2^-24
-        uint32_t w[4];  // of columns 2 q and 2 q + 1 at bits 4 q of two halves, for 8 columns; or of four and four
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float part[2] = {0.f, 0.f};  // four codes each, below 2^16: exact
-            constexpr float kScale[4] = {1.f, 16.f, 256.f, 4096.f};
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float val = wide<BF>(x[4 * e + q / 2], q % 2), t = fmaf(val, more, -lo), near = fmaf(t, inv, 0x1.8p23f) - 0x1.8p23f;
-                float code = near;  // the quotient, within 2^-18 where it is below 16, to the nearest
-                if (fabsf(fmaf(t, inv, -near)) > 0.5f - 0x1p-17f) code = code_at_border(val * more, lo, t, t * inv, s);
-                code = fminf(code, 15.f);
-                part[v ? q / 4 : q % 2] = fmaf(code, kScale[v ? q % 4 : q / 2], part[v ? q / 4 : q % 2]);
+                for (int i = 0; i < (20 * DG + 31) / 32; ++i)
+                    if (lane + 32 * i < 20 * DG) __stcs(to + lane + 32 * i, reinterpret_cast<const uint4 *>(image)[lane + 32 * i]);
+                __syncwarp();
             }
-            w[2 * e] = finite ? uint32_t(part[0]) : 0;
-            w[2 * e + 1] = finite ? uint32_t(part[1]) : 0;
-        }
-        if (!there) continue;
-        unsigned char *const strip = static_cast<unsigned char *>(kv.pool) + page * kv_page_bytes(kv) +
-                                     ((int64_t(a.layer) * 2 + v) * H + h) * kv_head_bytes(kv) + int(slot & (P - 1)) / kStrip * kv_strip_bytes(kv);
-        const int T = int(slot & (kStrip - 1));
-        if (v == 0) {
-            uint32_t *const to = reinterpret_cast<uint32_t *>(strip + 16 * G * T + 4 * G * u + 4 * j);
-            to[0] = w[0] | w[1] << 16;
-            to[2 * G] = w[2] | w[3] << 16;
-            if (u == 0) *reinterpret_cast<uint32_t *>(strip + 256 * G + 4 * G * T + 4 * j) = step | base << 16;
-        } else {
-            uint16_t *const to = reinterpret_cast<uint16_t *>(strip + 128 * G * (T / 8) + 4 * G * (T % 8 / 2) + 32 * G * u + 4 * j + 2 * (T % 2));
-            to[0] = uint16_t(w[0]);
-            to[8 * G] = uint16_t(w[1]);
-            to[32 * G] = uint16_t(w[2]);
-            to[40 * G] = uint16_t(w[3]);
-            uint16_t *const sc = reinterpret_cast<uint16_t *>(strip + 256 * G + 8 * G * (T / 2) + 8 * j + 2 * (T % 2));
-            sc[2 * u] = uint16_t(u ? base : step);
         }
     }
 }
@@ -295,10 +383,15 @@ int blocks_for(int64_t items, int per_block, int per_sm) {
 cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_t st) {
     const auto aligned = [](const void *p, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && a % 8 == 0 && b % 8 == 0; };
     const bool vec = aligned(w.k, w.kt, w.kh) && aligned(w.v, w.vt, w.vh);
-    const auto k = kv_bf(kv) ? (vec ? k_write_4bit<true, true> : k_write_4bit<true, false>) : vec ? k_write_4bit<false, true> : k_write_4bit<false, false>;
-    const int G = kv_dim_groups(kv), per_row = 2 * G * kv.n_kv_heads;  // lanes for a token's keys, or its values
-    const int blocks = blocks_for(int64_t(w.n_new) * 2 * per_row, kWrite, 4096);
-    return launch_chained(k, blocks, kWrite, 0, st, kv, w, FastDiv(per_row), FastDiv(G));
+    using Fn = void (*)(const sim_kv, const KvWrite, int);
+    constexpr Fn of[2][2][4] = {{{k_write_4bit<1, false, false>, k_write_4bit<2, false, false>, k_write_4bit<3, false, false>, k_write_4bit<4, false, false>},
+                                 {k_write_4bit<1, false, true>, k_write_4bit<2, false, true>, k_write_4bit<3, false, true>, k_write_4bit<4, false, true>}},
+                                {{k_write_4bit<1, true, false>, k_write_4bit<2, true, false>, k_write_4bit<3, true, false>, k_write_4bit<4, true, false>},
+                                 {k_write_4bit<1, true, true>, k_write_4bit<2, true, true>, k_write_4bit<3, true, true>, k_write_4bit<4, true, true>}}};
+    const int64_t chunks = (int64_t(w.n_new) + kStrip - 1) / kStrip;
+    const int each = chunks * 2 * kv.n_kv_heads >= int64_t(kv_sm_count()) * 96 ? 4 : 1;
+    const int blocks = blocks_for(chunks * ((2 * kv.n_kv_heads + each - 1) / each), kWrite / 32, 4096);
+    return launch_chained(of[kv_bf(kv)][vec][kv_dim_groups(kv) - 1], blocks, kWrite, 0, st, kv, w, each);
 }
 
 cudaError_t launch_kv_read(const sim_kv &kv, const KvRead &r, cudaStream_t st) {
