@@ -69,8 +69,18 @@ __device__ __forceinline__ void values4(uint32_t w, uint32_t step, uint32_t lo, 
     x[2] = values<BF, 2>(w, step, lo);
     x[3] = values<BF, 3>(w, step, lo);
 }
-__device__ __forceinline__ uint32_t low_twice(uint32_t x) { return __byte_perm(x, 0, 0x1010); }
-__device__ __forceinline__ uint32_t high_twice(uint32_t x) { return __byte_perm(x, 0, 0x3232); }
+// The lower, the upper half twice: as moves, which the instruction that takes them can do by itself (as permutations: 168 instead of
+// 161 us for 384 sequences of up to 2600 keys).
+__device__ __forceinline__ uint32_t low_twice(uint32_t x) {
+    uint32_t d;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tmov.b32 %0, {l, l};\n\t}" : "=r"(d) : "r"(x));
+    return d;
+}
+__device__ __forceinline__ uint32_t high_twice(uint32_t x) {
+    uint32_t d;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tmov.b32 %0, {h, h};\n\t}" : "=r"(d) : "r"(x));
+    return d;
+}
 
 }  // namespace
 

@@ -20,14 +20,14 @@ constexpr int kStrips = kTileKeys / kStrip;  // of a tile
 // DG groups of 32 columns, NT times 8 query rows in a pass, W warps that compute and one that loads.
 template <int DG, int NT, int W>
 struct Shape {
-    static constexpr int kSteps = NT > 2 ? 1 : kStrips / W;  // strips that a warp takes at a time
+    static constexpr int kSteps = NT > 2 ? 1 : kStrips / W;   // strips that a warp takes at a time
     static constexpr int kThreads = 32 * (W + 1);
     static constexpr int kRows = 8 * NT;
     static constexpr int kBytesStrip = 320 * DG;
     static constexpr int kStage = 2 * kStrips * kBytesStrip;  // a tile's keys, then its values
     static constexpr int kPitch = 32 * DG + 4;                // floats between rows of the warps' O
     static constexpr int kPerSm = NT == 1 ? 3 : 2;            // blocks, as in kv_per_sm
-    static constexpr int kRoom = kPerSm == 3 ? 76800 : 115712;
+    static constexpr int kRoom = 233472 / kPerSm - 1024;
     // Queries and sums twice, so that one barrier for each part of a segment is enough.
     static constexpr int kSizeQ = NT * DG * 512, kSizeO = W * 8 * kPitch * 4, kSizeM = W * kRows * 8;
     static constexpr int kOffQ = 0;                           // queries: [NT][DG][lane] 16 bytes
@@ -35,7 +35,7 @@ struct Shape {
     static constexpr int kOffM = kOffO + kSizeO;              // [W][kRows] off and sum
     static constexpr int kOffSeg = kOffM + 2 * kSizeM;
     static constexpr int kFixed = kOffSeg + kSegs * int(sizeof(Segment)) + 256;
-    static constexpr int kStages = (kRoom - kFixed) / kStage < 4 ? (kRoom - kFixed) / kStage : 4;
+    static constexpr int kStages = (kRoom - kFixed) / kStage < 8 ? (kRoom - kFixed) / kStage : 8;
     static constexpr int kOffRing = (kOffSeg + kSegs * int(sizeof(Segment)) + 127) / 128 * 128;
     static constexpr int kOffBar = kOffRing + kStages * kStage;
     static constexpr int kBars = 2 * kStages + 2 * kSegs + 2;
@@ -72,8 +72,13 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
     volatile int *const gave_up = reinterpret_cast<int *>(base + Sh::kOffGone + NS * 4);
     uint32_t *const gone = reinterpret_cast<uint32_t *>(base + Sh::kOffGone);
     Segment *const segs = reinterpret_cast<Segment *>(base + Sh::kOffSeg);
-    const auto full = [&](uint32_t x) { return bars + 8 * (x % NS); };
-    const auto empty = [&](uint32_t x) { return bars + 8 * (NS + x % NS); };
+    const auto full = [&](uint32_t slot) { return bars + 8 * slot; };
+    const auto empty = [&](uint32_t slot) { return bars + 8 * (NS + slot); };
+    uint32_t slot = 0, turn = 0;  // of the ring
+    const auto next_slot = [&] {
+        slot = slot + 1 == NS ? 0 : slot + 1;
+        turn ^= slot == 0;
+    };
     const auto seg_full = [&](uint32_t x) { return bars + 8 * (2 * NS + x % kSegs); };
     const auto seg_empty = [&](uint32_t x) { return bars + 8 * (2 * NS + kSegs + x % kSegs); };
     const uint32_t joined = bars + 8 * (2 * NS + 2 * kSegs), cleared = joined + 8;
@@ -97,13 +102,14 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
     const int G = b.q_heads / kv.n_kv_heads, D = kv.head_dim;
 
     if (warp == W) {
-        // ---- the line of work, and loads: lane l brings the keys of strip l, lane 8 + l its values
+        // ---- the line of work, and loads: lane l brings the keys of strip l, lane kStrips + l its values, those of a page's first
+        // strip the others' of that page with them
         const KvPlan plan = kv_plan(kv, b);
         Line line(plan, kv.n_kv_heads, 1, blockIdx.x, a.sms);
-        const int P = kv.page_size, strip = lane % kStrips;
+        const int P = kv.page_size, strip = lane % kStrips, per = min(kStrips, P / kStrip);  // per: strips of a tile on one page
         const int64_t head_bytes = kv_head_bytes(kv), page_bytes = kv_page_bytes(kv);
         const unsigned char *const layer = static_cast<const unsigned char *>(kv.pool) + int64_t(a.layer) * 2 * kv.n_kv_heads * head_bytes;
-        uint32_t at = 0, x = 0;  // tiles loaded, segments told of
+        uint32_t x = 0;  // segments told of
         bool ok = true;
         const auto tell = [&](const Segment &sg) {
             ok = __all_sync(FULL, bar_wait(seg_empty(x), (x / kSegs + 1) & 1, gave_up));
@@ -130,20 +136,21 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                     return j < sg.n && key < sg.kv1 ? row[key / P] : -1;
                 };
                 int page = page_of(0);
-                for (int j = 0; j < sg.n && ok; ++j, ++at) {
+                for (int j = 0; j < sg.n && ok; ++j, next_slot()) {
                     const int next_page = page_of(j + 1), key = sg.k0 + j * kTileKeys + strip * kStrip;
                     const bool in = key < sg.kv1, there = in && unsigned(page) < unsigned(kv.n_pages);
-                    ok = __all_sync(FULL, bar_wait(empty(at), (at / NS + 1) & 1, gave_up));
+                    ok = __all_sync(FULL, bar_wait(empty(slot), turn ^ 1, gave_up));
                     if (!ok) break;
                     const unsigned none = __ballot_sync(FULL, lane < kStrips && in && !there), some = __ballot_sync(FULL, lane < 2 * kStrips && there);
                     if (lane == 0) {
-                        gone[at % NS] = none;
-                        bar_expect(full(at), __popc(some) * KS);
+                        gone[slot] = none;
+                        bar_expect(full(slot), __popc(some) * KS);
                     }
                     __syncwarp();
-                    if (lane < 2 * kStrips && there)
-                        bulk_load(sbase + Sh::kOffRing + (at % NS) * Sh::kStage + lane * KS,
-                                  layer + page * page_bytes + ((lane / kStrips) * kv.n_kv_heads + sg.h) * head_bytes + key % P / kStrip * KS, KS, full(at));
+                    if (lane < 2 * kStrips && there && strip % per == 0)
+                        bulk_load(sbase + Sh::kOffRing + slot * Sh::kStage + lane * KS,
+                                  layer + page * page_bytes + ((lane / kStrips) * kv.n_kv_heads + sg.h) * head_bytes + key % P / kStrip * KS,
+                                  KS * min(per, (sg.kv1 - key + kStrip - 1) / kStrip), full(slot));
                     page = next_page;
                 }
             }
@@ -151,8 +158,8 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
         all.n = 0;
         if (ok) tell(all);
         if (!ok) {  // let what is on its way arrive
-            for (uint32_t k = at > NS ? at - NS : 0; k < at; ++k)
-                for (int n = 0; n < 1000000 && !bar_try(full(k), (k / NS) & 1); ++n) {
+            for (int k = 0; k < NS; ++k, next_slot())  // (a slot that was never asked for is in its first turn, as is this wait)
+                for (int n = 0; n < 1000000 && !bar_try(full(slot), turn ^ 1); ++n) {
                 }
             if (lane == 0) atomicMin(kv.status, SIM_E_STATE);
         }
@@ -162,7 +169,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
     // ---- products, softmax, results: lane 4 g + t
     const int g = lane >> 2, t = lane & 3;
     const float c = a.scale_log2;
-    uint32_t at = 0, nj = 0, no = 0;
+    uint32_t nj = 0, no = 0;
     bool ok = true;
     const auto join = [&] {  // the warps, by a barrier whose wait ends even if some have given up
         __syncwarp();
@@ -221,21 +228,21 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
             sum[i][0] = sum[i][1] = 0.f;
         }
 #pragma unroll 1
-        for (int tile = 0; tile < n; ++tile, ++at) {
+        for (int tile = 0; tile < n; ++tile, next_slot()) {
             if (tile == n - 1) {  // the next segment's queries are on their way while this one ends
                 ok = take(x + 1);
                 if (!ok) break;
                 if (next.n > 0) fetch(next);
             }
-            ok = __all_sync(FULL, bar_wait(full(at), (at / NS) & 1, gave_up));
+            ok = __all_sync(FULL, bar_wait(full(slot), turn, gave_up));
             if (!ok) break;
-            const unsigned char *const stage = base + Sh::kOffRing + (at % NS) * Sh::kStage;
+            const unsigned char *const from = base + Sh::kOffRing + slot * Sh::kStage;
 #pragma unroll 1
             for (int step = 0; step < kStrips / W; step += SP) {
                 const int strip0 = warp * (kStrips / W) + step, key0 = sg.k0 + tile * kTileKeys + strip0 * kStrip;
                 if (key0 >= kv1) break;
-                const unsigned char *const ks = stage + strip0 * KS, *const vs = ks + kStrips * KS;
-                const uint32_t none = gone[at % NS] >> strip0;  // strips on pages that the pool does not have: zeros
+                const unsigned char *const ks = from + strip0 * KS, *const vs = ks + kStrips * KS;
+                const uint32_t none = gone[slot] >> strip0;  // strips on pages that the pool does not have: zeros
                 // S': lane has keys g and g + 8, rows 2 t and 2 t + 1 of each 8
                 float s[SP][NT][4];
 #pragma unroll
@@ -372,7 +379,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                 }
             }
             __syncwarp();
-            if (lane == 0) bar_arrive(empty(at));
+            if (lane == 0) bar_arrive(empty(slot));
         }
         if (!ok) break;
         place(x + 1);

@@ -404,6 +404,7 @@ struct Pieces {
 
 constexpr int kJoin = 128;      // threads
 constexpr int kJoinRows = 8;    // rows of a block at a time, 16 lanes each: as many as a token has heads in a group, often
+constexpr int kJoinMany = 16;   // pieces; rows of more in a 4-bit cache are joined by all half warps of a block
 constexpr int kJoinHeavy = 16;  // blocks for each cut of a heavy item, of a light one
 constexpr int kJoinLight = 4;
 
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
         // rows z, z + step, .. below z1 of query tokens from q0 on, and kv head h
         Pieces first, own;
         KvSource x;
-        int q0, h, z, z1, step;
+        int q0, h, z, z1, step, cut_rows = 0;
         const bool by_cut = y < cuts;
         if (by_cut) {
             const bool light = y >= heavy;
@@ -450,6 +451,7 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
             h = cut.h;
             z = cut.row0 + int(nth - c * per) * kJoinRows + sub;
             z1 = cut.row0 + cut.rows;
+            cut_rows = cut.rows;
             step = kJoinRows * int(per);
         } else {
             const uint32_t pairs = uint32_t(plan.hdr[17]) * uint32_t(H), part = (y - cuts) / pairs, ih = (y - cuts) - part * pairs, i = ih / uint32_t(H);
@@ -460,41 +462,16 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
             z1 = x.rows;
             step = kJoinRows * parts;
         }
-#pragma unroll 1
-        for (; z < z1; z += step) {
-            const int dt = a.group.div(z), t = q0 + dt, qh = h * G + z - dt * G;
-            int in = z, pin = 0;
-            if (!by_cut) {
-                if (x.prefix < 0) {  // only rows of items without keys: the item's last row sees the most
-                    const int end = min(z / per_item * per_item + per_item, x.rows);
-                    if (min(x.kv1, x.pos0 + int(a.group.div(end - 1)) + 1) > 0) continue;
-                } else {
-                    const int nth = z / kAttRows;
-                    in = z % kAttRows;
-                    if (nth >= x.n_heavy) {
-                        own = Pieces(share1, base1, x.unit, x.tiles, x.row_off, min(x.rows - nth * kAttRows, kAttRows), h, 1);
-                    } else {
-                        const KvItem it = plan.items[0][x.heavy0 + nth];
-                        own = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
-                    }
-                    const KvSource px = plan.source[x.prefix];
-                    const int row = (q0 - px.q0) * G + z, pth = row / kAttRows;
-                    pin = row % kAttRows;
-                    if (pth >= px.n_heavy) {
-                        first = Pieces(share1, base1, px.unit, px.tiles, px.row_off, min(px.rows - pth * kAttRows, kAttRows), h, 1);
-                    } else {
-                        const KvItem it = plan.items[0][px.heavy0 + pth];
-                        first = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
-                    }
-                }
-            }
-            const int n = first.n + own.n;
-            float top = -INFINITY, total = 0.f;
-            float4 acc[2] = {};
+        float top, total;
+        float4 acc[2];
+        const auto gather = [&](int n, auto &&piece) {  // n pieces' rows, by a half warp
+            top = -INFINITY;
+            total = 0.f;
+            acc[0] = acc[1] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
             for (int p0 = 0; p0 < n; p0 += 16) {
                 const int p = p0 + sl;
-                int64_t at = p < first.n ? first.at(p, pin) : own.at(p - first.n, in);
+                int64_t at = p < n ? piece(p) : -1;
                 const float s = at >= 0 ? __ldcg(a.part_lse + at) : -INFINITY;
                 const int64_t some = __shfl_sync(mine, at, 0, 16);
                 at = at >= 0 ? at : some;  // a piece that is not there: another, with weight 0
@@ -532,6 +509,65 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
                     }
                 }
             }
+        };
+        // In a 4-bit cache, rows in many pieces: each half warp an eighth of them, joined in shared memory (one sequence of 131071 keys, 57 pieces
+        // for each of 64 rows: the whole call 50 instead of 56 us).  By whole blocks.
+        if (by_cut && kv_4bit(kv) && own.n > kJoinMany) {
+            __shared__ float part_o[kJoinRows][128], part_top[kJoinRows], part_sum[kJoinRows];
+            const int each = (own.n + kJoinRows - 1) / kJoinRows;
+#pragma unroll 1
+            for (int y = z1 - cut_rows + (z - sub - (z1 - cut_rows)) / kJoinRows; y < z1; y += step / kJoinRows) {
+                gather(max(min(own.n - sub * each, each), 0), [&](int p) { return own.at(sub * each + p, y); });
+#pragma unroll
+                for (int q = 0; q < 2; ++q) *reinterpret_cast<float4 *>(&part_o[sub][4 * (sl + 16 * q)]) = acc[q];
+                if (sl == 0) part_top[sub] = top, part_sum[sub] = total;
+                __syncthreads();
+                float up = -INFINITY, sum = 0.f, v = 0.f;
+#pragma unroll
+                for (int i = 0; i < kJoinRows; ++i) up = fmaxf(up, part_top[i]);
+#pragma unroll
+                for (int i = 0; i < kJoinRows; ++i) {
+                    const float w = part_top[i] == -INFINITY ? 0.f : ex2(part_top[i] - up);
+                    sum = fmaf(part_sum[i], w, sum);
+                    if (w != 0.f) v = fmaf(part_o[i][threadIdx.x], w, v);
+                }
+                const int dt = a.group.div(y), t = q0 + dt, qh = h * G + y - dt * G;
+                v = sum == 0.f ? 0.f : v / sum;
+                if (threadIdx.x < D) (static_cast<uint16_t *>(a.out) + int64_t(t) * a.ot + int64_t(qh) * a.oh)[threadIdx.x] = uint16_t(pack<BF>(v, v));
+                if (threadIdx.x == 0 && a.lse) a.lse[int64_t(t) * b.q_heads + qh] = sum == 0.f ? -INFINITY : (up + log2f(sum)) * 0.69314718055994531f;
+                __syncthreads();
+            }
+            continue;
+        }
+#pragma unroll 1
+        for (; z < z1; z += step) {
+            const int dt = a.group.div(z), t = q0 + dt, qh = h * G + z - dt * G;
+            int in = z, pin = 0;
+            if (!by_cut) {
+                if (x.prefix < 0) {  // only rows of items without keys: the item's last row sees the most
+                    const int end = min(z / per_item * per_item + per_item, x.rows);
+                    if (min(x.kv1, x.pos0 + int(a.group.div(end - 1)) + 1) > 0) continue;
+                } else {
+                    const int nth = z / kAttRows;
+                    in = z % kAttRows;
+                    if (nth >= x.n_heavy) {
+                        own = Pieces(share1, base1, x.unit, x.tiles, x.row_off, min(x.rows - nth * kAttRows, kAttRows), h, 1);
+                    } else {
+                        const KvItem it = plan.items[0][x.heavy0 + nth];
+                        own = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
+                    }
+                    const KvSource px = plan.source[x.prefix];
+                    const int row = (q0 - px.q0) * G + z, pth = row / kAttRows;
+                    pin = row % kAttRows;
+                    if (pth >= px.n_heavy) {
+                        first = Pieces(share1, base1, px.unit, px.tiles, px.row_off, min(px.rows - pth * kAttRows, kAttRows), h, 1);
+                    } else {
+                        const KvItem it = plan.items[0][px.heavy0 + pth];
+                        first = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
+                    }
+                }
+            }
+            gather(first.n + own.n, [&](int p) { return p < first.n ? first.at(p, pin) : own.at(p - first.n, in); });
             const float f = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
             for (int q = 0; q < 2; ++q) acc[q] = make_float4(acc[q].x * f, acc[q].y * f, acc[q].z * f, acc[q].w * f);

@@ -105,11 +105,7 @@ __host__ __device__ inline int kv_per_sm(const sim_kv &kv, const sim_kv_batch &b
 constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.
-#ifndef KLEAD4
-#define KLEAD4 2
-#endif
-constexpr int kLead4 = KLEAD4;
-__host__ __device__ inline int kv_lead(const sim_kv &kv, int light) { return light ? (kv_4bit(kv) ? kLead4 : 1) : 4; }
+__host__ __device__ inline int kv_lead(const sim_kv &kv, int light) { return light ? (kv_4bit(kv) ? 2 : 1) : 4; }
 __host__ __device__ inline int kv_span(int tiles, int lead) { return tiles > 0 ? tiles + lead : 0; }
 
 // A run of query rows (token x head of the group, for every kv head alike) against a range of one table's keys.
