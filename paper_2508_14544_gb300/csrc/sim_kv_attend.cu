@@ -415,7 +415,8 @@ constexpr int kJoinLight = 4;
 // and rows without keys, by kv head (`parts` blocks for each).  Loads of pieces that are not there are made all the same, from
 // another piece's row, so that the four of a lane need not be told apart (64 rows in 38 pieces: 118 us the whole call either way).
 // 18 us for 16384 rows with a prefix in 3 or 4 pieces and their own keys, 15 us for the cuts of 152 heavy stretches.
-template <bool BF>
+// MANY: rows in many pieces are joined by whole blocks.
+template <bool BF, bool MANY>
 __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
         };
         // In a 4-bit cache, rows in many pieces: each half warp an eighth of them, joined in shared memory (one sequence of 131071 keys, 57 pieces
         // for each of 64 rows: the whole call 50 instead of 56 us).  By whole blocks.
-        if (by_cut && kv_4bit(kv) && own.n > kJoinMany) {
+        if constexpr (MANY) if (by_cut && own.n > kJoinMany) {
             __shared__ float part_o[kJoinRows][128], part_top[kJoinRows], part_sum[kJoinRows];
             const int each = (own.n + kJoinRows - 1) / kJoinRows;
 #pragma unroll 1
@@ -639,7 +640,9 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     // blocks for an entry and head: for twice the rows that they have on average
     const int64_t parts = std::min<int64_t>(std::max<int64_t>((2 * rows / kv.n_kv_heads / std::max(b.n, 1) + kJoinRows - 1) / kJoinRows, 1), 16);
     const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 5));
-    return launch_chained(kv_bf(kv) ? k_combine<true> : k_combine<false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
+    // few rows of a 4-bit cache: their pieces are many
+    const bool many = packed && rows <= int64_t(a.sms) * kJoinRows;
+    return launch_chained(kv_bf(kv) ? (many ? k_combine<true, true> : k_combine<true, false>) : many ? k_combine<false, true> : k_combine<false, false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 
 }  // namespace simgb
