@@ -12,6 +12,7 @@ namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int kWrite = 256, kRead = 256;  // threads
+constexpr int kFewEntries = 1024;
 
 template <bool BF>
 __device__ __forceinline__ float wide(uint32_t x, int half) {
@@ -96,16 +97,17 @@ __device__ __noinline__ uint32_t codes_exactly(uint4 x, float lo, float s, bool 
 // each for itself (a list's tokens lie on strips in any way, but those of a prompt fill most that they touch).
 // VEC: the sources are 16-byte aligned.
 template <int DG, bool BF, bool VEC>
-__global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const KvWrite a, int each) {
+__global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const KvWrite a, int each, int few) {
     __shared__ __align__(16) unsigned char images[kWrite / 32][320 * DG];
     kv_wait_previous();
     const int P = kv.page_size, D = kv.head_dim, H = kv.n_kv_heads, shift = __ffs(P) - 1, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     unsigned char *const image = images[threadIdx.x >> 5];
-    const int parts = (2 * H + each - 1) / each;  // of a chunk's heads: `each` for a warp
+    // A warp takes `each` of a chunk's heads; of few tokens, one head's 8 of the 16, whatever they fill.
+    const int parts = few ? 4 * H : (2 * H + each - 1) / each;
     const int64_t jobs = (int64_t(a.n_new) + kStrip - 1) / kStrip * parts;
-    for (int64_t job = int64_t(blockIdx.x) * (kWrite / 32) + (threadIdx.x >> 5); job < jobs; job += int64_t(gridDim.x) * (kWrite / 32)) {
+    for (int64_t job = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5); job < jobs; job += int64_t(gridDim.x) * (blockDim.x >> 5)) {
         const int64_t chunk = job / parts;
-        const int first = int(chunk) * kStrip - kStrip, hv0 = int(job - chunk * parts) * each;  // first: of a window of 48 tokens
+        const int first = int(chunk) * kStrip - kStrip, part = int(job - chunk * parts), hv0 = few ? part >> 1 : part * each;  // first: of a window of 48 tokens
         const auto slot_of = [&](int64_t i) -> int64_t {
             const int64_t slot = i >= 0 && i < a.n_new ? a.slots[i] : -1;
             return (slot >> shift) < kv.n_pages ? slot : -1;
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
         run &= run >> 7;  // 15 in a row
         const uint32_t fills = uint32_t(run) & __ballot_sync(FULL, s0 >= 0 && s0 % kStrip == 0);
         const uint32_t before = fills & 0xfffeu, here = fills >> 16;  // at most one each that reaches into the chunk
-        const int done = before ? 32 - __clz(before) - 1 + kStrip : kStrip, own = here ? __ffs(here) - 1 + kStrip : 2 * kStrip;
+        const int done = few ? kStrip : before ? 32 - __clz(before) - 1 + kStrip : kStrip, own = !few && here ? __ffs(here) - 1 + kStrip : 2 * kStrip;
 #pragma unroll 1
         for (int hw = 2 * hv0; hw < 2 * min(hv0 + each, 2 * H); ++hw) {  // the chunk's tokens that fill no strip; the strip that begins in it
         const int hv = hw >> 1, whole = hw & 1, v = hv >= H, h = hv - v * H;
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
             return heads + (slot >> shift) * kv_page_bytes(kv) + int(slot & (P - 1)) / kStrip * kv_strip_bytes(kv);
         };
 #pragma unroll 1
-            for (int e = 0; e < 2; ++e) {
+            for (int e = few ? part & 1 : 0; e < (few ? (part & 1) + 1 : 2); ++e) {
                 const int at = (whole ? own : kStrip) + g + 8 * e;  // in the window
                 const int64_t lo_slot = __shfl_sync(FULL, s0, at & 31), hi_slot = __shfl_sync(FULL, s1, at & 31), slot = at < 32 ? lo_slot : hi_slot;
                 const bool in = whole || (at >= done && at < own && slot >= 0);
@@ -256,15 +258,15 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
 
 // Entry i's rows lie on strips of its sequence; they have the numbers from cu[i] / 16 + 2 i on, which leave each entry at least as many
 // as it needs.
-__device__ __forceinline__ int64_t first_strip(const KvRead &r, int i) { return r.cu[i] / kStrip + 2 * int64_t(i); }
+__device__ __forceinline__ int64_t first_strip(const int32_t *cu, int i) { return cu[i] / kStrip + 2 * int64_t(i); }
 
 // The last entry whose strips begin at or before x, by a warp: a 32nd of what is left at a time.
-__device__ __forceinline__ int entry_of_strip(const KvRead &r, int64_t x) {
+__device__ __forceinline__ int entry_of_strip(const int32_t *cu, int n, int64_t x) {
     const int lane = threadIdx.x & 31;
-    int lo = 0, hi = r.n;  // in [lo, hi)
+    int lo = 0, hi = n;  // in [lo, hi)
     while (hi - lo > 1) {
         const int each = (hi - lo + 31) / 32, at = lo + lane * each;
-        const int k = __popc(__ballot_sync(FULL, at < hi && first_strip(r, at) <= x));
+        const int k = __popc(__ballot_sync(FULL, at < hi && first_strip(cu, at) <= x));
         lo += max(k - 1, 0) * each;
         hi = min(lo + each, hi);
     }
@@ -276,8 +278,17 @@ template <int DG, bool BF>
 __global__ void __launch_bounds__(kRead) k_read(const sim_kv kv, const KvRead r) {
     kv_wait_previous();
     const int lane = threadIdx.x & 31, H = kv.n_kv_heads, D = kv.head_dim, P = kv.page_size;
+    // Offsets of a few entries are searched where they have been read to, in shared memory.
+    __shared__ int32_t few_cu[kFewEntries + 1];
+    const bool few = r.n <= kFewEntries;
+    const int32_t *const cu = few ? few_cu : r.cu;
     bool order = true;
-    for (int i = threadIdx.x; i < r.n; i += kRead) order = order && 0 <= r.cu[i] && r.cu[i] <= r.cu[i + 1] && r.cu[i + 1] <= r.total;
+    for (int i = threadIdx.x; i < r.n; i += kRead) {
+        const int a = r.cu[i], b = r.cu[i + 1];
+        order = order && 0 <= a && a <= b && b <= r.total;
+        if (few) few_cu[i] = a;
+        if (few && i + 1 == r.n) few_cu[i + 1] = b;
+    }
     order = __syncthreads_and(order);
     if (!order && blockIdx.x == 0 && threadIdx.x == 0) atomicMin(kv.status, SIM_E_INVAL);
     uint16_t *const to[2] = {static_cast<uint16_t *>(r.k), static_cast<uint16_t *>(r.v)};
@@ -286,20 +297,23 @@ __global__ void __launch_bounds__(kRead) k_read(const sim_kv kv, const KvRead r)
         for (int d = 8 * lane; d < 2 * D; d += 256) *reinterpret_cast<uint4 *>(row(d >= D, y, h) + (d >= D ? d - D : d)) = make_uint4(0, 0, 0, 0);
     };
     const int64_t warp0 = int64_t(blockIdx.x) * (kRead / 32) + (threadIdx.x >> 5), warps = int64_t(gridDim.x) * (kRead / 32);
-    const int64_t x0 = order && r.n > 0 ? first_strip(r, 0) : 0, all = order && r.n > 0 ? (first_strip(r, r.n) - x0) * H : 0;
+    const int64_t x0 = order && r.n > 0 ? first_strip(cu, 0) : 0, all = order && r.n > 0 ? (first_strip(cu, r.n) - x0) * H : 0;
     for (int64_t z = warp0; z < all; z += warps) {
         const int64_t x = x0 + z / H;
-        const int h = int(z % H), i = entry_of_strip(r, x), a = r.cu[i], count = r.cu[i + 1] - a, nth = int(x - first_strip(r, i));
+        const int h = int(z % H), i = entry_of_strip(cu, r.n, x), a = cu[i], count = cu[i + 1] - a, nth = int(x - first_strip(cu, i));
         if (count == 0) continue;
         const int s = r.seqs[i], f = r.first ? r.first[i] : 0;
-        if (unsigned(s) >= unsigned(kv.max_seqs) || f < 0 || int64_t(f) + count > kv.length[s] || kv.length[s] > kv.max_pages * P) {
+        const bool known = unsigned(s) < unsigned(kv.max_seqs) && f >= 0 && int64_t(f) + count <= int64_t(kv.max_pages) * P;
+        const int T0 = known ? (f / kStrip + nth) * kStrip : 0;  // token of the strip's first place
+        // the length and the page at once: a strip past the entry's tokens may have none
+        const int length = known ? kv.length[s] : 0, page = known && T0 < f + count ? kv.table[int64_t(s) * kv.max_pages + T0 / P] : -1;
+        if (!known || f + count > length) {
             if (lane == 0) atomicMin(kv.status, SIM_E_INVAL);
             for (int y = nth * kStrip; y < min(nth * kStrip + kStrip, count); ++y) zeros(a + y, h);
             continue;
         }
-        const int T0 = (f / kStrip + nth) * kStrip;  // token of the strip's first place
         if (T0 >= f + count) continue;
-        const int page = kv.table[int64_t(s) * kv.max_pages + T0 / P], y0 = a - f + T0;
+        const int y0 = a - f + T0;
         const bool there = unsigned(page) < unsigned(kv.n_pages);
         const auto in = [&](int T) { return T0 + T >= f && T0 + T < f + count; };
         const unsigned char *const base = static_cast<const unsigned char *>(kv.pool) + (there ? page : 0) * kv_page_bytes(kv) +
@@ -366,7 +380,7 @@ __global__ void __launch_bounds__(kRead) k_read(const sim_kv kv, const KvRead r)
         }
     }
     // rows of no entry
-    const int before = order && r.n > 0 ? r.cu[0] : r.total, after = order && r.n > 0 ? r.cu[r.n] : r.total;
+    const int before = order && r.n > 0 ? cu[0] : r.total, after = order && r.n > 0 ? cu[r.n] : r.total;
     const int64_t rest = (int64_t(before) + r.total - after) * H;
     for (int64_t z = warp0; z < rest; z += warps) {
         const int y = int(z / H);
@@ -383,15 +397,16 @@ int blocks_for(int64_t items, int per_block, int per_sm) {
 cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_t st) {
     const auto aligned = [](const void *p, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && a % 8 == 0 && b % 8 == 0; };
     const bool vec = aligned(w.k, w.kt, w.kh) && aligned(w.v, w.vt, w.vh);
-    using Fn = void (*)(const sim_kv, const KvWrite, int);
+    using Fn = void (*)(const sim_kv, const KvWrite, int, int);
     constexpr Fn of[2][2][4] = {{{k_write_4bit<1, false, false>, k_write_4bit<2, false, false>, k_write_4bit<3, false, false>, k_write_4bit<4, false, false>},
                                  {k_write_4bit<1, false, true>, k_write_4bit<2, false, true>, k_write_4bit<3, false, true>, k_write_4bit<4, false, true>}},
                                 {{k_write_4bit<1, true, false>, k_write_4bit<2, true, false>, k_write_4bit<3, true, false>, k_write_4bit<4, true, false>},
                                  {k_write_4bit<1, true, true>, k_write_4bit<2, true, true>, k_write_4bit<3, true, true>, k_write_4bit<4, true, true>}}};
     const int64_t chunks = (int64_t(w.n_new) + kStrip - 1) / kStrip;
-    const int each = chunks * 2 * kv.n_kv_heads >= int64_t(kv_sm_count()) * 96 ? 4 : 1;
-    const int blocks = blocks_for(chunks * ((2 * kv.n_kv_heads + each - 1) / each), kWrite / 32, 4096);
-    return launch_chained(of[kv_bf(kv)][vec][kv_dim_groups(kv) - 1], blocks, kWrite, 0, st, kv, w, each);
+    const int64_t heads = chunks * 2 * kv.n_kv_heads;
+    const int few = heads <= int64_t(kv_sm_count()) * 4, each = few || heads < int64_t(kv_sm_count()) * 96 ? 1 : 4, threads = few ? 64 : kWrite;
+    const int blocks = blocks_for(few ? 2 * heads : chunks * ((2 * kv.n_kv_heads + each - 1) / each), threads / 32, 4096);
+    return launch_chained(of[kv_bf(kv)][vec][kv_dim_groups(kv) - 1], blocks, threads, 0, st, kv, w, each, few);
 }
 
 cudaError_t launch_kv_read(const sim_kv &kv, const KvRead &r, cudaStream_t st) {

@@ -20,7 +20,7 @@ constexpr int kStrips = kTileKeys / kStrip;  // of a tile
 // DG groups of 32 columns, NT times 8 query rows in a pass, W warps that compute and one that loads.
 template <int DG, int NT, int W>
 struct Shape {
-    static constexpr int kSteps = NT > 2 ? 1 : kStrips / W;   // strips that a warp takes at a time
+    static constexpr int kSteps = kStrips / W;                // strips that a warp takes at a time
     static constexpr int kThreads = 32 * (W + 1);
     static constexpr int kRows = 8 * NT;
     static constexpr int kBytesStrip = 320 * DG;
@@ -479,11 +479,7 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
 
 template <int DG, bool BF>
 cudaError_t launch_rows(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
-    switch (kv_pass_rows(kv, b)) {
-        case 8: return launch<DG, 1, BF>(kv, b, a, st);
-        case 16: return launch<DG, 2, BF>(kv, b, a, st);
-        default: return launch<DG, 4, BF>(kv, b, a, st);
-    }
+    return kv_pass_rows(kv, b) == 8 ? launch<DG, 1, BF>(kv, b, a, st) : launch<DG, 2, BF>(kv, b, a, st);
 }
 
 template <bool BF>

@@ -95,10 +95,12 @@ __host__ __device__ inline bool kv_light_only(const sim_kv &kv, const sim_kv_bat
     const int64_t G = b.q_heads / kv.n_kv_heads;
     return b.n_q * G <= kLightRows || (b.n_groups == 0 && G <= kLightRows && b.n_q <= b.n);
 }
-// Rows of a pass over a light item of a 4-bit cache, by what entries have on average: an item with more is gone over again.
+// Rows of a pass over a light item of a 4-bit cache, by what entries have on average: an item with more is gone over again.  32 at a
+// time do not leave enough registers (128 sequences of up to 2000 keys: with 16 query heads for each of 8 kv heads 75 us with 16 rows
+// a pass, 96 us with 8, 122 us with 32; with 32 heads for each of 4 85, 113, 89 us; with 1 to 4 tokens of 8 heads 135, 179, 150 us).
 __host__ __device__ inline int kv_pass_rows(const sim_kv &kv, const sim_kv_batch &b) {
     const int64_t rows = (int64_t(b.n_q) * (b.q_heads / kv.n_kv_heads) + b.n - 1) / (b.n > 0 ? b.n : 1);
-    return rows <= 8 ? 8 : rows <= 16 ? 16 : kLightRows;
+    return rows <= 8 ? 8 : 16;
 }
 // Blocks of the light list on an SM.
 __host__ __device__ inline int kv_per_sm(const sim_kv &kv, const sim_kv_batch &b) { return kv_4bit(kv) && kv_pass_rows(kv, b) == 8 ? 3 : 2; }
