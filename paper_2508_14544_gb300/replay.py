@@ -1,13 +1,13 @@
 """Run the key/value side of a simulated schedule on the GPU and fit the batch-time model to it.
 
   python -m paper_2508_14544_gb300.replay [--workload c1] [--instance 0] [--policy A_max] [--layers 4] [--kv-heads 8]
-                                          [--group 8] [--head-dim 128] [--page 16] [--prefix 0] [--steps N]
+                                          [--group 8] [--head-dim 128] [--page 16] [--bits 16] [--prefix 0] [--steps N]
 
 One instance is simulated under a policy that cancels nothing (A_max, H-SF, A_r), whose completions give every
 request's start: C_i - o_i.  Its batches are then run on a ``KVCache``, step by step: a request that starts gets
 pages for its prompt and first token, the others one token each; keys and values are written and attended to in every layer; a
 request that completes gives its pages back.  With ``--prefix`` all requests are forked from one sequence of that many
-tokens, which is read once for the batch.  Values are random: what is measured is the time of the memory that the
+tokens, which is read once for the batch; with ``--bits 4`` the cache holds keys and values in 4 bits.  Values are random: what is measured is the time of the memory that the
 schedulers count, not a model.
 
 The steps' times are fitted to Section 6's linear batch-time model, c0 + c1 |B| + c2 (KV tokens) + c3 (prompt tokens
@@ -38,7 +38,7 @@ def batches(start, completion) -> list:
 
 
 def run(w, row: int = 0, policy: str = "A_max", layers: int = 4, kv_heads: int = 8, group: int = 8, head_dim: int = 128,
-        page: int = 16, prefix: int = 0, max_steps: int | None = None) -> dict:
+        page: int = 16, prefix: int = 0, max_steps: int | None = None, bits: int = 16) -> dict:
     """Replay instance ``row`` of a Workload; see the module."""
     import torch
     if policy not in WITHOUT_CANCELLATIONS:
@@ -57,7 +57,7 @@ def run(w, row: int = 0, policy: str = "A_max", layers: int = 4, kv_heads: int =
         longest = prefix + int((s + o).max())
         # pages: each sequence's last one may be nearly empty, and its first tokens may share the prefix's last one
         n_pages = -(-prefix // page) + w.M // page + 2 * most + 2
-        kv = KVCache(n_pages, page, kv_heads, head_dim, most + 1, -(-longest // page) + 1, n_layers=layers)
+        kv = KVCache(n_pages, page, kv_heads, head_dim, most + 1, -(-longest // page) + 1, n_layers=layers, bits=bits)
         ints = lambda x: torch.tensor(np.ascontiguousarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
 
         def values(n, heads):
@@ -109,7 +109,7 @@ def run(w, row: int = 0, policy: str = "A_max", layers: int = 4, kv_heads: int =
     if max_steps is None:
         assert peak == int(res["peak_memory"]) and not kv.length[:most].any()
     return {"workload": w.name, "policy": policy, "requests": len(s), "M": int(w.M), "steps": len(ms), "peak_tokens": peak,
-            "layers": layers, "kv_heads": kv_heads, "q_heads": kv_heads * group, "head_dim": head_dim, "prefix": prefix,
+            "layers": layers, "kv_heads": kv_heads, "q_heads": kv_heads * group, "head_dim": head_dim, "bits": bits, "prefix": prefix,
             "us_per_step": float(ms[skip:].mean() * 1e3), "coef_us": coef, "total_latency_us": float(total),
             "makespan_us": float(makespan)}
 
@@ -124,11 +124,12 @@ def main(argv=None) -> None:
     ap.add_argument("--group", type=int, default=8, help="query heads per kv head")
     ap.add_argument("--head-dim", type=int, default=128)
     ap.add_argument("--page", type=int, default=16)
+    ap.add_argument("--bits", type=int, default=16, choices=(16, 4), help="of a cached value")
     ap.add_argument("--prefix", type=int, default=0, help="tokens of a prompt that all requests share")
     ap.add_argument("--steps", type=int, default=None, help="only the first N batches")
     args = ap.parse_args(argv)
     print(json.dumps(run(W.make_workload(args.workload, [args.instance]), 0, args.policy, args.layers, args.kv_heads, args.group,
-                         args.head_dim, args.page, args.prefix, args.steps)))
+                         args.head_dim, args.page, args.prefix, args.steps, args.bits)))
 
 
 if __name__ == "__main__":
