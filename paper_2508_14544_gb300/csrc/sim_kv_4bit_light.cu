@@ -119,44 +119,53 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
             }
             ++x;
         };
-        Segment all;
-        for (line.next(all); ok && all.n > 0; line.next(all)) {
-            for (int r0 = 0; ok && r0 < all.rows; r0 += R) {  // as many rows as a pass has room for
-                Segment sg = all;
-                sg.row0 = all.row0 + r0;
-                sg.rows = min(all.rows - r0, R);
-                sg.row = all.row + r0;
-                // no key that none of them sees
-                sg.kv1 = min(all.kv1, sg.pos0 + int(a.group.div(sg.row0 + sg.rows - 1)) + 1);
-                sg.n = min(all.n, max((sg.kv1 - sg.k0 + kTileKeys - 1) / kTileKeys, 1));
-                tell(sg);
-                const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
-                const auto page_of = [&](int j) {  // of this lane's strip in tile j, -1 past the keys
-                    const int key = sg.k0 + j * kTileKeys + strip * kStrip;
-                    return j < sg.n && key < sg.kv1 ? row[key / P] : -1;
-                };
-                int page = page_of(0);
-                for (int j = 0; j < sg.n && ok; ++j, next_slot()) {
-                    const int next_page = page_of(j + 1), key = sg.k0 + j * kTileKeys + strip * kStrip;
-                    const bool in = key < sg.kv1, there = in && unsigned(page) < unsigned(kv.n_pages);
-                    ok = __all_sync(FULL, bar_wait(empty(slot), turn ^ 1, gave_up));
-                    if (!ok) break;
-                    const unsigned none = __ballot_sync(FULL, lane < kStrips && in && !there), some = __ballot_sync(FULL, lane < 2 * kStrips && there);
-                    if (lane == 0) {
-                        gone[slot] = none;
-                        bar_expect(full(slot), __popc(some) * KS);
-                    }
-                    __syncwarp();
-                    if (lane < 2 * kStrips && there && strip % per == 0)
-                        bulk_load(sbase + Sh::kOffRing + slot * Sh::kStage + lane * KS,
-                                  layer + page * page_bytes + ((lane / kStrips) * kv.n_kv_heads + sg.h) * head_bytes + key % P / kStrip * KS,
-                                  KS * min(per, (sg.kv1 - key + kStrip - 1) / kStrip), full(slot));
-                    page = next_page;
-                }
+        // The line's segments, as many rows at a time as a pass has room for, without the keys that none of these sees.
+        Segment all = {}, sg, ahead;
+        int r0 = 0;
+        const auto advance = [&](Segment &to) {
+            if (r0 >= all.rows) {
+                line.next(all);
+                r0 = 0;
             }
+            to = all;
+            if (all.n == 0) return;
+            to.row0 = all.row0 + r0;
+            to.rows = min(all.rows - r0, R);
+            to.row = all.row + r0;
+            to.kv1 = min(all.kv1, to.pos0 + int(a.group.div(to.row0 + to.rows - 1)) + 1);
+            to.n = min(all.n, max((to.kv1 - to.k0 + kTileKeys - 1) / kTileKeys, 1));
+            r0 += R;
+        };
+        const auto page_of = [&](const Segment &s, int j) {  // of this lane's strip in tile j, -1 past the keys
+            const int key = s.k0 + j * kTileKeys + strip * kStrip;
+            return j < s.n && key < s.kv1 ? kv.table[int64_t(s.seq) * kv.max_pages + key / P] : -1;
+        };
+        advance(sg);
+        tell(sg);
+        int page = page_of(sg, 0);
+        while (ok && sg.n > 0) {
+            // The next segment is told of, and its first pages are on their way, before this one is loaded.
+            advance(ahead);
+            tell(ahead);
+            for (int j = 0; j < sg.n && ok; ++j, next_slot()) {
+                const int next_page = j + 1 < sg.n ? page_of(sg, j + 1) : page_of(ahead, 0), key = sg.k0 + j * kTileKeys + strip * kStrip;
+                const bool in = key < sg.kv1, there = in && unsigned(page) < unsigned(kv.n_pages);
+                ok = __all_sync(FULL, bar_wait(empty(slot), turn ^ 1, gave_up));
+                if (!ok) break;
+                const unsigned none = __ballot_sync(FULL, lane < kStrips && in && !there), some = __ballot_sync(FULL, lane < 2 * kStrips && there);
+                if (lane == 0) {
+                    gone[slot] = none;
+                    bar_expect(full(slot), __popc(some) * KS);
+                }
+                __syncwarp();
+                if (lane < 2 * kStrips && there && strip % per == 0)
+                    bulk_load(sbase + Sh::kOffRing + slot * Sh::kStage + lane * KS,
+                              layer + page * page_bytes + ((lane / kStrips) * kv.n_kv_heads + sg.h) * head_bytes + key % P / kStrip * KS,
+                              KS * min(per, (sg.kv1 - key + kStrip - 1) / kStrip), full(slot));
+                page = next_page;
+            }
+            sg = ahead;
         }
-        all.n = 0;
-        if (ok) tell(all);
         if (!ok) {  // let what is on its way arrive
             for (int k = 0; k < NS; ++k, next_slot())  // (a slot that was never asked for is in its first turn, as is this wait)
                 for (int n = 0; n < 1000000 && !bar_try(full(slot), turn ^ 1); ++n) {
@@ -209,7 +218,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
     }
     for (uint32_t x = 0; ok; ++x) {
         const Segment &sg = segs[x % kSegs], &next = segs[(x + 1) % kSegs];
-        const int n = sg.n, rows = sg.rows, kv1 = sg.kv1;
+        const int n = sg.n, rows = sg.rows, kv1 = sg.kv1, first = sg.k0 + warp * (kStrips / W) * kStrip;  // this warp's first key
         if (n == 0) break;
         const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
         const uint4 *const qs = queries(x);
@@ -236,13 +245,19 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
             }
             ok = __all_sync(FULL, bar_wait(full(slot), turn, gave_up));
             if (!ok) break;
-            const unsigned char *const from = base + Sh::kOffRing + slot * Sh::kStage;
+            unsigned char *const from = base + Sh::kOffRing + slot * Sh::kStage;
 #pragma unroll 1
             for (int step = 0; step < kStrips / W; step += SP) {
-                const int strip0 = warp * (kStrips / W) + step, key0 = sg.k0 + tile * kTileKeys + strip0 * kStrip;
+                const int strip0 = warp * (kStrips / W) + step, key0 = first + tile * kTileKeys + step * kStrip;
                 if (key0 >= kv1) break;
                 const unsigned char *const ks = from + strip0 * KS, *const vs = ks + kStrips * KS;
-                const uint32_t none = gone[slot] >> strip0;  // strips on pages that the pool does not have: zeros
+                if (const uint32_t none = gone[slot] >> strip0 & ((1u << SP) - 1)) {  // strips on pages that the pool does not have: zeros
+                    for (int y = 0; y < SP; ++y)
+                        for (int i = lane; i < 32 * DG && (none >> y & 1); i += 32)
+                            reinterpret_cast<uint32_t *>(from + (i < 16 * DG ? 0 : kStrips * KS) + (strip0 + y) * KS + 256 * DG)[i % (16 * DG)] = 0;  // step and lo
+                    smem_to_async();  // before the slot is loaded again
+                    __syncwarp();
+                }
                 // S': lane has keys g and g + 8, rows 2 t and 2 t + 1 of each 8
                 float s[SP][NT][4];
 #pragma unroll
@@ -254,10 +269,6 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                     words<DG>(ks + y * KS + 16 * DG * (g + 8) + 4 * DG * t, k1);
                     words<DG>(ks + y * KS + 256 * DG + 4 * DG * g, e0);
                     words<DG>(ks + y * KS + 256 * DG + 4 * DG * (g + 8), e1);
-                    if (none >> y & 1) {
-#pragma unroll
-                        for (int j = 0; j < DG; ++j) e0[j] = e1[j] = 0;
-                    }
 #pragma unroll
                     for (int j = 0; j < DG; ++j) {
                         uint32_t u[4], v[4];
@@ -285,14 +296,20 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                                 if (8 * y >= lim) s[y / 2][i][y % 2 * 2 + z] = -INFINITY;
                         }
                 }
-                float over = -INFINITY;
+                float e[SP][NT][4], over = -INFINITY;  // log2 of the weights, the highest of them
+                const auto exponents = [&] {
+#pragma unroll
+                    for (int y = 0; y < SP; ++y)
+#pragma unroll
+                        for (int i = 0; i < NT; ++i)
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) e[y][i][z] = fmaf(s[y][i][z], c, off[i][z & 1]);
+                };
+                exponents();
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
-                    for (int y = 0; y < SP; ++y) {
-                        over = max3(over, fmaf(s[y][i][0], c, off[i][0]), fmaf(s[y][i][1], c, off[i][1]));
-                        over = max3(over, fmaf(s[y][i][2], c, off[i][0]), fmaf(s[y][i][3], c, off[i][1]));
-                    }
+                    for (int y = 0; y < SP; ++y) over = max3(max3(over, e[y][i][0], e[y][i][1]), e[y][i][2], e[y][i][3]);
                 if (__any_sync(FULL, over > kv_lift(BF) + kGrow)) {
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
@@ -314,6 +331,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                                 }
                             }
                         }
+                    exponents();
                 }
                 uint32_t p[SP][NT][2];
 #pragma unroll
@@ -321,7 +339,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) s[y][i][z] = ex2(fmaf(s[y][i][z], c, off[i][z & 1]));
+                        for (int z = 0; z < 4; ++z) s[y][i][z] = ex2(e[y][i][z]);
                         sum[i][0] += s[y][i][0] + s[y][i][2];
                         sum[i][1] += s[y][i][1] + s[y][i][3];
                         p[y][i][0] = turned(pack<BF>(s[y][i][0], s[y][i][1]));
@@ -334,10 +352,10 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                     words<DG>(vs + y * KS + 128 * DG + 4 * DG * lane, v1);
                     words<2 * DG>(vs + y * KS + 256 * DG + 8 * DG * t, f0);
                     words<2 * DG>(vs + y * KS + 256 * DG + 8 * DG * (t + 4), f1);
-                    if (blind || none) {  // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                        const int key = key0 + y * kStrip + 2 * t, end = none >> y & 1 ? 0 : kv1;
-                        const uint32_t m0 = (key < end ? 0xffffu : 0u) | (key + 1 < end ? 0xffff0000u : 0u);
-                        const uint32_t m1 = (key + 8 < end ? 0xffffu : 0u) | (key + 9 < end ? 0xffff0000u : 0u);
+                    if (blind) {  // values past the end of the keys, whatever they are, must not meet their zero probabilities
+                        const int key = key0 + y * kStrip + 2 * t;
+                        const uint32_t m0 = (key < kv1 ? 0xffffu : 0u) | (key + 1 < kv1 ? 0xffff0000u : 0u);
+                        const uint32_t m1 = (key + 8 < kv1 ? 0xffffu : 0u) | (key + 9 < kv1 ? 0xffff0000u : 0u);
 #pragma unroll
                         for (int j = 0; j < DG; ++j) {
                             f0[2 * j] &= m0, f0[2 * j + 1] &= m0;
@@ -350,7 +368,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                             };
                             const bool b0 = odd(f0, 0), b1 = odd(f0, 1), b2 = odd(f1, 0), b3 = odd(f1, 1);
                             if (__any_sync(FULL, b0 || b1 || b2 || b3)) {
-                                const int first = __reduce_min_sync(FULL, b0 ? key : b1 ? key + 1 : b2 ? key + 8 : b3 ? key + 9 : INT_MAX);  // of such keys
+                                const int least = __reduce_min_sync(FULL, b0 ? key : b1 ? key + 1 : b2 ? key + 8 : b3 ? key + 9 : INT_MAX);  // of such keys
                                 const uint32_t n0 = (b0 ? 0u : 0xffffu) | (b1 ? 0u : 0xffff0000u), n1 = (b2 ? 0u : 0xffffu) | (b3 ? 0u : 0xffff0000u);
                                 f0[2 * j] &= n0, f0[2 * j + 1] &= n0;
                                 f1[2 * j] &= n1, f1[2 * j + 1] &= n1;
@@ -358,7 +376,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                                     for (int z = 0; z < 2; ++z)
-                                        if (first < sink.seen(8 * i + 2 * t + z)) {
+                                        if (least < sink.seen(8 * i + 2 * t + z)) {
                                             o[i][2 * j][z] = o[i][2 * j][2 + z] = NAN;
                                             o[i][2 * j + 1][z] = o[i][2 * j + 1][2 + z] = NAN;
                                         }
