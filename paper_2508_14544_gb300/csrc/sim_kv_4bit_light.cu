@@ -1,10 +1,20 @@
-// Attention over a 4-bit cache (see sim_kv_attend.cu for the plan, the lines of work and the joining of pieces).
+// Attention of light items (up to 32 query rows; see sim_kv_attend.cu) over a 4-bit cache: single tokens of one sequence and the few
+// rows of small groups.
 //
 // Keys and values become 16-bit floats in registers, in the very places that the matrix instructions take their first operand
 // from: the strips are laid out for that (include/sim_kv.h), so that a byte goes from HBM through shared memory into a register and no
-// further.  Per warp and strip of 16 keys: S' = K Q' (16 keys x 8 query rows at a time, D / 16 products), P' = exp2(c (S' - m)), whose
-// 8 x 8 parts are turned over between the lanes, and O' += V' P' (D x 8, one product for each 16 columns).  Each warp keeps its own
-// running maximum (as off), sum and O; the warps' shares are joined at the end of the segment.
+// further.  (The tensor unit of sim_kv_heavy.cu takes its operands from shared memory: unpacked values would pass it three times, at 2
+// bytes each, which at 128 bytes a cycle is all that it can give at HBM's rate.)  Per warp and strip of 16 keys: S' = K Q' (16 keys x 8 query
+// rows at a time, D / 16 products), P' = exp2(c S' + off), whose 8 x 8 parts are turned over between the lanes, and O' += V' P' (D x 8, a
+// product for each 16 columns).  Each warp keeps its own running maximum (as off), sum and O; the warps' shares are joined at the
+// end of the segment.  P is rounded to the cache's type, its sum is not.
+//
+// 384 sequences of up to 2600 keys, 8 query heads on each of 8 kv heads, D = 128, bfloat16: 142 us for 0.62 GB, 4.4 TB/s (the 16-bit cache: 316
+// us for 2.1 GB); one sequence of 131071 keys, float16: 38 us for 0.17 GB.  Unpacking bounds it: a strip's keys and values take a warp some 400
+// instructions, of which 64 fused multiply-adds, 64 additions, 64 selections and 48 shifts (16 in float16) are on pipes that take two a
+// cycle, and a mixture of these was measured at 2.9 to 3.05 a cycle; without loads the kernel takes 138 us, without arithmetic 107.  So it
+// does not matter whether a warp takes one strip at a time or two (157.6 and 157.7 us, plan and join included), whether three or four blocks
+// share an SM (161 and 166 us) or whether the queries' exponents are computed once or twice.  Eight warps in two blocks: 189 us.
 #include <algorithm>
 #include <cfloat>
 
@@ -20,7 +30,6 @@ constexpr int kStrips = kTileKeys / kStrip;  // of a tile
 // DG groups of 32 columns, NT times 8 query rows in a pass, W warps that compute and one that loads.
 template <int DG, int NT, int W>
 struct Shape {
-    static constexpr int kSteps = kStrips / W;                // strips that a warp takes at a time
     static constexpr int kThreads = 32 * (W + 1);
     static constexpr int kRows = 8 * NT;
     static constexpr int kBytesStrip = 320 * DG;
@@ -64,9 +73,9 @@ __device__ __forceinline__ uint32_t turned(uint32_t x) {
 }
 template <int DG, int NT, int W, bool BF>
 __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::kPerSm)
-    k_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a) {
+    k_light_4bit(const sim_kv kv, const sim_kv_batch b, const KvAttend a) {
     using Sh = Shape<DG, NT, W>;
-    constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip, SP = Sh::kSteps;
+    constexpr int NS = Sh::kStages, R = Sh::kRows, KS = Sh::kBytesStrip;
     extern __shared__ __align__(128) unsigned char base[];
     const uint32_t sbase = smem_addr(base), bars = sbase + Sh::kOffBar;
     volatile int *const gave_up = reinterpret_cast<int *>(base + Sh::kOffGone + NS * 4);
@@ -247,28 +256,26 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
             if (!ok) break;
             unsigned char *const from = base + Sh::kOffRing + slot * Sh::kStage;
 #pragma unroll 1
-            for (int step = 0; step < kStrips / W; step += SP) {
-                const int strip0 = warp * (kStrips / W) + step, key0 = first + tile * kTileKeys + step * kStrip;
+            for (int step = 0; step < kStrips / W; ++step) {
+                const int strip = warp * (kStrips / W) + step, key0 = first + tile * kTileKeys + step * kStrip;
                 if (key0 >= kv1) break;
-                const unsigned char *const ks = from + strip0 * KS, *const vs = ks + kStrips * KS;
-                if (const uint32_t none = gone[slot] >> strip0 & ((1u << SP) - 1)) {  // strips on pages that the pool does not have: zeros
-                    for (int y = 0; y < SP; ++y)
-                        for (int i = lane; i < 32 * DG && (none >> y & 1); i += 32)
-                            reinterpret_cast<uint32_t *>(from + (i < 16 * DG ? 0 : kStrips * KS) + (strip0 + y) * KS + 256 * DG)[i % (16 * DG)] = 0;  // step and lo
+                const unsigned char *const ks = from + strip * KS, *const vs = ks + kStrips * KS;
+                if (gone[slot] >> strip & 1) {  // on a page that the pool does not have: zeros
+                    for (int i = lane; i < 32 * DG; i += 32)
+                        reinterpret_cast<uint32_t *>(from + (i < 16 * DG ? 0 : kStrips * KS) + strip * KS + 256 * DG)[i % (16 * DG)] = 0;  // step and lo
                     smem_to_async();  // before the slot is loaded again
                     __syncwarp();
                 }
                 // S': lane has keys g and g + 8, rows 2 t and 2 t + 1 of each 8
-                float s[SP][NT][4];
+                float s[NT][4];
+                {
 #pragma unroll
-                for (int y = 0; y < SP; ++y) {
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) s[y][i][0] = s[y][i][1] = s[y][i][2] = s[y][i][3] = 0.f;
+                    for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
                     uint32_t k0[DG], k1[DG], e0[DG], e1[DG];
-                    words<DG>(ks + y * KS + 16 * DG * g + 4 * DG * t, k0);
-                    words<DG>(ks + y * KS + 16 * DG * (g + 8) + 4 * DG * t, k1);
-                    words<DG>(ks + y * KS + 256 * DG + 4 * DG * g, e0);
-                    words<DG>(ks + y * KS + 256 * DG + 4 * DG * (g + 8), e1);
+                    words<DG>(ks + 16 * DG * g + 4 * DG * t, k0);
+                    words<DG>(ks + 16 * DG * (g + 8) + 4 * DG * t, k1);
+                    words<DG>(ks + 256 * DG + 4 * DG * g, e0);
+                    words<DG>(ks + 256 * DG + 4 * DG * (g + 8), e1);
 #pragma unroll
                     for (int j = 0; j < DG; ++j) {
                         uint32_t u[4], v[4];
@@ -279,12 +286,12 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                             uint4 q;
                             if constexpr (NT == 1) q = q1[j];
                             else q = qs[(i * DG + j) * 32 + lane];
-                            product<BF>(s[y][i], u[0], v[0], u[1], v[1], q.x, q.y);
-                            product<BF>(s[y][i], u[2], v[2], u[3], v[3], q.z, q.w);
+                            product<BF>(s[i], u[0], v[0], u[1], v[1], q.x, q.y);
+                            product<BF>(s[i], u[2], v[2], u[3], v[3], q.z, q.w);
                         }
                     }
                 }
-                const bool blind = key0 + SP * kStrip > all_see;
+                const bool blind = key0 + kStrip > all_see;
                 if (blind) {
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
@@ -292,32 +299,26 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                         for (int z = 0; z < 2; ++z) {
                             const int lim = sink.seen(8 * i + 2 * t + z) - key0 - g;
 #pragma unroll
-                            for (int y = 0; y < 2 * SP; ++y)
-                                if (8 * y >= lim) s[y / 2][i][y % 2 * 2 + z] = -INFINITY;
+                            for (int y = 0; y < 2; ++y)
+                                if (8 * y >= lim) s[i][2 * y + z] = -INFINITY;
                         }
                 }
-                float e[SP][NT][4], over = -INFINITY;  // log2 of the weights, the highest of them
+                float e[NT][4], over = -INFINITY;  // log2 of the weights, the highest of them
                 const auto exponents = [&] {
 #pragma unroll
-                    for (int y = 0; y < SP; ++y)
+                    for (int i = 0; i < NT; ++i)
 #pragma unroll
-                        for (int i = 0; i < NT; ++i)
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) e[y][i][z] = fmaf(s[y][i][z], c, off[i][z & 1]);
+                        for (int z = 0; z < 4; ++z) e[i][z] = fmaf(s[i][z], c, off[i][z & 1]);
                 };
                 exponents();
 #pragma unroll
-                for (int i = 0; i < NT; ++i)
-#pragma unroll
-                    for (int y = 0; y < SP; ++y) over = max3(max3(over, e[y][i][0], e[y][i][1]), e[y][i][2], e[y][i][3]);
+                for (int i = 0; i < NT; ++i) over = max3(max3(over, e[i][0], e[i][1]), e[i][2], e[i][3]);
                 if (__any_sync(FULL, over > kv_lift(BF) + kGrow)) {
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
 #pragma unroll
                         for (int z = 0; z < 2; ++z) {
-                            float top = fmaxf(s[0][i][z], s[0][i][2 + z]);
-#pragma unroll
-                            for (int y = 1; y < SP; ++y) top = max3(top, s[y][i][z], s[y][i][2 + z]);
+                            float top = fmaxf(s[i][z], s[i][2 + z]);
 #pragma unroll
                             for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(FULL, top, d));
                             if (fmaf(top, c, off[i][z]) > kv_lift(BF) + kGrow) {  // each row for itself: what it becomes does not hang on the rows beside it
@@ -333,27 +334,24 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                         }
                     exponents();
                 }
-                uint32_t p[SP][NT][2];
+                uint32_t p[NT][2];
 #pragma unroll
-                for (int y = 0; y < SP; ++y)
+                for (int i = 0; i < NT; ++i) {
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) s[y][i][z] = ex2(e[y][i][z]);
-                        sum[i][0] += s[y][i][0] + s[y][i][2];
-                        sum[i][1] += s[y][i][1] + s[y][i][3];
-                        p[y][i][0] = turned(pack<BF>(s[y][i][0], s[y][i][1]));
-                        p[y][i][1] = turned(pack<BF>(s[y][i][2], s[y][i][3]));
-                    }
-#pragma unroll
-                for (int y = 0; y < SP; ++y) {
+                    for (int z = 0; z < 4; ++z) s[i][z] = ex2(e[i][z]);
+                    sum[i][0] += s[i][0] + s[i][2];
+                    sum[i][1] += s[i][1] + s[i][3];
+                    p[i][0] = turned(pack<BF>(s[i][0], s[i][1]));
+                    p[i][1] = turned(pack<BF>(s[i][2], s[i][3]));
+                }
+                {
                     uint32_t v0[DG], v1[DG], f0[2 * DG], f1[2 * DG];
-                    words<DG>(vs + y * KS + 4 * DG * lane, v0);
-                    words<DG>(vs + y * KS + 128 * DG + 4 * DG * lane, v1);
-                    words<2 * DG>(vs + y * KS + 256 * DG + 8 * DG * t, f0);
-                    words<2 * DG>(vs + y * KS + 256 * DG + 8 * DG * (t + 4), f1);
+                    words<DG>(vs + 4 * DG * lane, v0);
+                    words<DG>(vs + 128 * DG + 4 * DG * lane, v1);
+                    words<2 * DG>(vs + 256 * DG + 8 * DG * t, f0);
+                    words<2 * DG>(vs + 256 * DG + 8 * DG * (t + 4), f1);
                     if (blind) {  // values past the end of the keys, whatever they are, must not meet their zero probabilities
-                        const int key = key0 + y * kStrip + 2 * t;
+                        const int key = key0 + 2 * t;
                         const uint32_t m0 = (key < kv1 ? 0xffffu : 0u) | (key + 1 < kv1 ? 0xffff0000u : 0u);
                         const uint32_t m1 = (key + 8 < kv1 ? 0xffffu : 0u) | (key + 9 < kv1 ? 0xffff0000u : 0u);
 #pragma unroll
@@ -390,8 +388,8 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                         values4<BF>(v1[j], f1[2 * j], f1[2 * j + 1], v);
 #pragma unroll
                         for (int i = 0; i < NT; ++i) {
-                            product<BF>(o[i][2 * j], u[0], u[1], v[0], v[1], p[y][i][0], p[y][i][1]);
-                            product<BF>(o[i][2 * j + 1], u[2], u[3], v[2], v[3], p[y][i][0], p[y][i][1]);
+                            product<BF>(o[i][2 * j], u[0], u[1], v[0], v[1], p[i][0], p[i][1]);
+                            product<BF>(o[i][2 * j + 1], u[2], u[3], v[2], v[3], p[i][0], p[i][1]);
                         }
                     }
                 }
@@ -489,10 +487,10 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && dev != ready) {
-        e = cudaFuncSetAttribute((const void *)k_4bit<DG, NT, W, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
+        e = cudaFuncSetAttribute((const void *)k_light_4bit<DG, NT, W, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
         if (e == cudaSuccess) ready = dev;
     }
-    return e == cudaSuccess ? launch_chained(k_4bit<DG, NT, W, BF>, kv_blocks(a.sms, 1, Sh::kPerSm), Sh::kThreads, Sh::kBytes, st, kv, b, a) : e;
+    return e == cudaSuccess ? launch_chained(k_light_4bit<DG, NT, W, BF>, kv_blocks(a.sms, 1, Sh::kPerSm), Sh::kThreads, Sh::kBytes, st, kv, b, a) : e;
 }
 
 template <int DG, bool BF>
