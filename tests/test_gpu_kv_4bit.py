@@ -544,3 +544,50 @@ def test_what_is_refused():
         kv.read(c.ints([0]), c.ints([0, 70]), 70, layer=1)
     with pytest.raises(SimError):
         kv.write(slots, x, x, layer=5)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim,page,heads,most", [(128, 16, 8, 200), (128, 64, 8, 700), (80, 32, 3, 500), (32, 16, 1, 900), (64, 128, 4, 300)])
+def test_lists_of_many_tokens_in_any_order(dim, page, heads, most, dtype):
+    """Sequences' tokens one after the other, so that strips begin anywhere in the list; some tokens without a slot, some out of order."""
+    import torch
+
+    from paper_2508_14544_gb300 import KVCache
+    rng = np.random.default_rng(dim + page)
+    lens = [int(x) for x in rng.integers(0, most, 60)]
+    n_pages = sum(-(-x // page) for x in lens) + 5
+    order = rng.permutation(n_pages)
+    kv = KVCache(n_pages, page, heads, dim, 60, max(-(-x // page) for x in lens) + 1, n_layers=2, dtype=getattr(torch, dtype), bits=4)
+    kv.pool.fill_(0xff)
+    at, table, slots = 0, np.full(tuple(kv.table.shape), -1, np.int32), []
+    for i, x in enumerate(lens):
+        k = -(-x // page)
+        table[i, :k] = order[at: at + k]
+        at += k
+        pos = np.arange(x)
+        slots.append(table[i, pos // page].astype(np.int64) * page + pos % page)
+    kv.table.copy_(torch.from_numpy(table))
+    kv.length.copy_(torch.tensor(lens, dtype=torch.int32))
+    flat = np.concatenate(slots)
+    n = len(flat)
+    where = np.arange(n)
+    for a in rng.integers(0, n - 40, 8):  # pieces turned round
+        where[a: a + 33] = where[a: a + 33][::-1].copy()
+    none = rng.choice(n, 20, replace=False)
+    listed = flat[where]
+    k, v = (torch.randn(n, heads, dim, device="cuda", generator=torch.Generator("cuda").manual_seed(s)).to(kv.dtype) for s in (1, 2))
+    gaps = listed.copy()
+    gaps[none] = rng.choice([-1, -7, n_pages * page, 1 << 45], 20)
+    kv.write(torch.from_numpy(gaps).cuda(), k, v, layer=1)
+    at_none = torch.from_numpy(none).cuda()
+    kv.write(torch.from_numpy(listed[none]).cuda(), k[at_none], v[at_none], layer=1)
+    cu = np.cumsum([0, *lens])
+    ints = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    rk, rv = kv.read(ints(range(60)), ints(cu), n, layer=1)
+    back = np.empty(n, np.int64)
+    back[where] = np.arange(n)
+    back = torch.from_numpy(back).cuda()
+    same(rk, held(f64(k[back]), dtype))
+    same(rv, held(f64(v[back]), dtype))
+    assert (kv.pool[:, 0] == 0xff).all()  # the other layer
+    kv.check()
