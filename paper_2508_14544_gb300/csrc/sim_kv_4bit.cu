@@ -1,10 +1,10 @@
 // Keys and values of a 4-bit cache: quantised as they are written, and read back (16-bit caches are read here too).
 //   k_write_4bit - bound by arithmetic: some 19 instructions a value (the difference from the lowest, its quotient to the nearest float, that to
 //                the nearest whole number, 4 bits into their place; a third is what a group costs), 2.9 a cycle and SM.  343 us for
-//                524 million values, of which HBM needs 204.  With a thread for each group and its pieces stored apart 958 us: 45 sectors
-//                written for a token and head, where four warps' worth of a strip stored whole write 4.  Each lane the step of one group
-//                instead of all lanes those of all: 385 instead of 637 us; differences checked by two roundings only where lo lies on
-//                a border (bfloat16): 370; one row at a time, so that four blocks fit: 348.  10 us for 40 tokens, a chain of a few loads.
+//                524 million values, of which HBM needs 204.  With a thread for each group and its pieces stored apart 958 us, and 45
+//                sectors written for a token's keys of a head instead of 4.  Each lane the step of one group instead of all lanes those
+//                of all: 385 instead of 637 us; differences checked by two roundings only where lo lies on a border (bfloat16): 370;
+//                one row at a time, so that four blocks fit: 343.  5.6 us for 40 tokens, a chain of two loads and the arithmetic.
 //   k_read     - bound by HBM: 153 us for 0.95 GB, 6.2 TB/s; 6 us for a few tokens, a chain of dependent loads (offsets, entry, page, strip).
 #include <algorithm>
 #include <climits>
