@@ -185,32 +185,32 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(over) : "f"(of));
                 over = fmaf(fmaf(-of, over, 1.f), over, over);
                 if (!(of > (BF ? 0x1p-100f : 0x1p-18f) && of < (BF ? 0x1p100f : 0x1p14f))) over = 0.f;
-                // bfloat16: a difference that is not exact is one of numbers more than 15 powers of two apart, and is rounded to a border (13
-                // bits) only if the larger is one.  So where the step's borders miss -lo, and lo is 0 or not small, it does not matter.
-                if (BF) {
-                    const float q0 = -low * over, q1 = fmaf(fmaf(-q0, of, -low), over, q0);
-                    const bool on = fabsf(q1 - (q1 + 0x1.8p23f - 0x1.8p23f)) == 0.5f, small = low != 0.f && fabsf(low) < up * 0x1p-14f;
-                    over = on || small ? -over : over;
-                }
+                // A difference that is not exact is one of numbers whose last places lie more than 24 powers of two under the first: one is
+                // below 2^-15 (bfloat16) or 2^-12 (float16) of the difference.  It is rounded to a border only if the larger number lies
+                // that near to one: in bfloat16 on it, as borders have 13 bits; in float16 (16 bits) within a 2^12th of -lo.  So where -lo
+                // is not that near to one of the step's borders, and lo is 0 or not small, it does not matter.
+                const float q0 = -low * over, q1 = fmaf(fmaf(-q0, of, -low), over, q0), apart = fabsf(q1 - (q1 + 0x1.8p23f - 0x1.8p23f));
+                const bool on = BF ? apart == 0.5f : apart > 0.5f - 0x1p-8f, small = low != 0.f && fabsf(low) < up * (BF ? 0x1p-14f : 0x1p-10f);
+                over = on || small ? -over : over;
                 uint32_t code[DG];
                 const auto quantise = [&](auto values, int j) {  // the codes' places in a word: those of values or of keys
                     constexpr bool V = decltype(values)::value;
                     const uint32_t sc = __shfl_sync(FULL, scale, j, 4);
                     const float in1 = __shfl_sync(FULL, over, j, 4), inv = fabsf(in1), s = wide<BF>(sc, 0), lo = wide<BF>(sc, 1);
                     const uint4 y = x[j];
-                    // The difference where it is exact, its quotient by the step to the nearest float, and that to the nearest whole number,
-                    // ties to even.  A quotient on a border is a float; one next to it is more than half of a float's unit away, as
+                    // The difference, its quotient by the step to the nearest float, and that to the nearest whole number, ties to even.
+                    // Where the difference is exact, a quotient on a border is a float; one next to it is more than half of a float's unit away, as
                     // the difference is a float too.
-                    uint32_t cut = 0, w = 0u - 0x4b400000u * 0x11111111u;
+                    uint32_t w = 0u - 0x4b400000u * 0x11111111u;
                     const auto value = [&](int q) { return wide<BF>(q < 2 ? y.x : q < 4 ? y.y : q < 6 ? y.z : y.w, q % 2); };
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const float d = BF ? value(q) - lo : __fsub_rz(value(q), lo), q0 = d * inv, q1 = fmaf(fmaf(-q0, s, d), inv, q0);
-                        if (!BF) cut |= __float_as_uint(d) ^ __float_as_uint(__fsub_ru(value(q), lo));
+                        const float d = value(q) - lo, q0 = d * inv, q1 = fmaf(fmaf(-q0, s, d), inv, q0);
                         w += __float_as_uint(q1 + 0x1.8p23f) << (V ? 4 * q : 4 * (q / 2) + 16 * (q % 2));
                     }
-                    if (BF ? !(in1 > 0.f) : cut || in1 == 0.f) {
-                        if (BF && in1 < 0.f) {
+                    if (!(in1 > 0.f)) {
+                        uint32_t cut = 0;  // differences that are not exact
+                        if (in1 < 0.f) {
 #pragma unroll
                             for (int q = 0; q < 8; ++q) cut |= __float_as_uint(__fsub_rz(value(q), lo)) ^ __float_as_uint(__fsub_ru(value(q), lo));
                         }

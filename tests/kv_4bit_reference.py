@@ -25,7 +25,13 @@ def held(x, dtype):
         y = np.where(odd, 0.0, y)
         lo, hi = y.min(-1, keepdims=True), y.max(-1, keepdims=True)
         step = np.maximum(round16((hi - lo) / 15, dtype, down=True), 2.0 ** BITS[dtype][1])
-        code = np.minimum(np.rint((y - lo) / step), 15)
+        # y - lo as a sum of two floats, which is exact; a border between codes is a float, and the first one's place beside it is known
+        t = y - lo
+        rest = (y - (t - (t - y))) - (lo + (t - y))
+        k = np.floor(t / step)
+        border = (k + 0.5) * step
+        on = (t == border) & (rest == 0)
+        code = np.minimum(k + np.where(on, k % 2, (t > border) | ((t == border) & (rest > 0))), 15)
         out[..., a: a + 32] = np.where(odd, np.nan, round16(lo + code * step, dtype))
     return out
 

@@ -76,7 +76,7 @@ class Pool:
         return held(f64(self.k[at]), self.dtype), held(f64(self.v[at]), self.dtype)
 
 
-SPECIAL = ["ties", "large", "tiny", "mixed", "equal", "zeros", "integers"]
+SPECIAL = ["ties", "large", "tiny", "mixed", "equal", "zeros", "integers", "borders", "small lowest"]
 
 
 def special(kind, torch, dtype):
@@ -99,6 +99,19 @@ def special(kind, torch, dtype):
             x = x * 0
         elif kind == "integers":
             x = torch.round(x * 40)
+        elif kind == "borders":  # -lo on or next to a border, values on or next to borders, and others too small for an exact difference
+            bits, least, _ = BITS[dtype]
+            r = lambda lo, hi, *shape: torch.randint(lo, hi, shape or (n, 2, 1), generator=g, device="cuda").double()  # noqa: E731
+            s = r(2 ** (bits - 1), 2 ** bits) * 2.0 ** (r(-4, 5) - bits)
+            lo = -(r(0, 15) + 0.5) * s
+            lo = torch.from_numpy(round16((lo * (1 + r(-2, 3) * 2.0 ** -bits)).cpu().numpy(), dtype)).cuda()
+            x = lo + (r(0, 16, n, 2, 80) + 0.5 * r(0, 2, n, 2, 80)) * s * (1 + r(-1, 2, n, 2, 80) * 2.0 ** -bits)
+            tiny = r(-40, 41, n, 2, 80) * 2.0 ** (r(-24, -8, n, 2, 80) if dtype == "float16" else r(-60, -10, n, 2, 80))
+            x = torch.where(r(0, 3, n, 2, 80) == 0, tiny, x).clamp(min=lo, max=lo + 15 * s)
+            x[..., ::32], x[..., 1::32] = lo, lo + 15 * s
+        elif kind == "small lowest":  # lo next to nothing beside the others
+            x = torch.round(x.abs() * 64) / 8 + 0.125
+            x[..., ::32] = 2.0 ** -torch.randint(8, 24, (n, 2, 3), generator=g, device="cuda").double() * torch.where(x[..., 1::32][..., :3] > 1, 1.0, -1.0)
         return torch.from_numpy(round16(x.cpu().numpy(), dtype)).cuda()
     return make
 

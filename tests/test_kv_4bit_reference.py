@@ -12,6 +12,9 @@ def values(dtype, seed, n=40):
     x[1::5] *= 2.0 ** rng.integers(-20, 1, (len(x[1::5]), 32))
     x[2::10] = rng.integers(-20, 20, (len(x[2::10]), 32)) * 2.0 ** BITS[dtype][1]  # next to nothing
     x[7] = 0.75
+    x[8], x[9] = 1.5, 1.5  # differences of more bits than 64-bit floats have, next to borders
+    x[8, :6] = -7.5, 7.5, 2.0 ** -23, -2.0 ** -23, 0, 2.0 ** -24
+    x[9, :6] = (-7.5, 7.5, 2.0 ** -100, -2.0 ** -100, 0, 2.0 ** -60) if dtype == "bfloat16" else x[8, :6]
     return round16(x, dtype)
 
 
