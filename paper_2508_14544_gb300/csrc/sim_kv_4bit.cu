@@ -3,7 +3,7 @@
 //                the nearest whole number, 4 bits into their place; a third is what a group costs), 2.9 a cycle and SM.  343 us for
 //                524 million values, of which HBM needs 204.  With a thread for each group and its pieces stored apart 958 us, and 45
 //                sectors written for a token's keys of a head instead of 4.  Each lane the step of one group instead of all lanes those
-//                of all: 385 instead of 637 us; differences checked by two roundings only where lo lies on a border (bfloat16): 370;
+//                of all: 385 instead of 637 us; differences checked by two roundings only where -lo lies next to a border: 370;
 //                one row at a time, so that four blocks fit: 343.  5.6 us for 40 tokens, a chain of two loads and the arithmetic.
 //   k_read     - bound by HBM: 153 us for 0.95 GB, 6.2 TB/s; 6 us for a few tokens, a chain of dependent loads (offsets, entry, page, strip).
 #include <algorithm>
@@ -411,7 +411,10 @@ cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_
                                  {k_write_4bit<1, true, true>, k_write_4bit<2, true, true>, k_write_4bit<3, true, true>, k_write_4bit<4, true, true>}}};
     const int64_t chunks = (int64_t(w.n_new) + kStrip - 1) / kStrip;
     const int64_t heads = chunks * 2 * kv.n_kv_heads;
-    const int few = heads <= int64_t(kv_sm_count()) * 4, each = few || heads < int64_t(kv_sm_count()) * 96 ? 1 : 4, threads = few ? 64 : kWrite;
+    // Heads that a warp takes, so that what it learns of the slots serves all, as long as there are warps enough for that: 4 instead of 2 for 250
+    // prompts (store and read 554 instead of 563 us, 604 with 1), 2 instead of 4 for 77 of 3 heads (89 instead of 99 us).
+    const int64_t per_sm = heads / kv_sm_count();
+    const int few = per_sm < 4, each = per_sm < 96 ? 1 : per_sm < 512 ? 2 : 4, threads = few ? 64 : kWrite;
     const int blocks = blocks_for(few ? 2 * heads : chunks * ((2 * kv.n_kv_heads + each - 1) / each), threads / 32, 4096);
     return launch_chained(of[kv_bf(kv)][vec][kv_dim_groups(kv) - 1], blocks, threads, 0, st, kv, w, each, few);
 }

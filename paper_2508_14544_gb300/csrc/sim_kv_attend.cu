@@ -33,6 +33,11 @@ namespace {
 // The rule takes the faster side of these four.  With 2 kv heads of 4 query heads and D = 64 it shares a little early: 64 groups with
 // 2048 keys 59 against 50 us (8192: 88 against 102), 16 groups with 1024 keys 48 against 42 us (4096: 59 against 63).
 constexpr int kShareItem = 3, kShareRows = 7, kShareOnce = 2;
+// Of a 4-bit cache, over the number of groups of 32 columns: how many times as much that is, as its light items' tiles take less time (row_cost).
+// Shared (or, by this rule, not) and without groups: 128 sequences of 8 kv heads with 8 query heads in 64 groups with a prefix of 2048 and of 8192 keys
+// 104 and 95, 288 and 276 us (by the rule for 16 bits 212 and 568), in 16 groups of 1024, 2048, 4096 keys 71 and 62, 81 and 93, 104 and 149 us
+// (108, 95, 159).  With 6 or 10 instead of 8 the same within 2 us, but 114 for 64 groups of 2048 keys with 6.
+constexpr int kShare4 = 8;
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -138,6 +143,14 @@ __device__ __forceinline__ int tile_rows(int r) {
     const int rem = r % kAttRows;
     return 2 * (r / kAttRows) + (rem > kAttRows / 2 ? 2 : rem > 0);
 }
+// What they cost a tile of keys: in a 16-bit cache that; in a 4-bit one, in the time of a pass over a light item, which is short: a
+// heavy item's tile takes two or three (2300 and 3400 to 4300 cycles of an SM against 1300), a light one's as many as there are passes and,
+// as the line of work does not know of them, so that the block with such an item is the last, much more.
+__device__ __forceinline__ int row_cost(const sim_kv &kv, int pass, int r) {
+    if (!kv_4bit(kv)) return tile_rows(r);
+    const int rem = r % kAttRows, passes = (rem + pass - 1) / pass;
+    return 3 * (r / kAttRows) + (rem > kAttRows / 2 ? 3 : rem > kLightRows ? 2 : passes > 1 ? 4 * passes : passes);
+}
 __device__ __forceinline__ int heavy_items(int r, bool only) { return only ? 0 : r / kAttRows + (r % kAttRows > kLightRows); }
 __device__ __forceinline__ int light_items(int r, bool only) {
     return only ? ceil_div(r, kLightRows) : r % kAttRows > 0 && r % kAttRows <= kLightRows;
@@ -178,6 +191,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
     int32_t *const first0 = FEW ? few_first[0] : p.first[0], *const first1 = FEW ? few_first[FEW ? 1 : 0] : p.first[1];
     const int tid = threadIdx.x, ng = b.n_groups, n_src = ng + b.n, G = b.q_heads / kv.n_kv_heads, P = kv.page_size;
     const bool only = kv_light_only(kv, b);
+    const int pass = kv_pass_rows(kv, b), scale = kv_4bit(kv) ? kShare4 / kv_dim_groups(kv) : 1;
     if (tid < 3) counts[tid] = 0;
     if (tid == 0) saved = 0;
     // Offsets that are not in order: no queries at all, or no groups.
@@ -200,7 +214,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
 #pragma unroll 1
         for (int i0 = 0; i0 < b.n; i0 += kPlan) {  // the least number of pages of each group, the sum of its tile rows
             const int i = i0 + tid, g = i < b.n ? group_of(b, i) : -1, v = g < 0 ? INT_MAX : p.same[i];
-            const int t = g < 0 ? 0 : tile_rows(entry_at(kv, b, i).t * G);
+            const int t = g < 0 ? 0 : row_cost(kv, pass, entry_at(kv, b, i).t * G);
             int same_group;
             __match_all_sync(FULL, g, &same_group);
             if (same_group) {
@@ -226,7 +240,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             if (a < z) {
                 x.q0 = b.cu_q[a];
                 const int rows = (b.cu_q[z] - x.q0) * G, found = used[g] != INT_MAX ? used[g] : 0;
-                const int64_t saves = int64_t(found * P / kTileKeys) * (alone[g] - tile_rows(rows)) - kShareItem - int64_t(rows) * kShareRows / 32;
+                const int64_t saves = int64_t(found * P / kTileKeys) * (alone[g] - row_cost(kv, pass, rows)) - scale * (kShareItem + int64_t(rows) * kShareRows / 32);
                 if (saves > 0) {
                     net += saves;
                     x.rows = rows;
@@ -239,7 +253,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
         }
         if (net > 0) atomicAdd(&saved, static_cast<unsigned long long>(net));
         __syncthreads();
-        if (int64_t(saved) * kv.n_kv_heads < int64_t(kShareOnce) * kv_blocks(sms, 1)) {
+        if (int64_t(saved) * kv.n_kv_heads < int64_t(scale * kShareOnce) * kv_blocks(sms, 1)) {
 #pragma unroll 1
             for (int g = tid; g < ng; g += kPlan) source[g].rows = source[g].kv1 = 0;
             __syncthreads();
