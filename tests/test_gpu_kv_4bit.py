@@ -604,3 +604,36 @@ def test_lists_of_many_tokens_in_any_order(dim, page, heads, most, dtype):
     same(rv, held(f64(v[back]), dtype))
     assert (kv.pool[:, 0] == 0xff).all()  # the other layer
     kv.check()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim,page", [(128, 32), (80, 16), (24, 64), (64, 16)])
+def test_the_pool_is_laid_out_as_the_header_says(dim, page, dtype):
+    from paper_2508_14544_gb300 import _lib
+    n, G, heads = 45, -(-dim // 32), 2
+    c = Pool([n], kv_heads=heads, dim=dim, page=page, dtype=dtype, fill=0)
+    assert tuple(c.kv.pool.shape[1:]) == (1, 2, heads, page, 20 * G) and c.kv.bits == 4
+    assert c.kv.pool.numel() == _lib.lib().sim_kv_pool_bytes(c.kv._ref)
+    pool = c.kv.pool.cpu().numpy().reshape(-1, 2, heads, page // 16, 320 * G)
+    got = np.zeros((2, n, heads, dim))
+
+    def number(strip, at):  # a 16-bit float
+        bits = np.array([int(strip[at]) | int(strip[at + 1]) << 8], np.uint32)
+        return float((bits << 16).view(np.float32)[0]) if dtype == "bfloat16" else float(bits.astype(np.uint16).view(np.float16)[0])
+    for t in range(n):
+        where = pool[c.table[0, t // page], :, :, t % page // 16]
+        T = t % 16
+        for h in range(heads):
+            k, v = where[0, h], where[1, h]
+            for i in range(dim):
+                g, d = divmod(i, 32)
+                at = 16 * G * T + 4 * G * (d // 8) + 4 * g
+                code = int.from_bytes(k[at: at + 4].tobytes(), "little") >> (4 * (d % 8 // 2) + 16 * (d % 2)) & 15
+                at = 256 * G + 4 * G * T + 4 * g
+                got[0, t, h, i] = number(k, at + 2) + code * number(k, at)
+                at = 128 * G * (T // 8) + 4 * G * (4 * (d // 4) + T % 8 // 2) + 4 * g + 2 * (T % 2)
+                code = int.from_bytes(v[at: at + 2].tobytes(), "little") >> (4 * (d % 4)) & 15
+                at = 256 * G + 8 * G * (T // 2) + 8 * g + 2 * (T % 2)
+                got[1, t, h, i] = number(v, at + 4) + code * number(v, at)
+    for x, want in zip(got, c.want(0)):
+        assert np.array_equal(round16(x, dtype), want)
