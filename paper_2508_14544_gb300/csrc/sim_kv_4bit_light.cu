@@ -1,5 +1,5 @@
-// Attention of light items (up to 32 query rows; see sim_kv_attend.cu) over a 4-bit cache: single tokens of one sequence and the few
-// rows of small groups.
+// Attention of light items (up to 8 or 16 query rows, kv_light_rows; see sim_kv_attend.cu) over a 4-bit cache: single tokens of one sequence
+// and the few rows of small groups.
 //
 // Keys and values become 16-bit floats in registers, in the very places that the matrix instructions take their first operand
 // from: the strips are laid out for that (include/sim_kv.h), so that a byte goes from HBM through shared memory into a register and no
@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kStrips = kTileKeys / kStrip;  // of a tile
 
-// DG groups of 32 columns, NT times 8 query rows in a pass, W warps that compute and one that loads.
+// DG groups of 32 columns, NT times 8 query rows (kv_light_rows), W warps that compute and one that loads.
 template <int DG, int NT, int W>
 struct Shape {
     static constexpr int kThreads = 32 * (W + 1);
@@ -128,33 +128,17 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
             }
             ++x;
         };
-        // The line's segments, as many rows at a time as a pass has room for, without the keys that none of these sees.
-        Segment all = {}, sg, ahead;
-        int r0 = 0;
-        const auto advance = [&](Segment &to) {
-            if (r0 >= all.rows) {
-                line.next(all);
-                r0 = 0;
-            }
-            to = all;
-            if (all.n == 0) return;
-            to.row0 = all.row0 + r0;
-            to.rows = min(all.rows - r0, R);
-            to.row = all.row + r0;
-            to.kv1 = min(all.kv1, to.pos0 + int(a.group.div(to.row0 + to.rows - 1)) + 1);
-            to.n = min(all.n, max((to.kv1 - to.k0 + kTileKeys - 1) / kTileKeys, 1));
-            r0 += R;
-        };
+        Segment sg, ahead;
         const auto page_of = [&](const Segment &s, int j) {  // of this lane's strip in tile j, -1 past the keys
             const int key = s.k0 + j * kTileKeys + strip * kStrip;
             return j < s.n && key < s.kv1 ? kv.table[int64_t(s.seq) * kv.max_pages + key / P] : -1;
         };
-        advance(sg);
+        line.next(sg);
         tell(sg);
         int page = page_of(sg, 0);
         while (ok && sg.n > 0) {
             // The next segment is told of, and its first pages are on their way, before this one is loaded.
-            advance(ahead);
+            line.next(ahead);
             tell(ahead);
             for (int j = 0; j < sg.n && ok; ++j, next_slot()) {
                 const int next_page = j + 1 < sg.n ? page_of(sg, j + 1) : page_of(ahead, 0), key = sg.k0 + j * kTileKeys + strip * kStrip;
@@ -495,7 +479,7 @@ cudaError_t launch(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, c
 
 template <int DG, bool BF>
 cudaError_t launch_rows(const sim_kv &kv, const sim_kv_batch &b, const KvAttend &a, cudaStream_t st) {
-    return kv_pass_rows(kv, b) == 8 ? launch<DG, 1, BF>(kv, b, a, st) : launch<DG, 2, BF>(kv, b, a, st);
+    return kv_light_rows(kv, b) == 8 ? launch<DG, 1, BF>(kv, b, a, st) : launch<DG, 2, BF>(kv, b, a, st);
 }
 
 template <bool BF>

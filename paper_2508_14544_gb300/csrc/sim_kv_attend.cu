@@ -143,17 +143,16 @@ __device__ __forceinline__ int tile_rows(int r) {
     const int rem = r % kAttRows;
     return 2 * (r / kAttRows) + (rem > kAttRows / 2 ? 2 : rem > 0);
 }
-// What they cost a tile of keys: in a 16-bit cache that; in a 4-bit one, in the time of a pass over a light item, which is short: a
-// heavy item's tile takes two or three (2300 and 3400 to 4300 cycles of an SM against 1300), a light one's as many as there are passes and,
-// as the line of work does not know of them, so that the block with such an item is the last, much more.
-__device__ __forceinline__ int row_cost(const sim_kv &kv, int pass, int r) {
+// What they cost a tile of keys: in a 16-bit cache that; in a 4-bit one, in the time that a light item takes for it, which is short: a heavy
+// item takes two or three times as long (2300 and 3400 to 4300 cycles of an SM against 1300).
+__device__ __forceinline__ int row_cost(const sim_kv &kv, int item, int r) {
     if (!kv_4bit(kv)) return tile_rows(r);
-    const int rem = r % kAttRows, passes = (rem + pass - 1) / pass;
-    return 3 * (r / kAttRows) + (rem > kAttRows / 2 ? 3 : rem > kLightRows ? 2 : passes > 1 ? 4 * passes : passes);
+    const int rem = r % kAttRows;
+    return 3 * (r / kAttRows) + (rem > kAttRows / 2 ? 3 : rem > kLightRows ? 2 : ceil_div(rem, item));
 }
 __device__ __forceinline__ int heavy_items(int r, bool only) { return only ? 0 : r / kAttRows + (r % kAttRows > kLightRows); }
-__device__ __forceinline__ int light_items(int r, bool only) {
-    return only ? ceil_div(r, kLightRows) : r % kAttRows > 0 && r % kAttRows <= kLightRows;
+__device__ __forceinline__ int light_items(int r, bool only, int item) {
+    return only ? ceil_div(r, item) : r % kAttRows <= kLightRows ? ceil_div(r % kAttRows, item) : 0;
 }
 
 constexpr int kFewSources = 448, kFewItems = 1024;
@@ -191,7 +190,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
     int32_t *const first0 = FEW ? few_first[0] : p.first[0], *const first1 = FEW ? few_first[FEW ? 1 : 0] : p.first[1];
     const int tid = threadIdx.x, ng = b.n_groups, n_src = ng + b.n, G = b.q_heads / kv.n_kv_heads, P = kv.page_size;
     const bool only = kv_light_only(kv, b);
-    const int pass = kv_pass_rows(kv, b), scale = kv_4bit(kv) ? kShare4 / kv_dim_groups(kv) : 1;
+    const int item = kv_light_rows(kv, b), scale = kv_4bit(kv) ? kShare4 / kv_dim_groups(kv) : 1;
     if (tid < 3) counts[tid] = 0;
     if (tid == 0) saved = 0;
     // Offsets that are not in order: no queries at all, or no groups.
@@ -214,7 +213,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
 #pragma unroll 1
         for (int i0 = 0; i0 < b.n; i0 += kPlan) {  // the least number of pages of each group, the sum of its tile rows
             const int i = i0 + tid, g = i < b.n ? group_of(b, i) : -1, v = g < 0 ? INT_MAX : p.same[i];
-            const int t = g < 0 ? 0 : row_cost(kv, pass, entry_at(kv, b, i).t * G);
+            const int t = g < 0 ? 0 : row_cost(kv, item, entry_at(kv, b, i).t * G);
             int same_group;
             __match_all_sync(FULL, g, &same_group);
             if (same_group) {
@@ -240,7 +239,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             if (a < z) {
                 x.q0 = b.cu_q[a];
                 const int rows = (b.cu_q[z] - x.q0) * G, found = used[g] != INT_MAX ? used[g] : 0;
-                const int64_t saves = int64_t(found * P / kTileKeys) * (alone[g] - row_cost(kv, pass, rows)) - scale * (kShareItem + int64_t(rows) * kShareRows / 32);
+                const int64_t saves = int64_t(found * P / kTileKeys) * (alone[g] - row_cost(kv, item, rows)) - scale * (kShareItem + int64_t(rows) * kShareRows / 32);
                 if (saves > 0) {
                     net += saves;
                     x.rows = rows;
@@ -279,7 +278,7 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             x.blind = e.len < e.t;
         }
         Two total;
-        const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows, only)) << 32 | heavy_items(x.rows, only), 0}, sums, total).a;
+        const int64_t before = sum + plan_scan<kPlan / 32>({int64_t(light_items(x.rows, only, item)) << 32 | heavy_items(x.rows, only), 0}, sums, total).a;
         sum += total.a;
         if (s < n_src) {
             x.heavy0 = first0[s] = int(before & 0xffffffff);
@@ -312,8 +311,8 @@ __global__ void __launch_bounds__(FEW ? 512 : 1024) k_plan_items(const sim_kv kv
             if (k < n_items) {
                 const int s = last_at_most(first, n_src, k);
                 const KvSource x = source[s];
-                it.row0 = only ? (k - x.light0) * kLightRows : (light ? x.n_heavy : k - x.heavy0) * kAttRows;
-                it.rows = min(x.rows - it.row0, kv_rows(light));
+                it.row0 = light ? x.n_heavy * kAttRows + (k - x.light0) * item : (k - x.heavy0) * kAttRows;
+                it.rows = min(x.rows - it.row0, light ? item : kAttRows);
                 it.q0 = x.q0;
                 it.seq = x.seq;
                 it.kv0 = x.kv0;
@@ -429,8 +428,9 @@ constexpr int kJoinLight = 4;
 // and rows without keys, by kv head (`parts` blocks for each).  Loads of pieces that are not there are made all the same, from
 // another piece's row, so that the four of a lane need not be told apart (64 rows in 38 pieces: 118 us the whole call either way).
 // 18 us for 16384 rows with a prefix in 3 or 4 pieces and their own keys, 15 us for the cuts of 152 heavy stretches.
-// MANY: rows in many pieces are joined by whole blocks.
-template <bool BF, bool MANY>
+// PACKED: of a 4-bit cache, whose sources may have several light items (for 16 bits this takes 1 to 2 us more); MANY: rows in many pieces
+// are joined by whole blocks.
+template <bool BF, bool PACKED, bool MANY>
 __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim_kv_batch b, const KvAttend a, int parts) {
     kv_wait_previous();
     const KvPlan plan = kv_plan(kv, b);
@@ -446,8 +446,22 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
     const uint32_t heavy = uint32_t(plan.hdr[7]) * kJoinHeavy, cuts = heavy + uint32_t(plan.hdr[23]) * kJoinLight;
     const uint32_t all = cuts + uint32_t(plan.hdr[17]) * uint32_t(H) * uint32_t(parts);  // at most 2^30 and the cuts
     const Share share0(plan, 0), share1(plan, 1);
-    const int per_item = kv_rows(kv_light_only(kv, b));
+    const int shift = PACKED ? kv_light_shift(kv, b) : 5, item = 1 << shift;
     const int64_t base1 = list_base(plan, 1, a.sms);
+    // Row z of a source in the pieces of its item; in: its number there.
+    const auto pieces = [&](const KvSource &s, int z, int h, int &in) {
+        const int nth = z / kAttRows, zl = z - s.n_heavy * kAttRows;
+        if (nth < s.n_heavy) {
+            const KvItem it = plan.items[0][s.heavy0 + nth];
+            in = z % kAttRows;
+            return Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
+        }
+        const int e = PACKED ? zl >> shift : 0;
+        in = zl - e * item;
+        if (!PACKED || e == 0) return Pieces(share1, base1, s.unit, s.tiles, s.row_off, min(s.rows - s.n_heavy * kAttRows, PACKED ? item : kAttRows), h, 1);
+        const KvItem it = plan.items[1][s.light0 + e];
+        return Pieces(share1, base1, it.unit, it.tiles, it.row_off, it.rows, h, 1);
+    };
 #pragma unroll 1
     for (uint32_t y = blockIdx.x; y < all; y += gridDim.x) {
         // rows z, z + step, .. below z1 of query tokens from q0 on, and kv head h
@@ -560,26 +574,13 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
             int in = z, pin = 0;
             if (!by_cut) {
                 if (x.prefix < 0) {  // only rows of items without keys: the item's last row sees the most
-                    const int end = min(z / per_item * per_item + per_item, x.rows);
+                    const int own0 = x.n_heavy * kAttRows;
+                    const int end = min(z < own0 ? z / kAttRows * kAttRows + kAttRows : own0 + ((z - own0) >> shift << shift) + item, x.rows);
                     if (min(x.kv1, x.pos0 + int(a.group.div(end - 1)) + 1) > 0) continue;
                 } else {
-                    const int nth = z / kAttRows;
-                    in = z % kAttRows;
-                    if (nth >= x.n_heavy) {
-                        own = Pieces(share1, base1, x.unit, x.tiles, x.row_off, min(x.rows - nth * kAttRows, kAttRows), h, 1);
-                    } else {
-                        const KvItem it = plan.items[0][x.heavy0 + nth];
-                        own = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
-                    }
+                    own = pieces(x, z, h, in);
                     const KvSource px = plan.source[x.prefix];
-                    const int row = (q0 - px.q0) * G + z, pth = row / kAttRows;
-                    pin = row % kAttRows;
-                    if (pth >= px.n_heavy) {
-                        first = Pieces(share1, base1, px.unit, px.tiles, px.row_off, min(px.rows - pth * kAttRows, kAttRows), h, 1);
-                    } else {
-                        const KvItem it = plan.items[0][px.heavy0 + pth];
-                        first = Pieces(share0, 0, it.unit, it.tiles, it.row_off, it.rows, h, 0);
-                    }
+                    first = pieces(px, (q0 - px.q0) * G + z, h, pin);
                 }
             }
             gather(first.n + own.n, [&](int p) { return p < first.n ? first.at(p, pin) : own.at(p - first.n, in); });
@@ -631,7 +632,7 @@ cudaError_t launch_kv_plan(const sim_kv &kv, const sim_kv_batch &b, cudaStream_t
         if (e != cudaSuccess) return e;
     }
     const KvPlan p = kv_plan(kv, b);
-    const bool few = b.n_groups + b.n <= kFewSources && int64_t(p.max_heavy) <= kFewItems;  // at most one light item a source
+    const bool few = b.n_groups + b.n <= kFewSources && p.max_heavy <= kFewItems && p.max_light <= kFewItems;
     return launch_chained(few ? k_plan_items<true> : k_plan_items<false>, 1, few ? 512 : 1024, 0, st, kv, b, kv_sm_count());
 }
 
@@ -656,7 +657,8 @@ cudaError_t launch_kv_attend(const sim_kv &kv, const sim_kv_batch &b, const KvAt
     const int blocks = int(std::min<int64_t>(rows, int64_t(a.sms) * 5));
     // few rows of a 4-bit cache: their pieces are many
     const bool many = packed && rows <= int64_t(a.sms) * kJoinRows;
-    return launch_chained(kv_bf(kv) ? (many ? k_combine<true, true> : k_combine<true, false>) : many ? k_combine<false, true> : k_combine<false, false>, blocks, kJoin, 0, st, kv, b, a, int(parts));
+    return launch_chained(kv_bf(kv) ? (many ? k_combine<true, true, true> : packed ? k_combine<true, true, false> : k_combine<true, false, false>)
+                                    : (many ? k_combine<false, true, true> : packed ? k_combine<false, true, false> : k_combine<false, false, false>), blocks, kJoin, 0, st, kv, b, a, int(parts));
 }
 
 }  // namespace simgb

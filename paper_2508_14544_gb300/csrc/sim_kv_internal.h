@@ -88,23 +88,26 @@ cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_
 constexpr int kAttRows = 256;   // query rows of a heavy item, at most
 constexpr int kLightRows = 32;  // of a light one
 __host__ __device__ constexpr int kv_rows(int light) { return light ? kLightRows : kAttRows; }
-// Batches that look like single tokens (no more of them than entries, no groups): all rows are light items, more than one
-// if an entry has more than kLightRows after all, and the heavy kernel is not launched: over an empty list it costs the
+// Batches that look like single tokens (no more of them than entries, no groups): all rows are light items, as many as it takes
+// if an entry has many after all, and the heavy kernel is not launched: over an empty list it costs the
 // host 1.6 us and the GPU 2 to 3 us of a step that takes 26.
 __host__ __device__ inline bool kv_light_only(const sim_kv &kv, const sim_kv_batch &b) {
     const int64_t G = b.q_heads / kv.n_kv_heads;
     return b.n_q * G <= kLightRows || (b.n_groups == 0 && G <= kLightRows && b.n_q <= b.n);
 }
-// Rows of a pass over a light item of a 4-bit cache, by what entries have on average: an item with more is gone over again.  32 at a
-// time do not leave enough registers (128 sequences of up to 2000 keys: with 16 query heads for each of 8 kv heads 75 us with 16 rows
-// a pass, 96 us with 8, 122 us with 32; with 32 heads for each of 4 85, 113, 89 us; with 1 to 4 tokens of 8 heads 135, 179, 150 us).
-__host__ __device__ inline int kv_pass_rows(const sim_kv &kv, const sim_kv_batch &b) {
-    const int64_t rows = (int64_t(b.n_q) * (b.q_heads / kv.n_kv_heads) + b.n - 1) / (b.n > 0 ? b.n : 1);
-    return rows <= 8 ? 8 : 16;
+// Rows of a light item, at most.  Of a 4-bit cache, by what entries have on average: more than 16 do not leave enough registers (128
+// sequences of up to 2000 keys: with 16 query heads for each of 8 kv heads 75 us with 16 rows, 96 us with 8, 122 us with 32 at a time; with 32
+// heads for each of 4 85, 113, 89 us; with 1 to 4 tokens of 8 heads 135, 179, 150 us).
+// Every kernel asks for it, so there is no division (a 64-bit one for each kernel of a call takes 2 us).
+__host__ __device__ inline int kv_light_shift(const sim_kv &kv, const sim_kv_batch &b) {  // its logarithm
+    const int64_t rows = int64_t(b.n_q) * (b.q_heads / kv.n_kv_heads);
+    return !kv_4bit(kv) ? 5 : rows <= 8 * int64_t(b.n > 0 ? b.n : 1) ? 3 : 4;
 }
+__host__ __device__ inline int kv_light_rows(const sim_kv &kv, const sim_kv_batch &b) { return 1 << kv_light_shift(kv, b); }
+static_assert(kLightRows == 1 << 5, "kv_light_shift");
 // Blocks of the light list on an SM: three of a 4-bit cache where 8 rows a pass leave enough registers (384 sequences of up to 2600 keys: 167
 // instead of 183 us with two).
-__host__ __device__ inline int kv_per_sm(const sim_kv &kv, const sim_kv_batch &b) { return kv_4bit(kv) && kv_pass_rows(kv, b) == 8 ? 3 : 2; }
+__host__ __device__ inline int kv_per_sm(const sim_kv &kv, const sim_kv_batch &b) { return kv_light_rows(kv, b) == 8 ? 3 : 2; }
 constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
 // tiles.  (4-bit caches, 384 sequences of up to 2600 keys: 185, 183, 188, 193 us with 1, 2, 3, 4.)
@@ -133,10 +136,10 @@ struct alignas(16) KvSource {
     int32_t seq, kv0, kv1;    // row of the table, keys
     int32_t pos0;             // as KvItem's
     int32_t heavy0, n_heavy;  // its heavy items
-    int32_t light0;           // its light item, after them (kv_light_only: the first of them)
+    int32_t light0;           // the first of its light items, after them: one, in a 4-bit cache and with kv_light_only perhaps more
     int32_t prefix;           // source of the prefix that it shares, or -1
     int32_t blind;            // some of its rows see no key
-    int32_t tiles;            // of its light item, whose .unit and .row_off follow
+    int32_t tiles;            // of its first light item, whose .unit and .row_off follow
     int64_t unit, row_off;
 };
 static_assert(sizeof(KvSource) == 64, "KvSource");
@@ -167,6 +170,7 @@ struct KvPlan {
     int32_t *join;      // [n] entries with a shared prefix or rows without keys, in any order
     int64_t bytes;
     int32_t max_heavy;
+    int64_t max_light;
 };
 __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &b) {
     KvPlan p;
@@ -174,13 +178,17 @@ __host__ __device__ inline KvPlan kv_plan(const sim_kv &kv, const sim_kv_batch &
     // each query row is in one group and one entry; a source has one item of fewer than kAttRows rows at most
     const int64_t whole = 2 * (int64_t(b.n_q) * G / kAttRows) + src, small = 2 * (int64_t(b.n_q) * G / (kLightRows + 1));
     p.max_heavy = int32_t((whole < small ? whole : small) + 1);
+    // light items: where heavy ones take the most rows, those of 32 rows a source at most, or of all rows, each in an entry and perhaps in a group
+    const int shift = kv_light_shift(kv, b);
+    const int64_t most = src << (5 - shift), many = src + ((int64_t(b.n_q) * G << (b.n_groups > 0)) >> shift);
+    p.max_light = !kv_light_only(kv, b) && most < many ? most : many;
     p.hdr = static_cast<int32_t *>(b.plan);
     p.cut[0] = reinterpret_cast<KvCut *>(p.hdr + 32);
     p.cut[1] = p.cut[0] + kKvMaxSms;
     p.source = reinterpret_cast<KvSource *>(p.cut[1] + 3 * kKvMaxSms);
     p.items[0] = reinterpret_cast<KvItem *>(p.source + src);
     p.items[1] = p.items[0] + p.max_heavy;
-    p.start[0] = reinterpret_cast<int32_t *>(p.items[1] + src + (kv_light_only(kv, b) ? int64_t(b.n_q) * G / kLightRows : 0));
+    p.start[0] = reinterpret_cast<int32_t *>(p.items[1] + p.max_light);
     p.start[1] = p.start[0] + kKvMaxSms;
     p.first[0] = p.start[1] + 3 * kKvMaxSms;
     p.first[1] = p.first[0] + src + 1;
