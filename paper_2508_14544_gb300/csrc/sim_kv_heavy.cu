@@ -197,7 +197,7 @@ __device__ __forceinline__ void unpack_keys(const unsigned char *strip, unsigned
         }
     }
 }
-// keys: of the strip, the others' values are zeros; blind: so are those of keys with a group that is not a number, which are returned as bits.
+// keys: of the strip, the others' values are zeros; blind: so are groups that are not numbers, whose keys are returned as bits (Sink::spoil).
 template <int DG, bool BF>
 __device__ __forceinline__ uint32_t unpack_values(const unsigned char *strip, unsigned char *tile, int row0, int half, int keys, bool blind) {
     const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
@@ -210,17 +210,19 @@ __device__ __forceinline__ uint32_t unpack_values(const unsigned char *strip, un
         words<2 * DG>(strip + 256 * DG + 8 * DG * (t + 4 * e), f);
         if (keys < kStrip || blind) {
             const uint32_t kept = (y < keys ? 0xffffu : 0u) | (y + 1 < keys ? 0xffff0000u : 0u);
-            uint32_t odd = 0;
-            constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
 #pragma unroll
-            for (int j = 0; j < 2 * DG; ++j) {
-                f[j] &= kept;
-                odd |= ((f[j] & kExp) == kExp ? 0xffffu : 0u) | ((f[j] >> 16 & kExp) == kExp ? 0xffff0000u : 0u);
-            }
+            for (int j = 0; j < 2 * DG; ++j) f[j] &= kept;
             if (blind) {
-                bad |= (odd & 1) << y | (odd >> 31) << (y + 1);
+                constexpr uint32_t kExp = BF ? 0x7f80u : 0x7c00u;
 #pragma unroll
-                for (int j = 0; j < 2 * DG; ++j) f[j] &= ~odd;
+                for (int j = 0; j < DG; ++j) {  // each group for itself: a token's others keep their values
+                    uint32_t odd = 0;
+#pragma unroll
+                    for (int i = 2 * j; i < 2 * j + 2; ++i)
+                        odd |= ((f[i] & kExp) == kExp ? 0xffffu : 0u) | ((f[i] >> 16 & kExp) == kExp ? 0xffff0000u : 0u);
+                    f[2 * j] &= ~odd, f[2 * j + 1] &= ~odd;
+                    bad |= (odd & 1) << y | (odd >> 31) << (y + 1);
+                }
             }
         }
 #pragma unroll
