@@ -58,7 +58,7 @@ __device__ __forceinline__ uint32_t step_of(float lo, float hi) {
         step = __float_as_uint(q) >> 16;
         up = step + 1;
         step = 15.f * __uint_as_float(up << 16) <= span ? up : step;
-        if (large) step += 3 << 7;
+        if (large && step) step += 3 << 7;  // (a span of 0 has no step)
     } else {
         step = __half_as_ushort(__float2half_rz(q));
         up = step + 1;
