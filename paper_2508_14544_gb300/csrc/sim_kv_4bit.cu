@@ -181,9 +181,7 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
                 // One over the step, to the nearest float; 0 where that, or the quotients by the step, may leave the range, where the step
                 // leaves more than 15.5 of them, and where there is none.
                 const float of = wide<BF>(scale, 0);
-                float over;
-                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(over) : "f"(of));
-                over = fmaf(fmaf(-of, over, 1.f), over, over);
+                float over = __frcp_rn(of);
                 if (!(of > (BF ? 0x1p-100f : 0x1p-18f) && of < (BF ? 0x1p100f : 0x1p14f))) over = 0.f;
                 // A difference that is not exact is one of numbers whose last places lie more than 24 powers of two under the first: one is
                 // below 2^-15 (bfloat16) or 2^-12 (float16) of the difference.  It is rounded to a border only if the larger number lies
@@ -198,9 +196,10 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
                     const uint32_t sc = __shfl_sync(FULL, scale, j, 4);
                     const float in1 = __shfl_sync(FULL, over, j, 4), inv = fabsf(in1), s = wide<BF>(sc, 0), lo = wide<BF>(sc, 1);
                     const uint4 y = x[j];
-                    // The difference, its quotient by the step to the nearest float, and that to the nearest whole number, ties to even.
-                    // Where the difference is exact, a quotient on a border is a float; one next to it is more than half of a float's unit away, as
-                    // the difference is a float too.
+                    // The difference, its quotient by the step to the nearest float (Markstein, IBM J. Res. Dev. 34, 1990: a product with the rounded
+                    // reciprocal, corrected by its remainder, which is exact here as a step has 11 bits at most), and that to the nearest whole number,
+                    // ties to even.  Where the difference is exact, a quotient on a border is a float; one next to it is more than half of a float's
+                    // unit away, as the difference is a float too.
                     uint32_t w = 0u - 0x4b400000u * 0x11111111u;
                     const auto value = [&](int q) { return wide<BF>(q < 2 ? y.x : q < 4 ? y.y : q < 6 ? y.z : y.w, q % 2); };
 #pragma unroll

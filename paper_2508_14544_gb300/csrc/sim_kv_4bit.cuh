@@ -54,7 +54,8 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
 }
 
 // Codes at bits 4 I and 16 + 4 I of w, as the values that they stand for: a code is put under the exponent whose unit it is
-// (128 + code, 1024 + code), which is then taken away, exactly; lo + code step is rounded once.
+// (128 + code, 1024 + code), which is then taken away, exactly; lo + code step is rounded once.  (Whole numbers made floats by an exponent beside
+// them, for quantised weights: Kim, Henry, Fahim and Hassan Awadalla, arXiv 2211.10017.)
 template <bool BF, int I>
 __device__ __forceinline__ uint32_t values(uint32_t w, uint32_t step, uint32_t lo) {
     // float16 has room for a code four bits further up, as 1024 + 16 code: two of the three shifts are not needed
