@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
 #pragma unroll
                 for (int i = 0; i < kJoinRows; ++i) {
                     const float w = part_top[i] == -INFINITY ? 0.f : ex2(part_top[i] - up);
-                    sum = fmaf(part_sum[i], w, sum);
+                    sum = fmaf(part_sum[i], w, sum);  // with w = 0 too: a sum that is not a number has -infinity for its top
                     if (w != 0.f) v = fmaf(part_o[i][threadIdx.x], w, v);
                 }
                 const int dt = a.group.div(y), t = q0 + dt, qh = h * G + y - dt * G;

@@ -64,3 +64,38 @@ def test_a_group_that_all_rows_see(group, tokens, dtype):
         c.kv.write(slot, c.k[slot], c.v[slot])
     q, out, lse = attend(c, [tokens], group)
     right(c, tokens, q, out, lse, bad)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("group,tokens", [(1, 1), (8, 1), (8, 3), (40, 2)])
+@pytest.mark.parametrize("what", ["query", "last value", "first value", "last key"])
+def test_rows_in_many_pieces(what, group, tokens, dtype):
+    """Some 157 tiles of keys on all SMs: what is not a number in one piece of a row comes through the joining of all of them."""
+    import torch
+    n, dim = 20000, 64
+    c = Pool([n], kv_heads=1, dim=dim, page=64, dtype=dtype)
+    q, out, lse = attend(c, [tokens], group)
+    clean_o, clean_l = out.clone(), lse.clone()
+    if what == "query":
+        q[tokens - 1, 0, 3] = math.nan
+    else:
+        at = torch.from_numpy(c.slots(0, 0, 1) if what == "first value" else c.slots(0, n - 1, n)).cuda()
+        x = c.k if what == "last key" else c.v
+        x[at, 0, 40] = math.nan
+        c.kv.write(at, c.k[at], c.v[at])
+    _, out, lse = attend(c, [tokens], group, q=q)
+    odd_o, odd_l = torch.zeros_like(out, dtype=torch.bool), torch.zeros_like(lse, dtype=torch.bool)
+    if what == "query":
+        odd_o[-1, 0], odd_l[-1, 0] = True, True
+    elif what == "last key":
+        odd_o[-1], odd_l[-1] = True, True
+    else:
+        odd_o[-1 if what == "last value" else 0:, :, 32:] = True
+    assert torch.equal(out.isnan(), odd_o) and torch.equal(lse.isnan(), odd_l)
+    if what == "query":  # the other rows: the same bits
+        assert torch.equal(out[~odd_o], clean_o[~odd_o]) and torch.equal(lse[~odd_l], clean_l[~odd_l])
+    elif what == "last key":
+        assert torch.equal(out[:-1], clean_o[:-1]) and torch.equal(lse[:-1], clean_l[:-1])
+    else:
+        right(c, tokens, q, out, lse, [(n - 1 if what == "last value" else 0, 1)])
+    c.kv.check()
