@@ -621,7 +621,7 @@ bool kv_encode_map(const sim_kv &kv, CUtensorMap *map, int rank, const void *at,
     cuuint64_t dims[5], strides[5];
     for (int i = 0; i < rank; ++i) dims[i] = dim[i];
     for (int i = 0; i + 1 < rank; ++i) strides[i] = stride[i];
-    return encode && encode(map, kv.dtype == SIM_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void *>(at), dims, strides,
+    return encode && encode(map, kv_bf(kv) ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void *>(at), dims, strides,
                             box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
