@@ -213,7 +213,9 @@ class KVCache:
     def read(self, seqs, cu, n: int, layer: int = 0, first=None, stream: int | None = None):
         """Cached keys and values of one layer, each [n, n_kv_heads, head_dim], in order: rows cu[i] .. cu[i + 1] - 1 are the
         tokens of seqs[i] from first[i] on (0 by default).  Rows of an entry that is refused are zeros."""
-        m, st, torch = seqs.shape[0], self._stream(stream), self._torch
+        m, st = seqs.shape[0], self._stream(stream)
+        if not 0 <= n < 1 << 31:  # before the tensors are made; ctypes would cut it off
+            raise ValueError("n must be in [0, 2^31)")
         k, v = (self._empty(stream, (n, self._heads, self._dim), self.dtype) for _ in range(2))
         at = self._heads * self._dim, self._dim
         rc = self._lib.sim_kv_read(self._ref, layer, m, self._ints("seqs", seqs, m), self._ints("cu", cu, m + 1),
