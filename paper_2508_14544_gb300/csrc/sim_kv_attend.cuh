@@ -336,8 +336,9 @@ __device__ __forceinline__ bool clean_row(unsigned char *row, int half) {
     return true;
 }
 
-// Where the results of a segment go.
-template <bool BF>
+// Where the results of a segment go.  PACKED: of a 4-bit cache (as a question asked at run time, its spoil_4bit took the 16-bit k_light
+// 12 to 17 registers).
+template <bool BF, bool PACKED = false>
 struct Sink {
     const sim_kv &kv;
     const KvAttend &a;
@@ -355,8 +356,8 @@ struct Sink {
     // A row that sees values which clean_row took for zeros: its result in their columns is what they alone add up to, infinite
     // or not a number.  bad: a bit for each key of the tiles from blind_from on.  By one warp, a lane for four columns.
     __device__ void spoil(int y, const uint32_t *bad) const {
+        if constexpr (PACKED) return spoil_4bit(y, bad);
         const int lane = threadIdx.x & 31, P = kv.page_size, d = 4 * lane, from = blind_from(), stop = seen(y);
-        if (kv_4bit(kv)) return spoil_4bit(y, bad);
         const uint16_t *values = static_cast<const uint16_t *>(kv.pool) + a.layer * kv_layer_elems(kv) + kv_layer_elems(kv) / 2;
         float o[4] = {};
 #pragma unroll 1

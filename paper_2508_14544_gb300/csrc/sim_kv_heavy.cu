@@ -35,8 +35,8 @@ constexpr int kStage = 128 * kPitch;  // words through which the results of 128 
 
 // The results of a warp's 32 rows from row0 on, 16 words of each at a time through `mine` (32 x kPitch words), so that stores
 // fill sectors; what the lane's row is multiplied by, and what it has in the workspace (Sink::joint).
-template <int DP, bool BF>
-__device__ __forceinline__ void store_rows(const Sink<BF> &sink, uint32_t t_o, uint32_t *mine, int row0, int rows, float f, float fb) {
+template <int DP, bool BF, bool PACKED>
+__device__ __forceinline__ void store_rows(const Sink<BF, PACKED> &sink, uint32_t t_o, uint32_t *mine, int row0, int rows, float f, float fb) {
     const Segment &sg = sink.sg;
     const int lane = threadIdx.x & 31;
     char *to[4];  // this lane's 16 bytes of four rows
@@ -242,6 +242,7 @@ template <int DP, bool BF, int DG>
 __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
     k_heavy(const sim_kv kv, const sim_kv_batch b, const KvAttend a, const __grid_constant__ KvMaps maps) {
     using Sh = Shape<DP, DG>;
+    using Results = Sink<BF, (DG > 0)>;
     constexpr int NS = Sh::kSlots, NG = Sh::kGroups;
     extern __shared__ unsigned char raw[];
     unsigned char *const base = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
                     }
                     continue;
                 }
-                const int clean_from = Sink<BF>{kv, a, sg, G, D, b.q_heads}.clean_from();
+                const int clean_from = Results{kv, a, sg, G, D, b.q_heads}.clean_from();
                 const int32_t *row = kv.table + int64_t(sg.seq) * kv.max_pages;
                 const int first = sg.k0 / P + lane;
                 const auto page_of = [&](int j) {  // of this lane in tile j; past the keys: none, zeros
@@ -417,7 +418,7 @@ __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
                 uint32_t at = 0, np = 0;
                 bool ok = true;
                 for (uint32_t x = 0; ok && take(x, sg) && sg.n > 0; ++x) {
-                    const int blind_from = Sink<BF>{kv, a, sg, G, D, b.q_heads}.blind_from();
+                    const int blind_from = Results{kv, a, sg, G, D, b.q_heads}.blind_from();
                     uint16_t *const bad = reinterpret_cast<uint16_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 8;
                     for (int j = 0; j < sg.n && ok; ++j, ++np) {
                         const unsigned char *const pack = base + Sh::kOffPack + (np % Sh::kPacks) * Sh::kPack;
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
             for (uint32_t x = 0; (ok = take(x, sg)); ++x) {
                 const int n = __shfl_sync(FULL, sg.n, 0), last = __shfl_sync(FULL, sg.rows, 0) > 128;  // group with rows
                 if (n == 0) break;
-                const int clean_from = __shfl_sync(FULL, Sink<BF>{kv, a, sg, G, D, b.q_heads}.clean_from(), 0);
+                const int clean_from = __shfl_sync(FULL, Results{kv, a, sg, G, D, b.q_heads}.clean_from(), 0);
                 const auto keys = [&](int j, int g) {  // S of group g and tile j
                     if (elect_one()) {
                         const uint32_t slot = (at + 2 * j) % NS;
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
             const bool has = j * 8 < D;
             const auto look = [&](const Segment &s, uint32_t x, uint32_t at, uint32_t &nc) {
                 if (DG) return true;
-                const Sink<BF> sink = {kv, a, s, G, D, b.q_heads};
+                const Results sink = {kv, a, s, G, D, b.q_heads};
                 const int blind_from = sink.blind_from();
                 uint32_t *const bad = reinterpret_cast<uint32_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 4;
                 for (int t = sink.clean_from(); t < s.n; ++t, ++nc) {
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
             const int r = g * 128 + lr;  // the row in this thread's lane
             // key position that it sees last; lanes past the rows see all: theirs are no reason to mask a tile
             const int last = r < sg.rows ? min(sg.kv1 - 1, sg.pos0 + int(a.group.div(sg.row0 + r))) : sg.kv1 - 1;
-            const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
+            const Results sink = {kv, a, sg, G, D, b.q_heads};
             const int blind_from = sink.blind_from();
             const uint32_t *const bad = reinterpret_cast<const uint32_t *>(base + Sh::kOffBad) + x % (2 * kSegs) * kBlindTiles * 4;
             float m = -INFINITY, l = 0.f;
@@ -659,7 +660,7 @@ __global__ void __launch_bounds__(Shape<DP, DG>::kThreads, 1)
                 if (lane == 0) bar_arrive(p_ready(g));
             }
             if (!ok) break;
-            const typename Sink<BF>::Joint joint = sink.joint(m * c - kv_lift(BF), l, r < sg.rows ? sink.before(r) : -INFINITY);
+            const typename Results::Joint joint = sink.joint(m * c - kv_lift(BF), l, r < sg.rows ? sink.before(r) : -INFINITY);
             if (r < sg.rows) sink.lse(r, joint.e);
             ok = __all_sync(FULL, bar_wait(o_full(g), no++ & 1, gave_up));
             if (!ok) break;
