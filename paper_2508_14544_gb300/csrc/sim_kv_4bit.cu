@@ -181,8 +181,10 @@ __global__ void __launch_bounds__(kWrite, 4) k_write_4bit(const sim_kv kv, const
                 // One over the step, to the nearest float; 0 where that, or the quotients by the step, may leave the range, where the step
                 // leaves more than 15.5 of them, and where there is none.
                 const float of = wide<BF>(scale, 0);
-                float over = __frcp_rn(of);
-                if (!(of > (BF ? 0x1p-100f : 0x1p-18f) && of < (BF ? 0x1p100f : 0x1p14f))) over = 0.f;
+                // (of 1 where it is not used: the call takes a longer way out of the range)
+                const bool plain = of > (BF ? 0x1p-100f : 0x1p-18f) && of < (BF ? 0x1p100f : 0x1p14f);
+                float over = __frcp_rn(plain ? of : 1.f);
+                if (!plain) over = 0.f;
                 // A difference that is not exact is one of numbers whose last places lie more than 24 powers of two under the first: one is
                 // below 2^-15 (bfloat16) or 2^-12 (float16) of the difference.  It is rounded to a border only if the larger number lies
                 // that near to one: in bfloat16 on it, as borders have 13 bits; in float16 (16 bits) within a 2^12th of -lo.  So where -lo
