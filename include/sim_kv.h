@@ -46,9 +46,9 @@ typedef enum { SIM_KV_BF16 = 0, SIM_KV_F16 = 1, SIM_KV_BF16_4BIT = 16, SIM_KV_F1
  *         that is 0 and hi > lo,
  *   code  the nearest of 0 .. 15 to (x - lo) / step, ties to even (0 where step is 0),
  * and in x's place the cache holds the 16-bit float nearest to lo + code step: |held - x| is at most step / 2 (or 15
- * times the smallest positive float, if that is more) and a rounding.  If one of the group is infinite or not a number, all of it is held as not a number.  Everything below goes
- * by the values held.  The pool is [n_pages][n_layers][2][n_kv_heads][page_size / 16] strips of 16 tokens, each, with
- * G = ceil(head_dim / 32) groups, 320 G bytes (5 bits a value), in the order in which the matrix instructions of sim_kv_attend take
+ * times the smallest positive float, if that is more) and a rounding, which is not more again, as x is such a float.  If one of
+ * the group is infinite or not a number, all of it is held as not a number.  Everything below goes by the values held.  The pool is [n_pages][n_layers][2][n_kv_heads][page_size / 16] strips of 16 tokens, each, with
+ * G = ceil(head_dim / 32) groups, 320 G bytes (5 bits a value if head_dim = 32 G), in the order in which the matrix instructions of sim_kv_attend take
  * them.  With token T (0 .. 15) of the strip and group g, whose dimension d is 32 g + d:
  *   keys    32-bit word at 16 G T + 4 G (d / 8) + 4 g: code of d at bit 4 (d % 8 / 2) + 16 (d % 2); step and lo, 16 bits each, from
  *           256 G + 4 G T + 4 g on;
@@ -135,6 +135,7 @@ int sim_kv_compact(const sim_kv *kv, int32_t *to, void *cuda_stream);
  *            dimension contiguous, 16-byte aligned.
  * Rows of an entry whose sequence is out of range or does not have its tokens (SIM_E_INVAL in kv->status) are zeros, as are
  * tokens of pages that the pool does not have and rows of no entry.  With offsets that are not in order (SIM_E_INVAL) all rows are.
+ * Every block reads the offsets: entries cost some 20 ns each beyond their rows where there are 10^5 of them.
  */
 int sim_kv_read(const sim_kv *kv, int32_t layer, int32_t n, const int32_t *seqs, const int32_t *cu, const int32_t *first,
                 int32_t total, void *k, int64_t k_token_stride, int64_t k_head_stride, void *v, int64_t v_token_stride,
@@ -176,7 +177,8 @@ int sim_kv_plan(const sim_kv *kv, const sim_kv_batch *b, void *cuda_stream);
  * A query that sees no key gets zeros, and -infinity for lse.  Cached values past a sequence's length are
  * never used, whatever they are, nor are those that a query does not see.  Sums and the softmax are in 32 bits, those
  * of the products (which cut off what does not fit) over 2^15 keys at most; the probabilities are rounded to that type for
- * the product with the values.
+ * the product with the values.  A value that is infinite or not a number makes the result so for the queries that see it; where its
+ * probability is below 2^-126 of the row's largest, only if the row's keys have not been divided there.
  */
 int sim_kv_attend(const sim_kv *kv, const sim_kv_batch *b, int32_t layer, const void *q, int64_t q_token_stride,
                   int64_t q_head_stride, float scale, void *out, int64_t out_token_stride, int64_t out_head_stride,

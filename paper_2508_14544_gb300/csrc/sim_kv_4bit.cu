@@ -1,11 +1,16 @@
 // Keys and values of a 4-bit cache: quantised as they are written, and read back (16-bit caches are read here too).
 //   k_write_4bit - bound by arithmetic: some 19 instructions a value (the difference from the lowest, its quotient to the nearest float, that to
 //                the nearest whole number, 4 bits into their place; a third is what a group costs), 2.9 a cycle and SM.  343 us for
-//                524 million values, of which HBM needs 204.  With a thread for each group and its pieces stored apart 958 us, and 45
-//                sectors written for a token's keys of a head instead of 4.  Each lane the step of one group instead of all lanes those
-//                of all: 385 instead of 637 us; differences checked by two roundings only where -lo lies next to a border: 370;
-//                one row at a time, so that four blocks fit: 343.  5.6 us for 40 tokens, a chain of two loads and the arithmetic.
-//   k_read     - bound by HBM: 153 us for 0.95 GB, 6.2 TB/s; 6 us for a few tokens, a chain of dependent loads (offsets, entry, page, strip).
+//                524 million values, of which HBM needs 204; 5.6 us for 40 tokens, a chain of two loads and the arithmetic.  The way
+//                there, each from the one before: a thread for each group, its pieces stored apart 958 us, and 45
+//                sectors written for a token's keys of a head instead of 4; by warps 637; each lane the step of one group instead of all
+//                lanes those of all 385; differences checked by two roundings only where -lo lies next to a border 370; one row at a time,
+//                so that four blocks fit 343.
+//   k_read     - bound by HBM: 151 us for 0.95 GB, 6.3 TB/s; 6 us for a few tokens, a chain of dependent loads (offsets, entry, page, strip).
+//                Of a 16-bit cache 277 us for 1.57 GB, 5.7 TB/s: what a lane keeps until it stores takes 128 registers, so that two blocks
+//                fit an SM.  Every block walks the whole list of offsets to see that they are in order, which is nothing for the
+//                lists of a batch (1500 entries: as fast as 1000) and most of the time of long ones: 10^5 entries of three tokens 1.8 ms
+//                (16 bits: 2.3), of which their rows need 0.2 and 0.36.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -412,8 +417,11 @@ cudaError_t launch_kv_write_4bit(const sim_kv &kv, const KvWrite &w, cudaStream_
                                  {k_write_4bit<1, true, true>, k_write_4bit<2, true, true>, k_write_4bit<3, true, true>, k_write_4bit<4, true, true>}}};
     const int64_t chunks = (int64_t(w.n_new) + kStrip - 1) / kStrip;
     const int64_t heads = chunks * 2 * kv.n_kv_heads;
-    // Heads that a warp takes, so that what it learns of the slots serves all, as long as there are warps enough for that: 4 instead of 2 for 250
-    // prompts (store and read 554 instead of 563 us, 604 with 1), 2 instead of 4 for 77 of 3 heads (89 instead of 99 us).
+    // Heads that a warp takes, so that what it learns of the slots serves all, as long as there are warps enough for that.  k_write_4bit by
+    // per_sm, with 1, 2, 4 heads (8 heads of 128, bfloat16 | 3 heads of 80, float16), us: 48: 23, 25, 36 | 21, 23, 33; 140: 44, 46, 54 | 40, 42,
+    // 52; 284: 76, 74, 81 | 68, 66, 79; 400: 103, 99, 103 | 93, 89, 101; 700: 171, 158, 160 | 154, 142, 156; 1700: 400, 359, 351 | 359, 324, 343.
+    // So 2 is right from some 200 on, where 96 takes it (2 us too many in between), and 4 from some 800 on if it divides the heads: with
+    // 6 heads of keys and values, every second warp has half of them, and it costs 6 to 13 %.
     const int64_t per_sm = heads / kv_sm_count();
     const int few = per_sm < 4, each = per_sm < 96 ? 1 : per_sm < 512 ? 2 : 4, threads = few ? 64 : kWrite;
     const int blocks = blocks_for(few ? 2 * heads : chunks * ((2 * kv.n_kv_heads + each - 1) / each), threads / 32, 4096);

@@ -13,8 +13,9 @@
 // us for 2.1 GB); one sequence of 131071 keys, float16: 38 us for 0.17 GB.  Unpacking bounds it: a strip's keys and values take a warp some 400
 // instructions, of which 64 fused multiply-adds, 64 additions, 64 selections and 48 shifts (16 in float16) are on pipes that take two a
 // cycle, and a mixture of these was measured at 2.9 to 3.05 a cycle; without loads the kernel takes 138 us, without arithmetic 107.  So it
-// does not matter whether a warp takes one strip at a time or two (157.6 and 157.7 us, plan and join included), whether three or four blocks
-// share an SM (161 and 166 us) or whether the queries' exponents are computed once or twice.  Eight warps in two blocks: 189 us.
+// does not matter whether a warp takes one strip at a time or two (157.6 and 157.7 us, plan and join included) or whether the
+// queries' exponents are computed once or twice.  When blocks were chosen (that call took 161 us then): three an SM 161, four with half
+// tiles 166, two of eight warps 189 us.
 #include <algorithm>
 #include <cfloat>
 

@@ -34,9 +34,12 @@ namespace {
 // 2048 keys 59 against 50 us (8192: 88 against 102), 16 groups with 1024 keys 48 against 42 us (4096: 59 against 63).
 constexpr int kShareItem = 3, kShareRows = 7, kShareOnce = 2;
 // Of a 4-bit cache, over the number of groups of 32 columns: how many times as much that is, as its light items' tiles take less time (row_cost).
-// Shared (or, by this rule, not) and without groups: 128 sequences of 8 kv heads with 8 query heads in 64 groups with a prefix of 2048 and of 8192 keys
-// 104 and 95, 288 and 276 us (by the rule for 16 bits 212 and 568), in 16 groups of 1024, 2048, 4096 keys 71 and 62, 81 and 93, 104 and 149 us
-// (108, 95, 159).  With 6 or 10 instead of 8 the same within 2 us, but 114 for 64 groups of 2048 keys with 6.
+// By this rule and without groups, us (8 kv heads of 8 query heads, D = 128 | 2 of 4, D = 64 | 8 of 8, D = 64, float16): 64 groups of two with 2048 keys
+// 116, 109 | 46, 38 | 85, 77 and with 8192 321, 312 | 63, 75 | 226, 216; 16 of eight with 1024 69, 71 | 40, 32 | 60, 54, with 2048 79, 104 | 46, 39 | 67,
+// 77 and with 4096 104, 172 | 48, 50 | 83, 123; one of 32 with 4096 50, 61 | 34, 28 | 44, 48; one of 256 with 1024 81, 114 | 46, 40 | 91, 83 and with
+// 8192 122, 579 | 50, 128 | 97, 407.  8 to 10 of what it loses where it does not share is what naming groups costs (k_plan_shared, a heavy list
+// that is asked for).  With 6 instead of 8 the same within 2 us but for the group of 256 with 1024 keys, D = 64 (67 instead of 91: it is shared; with
+// D = 32 56 instead of 87) and 32 with 1024, D = 128 (48 instead of 44); with 12 sharing begins too late (16 with 2048, D = 64: 83 instead of 67).
 constexpr int kShare4 = 8;
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -539,8 +542,9 @@ __global__ void __launch_bounds__(kJoin, 5) k_combine(const sim_kv kv, const sim
                 }
             }
         };
-        // In a 4-bit cache, rows in many pieces: each half warp an eighth of them, joined in shared memory (one sequence of 131071 keys, 57 pieces
-        // for each of 64 rows: the whole call 50 instead of 56 us).  By whole blocks.
+        // In a 4-bit cache, rows in many pieces: each half warp an eighth of them, joined in shared memory, by whole blocks.  One sequence,
+        // the whole call: 131071 keys, 57 pieces for each of 64 rows 63 instead of 68 us, 450 for each of 8 rows 44 instead of 89; 20000 keys
+        // 33 instead of 40; 128 rows, 16 an item, 76 instead of 71: here it loses.
         if constexpr (MANY) if (by_cut && own.n > kJoinMany) {
             __shared__ float part_o[kJoinRows][128], part_top[kJoinRows], part_sum[kJoinRows];
             const int each = (own.n + kJoinRows - 1) / kJoinRows;

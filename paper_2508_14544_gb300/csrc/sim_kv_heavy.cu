@@ -18,9 +18,10 @@
 //
 // Of a 4-bit cache, strips come by bulk copies and four more warps turn them into the tiles that TMA brings of a 16-bit one: the same
 // products on the same layout, 16 registers a thread fewer for the softmax and three tiles in flight instead of four.  16 prompts'
-// own tokens on 3718 + 600 keys each (12 % more work than above): 646 us, 1.33 PFLOP/s.  Shared memory has to give 40 KB more a tile, a sixth;
-// without the unpacking (and with wrong results) the whole call takes 608 instead of 702 us, and the 16-bit kernel with three tiles 3 % more
-// than with four.  Four tiles and strips of three halves of a tile, in the place of the stage for results: 755 instead of 715 us.
+// own tokens on 3718 + 600 keys each (12 % more work than above): 646 us, 1.33 PFLOP/s, the whole call 695 to 714 by machine.  Shared memory has
+// to give 40 KB more a tile, a sixth; without the unpacking (and with wrong results) the call took 608 instead of 702 us on one machine, and the
+// 16-bit kernel with three tiles 3 % more than with four.  Four tiles and strips of three halves of a tile, in the place of the stage for results,
+// when that was chosen: 755 instead of 715 us.
 #include <type_traits>
 
 #include "sim_kv_4bit.cuh"

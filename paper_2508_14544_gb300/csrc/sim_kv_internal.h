@@ -95,7 +95,7 @@ __host__ __device__ inline bool kv_light_only(const sim_kv &kv, const sim_kv_bat
     const int64_t G = b.q_heads / kv.n_kv_heads;
     return b.n_q * G <= kLightRows || (b.n_groups == 0 && G <= kLightRows && b.n_q <= b.n);
 }
-// Rows of a light item, at most.  Of a 4-bit cache, by what entries have on average: more than 16 do not leave enough registers (128
+// Rows of a light item, at most.  Of a 4-bit cache, by what entries have on average: more than 16 do not leave enough registers (when chosen: 128
 // sequences of up to 2000 keys: with 16 query heads for each of 8 kv heads 75 us with 16 rows, 96 us with 8, 122 us with 32 at a time; with 32
 // heads for each of 4 85, 113, 89 us; with 1 to 4 tokens of 8 heads 135, 179, 150 us).
 // Every kernel asks for it, so there is no division (a 64-bit one for each kernel of a call takes 2 us).
@@ -105,12 +105,12 @@ __host__ __device__ inline int kv_light_shift(const sim_kv &kv, const sim_kv_bat
 }
 __host__ __device__ inline int kv_light_rows(const sim_kv &kv, const sim_kv_batch &b) { return 1 << kv_light_shift(kv, b); }
 static_assert(kLightRows == 1 << 5, "kv_light_shift");
-// Blocks of the light list on an SM: three of a 4-bit cache where 8 rows a pass leave enough registers (384 sequences of up to 2600 keys: 167
-// instead of 183 us with two).
+// Blocks of the light list on an SM: three of a 4-bit cache where 8 rows a pass leave enough registers (384 sequences of up to 2600 keys, when
+// chosen: 167 instead of 183 us with two).
 __host__ __device__ inline int kv_per_sm(const sim_kv &kv, const sim_kv_batch &b) { return kv_light_rows(kv, b) == 8 ? 3 : 2; }
 constexpr int kTileKeys = 128;  // keys of a tile
 // What taking up an item and writing its results costs, in tiles: on the line of work, that much lies before an item's
-// tiles.  (4-bit caches, 384 sequences of up to 2600 keys: 185, 183, 188, 193 us with 1, 2, 3, 4.)
+// tiles.  (4-bit caches, 384 sequences of up to 2600 keys, when chosen: 185, 183, 188, 193 us with 1, 2, 3, 4.)
 __host__ __device__ inline int kv_lead(const sim_kv &kv, int light) { return light ? (kv_4bit(kv) ? 2 : 1) : 4; }
 __host__ __device__ inline int kv_span(int tiles, int lead) { return tiles > 0 ? tiles + lead : 0; }
 

@@ -54,10 +54,10 @@ class KVCache:
     head_dim], ``table`` [max_seqs, max_pages], ``length`` [max_seqs] and ``ref`` [n_pages] are its state.
 
     With ``bits=4`` keys and values of the type ``dtype`` are quantised as they are written: each 32 of a token's head (the last ones:
-    fewer) are held as their lowest, a step and 4 bits each, 5 bits a value in all; ``pool`` is then uint8 [n_pages, n_layers, 2,
-    n_kv_heads, page_size, 20 ceil(head_dim / 32)], in strips of 16 tokens (``include/sim_kv.h``).  A value read back, or attended to, is
-    the 16-bit float nearest to lowest + code step, within half a step (a 30th of the distance from the lowest of its 32 to the highest, at most) of
-    the one written."""
+    fewer) are held as their lowest, a step and 4 bits each, in 20 bytes (5 bits a value if head_dim is a multiple of 32); ``pool`` is then
+    uint8 [n_pages, n_layers, 2, n_kv_heads, page_size, 20 ceil(head_dim / 32)], in strips of 16 tokens (``include/sim_kv.h``).  A value
+    read back, or attended to, is the 16-bit float nearest to lowest + code step: half a step and a rounding from the one written, together at
+    most a step, which is at most a 15th of the distance from the lowest of its 32 to the highest (or 15 times the type's smallest float)."""
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, max_seqs: int, max_pages: int,
                  n_layers: int = 1, dtype=None, device="cuda", bits: int = 16):
