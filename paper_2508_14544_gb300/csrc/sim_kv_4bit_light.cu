@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
         const Segment &sg = segs[x % kSegs], &next = segs[(x + 1) % kSegs];
         const int n = sg.n, rows = sg.rows, kv1 = sg.kv1, first = sg.k0 + warp * (kStrips / W) * kStrip;  // this warp's first key
         if (n == 0) break;
-        const Sink<BF> sink = {kv, a, sg, G, D, b.q_heads};
+        const Sink<BF, true> sink = {kv, a, sg, G, D, b.q_heads};
         const uint4 *const qs = queries(x);
         uint4 q1[NT == 1 ? DG : 1];  // 8 rows: in registers
         if constexpr (NT == 1)
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(Shape<DG, NT, W>::kThreads, Shape<DG, NT, W>::
                     const float4 u = *reinterpret_cast<const float4 *>(all_o + (w * 8 + in) * Sh::kPitch + d);
                     v = make_float4(fmaf(u.x, f, v.x), fmaf(u.y, f, v.y), fmaf(u.z, f, v.z), fmaf(u.w, f, v.w));
                 }
-                const typename Sink<BF>::Joint joint = sink.joint(-off0, total, sink.before(y));
+                const typename Sink<BF, true>::Joint joint = sink.joint(-off0, total, sink.before(y));
                 const float f = joint.mine, fb = joint.before;
                 v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
                 float4 *const part = reinterpret_cast<float4 *>(a.part + (sg.row + y) * D + d);
